@@ -444,6 +444,32 @@ dgc_status_t dgc_stale_filter_static(const void* E, int64_t lde, void* L, int64_
                                      double theta, float* dist, int64_t* send_idx, void* send_buf, int64_t lds,
                                      dgc_stale_result_t* result, void* stream);
 
+/* Operators on plain tensors: what stands between stacked DGNN blocks (Section 2.1: "blocks stack"), and a time encoder
+ * whose state is carried from window to window.  They belong to no layer: all memory is the caller's, workspaces
+ * are device memory with any contents, 16-byte aligned, not shared by calls that overlap in time (two captured graphs
+ * that may run side by side need one each).  They only enqueue work on `stream`, whose device is current, allocate
+ * nothing and may be captured into a HIP graph; argument errors return at once with the text in
+ * dgc_last_error(NULL).  A tensor of rows is R rows of F elements at the pitch ld* of the conventions above; columns
+ * from F up to the pitch are neither used nor written.  The same inputs give the same bits. */
+
+/* Layer norm over the F columns of every row (F in [1, 8192]).
+ *  forward:  m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = (x - m) r gamma + beta.
+ *   gamma, beta device fp32 [F], NULL = ones, zeros.  mean, rstd device fp32 [R], NULL = not written.  y may be x.
+ *  backward: with xh = (x - mean) rstd and g = dy gamma,
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) + add;  dgamma = sum dy xh, dbeta = sum dy over the rows.
+ *   add (same element type) may be NULL: the gradient that reaches x by another way, a residual branch.  dx may be
+ *   dy, x or add.  dgamma, dbeta device fp32 [F], NULL = not wanted; if one is, workspace holds
+ *   dgc_norm_workspace_bytes(R, F) bytes (negative for sizes outside the range).
+ * Statistics and sums are fp32 or wider; each output is rounded once. */
+int64_t dgc_norm_workspace_bytes(int64_t R, int32_t F);
+dgc_status_t dgc_norm_forward(const void* x, int64_t ldx, int64_t R, int32_t F, int32_t dtype, const float* gamma,
+                              const float* beta, float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                              void* stream);
+dgc_status_t dgc_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean,
+                               const float* rstd, int64_t R, int32_t F, int32_t dtype, const float* gamma,
+                               const void* add, int64_t ldadd, void* dx, int64_t lddx, float* dgamma, float* dbeta,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Text of the last error on this layer, or (layer = NULL) of the last failed create or layer-less
  * call on the calling thread.  Never NULL; valid until the next call on the same layer / thread. */
 const char* dgc_last_error(const dgc_layer_t* layer);

@@ -31,7 +31,8 @@ EXPORTS = ["dgc_layer_create", "dgc_layer_destroy", "dgc_layer_set_param", "dgc_
            "dgc_layer_packing", "dgc_layer_set_presence", "dgc_layer_set_labels", "dgc_layer_set_profiling", "dgc_layer_stage_times", "dgc_last_error",
            "dgc_version", "dgc_stale_theta_factor", "dgc_stale_workspace_bytes", "dgc_stale_filter",
            "dgc_stale_static_max_candidates", "dgc_stale_filter_static",
-           "dgc_layer_shared_rows", "dgc_fusion_select", "dgc_chunk_assign", "dgc_chunk_generate"]
+           "dgc_layer_shared_rows", "dgc_fusion_select", "dgc_chunk_assign", "dgc_chunk_generate",
+           "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward"]
 THETA_VARIANT = {"printed": 0, "sigmoid": 1}
 N_STAGES = 13
 
@@ -101,9 +102,16 @@ def load() -> ct.CDLL:
                                             i64, vp, vp]
     lib.dgc_stale_static_max_candidates.argtypes = []
     lib.dgc_stale_static_max_candidates.restype = i64
+    f32 = ct.c_float
+    lib.dgc_norm_forward.argtypes = [vp, i64, i64, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]
+    lib.dgc_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.dgc_norm_workspace_bytes.argtypes = [i64, i32]
+    sizes = ("dgc_norm_workspace_bytes",)
+    for name in sizes:
+        getattr(lib, name).restype = i64
     for name in EXPORTS:
         if name not in ("dgc_last_error", "dgc_version", "dgc_stale_theta_factor", "dgc_stale_workspace_bytes",
-                        "dgc_stale_static_max_candidates"):
+                        "dgc_stale_static_max_candidates") + sizes:
             getattr(lib, name).restype = ct.c_int
     _lib = lib
     return lib
@@ -393,3 +401,113 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
     if rc != 0:
         raise DgcError(rc, lib.dgc_last_error(None).decode())
     return it.value, bool(conv.value)
+
+
+# --------------------------------------------------------------------------- layer norm
+#
+# Operators on plain device tensors: nothing is allocated, outputs and workspaces are the caller's, work is only
+# enqueued on `stream` (default: the current stream of the tensors' device).
+
+
+def _op_dtype(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 1
+    if t.dtype == torch.float32:
+        return 0
+    raise ValueError(f"{name} must be float32 or bfloat16")
+
+
+def _op_rows(t, name: str, like=None, shape=None):
+    """(address, pitch) of [..., F] rows at one pitch; `like`: a tensor of the same element type and device; `shape`: (R, F)."""
+    if t is None:
+        return None, 0
+    st, sh = t.stride(), t.shape
+    n = len(sh)
+    if n < 2 or (sh[-1] != 1 and st[-1] != 1):
+        raise ValueError(f"{name} must be rows [..., F] with a contiguous last dimension")
+    for d in range(n - 2):
+        inner = sh[d + 1] * st[d + 1]
+        if sh[d] != 1 and st[d] != inner and t.numel():
+            raise ValueError(f"{name}: its rows must lie at one pitch")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} has another element type or device than the first tensor")
+    if shape is not None and (sh[-1] != shape[1] or t.numel() != shape[0] * shape[1]):
+        raise ValueError(f"{name} must hold {shape[0]} rows of {shape[1]}, not {tuple(sh)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    per = 16 // t.element_size()
+    pitch = st[-2] if sh[-2] != 1 else (st[-3] if n > 2 and t.numel() > sh[-1] else -(-sh[-1] // per) * per)
+    if n > 2 and sh[-2] == 1:       # leading sizes of 1 leave their strides free: the pitch is that of the first longer one
+        pitch = next((st[d] for d in range(n - 3, -1, -1) if sh[d] != 1), pitch)
+    return t.data_ptr(), pitch
+
+
+def _op_flat(t, name: str, numel: int, like, dtype=None):
+    """Address of a contiguous device tensor of `numel` elements (fp32 unless `dtype` says otherwise), or None."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != (dtype or torch.float32) or not t.is_contiguous() or t.numel() != numel or t.device != like.device:
+        raise ValueError(f"{name} must be a contiguous {str(dtype or torch.float32)[6:]} tensor of {numel} elements on the first tensor's device")
+    return t.data_ptr()
+
+
+def _op_workspace(t, like):
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or t.device != like.device:
+        raise ValueError("workspace must be contiguous and on the first tensor's device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _op_call(fn, like, stream, *args):
+    """Calls fn(*args, stream) with the tensors' device current."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(like.device)
+    elif stream.device != like.device:
+        raise ValueError("stream belongs to another device than the tensors")
+    if torch.cuda.current_device() == like.device.index:
+        rc = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(like.device):
+            rc = fn(*args, stream.cuda_stream)
+    if rc:
+        raise DgcError(rc, _lib.dgc_last_error(None).decode())
+
+
+def norm_workspace_bytes(R: int, F: int) -> int:
+    return int(load().dgc_norm_workspace_bytes(int(R), int(F)))
+
+
+def norm_forward(x, y, *, gamma=None, beta=None, mean=None, rstd=None, eps: float = 1e-5, stream=None):
+    """dgc_norm_forward: y = layer norm of the rows of x [..., F] (y may be x); gamma, beta fp32 [F] or None (1, 0);
+    mean, rstd fp32, one entry a row, written if given."""
+    lib = load()
+    dt = _op_dtype(x, "x")
+    px, ldx = _op_rows(x, "x")
+    F = x.shape[-1]
+    R = x.numel() // F if F else 0
+    py, ldy = _op_rows(y, "y", x, (R, F))
+    _op_call(lib.dgc_norm_forward, x, stream, px, ldx, R, F, dt, _op_flat(gamma, "gamma", F, x), _op_flat(beta, "beta", F, x),
+             float(eps), py, ldy, _op_flat(mean, "mean", R, x), _op_flat(rstd, "rstd", R, x))
+    return y
+
+
+def norm_backward(dy, x, mean, rstd, dx, *, gamma=None, add=None, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """dgc_norm_backward: dx = gradient of x, plus `add` if given (dx may be dy, x or add); dgamma, dbeta fp32 [F], written if
+    given (they need `workspace`, norm_workspace_bytes(R, F) device bytes)."""
+    lib = load()
+    dt = _op_dtype(x, "x")
+    px, ldx = _op_rows(x, "x")
+    F = x.shape[-1]
+    R = x.numel() // F if F else 0
+    pdy, lddy = _op_rows(dy, "dy", x, (R, F))
+    padd, ldadd = _op_rows(add, "add", x, (R, F))
+    pdx, lddx = _op_rows(dx, "dx", x, (R, F))
+    ws, ws_bytes = _op_workspace(workspace, x)
+    _op_call(lib.dgc_norm_backward, x, stream, pdy, lddy, px, ldx, _op_flat(mean, "mean", R, x), _op_flat(rstd, "rstd", R, x), R, F,
+             dt, _op_flat(gamma, "gamma", F, x), padd, ldadd, pdx, lddx, _op_flat(dgamma, "dgamma", F, x),
+             _op_flat(dbeta, "dbeta", F, x), ws, ws_bytes)
+    return dx

@@ -1,0 +1,73 @@
+"""Refusals of the operators on plain tensors, without a GPU: every bad argument is answered with its status and a text
+before the device is used."""
+import os
+
+import pytest
+
+from paper_2309_03523_amd import binding
+
+OK, INVALID, UNSUPPORTED = 0, 1, 4
+A, B, C = 0x10000000, 0x20000000, 0x30000000      # aligned addresses far apart: never read, every check fails before
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(binding.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return binding.load()
+
+
+def _text(lib):
+    return lib.dgc_last_error(None).decode()
+
+
+def test_norm_refusals(lib):
+    good = dict(x=A, ldx=32, R=10, F=30, dtype=0, gamma=None, beta=None, eps=1e-5, y=B, ldy=32, mean=None, rstd=None, stream=None)
+
+    def fwd(**kw):
+        return lib.dgc_norm_forward(*{**good, **kw}.values())
+
+    for kw in (dict(x=None), dict(y=None), dict(x=A + 4), dict(y=B + 8), dict(ldx=28), dict(ldx=30), dict(ldy=29), dict(F=0), dict(F=8193, ldx=8196, ldy=8196),
+               dict(R=-1), dict(dtype=2), dict(eps=-1.0), dict(eps=float("nan")), dict(dtype=1, ldx=36), dict(ldx=1 << 62),
+               dict(y=A + 4 * 4 * 32), dict(y=A, ldy=36), dict(y=A + 16)):     # overlaps that are not the same rows
+        assert fwd(**kw) == INVALID, kw
+        assert "norm" in _text(lib)
+    assert fwd(R=0, x=None, y=None) == OK
+    good = dict(dy=C, lddy=32, x=A, ldx=32, mean=A, rstd=A, R=10, F=30, dtype=0, gamma=None, add=None, ldadd=0, dx=B, lddx=32, dgamma=None,
+                dbeta=None, ws=None, ws_bytes=0, stream=None)
+
+    def bwd(**kw):
+        return lib.dgc_norm_backward(*{**good, **kw}.values())
+
+    need = lib.dgc_norm_workspace_bytes(10, 30)
+    for kw in (dict(dy=None), dict(mean=None), dict(rstd=None), dict(dx=None), dict(add=B + 16, ldadd=32), dict(dx=A + 32, lddx=32), dict(dgamma=A),
+               dict(dbeta=A, ws=C, ws_bytes=need - 1), dict(dgamma=A, ws=C + 4, ws_bytes=need), dict(add=A, ldadd=29), dict(F=9000)):
+        assert bwd(**kw) == INVALID, kw
+        assert "norm" in _text(lib)
+    sizes = [lib.dgc_norm_workspace_bytes(r, 100) for r in (0, 1, 100, 10 ** 5, 10 ** 7, 10 ** 9)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
+    assert lib.dgc_norm_workspace_bytes(-1, 10) < 0 and lib.dgc_norm_workspace_bytes(1, 0) < 0 and lib.dgc_norm_workspace_bytes(1, 8193) < 0
+
+
+def test_columns_side_by_side_do_not_overlap(lib):
+    """Slices of one buffer, as a fused product leaves them, may be input and output of one call; a device is the next thing it needs."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    rc = lib.dgc_norm_forward(A, 64, 10, 30, 0, None, None, 1e-5, A + 32 * 4, 64, None, None, None)
+    assert rc == 6, _text(lib)
+
+
+def test_binding_refusals():
+    """What the binding itself refuses: element types, layouts, shapes, host tensors."""
+    import torch
+    x = torch.zeros(4, 32)
+    with pytest.raises(ValueError, match="device tensor"):
+        binding.norm_forward(x, x)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        binding.norm_forward(x.double(), x)
+    with pytest.raises(ValueError, match="contiguous last"):
+        binding._op_rows(torch.zeros(32, 4).t(), "x")
+    with pytest.raises(ValueError, match="one pitch"):
+        binding._op_rows(torch.zeros(4, 5, 8)[:, :3], "x")
