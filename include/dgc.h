@@ -470,6 +470,27 @@ dgc_status_t dgc_norm_backward(const void* dy, int64_t lddy, const void* x, int6
                                const void* add, int64_t ldadd, void* dx, int64_t lddx, float* dgamma, float* dbeta,
                                void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Products of R rows with a weight matrix, and their gradients.  x [R, K], w [M, K] (out, in), y [R, M].
+ *  forward:  p = x w^T + bias, y = act(p) + residual.  bias device fp32 [M], residual and pre [R, M], each NULL = none;
+ *   pre receives p, which the gradients of an activation need.  y may be residual itself.
+ *   act: RELU max(p, 0); GELU p P(X <= p) of a standard normal X; SILU p / (1 + e^-p).
+ *  backward: dp = dy act'(p) with p read from pre (NULL allowed with act NONE),
+ *   dx = dp w, dw = dp^T x, dbias = sum of dp over the rows (fp32 [M]); each may be NULL = not wanted (then x or w, which only
+ *   dw or dx read, may be NULL).  The residual's gradient is dy itself.  RELU's slope at 0 is 0.
+ *   workspace: dgc_linear_workspace_bytes(R, K, M, dtype, act) bytes (negative for arguments outside the range).
+ * K and M in [1, 65536].  x, w, residual, y, pre and the gradients dx, dw have the element type `dtype`, each rounded once from
+ * fp32 sums; dp is rounded to `dtype` before the products of dx and dw.  With fp32, products and sums are as exact as fp32
+ * arithmetic. */
+enum { DGC_LINEAR_NONE = 0, DGC_LINEAR_RELU = 1, DGC_LINEAR_GELU = 2, DGC_LINEAR_SILU = 3 };
+int64_t dgc_linear_workspace_bytes(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act);
+dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
+                                int32_t dtype, const float* bias, int32_t act, const void* residual, int64_t ldr,
+                                void* y, int64_t ldy, void* pre, int64_t ldpre, void* stream);
+dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                 int64_t R, int32_t K, int32_t M, int32_t dtype, const void* pre, int64_t ldpre,
+                                 int32_t act, void* dx, int64_t lddx, void* dw, int64_t lddw, float* dbias,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Text of the last error on this layer, or (layer = NULL) of the last failed create or layer-less
  * call on the calling thread.  Never NULL; valid until the next call on the same layer / thread. */
 const char* dgc_last_error(const dgc_layer_t* layer);

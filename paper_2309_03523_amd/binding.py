@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libdgc.so")
 
 TIME_KIND = {"none": 0, "gru": 1, "lstm": 2, "self_attn": 3}
 ACT = {"none": 0, "relu": 1}
+LINEAR_ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 GATHER = {"in_place": 0, "staged": 1}
 DENSE = {"auto": 0, "tile": 1, "wave": 2}
 AGG = {"table": 0, "walk": 1}
@@ -32,7 +33,8 @@ EXPORTS = ["dgc_layer_create", "dgc_layer_destroy", "dgc_layer_set_param", "dgc_
            "dgc_version", "dgc_stale_theta_factor", "dgc_stale_workspace_bytes", "dgc_stale_filter",
            "dgc_stale_static_max_candidates", "dgc_stale_filter_static",
            "dgc_layer_shared_rows", "dgc_fusion_select", "dgc_chunk_assign", "dgc_chunk_generate",
-           "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward"]
+           "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward",
+           "dgc_linear_workspace_bytes", "dgc_linear_forward", "dgc_linear_backward"]
 THETA_VARIANT = {"printed": 0, "sigmoid": 1}
 N_STAGES = 13
 
@@ -106,7 +108,10 @@ def load() -> ct.CDLL:
     lib.dgc_norm_forward.argtypes = [vp, i64, i64, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]
     lib.dgc_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
     lib.dgc_norm_workspace_bytes.argtypes = [i64, i32]
-    sizes = ("dgc_norm_workspace_bytes",)
+    lib.dgc_linear_forward.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp]
+    lib.dgc_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp]
+    lib.dgc_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes")
     for name in sizes:
         getattr(lib, name).restype = i64
     for name in EXPORTS:
@@ -403,7 +408,7 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
     return it.value, bool(conv.value)
 
 
-# --------------------------------------------------------------------------- layer norm
+# --------------------------------------------------------------------------- layer norm, products of rows
 #
 # Operators on plain device tensors: nothing is allocated, outputs and workspaces are the caller's, work is only
 # enqueued on `stream` (default: the current stream of the tensors' device).
@@ -511,3 +516,45 @@ def norm_backward(dy, x, mean, rstd, dx, *, gamma=None, add=None, dgamma=None, d
              dt, _op_flat(gamma, "gamma", F, x), padd, ldadd, pdx, lddx, _op_flat(dgamma, "dgamma", F, x),
              _op_flat(dbeta, "dbeta", F, x), ws, ws_bytes)
     return dx
+
+
+def linear_workspace_bytes(R: int, K: int, M: int, *, dtype: str = "f32", act: str = "gelu") -> int:
+    """Bytes that linear_backward needs; without an activation it needs less."""
+    return int(load().dgc_linear_workspace_bytes(int(R), int(K), int(M), DTYPE[dtype], LINEAR_ACT[act]))
+
+
+def linear_forward(x, w, y, *, bias=None, act: str = "none", residual=None, pre=None, stream=None):
+    """dgc_linear_forward: y = act(x w^T + bias) + residual for rows x [..., K], w [M, K] (out, in), y [..., M] of one element
+    type; bias fp32 [M]; pre [..., M] receives the activation's argument; y may be residual itself."""
+    lib = load()
+    dt = _op_dtype(x, "x")
+    px, ldx = _op_rows(x, "x")
+    K = x.shape[-1]
+    R = x.numel() // K if K else 0
+    M = w.shape[0]
+    pw, ldw = _op_rows(w, "w", x, (M, K))
+    py, ldy = _op_rows(y, "y", x, (R, M))
+    pr, ldr = _op_rows(residual, "residual", x, (R, M))
+    pp, ldp = _op_rows(pre, "pre", x, (R, M))
+    _op_call(lib.dgc_linear_forward, x, stream, px, ldx, pw, ldw, R, K, M, dt, _op_flat(bias, "bias", M, x), LINEAR_ACT[act], pr, ldr,
+             py, ldy, pp, ldp)
+    return y
+
+
+def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, dbias=None, workspace, stream=None):
+    """dgc_linear_backward: the wanted ones of dx [..., K], dw [M, K] and dbias fp32 [M] from dy [..., M]; `pre`: what
+    linear_forward left, needed with an activation; workspace: linear_workspace_bytes device bytes."""
+    lib = load()
+    dt = _op_dtype(x, "x")
+    px, ldx = _op_rows(x, "x")
+    K = x.shape[-1]
+    R = x.numel() // K if K else 0
+    M = w.shape[0]
+    pw, ldw = _op_rows(w, "w", x, (M, K))
+    pdy, lddy = _op_rows(dy, "dy", x, (R, M))
+    pp, ldp = _op_rows(pre, "pre", x, (R, M))
+    pdx, lddx = _op_rows(dx, "dx", x, (R, K))
+    pdw, lddw = _op_rows(dw, "dw", x, (M, K))
+    ws, ws_bytes = _op_workspace(workspace, x)
+    _op_call(lib.dgc_linear_backward, x, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, dt, pp, ldp, LINEAR_ACT[act], pdx, lddx, pdw, lddw,
+             _op_flat(dbias, "dbias", M, x), ws, ws_bytes)

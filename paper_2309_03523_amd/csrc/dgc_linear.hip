@@ -1,0 +1,683 @@
+// Products of rows with a weight matrix, with bias, activation and residual in the epilogue, and their gradients.
+//
+//   p = x w^T + bias, y = act(p) + residual          x [R, K], w [M, K], y [R, M]
+//   dp = dy act'(p), dx = dp w, dw = dp^T x, dbias = sum over rows of dp
+//
+// One tile kernel does the three products: out[q][p] = sum over c of Q(q, c) P(p, c), where either operand's contraction
+// index c lies along its rows (x, w, dp in the forward pass and in dx) or across them (w in dx; dp and x in dw).  It runs on
+// v_mfma_f32_32x32x16_bf16 with P as the A operand: lane l holds outputs p = 8g + 4(l/32) + e of its own row q = l%32.
+//
+//  - Operand tiles are staged through registers into LDS, in units of 8 numbers along c, while the tile before is multiplied.
+//    Tiles across c are read in pieces of a few columns by 8 rows and turned in registers.  A unit's place within its row
+//    is rotated by the row, so that neither the fragments' reads nor the writes of turned pieces meet in a bank.
+//  - bf16 numbers are taken as they are and summed in fp32.  An fp32 number is split into three bf16 parts, which hold it exactly
+//    (dgc_split_dev.h), and a product is the sum of the six part products above 2^-24 of it.  The matrix unit cuts its sums off,
+//    so for fp32 those of 32 terms are added up by the vector unit, which rounds: errors as of an fp32 product, 2e-7.
+//  - dw is a sum over all rows with a small result: the rows are split over workgroups, each writes an fp32 partial, and a
+//    second kernel adds them in order.  No atomics: the same inputs give the same bits.
+//  - Up to 32 rows (a few vertices served at once) read every weight once and multiply little: a workgroup takes 32 output
+//    columns, its 8 waves a share of the contraction each, and fragments come straight from memory.
+#include <algorithm>
+
+#include "dgc_ops.h"
+#include "dgc_split_dev.h"
+
+namespace dgc {
+namespace {
+
+using ops::Elem;
+using split::as_frag;
+using split::bf16x8;
+using split::floatx16;
+
+constexpr int kMaxDim = 65536;      // K, M
+constexpr int kFewRows = 32;
+constexpr int64_t kMostTiles = 1 << 20;   // workgroups of one launch; more tiles are taken in turns
+constexpr int kSplitBlocks = 1024;  // workgroups that dw is split over, about
+constexpr int kSplitRows = 512;     // rows of a share of dw at least
+constexpr int kSumBlocks = 1024, kMostSums = 512;   // as for the norm's weight gradients
+
+// ---------------------------------------------------------------------------------------------- activations
+// erfc(z) exp(z^2) for z >= 0 by Abramowitz and Stegun 7.1.26, off by at most 1.5e-7 exp(z^2): a fp32 rounding of erf, and far
+// below a bf16 one.  A fifth of the library call's instructions, which took longer than the memory traffic of a wide layer.
+__device__ __forceinline__ float erfc_scaled(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+  float s = fmaf(1.061405429f, t, -1.453152027f);
+  s = fmaf(s, t, 1.421413741f);
+  s = fmaf(s, t, -0.284496736f);
+  return fmaf(s, t, 0.254829592f) * t;
+}
+constexpr float kRootHalf = 0.70710678118654752f, kInvRoot2Pi = 0.39894228040143268f, kLog2e = 1.4426950408889634f;
+
+template <class T>
+__device__ __forceinline__ float normal_below(float p, float& density) {   // P(X <= p), and exp(-p^2 / 2)
+  if constexpr (sizeof(T) == 4) {
+    density = expf(-0.5f * p * p);
+    return 0.5f * erfcf(-p * kRootHalf);
+  } else {
+    density = __builtin_amdgcn_exp2f(-0.5f * kLog2e * p * p);
+    const float tail = 0.5f * erfc_scaled(fabsf(p) * kRootHalf) * density;
+    return p < 0.f ? tail : 1.f - tail;
+  }
+}
+template <class T>
+__device__ __forceinline__ float logistic(float p) {
+  if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-p));
+  else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * p));
+}
+template <class T>
+__device__ __forceinline__ float activate(float p, int act) {
+  float e;
+  if (act == DGC_LINEAR_RELU) return p <= 0.f ? 0.f : p;     // a NaN stays one
+  if (act == DGC_LINEAR_GELU) return p * normal_below<T>(p, e);
+  if (act == DGC_LINEAR_SILU) return p * logistic<T>(p);
+  return p;
+}
+template <class T>
+__device__ __forceinline__ float slope_times(float dy, float p, int act) {
+  if (act == DGC_LINEAR_RELU) return p <= 0.f ? 0.f : dy;
+  if (act == DGC_LINEAR_GELU) {
+    float e;
+    const float below = normal_below<T>(p, e);
+    return dy * fmaf(p * kInvRoot2Pi, e, below);
+  }
+  if (act == DGC_LINEAR_SILU) {
+    const float s = logistic<T>(p);
+    return dy * s * fmaf(p, 1.f - s, 1.f);
+  }
+  return dy;
+}
+
+// ---------------------------------------------------------------------------------------------- operands
+
+template <class T> struct Kind;
+template <> struct Kind<uint16_t> { static constexpr int kBK = 64, kParts = 1; };
+template <> struct Kind<float> { static constexpr int kBK = 32, kParts = 3; };
+
+// The unit of 8 numbers `u` of tile row r: its place in LDS.
+template <int UK>
+__device__ __forceinline__ int place(int r, int u) {
+  if constexpr (UK == 8) return r * 8 + (u ^ ((r + (r >> 3)) & 7));
+  else return r * 4 + (u ^ (((r >> 1) + (r >> 3)) & 3));
+}
+__device__ __forceinline__ void put_unit(uint4* lds, int stride, int at, const uint4& u) { lds[at] = u; }
+__device__ __forceinline__ void put_unit(uint4* lds, int stride, int at, const float (&x)[8]) {
+  uint4 p[3];
+  split::split8(x, p);
+#pragma unroll
+  for (int q = 0; q < 3; ++q) lds[q * stride + at] = p[q];
+}
+
+// Eight numbers along the contraction from `k` of row `p`; from K on they are zero (a pitch's padding may hold anything).
+__device__ __forceinline__ void load_unit(const uint16_t* p, int64_t k, int64_t K, uint4& u) {
+  u = *reinterpret_cast<const uint4*>(p + k);
+  if (k + 8 > K) {
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] &= (k + 2 * i < K ? 0xffffu : 0u) | (k + 2 * i + 1 < K ? 0xffff0000u : 0u);
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+__device__ __forceinline__ void load_unit(const float* p, int64_t k, int64_t K, float (&x)[8]) {
+  ops::load_vec(p + k, 0, (int)min((int64_t)8, K - k), x);
+  ops::load_vec(p + k, 4, (int)min((int64_t)8, K - k), x + 4);
+}
+__device__ __forceinline__ void zero_unit(uint4& u) { u = make_uint4(0, 0, 0, 0); }
+__device__ __forceinline__ void zero_unit(float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = 0.f;
+}
+template <class T> struct UnitOf { typedef uint4 type; };
+template <> struct UnitOf<float> { typedef float type[8]; };
+
+// A tile of BX rows (of P or Q) by kBK of the contraction on its way from memory to LDS, by 256 threads.
+template <class T, int BX, bool ACROSS> struct Stage;
+
+template <class T, int BX> struct Stage<T, BX, false> {   // the contraction lies along the tensor's rows
+  static constexpr int BK = Kind<T>::kBK, UK = BK / 8, N = BX * UK / 256;
+  typename UnitOf<T>::type unit[N];
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t K) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      const int64_t x = x0 + idx / UK, k = k0 + idx % UK * 8;
+      if (x < X && k < K) load_unit(base + x * ld, k, K, unit[i]);
+      else zero_unit(unit[i]);
+    }
+  }
+  __device__ __forceinline__ void store(uint4* lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      put_unit(lds, BX * UK, place<UK>(idx / UK, idx % UK), unit[i]);
+    }
+  }
+};
+
+template <class T, int BX> struct Stage<T, BX, true> {    // the contraction goes from row to row: pieces of W columns by 8 rows
+  static constexpr int BK = Kind<T>::kBK, UK = BK / 8, W = BX * UK / 256, WORDS = W * (int)sizeof(T) / 4;
+  uint32_t piece[8][WORDS];
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t K) {
+    const int64_t x = x0 + threadIdx.x % (BX / W) * W, k = k0 + threadIdx.x / (BX / W) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // a piece with a column below X lies within the pitch; its columns from X on reach no output that is kept
+      const bool in = x < X && k + j < K;
+      const T* at = base + (k + j) * ld + x;
+      if constexpr (WORDS == 2) {
+        const uint2 v = in ? *reinterpret_cast<const uint2*>(at) : make_uint2(0, 0);
+        piece[j][0] = v.x; piece[j][1] = v.y;
+      } else {
+        piece[j][0] = in ? *reinterpret_cast<const uint32_t*>(at) : 0u;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint4* lds) const {
+    const int row = threadIdx.x % (BX / W) * W, u = threadIdx.x / (BX / W);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t sel = w & 1 ? 0x07060302u : 0x05040100u;   // the upper or lower halves of two words
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_perm(piece[2 * i + 1][w / 2], piece[2 * i][w / 2], sel);
+        put_unit(lds, BX * UK, place<UK>(row + w, u), make_uint4(o[0], o[1], o[2], o[3]));
+      } else {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(piece[j][w]);
+        put_unit(lds, BX * UK, place<UK>(row + w, u), x);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------------------------- the tile kernel
+
+struct LinearArgs {
+  const void* P; int64_t ldp; int64_t NP;   // NP columns of the output
+  const void* Q; int64_t ldq; int64_t NQ;   // NQ rows of it
+  int64_t C;                                // contraction
+  int64_t share;                            // contraction of one part (a multiple of kBK); parts > 1: partial sums
+  int32_t parts;
+  int32_t act;
+  void* out; int64_t ldo;
+  const float* bias;
+  const void* residual; int64_t ldr;
+  void* pre; int64_t ldpre;
+  float* partial;                           // [parts][NQ][NP rounded up to 4]
+};
+
+// Four outputs of one row from column p (a multiple of 4) on: bias, pre-activation, activation, residual.
+template <class T>
+__device__ __forceinline__ void finish4(const LinearArgs& a, int64_t q, int64_t p, float (&v)[4]) {
+  typedef typename std::conditional<sizeof(T) == 4, uint4, uint2>::type Pack;
+  const int n = (int)min((int64_t)4, a.NP - p);
+  auto store = [&](void* base, int64_t ld, const float (&x)[4]) {
+    T* to = static_cast<T*>(base) + q * ld + p;
+    if (n == 4) {
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<Pack*>(to) = Elem<float>::pack(x);
+      else *reinterpret_cast<Pack*>(to) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) { if (i < n) to[i] = Elem<T>::one(x[i]); }
+    }
+  };
+  if (a.bias) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += i < n ? a.bias[p + i] : 0.f;
+  }
+  if (a.pre) store(a.pre, a.ldpre, v);
+  if (a.act != DGC_LINEAR_NONE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = activate<T>(v[i], a.act);
+  }
+  if (a.residual) {
+    const T* from = static_cast<const T*>(a.residual) + q * a.ldr + p;    // four of a row's pitch, at least one of them below NP
+    float r[4];
+    if constexpr (sizeof(T) == 4) {
+      Elem<float>::unpack(*reinterpret_cast<const uint4*>(from), r);
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(from);
+      r[0] = split::bf_lo(u.x); r[1] = split::bf_hi(u.x); r[2] = split::bf_lo(u.y); r[3] = split::bf_hi(u.y);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += r[i];
+  }
+  store(a.out, a.ldo, v);
+}
+
+// BP x BQ outputs a workgroup, a quarter of them a wave.
+template <class T, int BP, int BQ, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
+__global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
+  constexpr int BK = Kind<T>::kBK, UK = BK / 8, PARTS = Kind<T>::kParts, FP = BP / 64, FQ = BQ / 64;
+  __shared__ uint4 lds_p[PARTS * BP * UK];
+  __shared__ uint4 lds_q[PARTS * BQ * UK];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int wp = (wave & 1) * (BP / 2), wq = (wave >> 1) * (BQ / 2);
+  const int64_t np = (a.NP + BP - 1) / BP, nq = (a.NQ + BQ - 1) / BQ, tiles = np * nq * a.parts;
+  // Workgroups go round the 8 XCDs: neighbours in the list of tiles, which share rows of Q, stay on one of them and its L2.
+  const int64_t per = (tiles + 7) / 8;
+  for (int64_t local = blockIdx.x >> 3; local < per; local += gridDim.x >> 3) {
+    const int64_t id = (int64_t)(blockIdx.x & 7) * per + local;
+    if (id >= tiles) break;
+    const int64_t p0 = id % np * BP, q0 = id / np % nq * BQ;
+    const int part = (int)(id / (np * nq));
+    const int64_t c0 = (int64_t)part * a.share, c1 = min(a.C, c0 + a.share);
+    const T* P = static_cast<const T*>(a.P);
+    const T* Q = static_cast<const T*>(a.Q);
+    Stage<T, BP, ACROSS_P> sp;
+    Stage<T, BQ, ACROSS_Q> sq;
+    floatx16 acc[FP][FQ];
+#pragma unroll
+    for (int i = 0; i < FP; ++i) {
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[i][j] = floatx16{};
+    }
+    sp.load(P, a.ldp, p0, a.NP, c0, c1);
+    sq.load(Q, a.ldq, q0, a.NQ, c0, c1);
+    for (int64_t c = c0; c < c1; c += BK) {
+      __syncthreads();
+      sp.store(lds_p);
+      sq.store(lds_q);
+      __syncthreads();
+      if (c + BK < c1) {
+        sp.load(P, a.ldp, p0, a.NP, c + BK, c1);
+        sq.load(Q, a.ldq, q0, a.NQ, c + BK, c1);
+      }
+      if constexpr (PARTS == 1) {
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+          bf16x8 fp[FP], fq[FQ];
+#pragma unroll
+          for (int i = 0; i < FP; ++i) fp[i] = as_frag(lds_p[place<UK>(wp + 32 * i + (lane & 31), 2 * s + half)]);
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) fq[j] = as_frag(lds_q[place<UK>(wq + 32 * j + (lane & 31), 2 * s + half)]);
+#pragma unroll
+          for (int i = 0; i < FP; ++i) {
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+          }
+        }
+      } else {
+        floatx16 sum[FP][FQ];
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) sum[i][j] = floatx16{};
+        }
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+          uint4 fp[FP][3], fq[FQ][3];
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+#pragma unroll
+            for (int i = 0; i < FP; ++i) fp[i][k] = lds_p[k * BP * UK + place<UK>(wp + 32 * i + (lane & 31), 2 * s + half)];
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fq[j][k] = lds_q[k * BQ * UK + place<UK>(wq + 32 * j + (lane & 31), 2 * s + half)];
+          }
+#pragma unroll
+          for (int i = 0; i < FP; ++i) {
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) split::six(sum[i][j], sum[i][j], fp[i], fq[j]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) acc[i][j] += sum[i][j];
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int64_t q = q0 + wq + 32 * j + (lane & 31);
+      if (q >= a.NQ) continue;
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int64_t p = p0 + wp + 32 * i + 8 * g + 4 * half;
+          if (p >= a.NP) continue;
+          float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          if constexpr (PARTIAL) {
+            const int64_t pitch = (a.NP + 3) / 4 * 4;
+            *reinterpret_cast<uint4*>(a.partial + ((int64_t)part * a.NQ + q) * pitch + p) = Elem<float>::pack(v);
+          } else {
+            finish4<T>(a, q, p, v);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Up to 32 rows of Q: 32 columns a workgroup, 8 waves that take 64 of the contraction at a time in turn.
+template <class T>
+__global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
+  __shared__ float joined[8][16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int64_t p0 = (int64_t)blockIdx.x * 32, p = p0 + (lane & 31), q = lane & 31;
+  const T* P = static_cast<const T*>(a.P) + p * a.ldp;
+  const T* Q = static_cast<const T*>(a.Q) + q * a.ldq;
+  floatx16 acc = floatx16{};
+  for (int64_t c = wave * 64; c < a.C; c += 8 * 64) {
+    typename UnitOf<T>::type up[4], uq[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int64_t k = c + 16 * s + 8 * half;
+      if (p < a.NP && k < a.C) load_unit(P, k, a.C, up[s]);
+      else zero_unit(up[s]);
+      if (q < a.NQ && k < a.C) load_unit(Q, k, a.C, uq[s]);
+      else zero_unit(uq[s]);
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(up[s]), as_frag(uq[s]), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; s += 2) {
+        floatx16 sum = floatx16{};
+#pragma unroll
+        for (int t = s; t < s + 2; ++t) {
+          uint4 fp[3], fq[3];
+          split::split8(up[t], fp);
+          split::split8(uq[t], fq);
+          split::six(sum, sum, fp, fq);
+        }
+        acc += sum;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) joined[wave][i][lane] = acc[i];
+  __syncthreads();
+  // a thread finishes four columns of a row: register 4 g + e of lane (row, half) is column 8 g + 4 half + e
+  if (threadIdx.x < 256) {
+    const int g = threadIdx.x >> 6;
+    const int64_t col = p0 + 8 * g + 4 * half;
+    float v[4] = {};
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += joined[w][4 * g + e][lane];
+    }
+    if (q < a.NQ && col < a.NP) finish4<T>(a, q, col, v);
+  }
+}
+
+// The partial sums of dw, in the order of the rows.
+template <class T>
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+  const int64_t pitch = (a.NP + 3) / 4, n = a.NQ * pitch;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t q = i / pitch, p = i % pitch * 4;
+    float v[4] = {};
+    for (int part = 0; part < a.parts; ++part) {
+      float x[4];
+      Elem<float>::unpack(*reinterpret_cast<const uint4*>(a.partial + (part * n + i) * 4), x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e];
+    }
+    finish4<T>(a, q, p, v);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- dp and dbias
+
+struct SlopeArgs {
+  const void* dy; int64_t lddy;
+  const void* pre; int64_t ldpre;
+  void* dp; int64_t lddp;        // nullptr: act is none, dp is dy itself
+  float* partial;                // [workgroups][M], or nullptr
+  int64_t R;
+  int32_t M;
+  int32_t act;
+};
+
+// LPR lanes a row, 256 / LPR rows at a time; blockIdx.y: which LPR vectors of a wide row.
+template <class T, int LPR>
+__global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs a) {
+  constexpr int VN = Elem<T>::kPer, GROUPS = 256 / LPR, U = 4;
+  __shared__ float joined[256 * VN];
+  const int sub = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  const int col = ((int)blockIdx.y * LPR + sub) * VN;
+  float sum[VN] = {};
+  for (int64_t base = (int64_t)blockIdx.x * (GROUPS * U); base < a.R; base += (int64_t)gridDim.x * (GROUPS * U)) {
+    float dy[U][VN], p[U][VN];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = base + u * GROUPS + grp;
+      ops::load_vec(static_cast<const T*>(a.dy) + r * a.lddy, col, r < a.R ? a.M : 0, dy[u]);
+      if (a.dp) ops::load_vec(static_cast<const T*>(a.pre) + r * a.ldpre, col, r < a.R ? a.M : 0, p[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = base + u * GROUPS + grp;
+      if (a.dp) {
+#pragma unroll
+        for (int i = 0; i < VN; ++i) dy[u][i] = slope_times<T>(dy[u][i], p[u][i], a.act);
+        // dp is rounded to the element type, the form in which the matrix unit takes it; dbias sums what it was before
+        if (r < a.R && col < a.M) *reinterpret_cast<uint4*>(static_cast<T*>(a.dp) + r * a.lddp + col) = Elem<T>::pack(dy[u]);
+      }
+#pragma unroll
+      for (int i = 0; i < VN; ++i) sum[i] += dy[u][i];
+    }
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int i = 0; i < VN; ++i) joined[threadIdx.x * VN + i] = sum[i];
+  __syncthreads();
+  for (int c = threadIdx.x; c < LPR * VN; c += 256) {
+    const int64_t m = (int64_t)blockIdx.y * LPR * VN + c;
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) s += joined[k * LPR * VN + c];
+    if (m < a.M) a.partial[(int64_t)blockIdx.x * a.M + m] = s;
+  }
+}
+
+int slope_lanes(int32_t M, int per) {
+  const int vecs = (M + per - 1) / per;
+  int lpr = 8;
+  while (lpr < vecs && lpr < 256) lpr *= 2;
+  return lpr;
+}
+int64_t slope_blocks(int64_t R, int32_t M, int per) {
+  const int64_t rows = 256 / slope_lanes(M, per) * 4, turns = (R + rows - 1) / rows;
+  const int64_t wide = ((M + per - 1) / per + 255) / 256;      // blockIdx.y
+  return std::max<int64_t>(std::min<int64_t>(turns, std::max<int64_t>(kSumBlocks / wide, 64)), (turns * 4 + kMostSums - 1) / kMostSums);
+}
+
+template <class T>
+void launch_slope(const SlopeArgs& a, int64_t blocks, hipStream_t st) {
+  const int per = Elem<T>::kPer, lpr = slope_lanes(a.M, per), vecs = (a.M + per - 1) / per;
+  const dim3 grid((unsigned)blocks, (unsigned)((vecs + lpr - 1) / lpr));
+  if (lpr == 8) hipLaunchKernelGGL((k_linear_slope<T, 8>), grid, 256, 0, st, a);
+  else if (lpr == 16) hipLaunchKernelGGL((k_linear_slope<T, 16>), grid, 256, 0, st, a);
+  else if (lpr == 32) hipLaunchKernelGGL((k_linear_slope<T, 32>), grid, 256, 0, st, a);
+  else if (lpr == 64) hipLaunchKernelGGL((k_linear_slope<T, 64>), grid, 256, 0, st, a);
+  else if (lpr == 128) hipLaunchKernelGGL((k_linear_slope<T, 128>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_linear_slope<T, 256>), grid, 256, 0, st, a);
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+// 128 x 128 outputs a workgroup; 64 x 64 where that leaves compute units without work, or the output is that narrow.
+bool small_tiles(int64_t NP, int64_t NQ) { return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < 256; }
+
+template <class T, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
+void launch_tiles(const LinearArgs& a, bool small, hipStream_t st) {
+  const int64_t b = small ? 64 : 128, tiles = ((a.NP + b - 1) / b) * ((a.NQ + b - 1) / b) * a.parts;
+  const unsigned grid = (unsigned)(std::min<int64_t>((tiles + 7) / 8, kMostTiles / 8) * 8);
+  if (small) hipLaunchKernelGGL((k_linear<T, 64, 64, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_linear<T, 128, 128, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
+}
+
+// How dw's rows are split: enough shares to fill the chip, none below kSplitRows.
+struct Split { bool small; int32_t parts; int64_t share; };
+Split split_of(int64_t R, int64_t K, int64_t M) {
+  Split s;
+  s.small = K <= 64 || M <= 64;
+  const int64_t b = s.small ? 64 : 128, tiles = ((K + b - 1) / b) * ((M + b - 1) / b);
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kSplitBlocks / tiles, (R + kSplitRows - 1) / kSplitRows));
+  s.share = std::max<int64_t>(64, ((R + parts - 1) / parts + 63) / 64 * 64);
+  s.parts = (int32_t)std::max<int64_t>(1, (R + s.share - 1) / s.share);
+  return s;
+}
+
+struct Room { int64_t dp, sums, partial, all; };   // where each starts in the workspace, bytes
+Room room_of(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
+  const int e = ops::elem_bytes(dtype), per = 16 / e;
+  const Split s = split_of(R, K, M);
+  Room r;
+  r.dp = 0;
+  r.sums = act == DGC_LINEAR_NONE ? 0 : R * ((M + per - 1) / per * per) * e;
+  r.partial = r.sums + (slope_blocks(R, M, per) * M + 3) / 4 * 16;
+  r.all = r.partial + (s.parts > 1 ? 4 * (int64_t)s.parts * M * ((K + 3) / 4 * 4) : 0) + 16;
+  return r;
+}
+
+// Partial rows of dbias [parts][M] -> dbias, in double: 16 columns a workgroup, 64 partial rows at a time.
+__global__ __launch_bounds__(1024) void k_linear_dbias(const float* partial, int64_t parts, int32_t M, float* dbias) {
+  __shared__ double lds[64][16];
+  const int c = threadIdx.x & 15, p = threadIdx.x >> 4;
+  const int64_t col = (int64_t)blockIdx.x * 16 + c;
+  double s = 0.;
+  if (col < M) {
+    for (int64_t k = p; k < parts; k += 64) s += (double)partial[k * M + col];
+  }
+  lds[p][c] = s;
+  __syncthreads();
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    if (p < m) lds[p][c] += lds[p + m][c];
+    __syncthreads();
+  }
+  if (p == 0 && col < M) dbias[col] = (float)lds[0][c];
+}
+
+template <class T>
+void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
+              const void* pre, int64_t ldpre, int32_t act, void* dx, int64_t lddx, void* dw, int64_t lddw, float* dbias,
+              char* workspace, const Room& room, hipStream_t st) {
+  const void* dp = dy;
+  int64_t lddp = lddy;
+  const int64_t blocks = slope_blocks(R, M, Elem<T>::kPer);
+  float* sums = reinterpret_cast<float*>(workspace + room.sums);
+  if (R > 0 && (dbias || act != DGC_LINEAR_NONE)) {
+    SlopeArgs s{};
+    s.dy = dy; s.lddy = lddy; s.pre = pre; s.ldpre = ldpre; s.R = R; s.M = M; s.act = act;
+    s.partial = dbias ? sums : nullptr;
+    if (act != DGC_LINEAR_NONE) {
+      s.dp = workspace + room.dp;
+      s.lddp = (M + Elem<T>::kPer - 1) / Elem<T>::kPer * Elem<T>::kPer;
+      dp = s.dp; lddp = s.lddp;
+    }
+    launch_slope<T>(s, blocks, st);
+  }
+  if (dbias) hipLaunchKernelGGL(k_linear_dbias, (unsigned)((M + 15) / 16), 1024, 0, st, sums, R > 0 ? blocks : 0, M, dbias);
+  if (dw) {
+    const Split s = split_of(R, K, M);
+    LinearArgs a{};
+    a.P = x; a.ldp = ldx; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = M; a.C = R; a.share = s.share; a.parts = s.parts;
+    a.out = dw; a.ldo = lddw; a.partial = reinterpret_cast<float*>(workspace + room.partial);
+    if (s.parts == 1) {
+      launch_tiles<T, true, true, false>(a, s.small, st);
+    } else {
+      launch_tiles<T, true, true, true>(a, s.small, st);
+      const int64_t n = (int64_t)M * ((K + 3) / 4);
+      hipLaunchKernelGGL(k_linear_join<T>, (unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, st, a);
+    }
+  }
+  if (dx && R > 0) {
+    LinearArgs a{};
+    a.P = w; a.ldp = ldw; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
+    a.out = dx; a.ldo = lddx;
+    launch_tiles<T, true, false, false>(a, small_tiles(a.NP, a.NQ), st);
+  }
+}
+
+const char* check(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
+  if (dtype != DGC_DTYPE_F32 && dtype != DGC_DTYPE_BF16) return "linear: unknown dtype";
+  if (R < 0 || K < 1 || M < 1 || K > kMaxDim || M > kMaxDim) return "linear: R must be >= 0, K and M in [1, 65536]";
+  if (R > INT64_MAX / 8 / kMaxDim) return "linear: too many rows";
+  if (act < DGC_LINEAR_NONE || act > DGC_LINEAR_SILU) return "linear: unknown activation";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace dgc
+
+using namespace dgc;
+
+extern "C" {
+
+int64_t dgc_linear_workspace_bytes(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
+  if (check(R, K, M, dtype, act)) return -1;
+  return room_of(R, K, M, dtype, act).all;
+}
+
+dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
+                                int32_t dtype, const float* bias, int32_t act, const void* residual, int64_t ldr, void* y,
+                                int64_t ldy, void* pre, int64_t ldpre, void* stream) {
+  if (const char* msg = check(R, K, M, dtype, act)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
+  const int e = ops::elem_bytes(dtype);
+  if (!ops::good_rows(x, R, K, ldx, e) || !ops::good_rows(w, M, K, ldw, e) || !ops::good_rows(y, R, M, ldy, e) ||
+      (residual && !ops::good_rows(residual, R, M, ldr, e)) || (pre && !ops::good_rows(pre, R, M, ldpre, e)))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "linear: x, w, residual, y, pre need a 16-byte aligned base and a pitch that holds a row and is a multiple of 16 bytes");
+  if (ops::share(x, ldx, e, K, y, ldy, e, M, R) || ops::share(x, ldx, e, K, pre, ldpre, e, M, R) ||
+      ops::share(y, ldy, e, M, pre, ldpre, e, M, R) || ops::share(residual, ldr, e, M, pre, ldpre, e, M, R) ||
+      (!ops::same_place(residual, ldr, y, ldy) && ops::share(residual, ldr, e, M, y, ldy, e, M, R)) ||
+      ops::span_shared(w, ldw, e, K, M, y, ldy, e, M, R) || ops::span_shared(w, ldw, e, K, M, pre, ldpre, e, M, R))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "linear: y and pre lie apart from the inputs and each other (y may be residual itself)");
+  if (R == 0) return DGC_OK;
+  LinearArgs a{};
+  a.P = w; a.ldp = ldw; a.NP = M; a.Q = x; a.ldq = ldx; a.NQ = R; a.C = K; a.share = (K + 63) / 64 * 64; a.parts = 1; a.act = act;
+  a.out = y; a.ldo = ldy; a.bias = bias; a.residual = residual; a.ldr = ldr; a.pre = pre; a.ldpre = ldpre;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (R <= kFewRows) {
+    const unsigned grid = (unsigned)((M + 31) / 32);
+    if (dtype == DGC_DTYPE_F32) hipLaunchKernelGGL(k_linear_few<float>, grid, 512, 0, st, a);
+    else hipLaunchKernelGGL(k_linear_few<uint16_t>, grid, 512, 0, st, a);
+  } else if (dtype == DGC_DTYPE_F32) {
+    launch_tiles<float, false, false, false>(a, small_tiles(M, R), st);
+  } else {
+    launch_tiles<uint16_t, false, false, false>(a, small_tiles(M, R), st);
+  }
+  return ops::launched("linear");
+}
+
+dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R,
+                                 int32_t K, int32_t M, int32_t dtype, const void* pre, int64_t ldpre, int32_t act, void* dx,
+                                 int64_t lddx, void* dw, int64_t lddw, float* dbias, void* workspace, int64_t workspace_bytes,
+                                 void* stream) {
+  if (const char* msg = check(R, K, M, dtype, act)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
+  const int e = ops::elem_bytes(dtype);
+  const bool pre_used = act != DGC_LINEAR_NONE;
+  if (!ops::good_rows(dy, R, M, lddy, e) || (dw && !ops::good_rows(x, R, K, ldx, e)) || (dx && !ops::good_rows(w, M, K, ldw, e)) ||
+      (pre_used && !ops::good_rows(pre, R, M, ldpre, e)) || (dx && !ops::good_rows(dx, R, K, lddx, e)) ||
+      (dw && !ops::good_rows(dw, M, K, lddw, e)))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "linear: dy, x, w, pre, dx, dw need a 16-byte aligned base and a pitch that holds a row and is a multiple of 16 bytes");
+  if (!dw) x = nullptr;
+  if (!dx) w = nullptr;
+  if (!pre_used) pre = nullptr;
+  if (ops::share(dx, lddx, e, K, dy, lddy, e, M, R) || ops::share(dx, lddx, e, K, x, ldx, e, K, R) ||
+      ops::share(dx, lddx, e, K, pre, ldpre, e, M, R) || ops::span_shared(w, ldw, e, K, M, dx, lddx, e, K, R) ||
+      ops::span_shared(dw, lddw, e, K, M, dx, lddx, e, K, R) || ops::span_shared(dw, lddw, e, K, M, dy, lddy, e, M, R) ||
+      ops::span_shared(dw, lddw, e, K, M, x, ldx, e, K, R) || ops::span_shared(dw, lddw, e, K, M, pre, ldpre, e, M, R) ||
+      ops::share(dw, lddw, e, K, w, ldw, e, K, M))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "linear: dx and dw lie apart from the inputs and each other");
+  const Room room = room_of(R, K, M, dtype, act);
+  if (!workspace || !ops::aligned16(workspace) || workspace_bytes < room.all)
+    return ops::refuse(DGC_ERR_INVALID_ARG, "linear: workspace missing, too small (dgc_linear_workspace_bytes) or not 16-byte aligned");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  if (dtype == DGC_DTYPE_F32)
+    backward<float>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, act, dx, lddx, dw, lddw, dbias, ws, room, st);
+  else
+    backward<uint16_t>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, act, dx, lddx, dw, lddw, dbias, ws, room, st);
+  return ops::launched("linear");
+}
+
+}  // extern "C"

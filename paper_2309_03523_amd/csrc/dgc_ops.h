@@ -97,6 +97,12 @@ inline bool share(const void* a, int64_t lda, int ea, int64_t Fa, const void* b,
   const uint64_t d = a0 >= b0 ? (a0 - b0) % pa : (pa - (b0 - a0) % pa) % pa;   // where a row of a starts in one of b
   return d < wb || d + wa > pa;
 }
+// The same for tensors of different numbers of rows, by their spans alone.
+inline bool span_shared(const void* a, int64_t lda, int ea, int64_t Fa, int64_t Ra, const void* b, int64_t ldb, int eb, int64_t Fb, int64_t Rb) {
+  if (!a || !b || Ra == 0 || Rb == 0) return false;
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  return a0 < b0 + ((Rb - 1) * ldb + Fb) * eb && b0 < a0 + ((Ra - 1) * lda + Fa) * ea;
+}
 inline bool same_place(const void* a, int64_t lda, const void* b, int64_t ldb) { return a == b && lda == ldb; }
 
 }  // namespace ops

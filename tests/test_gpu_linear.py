@@ -1,0 +1,238 @@
+"""Products of rows with bias, activation and residual, and their gradients, against the formulas in double precision.
+
+Tolerances count roundings.  A result of the element type is off by half a step of it, eps/2 relative.  Before that a product's
+fp32 sum over n terms, cut off and not rounded by the matrix unit 16 terms at a time, is off by at most (n/16 + 32) 2^-23 of the
+sum of magnitudes (|x| |w|); fp32 numbers in three parts leave out part products below 2^-24 each, which the 32 covers.
+dp is rounded to the element type, so dx and dw are also off by eps/2 of |dp| |w| and |dp|^T |x|.  An activation's
+slope is at most 1.13, and its formula in bf16's kernels is off by up to 1e-6 (1 + |p|)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+ACTS = ["none", "relu", "gelu", "silu"]
+
+
+def _dt(dtype):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+
+
+def _rows(g, R, F, dtype, std=1.0, extra=0):
+    """A [R, F] view at a wider pitch, NaN in the padding."""
+    import torch
+    per = 4 if dtype == "f32" else 8
+    ld = -(-F // per) * per + extra * per
+    buf = torch.full((R, ld), float("nan"), dtype=_dt(dtype), device="cuda")
+    buf[:, :F] = (torch.randn(R, F, generator=g, device="cuda") * std).to(_dt(dtype))
+    return buf, buf[:, :F]
+
+
+def _act(p, act):
+    import torch
+    return {"none": lambda: p, "relu": lambda: torch.relu(p), "gelu": lambda: p * torch.special.ndtr(p),
+            "silu": lambda: p * torch.sigmoid(p)}[act]()
+
+
+def _mm(a, b):
+    return a.contiguous() @ b.contiguous()
+
+
+def _sum_tol(n):
+    return (n / 16 + 32) * 2.0 ** -23
+
+
+SHAPES = [(1, 1, 1), (1, 1024, 40), (8, 64, 96), (17, 513, 300), (32, 100, 33), (33, 100, 33), (64, 64, 64), (65, 63, 65),
+          (200, 172, 128), (129, 129, 257), (1000, 40, 8), (300, 520, 520), (33000, 70, 130), (32900, 130, 129)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward(shape, dtype):
+    import torch
+    from paper_2309_03523_amd import binding
+    R, K, M = shape
+    g = torch.Generator(device="cuda").manual_seed(R + K + M)
+    _, x = _rows(g, R, K, dtype, extra=R % 3)
+    _, w = _rows(g, M, K, dtype, K ** -0.5, extra=1)
+    _, res = _rows(g, R, M, dtype, extra=2)
+    bias = torch.randn(M, generator=g, device="cuda")
+    p = _mm(x.double(), w.double().t())
+    mag = _mm(x.double().abs(), w.double().abs().t())
+    for k, act in enumerate(ACTS):
+        buf, y = _rows(g, R, M, dtype, extra=k)
+        buf2, pre = _rows(g, R, M, dtype, extra=1)
+        b, r, q = (bias if k != 1 else None), (res if k in (0, 2) else None), (pre if k >= 2 else None)
+        binding.linear_forward(x, w, y, bias=b, act=act, residual=r, pre=q)
+        pp = p + (b.double() if b is not None else 0)
+        want = _act(pp, act) + (r.double() if r is not None else 0)
+        off = _sum_tol(K) * mag + 2.0 ** -22 * (mag + pp.abs())
+        tol = HALF[dtype] * want.abs() + 1.13 * off + (1e-6 * (1 + pp.abs()) if act in ("gelu", "silu") else 0)
+        assert bool(((y.double() - want).abs() <= tol + 2.0 ** -22 * want.abs() * (dtype == "f32")).all()), act
+        assert bool(torch.isnan(buf[:, M:]).all())
+        if q is not None:
+            assert bool(((pre.double() - pp).abs() <= HALF[dtype] * pp.abs() + off).all())
+            assert bool(torch.isnan(buf2[:, M:]).all())
+    # onto the residual itself
+    want = p + res.double()
+    binding.linear_forward(x, w, res, residual=res)
+    assert bool(((res.double() - want).abs() <= HALF[dtype] * want.abs() + _sum_tol(K) * mag + 2.0 ** -22 * (mag + want.abs())).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_backward(shape, dtype):
+    import torch
+    from paper_2309_03523_amd import binding
+    R, K, M = shape
+    g = torch.Generator(device="cuda").manual_seed(R + K + M + 1)
+    _, x = _rows(g, R, K, dtype, extra=1)
+    _, w = _rows(g, M, K, dtype, K ** -0.5, extra=R % 2)
+    _, dy = _rows(g, R, M, dtype, extra=1)
+    _, pre = _rows(g, R, M, dtype, 1.5)
+    for k, act in enumerate(ACTS):
+        bufx, dx = _rows(g, R, K, dtype, extra=k)
+        bufw, dw = _rows(g, M, K, dtype, extra=1)
+        db = torch.empty(M, device="cuda")
+        n = binding.linear_workspace_bytes(R, K, M, dtype=dtype, act=act)
+        ws = torch.full((n // 4 + 1,), float("nan"), device="cuda")
+        binding.linear_backward(dy, x, w, pre=pre if act != "none" else None, act=act, dx=dx, dw=dw, dbias=db, workspace=ws)
+        dp = dy.double()
+        half = 2.0 ** -22
+        if act != "none":
+            p = pre.double().requires_grad_()
+            dp, = torch.autograd.grad(_act(p, act), p, dp)
+            half = HALF[dtype] + 4e-6          # dp's own rounding, and its formula's error of at most 4e-6 |dy|
+        slack = 4e-6 * dy.double().abs() if act in ("gelu", "silu") else 0 * dp
+        for got, a, b, n in ((dx, dp, w.double(), M), (dw, dp.t(), x.double(), R)):
+            want = _mm(a, b)
+            mag = _mm(a.abs(), b.abs())
+            extra = _mm(slack if a is dp else slack.t(), b.abs())
+            tol = HALF[dtype] * want.abs() + (_sum_tol(min(n, 4096)) + half + 2.0 ** -20) * mag + extra
+            assert bool(((got.double() - want).abs() <= tol).all()), (act, n)
+        assert bool(((db.double() - dp.sum(0)).abs() <= 3e-5 * dp.abs().sum(0) + slack.sum(0) + 1e-30).all())
+        assert bool(torch.isnan(bufx[:, K:]).all()) and bool(torch.isnan(bufw[:, K:]).all())
+        # one gradient at a time, without what it does not read: the same bits
+        again = torch.empty_like(dx)
+        _, again = _rows(g, R, K, dtype)
+        binding.linear_backward(dy, x, w, pre=pre, act=act, dx=again, workspace=ws)
+        assert torch.equal(again, dx)
+        _, again = _rows(g, M, K, dtype)
+        binding.linear_backward(dy, x, w, pre=pre, act=act, dw=again, workspace=ws)
+        assert torch.equal(again, dw)
+
+
+def test_gradient_against_differences():
+    """fp32 gradients of sum(dy * y) against central differences of the formula in double."""
+    import torch
+    from paper_2309_03523_amd import binding
+    g = torch.Generator(device="cuda").manual_seed(9)
+    R, K, M = 5, 12, 20
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda") for s in ((R, K), (M, K), (R, M)))
+    b = torch.randn(M, generator=g, device="cuda")
+    ws = torch.empty(binding.linear_workspace_bytes(R, K, M, dtype="f32"), dtype=torch.uint8, device="cuda")
+    for act in ACTS:
+        y, pre, dx, dw, db = torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+        binding.linear_forward(x, w, y, bias=b, act=act, pre=pre)
+        binding.linear_backward(dy, x, w, pre=pre, act=act, dx=dx, dw=dw, dbias=db, workspace=ws)
+
+        def f(x, w, b):
+            return float((_act(x @ w.t() + b, act) * dy.double()).sum())
+
+        h = 1e-6
+        X, W, B = x.double(), w.double(), b.double()
+        for _ in range(5):
+            ex, ew, eb = (torch.randn(t.shape, generator=g, device="cuda").double() for t in (x, w, b))
+            for got, e, hi, lo in ((dx, ex, f(X + h * ex, W, B), f(X - h * ex, W, B)), (dw, ew, f(X, W + h * ew, B), f(X, W - h * ew, B)),
+                                   (db, eb, f(X, W, B + h * eb), f(X, W, B - h * eb))):
+                assert abs(float((got.double() * e).sum()) - (hi - lo) / (2 * h)) <= 1e-5 * float((got.double() * e).abs().sum()), act
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_rows(dtype):
+    import torch
+    from paper_2309_03523_amd import binding
+    x, dy = torch.empty(0, 40, dtype=_dt(dtype), device="cuda"), torch.empty(0, 24, dtype=_dt(dtype), device="cuda")
+    w = torch.randn(24, 40, device="cuda").to(_dt(dtype))
+    y, dw, db = torch.empty_like(dy), torch.full_like(w, 3.0), torch.full((24,), 3.0, device="cuda")
+    binding.linear_forward(x, w, y)
+    ws = torch.empty(binding.linear_workspace_bytes(0, 40, 24, dtype=dtype), dtype=torch.uint8, device="cuda")
+    binding.linear_backward(dy, x, w, dx=torch.empty_like(x), dw=dw, dbias=db, workspace=ws)
+    assert not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R", [20, 300])
+def test_values_that_are_not_finite_stay_where_they_belong(R, dtype):
+    """A row's infinities and NaNs reach its own outputs only; a weight's, its own column.  The others stay within their tolerance: an
+    fp32 number next to an infinity is split at other bits, into parts that still add up to it exactly, so not the same bits."""
+    import torch
+    from paper_2309_03523_amd import binding
+    x, w = torch.randn(R, 72, device="cuda").to(_dt(dtype)), torch.randn(88, 72, device="cuda").to(_dt(dtype))
+    y = torch.empty(R, 88, dtype=_dt(dtype), device="cuda")
+    mag = _mm(x.double().abs(), w.double().abs().t())
+    x[3, 5], x[11, 71], w[40, 0] = float("nan"), float("inf"), float("-inf")
+    binding.linear_forward(x, w, y)
+    want = _mm(x.double(), w.double().t())
+    finite = torch.isfinite(want)
+    assert torch.equal(finite, torch.isfinite(y))
+    assert bool(((y.double() - want).abs() <= HALF[dtype] * want.abs() + _sum_tol(72) * mag)[finite].all())
+    assert torch.equal(torch.isnan(want), torch.isnan(y)) and torch.equal(want[torch.isinf(want)], y[torch.isinf(want)].double())
+
+
+def test_large_and_small_numbers():
+    """fp32 keeps its range: products of 1e30 and 1e-30, and numbers near the largest."""
+    import torch
+    from paper_2309_03523_amd import binding
+    for R in (8, 200):
+        x = torch.randn(R, 64, device="cuda") * torch.logspace(-18, 18, 64, device="cuda")
+        w = torch.randn(96, 64, device="cuda") * torch.logspace(18, -18, 64, device="cuda")
+        y = torch.empty(R, 96, device="cuda")
+        binding.linear_forward(x, w, y)
+        X, W = x.double(), w.double()
+        assert bool(((y.double() - X @ W.t()).abs() <= 2.0 ** -17 * (X.abs() @ W.abs().t())).all())
+        x = torch.full((R, 64), 3.4e38, device="cuda")
+        w = torch.eye(64, device="cuda")
+        y = torch.empty(R, 64, device="cuda")
+        binding.linear_forward(x, w, y)
+        assert torch.equal(y, x)
+
+
+def test_streams_graphs_and_repeats():
+    import torch
+    from paper_2309_03523_amd import binding
+    R, K, M = 5000, 96, 200
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16) for s in ((R, K), (M, K), (R, M)))
+    b = torch.randn(M, generator=g, device="cuda")
+    n = binding.linear_workspace_bytes(R, K, M, dtype="bf16", act="silu")
+
+    def room():
+        return [torch.zeros(*s, dtype=torch.bfloat16, device="cuda") for s in ((R, M), (R, M), (R, K), (M, K))] + [
+            torch.zeros(M, device="cuda"), torch.empty(n, dtype=torch.uint8, device="cuda")]
+
+    def step(o, stream=None):
+        binding.linear_forward(x, w, o[0], bias=b, act="silu", pre=o[1], stream=stream)
+        binding.linear_backward(dy, x, w, pre=o[1], act="silu", dx=o[2], dw=o[3], dbias=o[4], workspace=o[5], stream=stream)
+
+    want, other, out = room(), room(), room()
+    step(want)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    step(other, s)              # beside the first, each with a workspace of its own
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(want[:5], other[:5]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for k in range(3):
+        x.mul_(0.75)
+        step(want)
+        torch.cuda.synchronize()
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(want[:5], out[:5])), k

@@ -71,3 +71,35 @@ def test_binding_refusals():
         binding._op_rows(torch.zeros(32, 4).t(), "x")
     with pytest.raises(ValueError, match="one pitch"):
         binding._op_rows(torch.zeros(4, 5, 8)[:, :3], "x")
+
+
+def test_linear_refusals(lib):
+    D, E = 0x40000000, 0x50000000
+    good = dict(x=A, ldx=32, w=B, ldw=32, R=10, K=30, M=20, dtype=0, bias=None, act=0, residual=None, ldr=0, y=C, ldy=20, pre=None, ldpre=0,
+                stream=None)
+
+    def fwd(**kw):
+        return lib.dgc_linear_forward(*{**good, **kw}.values())
+
+    for kw in (dict(x=None), dict(w=None), dict(y=None), dict(x=A + 4), dict(ldx=28), dict(ldw=31), dict(ldy=18), dict(K=0), dict(M=0), dict(K=65537, ldx=65540, ldw=65540),
+               dict(R=-1), dict(R=1 << 50), dict(dtype=3), dict(act=4), dict(act=-1), dict(y=A), dict(y=B), dict(residual=C + 16, ldr=20), dict(pre=C, ldpre=20),
+               dict(pre=A + 64, ldpre=32), dict(residual=D, ldr=19), dict(residual=D, ldr=20, pre=D, ldpre=20)):
+        assert fwd(**kw) == INVALID, kw
+        assert "linear" in _text(lib)
+    assert fwd(R=0, x=None, y=None) == OK
+    need = lib.dgc_linear_workspace_bytes(10, 30, 20, 0, 2)
+    good = dict(dy=C, lddy=20, x=A, ldx=32, w=B, ldw=32, R=10, K=30, M=20, dtype=0, pre=D, ldpre=20, act=2, dx=E, lddx=32, dw=E + 0x100000, lddw=32,
+                dbias=None, ws=0x60000000, ws_bytes=need, stream=None)
+
+    def bwd(**kw):
+        return lib.dgc_linear_backward(*{**good, **kw}.values())
+
+    for kw in (dict(dy=None), dict(x=None), dict(w=None), dict(pre=None), dict(ws=None), dict(ws_bytes=need - 1), dict(ws=0x60000008), dict(dx=C, lddx=32),
+               dict(dw=E, lddw=32), dict(dw=B), dict(dx=A), dict(dw=C), dict(act=7), dict(lddw=28)):
+        assert bwd(**kw) == INVALID, kw
+        assert "linear" in _text(lib)
+    size = lib.dgc_linear_workspace_bytes
+    assert size(10, 30, 20, 0, 0) <= need and size(-1, 1, 1, 0, 0) < 0 and size(1, 0, 1, 0, 0) < 0 and size(1, 1, 1, 5, 0) < 0 and size(1, 1, 1, 0, 9) < 0
+    for dt in (0, 1):
+        sizes = [size(r, 128, 512, dt, 2) for r in (0, 1, 1000, 10 ** 6, 10 ** 8)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
