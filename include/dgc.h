@@ -491,6 +491,37 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
                                  int32_t act, void* dx, int64_t lddx, void* dw, int64_t lddw, float* dbias,
                                  void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Linear attention with a decay per head: a time encoder whose state, a dk x dv matrix per sequence and head, is carried from
+ * window to window as H0 / HN are.  For token t of sequence i (a vertex) and each head, with g the head's decay:
+ *   S_t = l_t g S_{t-1} + k_t^T v_t,  S_{-1} = S0,  o_t = scale q_t S_t;   l_t = 0 where reset[t][i] is non-zero, else 1.
+ *  q, k, v, o: row (t, i) at base + t * stride_t + i * stride_n elements (both multiples of 16 bytes, bases aligned to 16), a row's
+ *   heads side by side: [heads][dk] or [heads][dv].  Inputs may repeat rows (a stride of 0).  An output's rows
+ *   lie apart, and outputs lie apart from inputs and each other (side by side in rows of one buffer is apart).
+ *  T, N: tokens and sequences; heads in [1, 1024]; dk, dv multiples of 8 in [8, 128].  decay device fp32 [heads], in [0, 1].
+ *  s0, sn device fp32 [N][heads][dk][dv], NULL = zeros, not wanted; sn may be s0.  lengths device int32 [N] or NULL (all
+ *   T): sequence i has its first lengths[i] tokens (clamped to [0, T]); rows behind them are neither read nor written, and sn is
+ *   the state after the last token (s0 of an empty sequence).  reset device uint8 [T][N] or NULL.
+ *  backward: gradients dq, dk, dv (each may be NULL) and ds0 (NULL = not wanted; may be dsn) from the output's gradient `go` and
+ *   the last state's, dsn (NULL = zeros).  The decays are constants.
+ *  workspace: dgc_decay_attn_workspace_bytes bytes (0 unless few long sequences are split; negative for sizes outside the range).
+ *  DGC_ERR_UNSUPPORTED for 2^31 and more sequences x heads x blocks of 32 columns.
+ * A token that holds an infinity or NaN reaches only the outputs that the formula lets it reach. */
+int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t backward);
+dgc_status_t dgc_decay_attn_forward(const void* q, int64_t q_stride_t, int64_t q_stride_n, const void* k, int64_t k_stride_t,
+                                    int64_t k_stride_n, const void* v, int64_t v_stride_t, int64_t v_stride_n,
+                                    int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t dtype,
+                                    const float* decay, float scale, const float* s0, const int32_t* lengths,
+                                    const uint8_t* reset, void* o, int64_t o_stride_t, int64_t o_stride_n, float* sn,
+                                    void* workspace, int64_t workspace_bytes, void* stream);
+dgc_status_t dgc_decay_attn_backward(const void* q, int64_t q_stride_t, int64_t q_stride_n, const void* k, int64_t k_stride_t,
+                                     int64_t k_stride_n, const void* v, int64_t v_stride_t, int64_t v_stride_n,
+                                     const void* go, int64_t go_stride_t, int64_t go_stride_n, int64_t T, int64_t N,
+                                     int32_t heads, int32_t dk, int32_t dv, int32_t dtype, const float* decay, float scale,
+                                     const float* s0, const float* dsn, const int32_t* lengths, const uint8_t* reset,
+                                     void* dq, int64_t dq_stride_t, int64_t dq_stride_n, void* dkey, int64_t dk_stride_t,
+                                     int64_t dk_stride_n, void* dval, int64_t dv_stride_t, int64_t dv_stride_n,
+                                     float* ds0, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Text of the last error on this layer, or (layer = NULL) of the last failed create or layer-less
  * call on the calling thread.  Never NULL; valid until the next call on the same layer / thread. */
 const char* dgc_last_error(const dgc_layer_t* layer);

@@ -34,7 +34,8 @@ EXPORTS = ["dgc_layer_create", "dgc_layer_destroy", "dgc_layer_set_param", "dgc_
            "dgc_stale_static_max_candidates", "dgc_stale_filter_static",
            "dgc_layer_shared_rows", "dgc_fusion_select", "dgc_chunk_assign", "dgc_chunk_generate",
            "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward",
-           "dgc_linear_workspace_bytes", "dgc_linear_forward", "dgc_linear_backward"]
+           "dgc_linear_workspace_bytes", "dgc_linear_forward", "dgc_linear_backward",
+           "dgc_decay_attn_workspace_bytes", "dgc_decay_attn_forward", "dgc_decay_attn_backward"]
 THETA_VARIANT = {"printed": 0, "sigmoid": 1}
 N_STAGES = 13
 
@@ -111,7 +112,12 @@ def load() -> ct.CDLL:
     lib.dgc_linear_forward.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp]
     lib.dgc_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp]
     lib.dgc_linear_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
-    sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes")
+    lib.dgc_decay_attn_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    seq = [vp, i64, i64]    # a tensor of rows (t, i): address, strides of t and i
+    dims = [i64, i64, i32, i32, i32, i32]
+    lib.dgc_decay_attn_forward.argtypes = seq * 3 + dims + [vp, f32, vp, vp, vp] + seq + [vp, vp, i64, vp]
+    lib.dgc_decay_attn_backward.argtypes = seq * 4 + dims + [vp, f32, vp, vp, vp, vp] + seq * 3 + [vp, vp, i64, vp]
+    sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes", "dgc_decay_attn_workspace_bytes")
     for name in sizes:
         getattr(lib, name).restype = i64
     for name in EXPORTS:
@@ -408,7 +414,7 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
     return it.value, bool(conv.value)
 
 
-# --------------------------------------------------------------------------- layer norm, products of rows
+# --------------------------------------------------------------------------- layer norm, products of rows, decaying attention
 #
 # Operators on plain device tensors: nothing is allocated, outputs and workspaces are the caller's, work is only
 # enqueued on `stream` (default: the current stream of the tensors' device).
@@ -558,3 +564,63 @@ def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, 
     ws, ws_bytes = _op_workspace(workspace, x)
     _op_call(lib.dgc_linear_backward, x, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, dt, pp, ldp, LINEAR_ACT[act], pdx, lddx, pdw, lddw,
              _op_flat(dbias, "dbias", M, x), ws, ws_bytes)
+
+
+def decay_attn_workspace_bytes(T: int, N: int, heads: int, dk: int, dv: int, *, backward: bool = False) -> int:
+    """Bytes that the calls need: none for short windows, segment states for few long sequences."""
+    return int(load().dgc_decay_attn_workspace_bytes(int(T), int(N), int(heads), int(dk), int(dv), int(backward)))
+
+
+def _op_seq(t, name: str, like, T: int, N: int, F: int):
+    """(address, stride of t, stride of i) of rows (t, i) in a [T, N, F] tensor or view."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor of the first tensor's element type and device")
+    if tuple(t.shape) != (T, N, F) or t.stride(2) != 1:
+        raise ValueError(f"{name} must be [{T}, {N}, {F}] with a contiguous last dimension")
+    return t.data_ptr(), (t.stride(0) if T > 1 else 0), (t.stride(1) if N > 1 else 0)
+
+
+def _decay_sizes(q, v, heads: int):
+    if q.dim() != 3 or v.dim() != 3 or heads < 1 or q.shape[2] % heads or v.shape[2] % heads:
+        raise ValueError("q, k, v must be [T, N, heads * size of a head]")
+    return q.shape[0], q.shape[1], q.shape[2] // heads, v.shape[2] // heads
+
+
+def decay_attn_forward(q, k, v, decay, o, *, heads: int, scale: float = 1.0, s0=None, sn=None, lengths=None, reset=None,
+                       workspace=None, stream=None):
+    """dgc_decay_attn_forward: S_t = g S_{t-1} + k_t^T v_t, o_t = scale q_t S_t for every sequence i and head.  q, k [T, N,
+    heads * dk], v, o [T, N, heads * dv], float32 or bfloat16, with any strides of t and i (a transposed [N, T, .] tensor is
+    fine); decay fp32 [heads], each in [0, 1]; s0, sn fp32 [N, heads, dk, dv] or None (sn may be s0); lengths int32 [N]: tokens
+    of each sequence, rows behind them are not written; reset uint8 [T, N]: a non-zero byte drops the state entering (t, i).
+    workspace: decay_attn_workspace_bytes device bytes, None where that is 0.  T = 1 is the form for one new snapshot."""
+    import torch
+    lib = load()
+    dt = _op_dtype(q, "q")
+    T, N, dk, dv = _decay_sizes(q, v, heads)
+    n_state = N * heads * dk * dv
+    ws, ws_bytes = _op_workspace(workspace, q)
+    _op_call(lib.dgc_decay_attn_forward, q, stream, *_op_seq(q, "q", q, T, N, heads * dk), *_op_seq(k, "k", q, T, N, heads * dk),
+             *_op_seq(v, "v", q, T, N, heads * dv), T, N, heads, dk, dv, dt, _op_flat(decay, "decay", heads, q), float(scale),
+             _op_flat(s0, "s0", n_state, q), _op_flat(lengths, "lengths", N, q, torch.int32), _op_flat(reset, "reset", T * N, q, torch.uint8),
+             *_op_seq(o, "o", q, T, N, heads * dv), _op_flat(sn, "sn", n_state, q), ws, ws_bytes)
+    return o
+
+
+def decay_attn_backward(q, k, v, decay, do, dq, dk, dv, *, heads: int, scale: float = 1.0, s0=None, dsn=None, ds0=None, lengths=None,
+                        reset=None, workspace=None, stream=None):
+    """dgc_decay_attn_backward: the gradients of decay_attn_forward's q, k, v (each may be None: not wanted) and s0 (ds0) from
+    do and the last state's gradient dsn (None: zero); ds0 may be dsn.  decay is a constant."""
+    import torch
+    lib = load()
+    dt = _op_dtype(q, "q")
+    T, N, nk, nv = _decay_sizes(q, v, heads)
+    n_state = N * heads * nk * nv
+    ws, ws_bytes = _op_workspace(workspace, q)
+    _op_call(lib.dgc_decay_attn_backward, q, stream, *_op_seq(q, "q", q, T, N, heads * nk), *_op_seq(k, "k", q, T, N, heads * nk),
+             *_op_seq(v, "v", q, T, N, heads * nv), *_op_seq(do, "do", q, T, N, heads * nv), T, N, heads, nk, nv, dt,
+             _op_flat(decay, "decay", heads, q), float(scale), _op_flat(s0, "s0", n_state, q), _op_flat(dsn, "dsn", n_state, q),
+             _op_flat(lengths, "lengths", N, q, torch.int32), _op_flat(reset, "reset", T * N, q, torch.uint8),
+             *_op_seq(dq, "dq", q, T, N, heads * nk), *_op_seq(dk, "dk", q, T, N, heads * nk), *_op_seq(dv, "dv", q, T, N, heads * nv),
+             _op_flat(ds0, "ds0", n_state, q), ws, ws_bytes)

@@ -1,0 +1,706 @@
+// Linear attention with a decay per head: a time encoder whose state is a matrix per sequence and head.
+//
+//   S_t = l_t g S_{t-1} + k_t^T v_t   (l_t = 0 where a reset flag is set, else 1),   o_t = s q_t S_t
+//
+// One kernel computes the forward pass and all gradients.  With roles A, B, C for q, k, v it is
+//   out_i = alpha sum_{j <= i} g^(i-j) (A_i . B_j) C_j + gam g^(i+1) A_i S_in,   S = g^n S_in + beta sum_j g^(n-1-j) B_j^T C_j
+// (sums over the tokens since the last reset, S_in only before the first), and the gradients are the same sums:
+//   dq: A, B, C = do, v, k from S_0^T;   with G_t = s q_t^T do_t + l_{t+1} g G_{t+1}, walked from the last token to the first,
+//   dv: A, B, C = k, q, do and dk: A, B, C = v, do, q from dS_N (not decayed) and its transpose;   dS_0 = l_0 g G_0.
+//
+// A wave takes 32 tokens of one sequence and head and 32 columns of C at a time and keeps its part of S in registers from one
+// 32 to the next.  All products run on v_mfma_f32_32x32x16_bf16, operands and results in registers, none in LDS:
+//  - scores D[j][i] = B_j . A_i leave lane i with 16 scores of its own token i in just the order in which a product that sums over
+//    j takes them; C, and B for the state, come into that order by a product with the identity, which is exact;
+//  - the state's rows are kept in the order that makes its registers the operand of A S: row 8g + 4(l/32) + e of a tile is
+//    number swap(8g + 4(l/32) + e) of B's, swap exchanging bits 2 and 3.
+// Rounding: bf16 tensors enter as they are.  Scores and states, which are fp32, enter in parts: two bf16 parts (2^-17) where the
+// result is rounded to bf16, three (all 24 bits) where it goes into the fp32 state; fp32 tensors always in three, six part
+// products a product.  The matrix unit cuts its sums off, so the state is carried from one 32 tokens to the next by the vector unit.
+// A zero score or weight times a value that is not finite would be NaN for tokens that do not see that value: 32 tokens with such
+// a value among k, v, their scores or the state go one by one (walk).
+//
+// Few long sequences are split into segments: a first pass leaves each segment's own state, a scan joins them into the states
+// that enter the segments, a second pass starts from those.  One token (serving a new snapshot) has a kernel of its own that
+// reads and writes the states as the stream they are.  No atomics: the same inputs give the same bits.
+#include <algorithm>
+
+#include "dgc_ops.h"
+#include "dgc_split_dev.h"
+
+namespace dgc {
+namespace {
+
+using ops::Elem;
+using split::as_frag;
+using split::floatx16;
+
+constexpr int kMaxHeads = 1024, kMaxDim = 128;
+constexpr int kTok = 32;               // tokens at a time
+constexpr int64_t kFillWaves = 2048;   // two a SIMD
+constexpr int64_t kSegTokens = 128;    // tokens of a segment at least
+
+struct Rows {          // row (t, i) at p + t st + i sn, in elements
+  const void* p;
+  int64_t st, sn;
+};
+
+struct DecayArgs {
+  Rows A, B, C, O;
+  int64_t T, N;
+  int32_t heads, dk, dv;        // dk: length of A's and B's rows, dv: of C's and O's, a head
+  int32_t blocks_v;             // 32 columns of C each
+  int32_t reversed;             // tokens from the last to the first
+  float alpha, beta, gam;
+  const float* decay;
+  const uint8_t* reset;         // [T][N] or nullptr
+  const int32_t* lengths;       // [N] or nullptr
+  const float* s_in;            // state (i, h) [seg] element (r, c) at s_in + ((seg N + i) heads + h) dk dv + r in_r + c in_c, or nullptr
+  int32_t in_r, in_c;
+  float* s_out;                 // the same, or nullptr
+  int32_t out_r, out_c;
+  int32_t out_link;             // the state is written times l_0 g (of no token: as it came in)
+  float* factor;                // first pass: what a segment keeps of the state entering it, [seg][N][heads]; -1: cut off by a reset
+  int32_t segs;
+  int64_t seg_len;
+};
+
+// The product of operands in parts, those below 2^-24 left out, the smallest first.
+template <int NX, int NY>
+__device__ __forceinline__ void mul(floatx16& c, const uint4 (&x)[NX], const uint4 (&y)[NY]) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s) {
+#pragma unroll
+    for (int i = 0; i <= s; ++i) {
+      if (i < NX && s - i < NY) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(x[i]), as_frag(y[s - i]), c, 0, 0, 0);
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void parts_of(const float (&x)[8], uint4 (&p)[N]) {
+  if constexpr (N == 3) {
+    split::split8(x, p);
+  } else {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = split::nearest(x[2 * i], x[2 * i + 1]);
+      l[i] = split::nearest(x[2 * i] - split::bf_lo(h[i]), x[2 * i + 1] - split::bf_hi(h[i]));
+    }
+    p[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    if constexpr (N == 2) p[1] = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+// How many parts: of a tensor's numbers, of scores and states in a product that is rounded to the tensors' type, of the state's.
+template <class T> struct Kind;
+template <> struct Kind<uint16_t> { static constexpr int kIn = 1, kMid = 2; };
+template <> struct Kind<float> { static constexpr int kIn = 3, kMid = 3; };
+
+// Eight numbers of a row as an operand.
+template <class T>
+__device__ __forceinline__ void load8(const T* p, bool in, uint4 (&f)[Kind<T>::kIn]) {
+  if constexpr (sizeof(T) == 2) {
+    f[0] = in ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+  } else {
+    float x[8] = {};
+    if (in) {
+      Elem<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
+      Elem<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
+    }
+    split::split8(x, f);
+  }
+}
+template <class T> __device__ __forceinline__ float to_float(T x);
+template <> __device__ __forceinline__ float to_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ float to_float<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+__device__ __forceinline__ int swap23(int x) { return (x & ~12) | (x & 4) << 1 | (x & 8) >> 1; }
+__device__ __forceinline__ uint4 identity(int c, int half, int n) {   // rows 16 c + 8 half + 0..7 of its column n
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 16 * c + 8 * half + 2 * i;
+    w[i] = (r == n ? 0x3f80u : 0u) | (r + 1 == n ? 0x3f800000u : 0u);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ float power(float g, int64_t n) {   // g^n in double, so that far powers keep their bits
+  return n == 0 ? 1.f : (float)exp2((double)n * log2((double)g));
+}
+__device__ __forceinline__ void not_finite(float& t, const floatx16& x) {   // t turns NaN if one of them is not finite
+#pragma unroll
+  for (int r = 0; r < 16; ++r) t = fmaf(x[r], 0.f, t);
+}
+
+// KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
+template <class T, int KD, bool OUT>
+__global__ __launch_bounds__(256) void k_decay(DecayArgs a) {
+  constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid;
+  __shared__ float pw_lds[4][kTok + 4];
+  const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
+  float* pw = pw_lds[threadIdx.x >> 6];
+  const uint4 eye[2] = {identity(0, half, tok), identity(1, half, tok)};
+  const uint4 turned[2] = {identity(0, half, swap23(tok)), identity(1, half, swap23(tok))};
+  const uint32_t units = (uint32_t)(a.N * a.heads * a.blocks_v * a.segs);
+  int last_h = -1;
+  float g = 0.f, near[16], fade0 = 0.f, fade1 = 0.f;   // near: g^(i-j) of the lane's scores; fade: g^i, g^(i+1)
+#pragma unroll
+  for (int r = 0; r < 16; ++r) near[r] = 0.f;
+
+  for (uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += gridDim.x * 4) {
+    const int b = unit % a.blocks_v;
+    const uint32_t ih = unit / a.blocks_v;
+    const int h = ih % a.heads;
+    const int64_t i = ih / a.heads % (uint32_t)a.N;
+    const int seg = ih / a.heads / (uint32_t)a.N;
+    if (h != last_h) {
+      last_h = h;
+      g = a.decay[h];
+      if (lane <= kTok) pw[lane] = power(g, lane);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = 8 * (r >> 2) + 4 * half + (r & 3);
+        near[r] = j <= tok ? pw[max(tok - j, 0)] : 0.f;
+      }
+      fade0 = pw[tok];
+      fade1 = pw[tok + 1];
+    }
+    const int64_t n = a.lengths ? min(a.T, (int64_t)max(a.lengths[i], 0)) : a.T;
+    const int64_t p_lo = seg * a.seg_len, p_hi = min(n, p_lo + a.seg_len);
+    const int dv0 = 32 * b;
+    const int64_t state_at = (((int64_t)seg * a.N + i) * a.heads + h) * a.dk * a.dv;
+    const int c = dv0 + tok;      // the lane's column of the state
+    floatx16 S[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
+        S[t][r] = a.s_in && row < a.dk && c < a.dv ? a.s_in[state_at + (int64_t)row * a.in_r + (int64_t)c * a.in_c] : 0.f;
+      }
+    }
+    bool holds = a.s_in != nullptr;       // whether the state may be other than zero
+    bool cut = false;                     // whether a reset was met
+    for (int64_t p0 = p_lo; p0 < p_hi; p0 += kTok) {
+      const int m = (int)min((int64_t)kTok, p_hi - p0);
+      const bool on = tok < m;
+      const bool fresh = a.reversed && p0 == 0;     // the state that comes in is that of the first token, not of one before
+      const int64_t pos = p0 + tok, t_of = a.reversed ? n - 1 - pos : pos;
+      uint32_t resets = 0;
+      if (a.reset) {
+        bool f = false;
+        if (on && half == 0) {
+          if (!a.reversed) f = a.reset[pos * a.N + i] != 0;
+          else if (pos > 0) f = a.reset[(n - pos) * a.N + i] != 0;
+        }
+        resets = (uint32_t)__ballot(f);
+        cut |= resets != 0;
+      }
+      const T* rowA = static_cast<const T*>(a.A.p) + t_of * a.A.st + i * a.A.sn + (int64_t)h * a.dk + 8 * half;
+      const T* rowB = static_cast<const T*>(a.B.p) + t_of * a.B.st + i * a.B.sn + (int64_t)h * a.dk + 8 * half;
+      const T* rowC = static_cast<const T*>(a.C.p) + t_of * a.C.st + i * a.C.sn + (int64_t)h * a.dv + dv0 + 8 * half;
+      const bool step = !OUT || a.s_out || p0 + kTok < p_hi;   // whether the state is wanted after these tokens
+
+      floatx16 P = {}, inter = {}, Bc[KT], Cc = {};
+#pragma unroll
+      for (int t = 0; t < KT; ++t) Bc[t] = floatx16{};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (dv0 + 16 * k < a.dv) {
+          uint4 f[IN];
+          load8(rowC + 16 * k, on && dv0 + 16 * k + 8 * half < a.dv, f);
+          mul(Cc, f, {eye[k]});
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        uint4 fa[IN], fb[IN];
+        load8(rowB + 16 * k, on && 16 * k + 8 * half < a.dk, fb);
+        if constexpr (OUT) {
+          load8(rowA + 16 * k, on && 16 * k + 8 * half < a.dk, fa);
+          mul(P, fb, fa);
+          if (holds) {
+            float x[8];
+            uint4 fs[MID];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = S[k / 2][8 * (k & 1) + e];
+            parts_of(x, fs);
+            mul(inter, fs, fa);
+          }
+        }
+        mul(Bc[k / 2], fb, {turned[k & 1]});
+      }
+      float bad = 0.f;
+      not_finite(bad, Cc);
+      if constexpr (OUT) not_finite(bad, P);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        not_finite(bad, Bc[t]);
+        if (holds) not_finite(bad, S[t]);
+      }
+      if (__builtin_expect(__any(bad != 0.f), 0)) {
+        // one by one: the state for each token, its row's product with it
+        for (int q = 0; q < m; ++q) {
+          const int64_t at = a.reversed ? n - 1 - (p0 + q) : p0 + q;
+          const T* qa = static_cast<const T*>(a.A.p) + at * a.A.st + i * a.A.sn + (int64_t)h * a.dk;
+          const T* qb = static_cast<const T*>(a.B.p) + at * a.B.st + i * a.B.sn + (int64_t)h * a.dk;
+          const float vc = c < a.dv ? to_float((static_cast<const T*>(a.C.p) + at * a.C.st + i * a.C.sn + (int64_t)h * a.dv)[c]) : 0.f;
+          const bool zero = resets >> q & 1;
+          const float keep = fresh && q == 0 ? 1.f : g;
+          float o = 0.f;
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
+              if (row < a.dk && c < a.dv) {
+                const float old = zero ? 0.f : holds || q > 0 ? keep * S[t][r] : 0.f;
+                S[t][r] = fmaf(a.beta * to_float(qb[row]), vc, old);
+                if constexpr (OUT) o = fmaf(to_float(qa[row]), S[t][r], o);
+              }
+            }
+          }
+          if constexpr (OUT) {
+            o += __shfl_xor(o, 32);
+            if (half == 0 && c < a.dv)
+              (static_cast<T*>(const_cast<void*>(a.O.p)) + at * a.O.st + i * a.O.sn + (int64_t)h * a.dv)[c] = Elem<T>::one(a.gam * o);
+          }
+        }
+        holds = true;
+        continue;
+      }
+      uint4 fc[2][IN];      // C with its tokens as the contraction
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = Cc[8 * k + e];
+        parts_of(x, fc[k]);
+      }
+      if constexpr (OUT) {
+        const uint32_t before = resets & ((2u << tok) - 1u);       // resets up to the lane's token (2 << 31 is 0: all of them)
+        const int since = before ? 31 - __clz(before) : 0;
+        floatx16 intra = {};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (16 * k < m) {
+            float x[8];
+            uint4 fp[MID];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int r = 8 * k + e, j = 8 * (r >> 2) + 4 * half + (r & 3);
+              x[e] = j >= since ? P[r] * near[r] : 0.f;
+            }
+            parts_of(x, fp);
+            mul(intra, fc[k], fp);
+          }
+        }
+        const float f = before || !holds ? 0.f : a.gam * (fresh ? fade0 : fade1);
+        T* out = static_cast<T*>(const_cast<void*>(a.O.p)) + t_of * a.O.st + i * a.O.sn + (int64_t)h * a.dv;
+        if (on) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int col = dv0 + 8 * q + 4 * half;
+            if (col < a.dv) {
+              float x[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = fmaf(a.alpha, intra[4 * q + e], f * inter[4 * q + e]);
+              if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(out + col) = Elem<float>::pack(x);
+              else *reinterpret_cast<uint2*>(out + col) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
+            }
+          }
+        }
+      }
+      if (step) {
+        const int last = resets ? 31 - __clz(resets) : 0;
+        const float keep = resets ? 0.f : pw[m - (fresh ? 1 : 0)];
+        float w[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 8 * (r >> 2) + 4 * half + (r & 3);
+          w[r] = j < m && j >= last ? a.beta * pw[max(m - 1 - j, 0)] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          floatx16 U = {};
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (16 * k < m) {
+              float x[8];
+              uint4 fb[3];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = Bc[t][8 * k + e] * w[8 * k + e];
+              parts_of(x, fb);
+              mul(U, fb, fc[k]);
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) S[t][r] = holds ? fmaf(keep, S[t][r], U[r]) : U[r];
+        }
+        holds = true;
+      }
+    }
+    if (a.s_out) {
+      float f = 1.f;
+      if (a.out_link && n > 0) f = a.reset && a.reset[i] ? 0.f : g;
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
+          if (row < a.dk && c < a.dv)
+            a.s_out[state_at + (int64_t)row * a.out_r + (int64_t)c * a.out_c] = f == 0.f && g != 0.f ? 0.f : f * S[t][r];
+        }
+      }
+    }
+    if (!OUT && a.factor && b == 0 && lane == 0) {
+      const int64_t len = max(p_hi - p_lo, (int64_t)0);
+      a.factor[((int64_t)seg * a.N + i) * a.heads + h] = cut ? -1.f : power(g, len - (a.reversed && seg == 0 && len > 0 ? 1 : 0));
+    }
+  }
+}
+
+// Joins the segments' own states: in place, each becomes the state that enters its segment; the last one goes to s_out.
+struct ScanArgs {
+  float* states;            // [segs][N][heads][dk dv]
+  const float* factor;
+  const float* s_in;        // [N][heads][dk dv] or nullptr
+  float* s_out;             // the same, or nullptr
+  int64_t N;
+  int32_t heads, size, segs;
+  int32_t out_link;
+  const float* decay;
+  const uint8_t* reset;
+  const int32_t* lengths;
+};
+__global__ __launch_bounds__(256) void k_decay_scan(ScanArgs a) {
+  const int64_t seqs = a.N * a.heads, all = seqs * a.size;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+    const int64_t ih = e / a.size;
+    const float g = a.decay[ih % a.heads];
+    float s = a.s_in ? a.s_in[e] : 0.f;
+    for (int seg = 0; seg < a.segs; ++seg) {
+      const float f = a.factor[seg * seqs + ih], own = a.states[seg * all + e];
+      a.states[seg * all + e] = s;
+      // a power that is zero only in fp32 leaves an infinity what it is
+      if (f == 0.f && g != 0.f) s = fabsf(s) <= 3.4028235e38f ? own : s + own;
+      else s = f < 0.f ? own : fmaf(f, s, own);
+    }
+    if (a.s_out) {
+      const int64_t i = ih / a.heads;
+      if (a.out_link && (!a.lengths || a.lengths[i] > 0)) s = a.reset && a.reset[i] ? 0.f : g * s;
+      a.s_out[e] = s;
+    }
+  }
+}
+
+// One token: a wave a sequence and head, dv / 4 lanes a row of the state, as many rows at a time as fit, eight times.
+template <class T>
+__global__ __launch_bounds__(256) void k_decay_step(DecayArgs a) {
+  __shared__ float4 sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lv = a.dv / 4, rows = 64 / lv, sub = lane / lv, col = lane % lv * 4;
+  const bool on = sub < rows;
+  constexpr int U = 8;
+  const int64_t units = a.N * a.heads;
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + wave; unit < units; unit += (int64_t)gridDim.x * 4) {
+    const int64_t i = unit / a.heads;
+    const int h = (int)(unit % a.heads);
+    const bool live = !a.lengths || a.lengths[i] > 0;
+    const bool zero = !a.s_in || (live && a.reset && a.reset[i]);
+    const float g = live ? a.decay[h] : 1.f;
+    const float* from = a.s_in + unit * a.dk * a.dv;
+    float* to = a.s_out + unit * a.dk * a.dv;
+    const T* q = static_cast<const T*>(a.A.p) + i * a.A.sn + (int64_t)h * a.dk;
+    const T* k = static_cast<const T*>(a.B.p) + i * a.B.sn + (int64_t)h * a.dk;
+    const T* v = static_cast<const T*>(a.C.p) + i * a.C.sn + (int64_t)h * a.dv;
+    float x[4] = {}, o[4] = {};
+    if (on && live) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = to_float(v[col + e]);
+    }
+    for (int r0 = 0; r0 < a.dk; r0 += rows * U) {
+      float4 s[U];
+      float qv[U], kv[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * rows + sub;
+        const bool in = on && r < a.dk;
+        s[u] = in && !zero ? *reinterpret_cast<const float4*>(from + r * a.dv + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+        qv[u] = in && live ? to_float(q[r]) : 0.f;
+        kv[u] = in && live ? to_float(k[r]) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * rows + sub;
+        if (on && r < a.dk) {
+          if (live) {
+            s[u].x = fmaf(kv[u], x[0], zero ? 0.f : g * s[u].x);
+            s[u].y = fmaf(kv[u], x[1], zero ? 0.f : g * s[u].y);
+            s[u].z = fmaf(kv[u], x[2], zero ? 0.f : g * s[u].z);
+            s[u].w = fmaf(kv[u], x[3], zero ? 0.f : g * s[u].w);
+            o[0] = fmaf(qv[u], s[u].x, o[0]);
+            o[1] = fmaf(qv[u], s[u].y, o[1]);
+            o[2] = fmaf(qv[u], s[u].z, o[2]);
+            o[3] = fmaf(qv[u], s[u].w, o[3]);
+          }
+          if (a.s_out) *reinterpret_cast<float4*>(to + r * a.dv + col) = s[u];
+        }
+      }
+    }
+    sums[wave][lane] = make_float4(o[0], o[1], o[2], o[3]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (live && lane < lv) {
+      float4 t = sums[wave][lane];
+      for (int r = 1; r < rows; ++r) {
+        const float4 y = sums[wave][r * lv + lane];
+        t.x += y.x; t.y += y.y; t.z += y.z; t.w += y.w;
+      }
+      T* out = static_cast<T*>(const_cast<void*>(a.O.p)) + i * a.O.sn + (int64_t)h * a.dv + col;
+      const float z[4] = {t.x * a.alpha, t.y * a.alpha, t.z * a.alpha, t.w * a.alpha};
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(out) = Elem<float>::pack(z);
+      else *reinterpret_cast<uint2*>(out) = make_uint2(Elem<uint16_t>::pack2(z[0], z[1]), Elem<uint16_t>::pack2(z[2], z[3]));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+struct Segments { int32_t n; int64_t len; };
+// Segments where sequences, heads and blocks of columns alone leave SIMDs without a wave.
+Segments segments_of(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv) {
+  const int64_t waves = N * heads * ((std::max(dk, dv) + 31) / 32);
+  if (waves == 0 || T <= kSegTokens || waves * 2 > kFillWaves) return {1, std::max<int64_t>(T, 1)};
+  const int64_t want = std::min((kFillWaves + waves - 1) / waves, (T + kSegTokens - 1) / kSegTokens);
+  const int64_t len = ((T + want - 1) / want + kTok - 1) / kTok * kTok;
+  return {(int32_t)((T + len - 1) / len), len};
+}
+
+template <class T, bool OUT>
+void launch(DecayArgs a, hipStream_t st) {
+  a.blocks_v = (a.dv + 31) / 32;
+  const int64_t units = a.N * a.heads * a.blocks_v * a.segs;
+  // Waves walk the units in steps of the grid: a grid that holds whole sequences keeps each wave at one head and its powers.
+  const int64_t seq = (int64_t)a.heads * a.blocks_v;
+  int64_t grid = (units + 3) / 4;
+  const int64_t most = 256 * 8 * 2;
+  if (grid > most) {
+    int64_t step = seq;
+    while (step % 4) step += seq;               // whole sequences and whole workgroups
+    grid = std::max<int64_t>(1, most * 4 / step) * step / 4;
+  }
+#define DGC_DECAY(KD) hipLaunchKernelGGL((k_decay<T, KD, OUT>), (unsigned)grid, 256, 0, st, a)
+  if (a.dk <= 16) DGC_DECAY(16);
+  else if (a.dk <= 32) DGC_DECAY(32);
+  else if (a.dk <= 64) DGC_DECAY(64);
+  else DGC_DECAY(128);
+#undef DGC_DECAY
+}
+
+struct Call {
+  int64_t T, N;
+  int32_t heads, dk, dv;
+  const float* decay;
+  float scale;
+  const int32_t* lengths;
+  const uint8_t* reset;
+  Segments seg;
+  float* states;     // workspace
+  float* factor;
+  hipStream_t st;
+};
+
+DecayArgs args_of(const Call& c, const Rows& A, const Rows& B, const Rows& C, const Rows& O, int32_t dk, int32_t dv) {
+  DecayArgs a{};
+  a.A = A; a.B = B; a.C = C; a.O = O; a.T = c.T; a.N = c.N; a.heads = c.heads; a.dk = dk; a.dv = dv;
+  a.decay = c.decay; a.reset = c.reset; a.lengths = c.lengths;
+  a.segs = c.seg.n; a.seg_len = c.seg.len;
+  a.alpha = c.scale; a.beta = 1.f; a.gam = c.scale;
+  a.in_r = a.out_r = dv; a.in_c = a.out_c = 1;
+  return a;
+}
+void backwards(DecayArgs& a, float scale) { a.reversed = 1; a.beta = scale; a.gam = 1.f; }
+
+// The states that enter the segments, from keys B and values C; the last one to s_out.
+template <class T>
+void join_segments(const Call& c, const DecayArgs& out_pass, const float* s_in, float* s_out, bool link) {
+  DecayArgs a = out_pass;
+  a.s_in = nullptr; a.s_out = c.states; a.out_r = a.dv; a.out_c = 1; a.out_link = 0; a.factor = c.factor;
+  launch<T, false>(a, c.st);
+  ScanArgs s{};
+  s.states = c.states; s.factor = c.factor; s.s_in = s_in; s.s_out = s_out; s.N = c.N; s.heads = c.heads; s.size = a.dk * a.dv;
+  s.segs = a.segs; s.out_link = link; s.decay = c.decay; s.reset = c.reset; s.lengths = c.lengths;
+  const int64_t n = c.N * c.heads * s.size;
+  hipLaunchKernelGGL(k_decay_scan, (unsigned)std::min<int64_t>((n + 255) / 256, 256 * 16), 256, 0, c.st, s);
+}
+
+template <class T>
+void forward(const Call& c, const Rows& q, const Rows& k, const Rows& v, const Rows& o, const float* s0, float* sn) {
+  DecayArgs a = args_of(c, q, k, v, o, c.dk, c.dv);
+  a.s_in = s0; a.s_out = sn;
+  if (c.T == 1) {
+    hipLaunchKernelGGL(k_decay_step<T>, (unsigned)std::min<int64_t>((c.N * c.heads + 3) / 4, 256 * 32), 256, 0, c.st, a);
+    return;
+  }
+  if (c.seg.n > 1) {
+    join_segments<T>(c, a, s0, sn, false);
+    a.s_in = c.states; a.s_out = nullptr;
+  }
+  launch<T, true>(a, c.st);
+}
+
+template <class T>
+void backward(const Call& c, const Rows& q, const Rows& k, const Rows& v, const Rows& go, const Rows& dq, const Rows& dk, const Rows& dv,
+              const float* s0, const float* dsn, float* ds0) {
+  const bool split = c.seg.n > 1;
+  if (dq.p) {
+    DecayArgs a = args_of(c, go, v, k, dq, c.dv, c.dk);
+    a.s_in = s0;
+    if (split) {
+      join_segments<T>(c, args_of(c, q, k, v, q, c.dk, c.dv), s0, nullptr, false);
+      a.s_in = c.states;
+    }
+    a.in_r = 1; a.in_c = c.dv;
+    launch<T, true>(a, c.st);
+  }
+  DecayArgs a = args_of(c, k, q, go, dv, c.dk, c.dv), b = args_of(c, v, go, q, dk, c.dv, c.dk);
+  backwards(a, c.scale);
+  backwards(b, c.scale);
+  a.s_in = b.s_in = dsn;
+  if (split && (dk.p || dv.p || ds0)) {
+    join_segments<T>(c, a, dsn, ds0, true);
+    a.s_in = b.s_in = c.states;
+  } else {
+    a.s_out = ds0; a.out_link = 1;      // after dk has read dsn: ds0 may be dsn
+  }
+  b.in_r = 1; b.in_c = c.dv;
+  if (dk.p) launch<T, true>(b, c.st);
+  if (dv.p) launch<T, true>(a, c.st);
+  else if (!split && ds0) launch<T, false>(a, c.st);
+}
+
+const char* check(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t dtype) {
+  if (dtype != DGC_DTYPE_F32 && dtype != DGC_DTYPE_BF16) return "decay attention: unknown dtype";
+  if (T < 0 || N < 0 || heads < 1 || heads > kMaxHeads) return "decay attention: T and N must be >= 0 and heads in [1, 1024]";
+  if (dk < 8 || dk > kMaxDim || dk % 8 || dv < 8 || dv > kMaxDim || dv % 8)
+    return "decay attention: dk and dv must be multiples of 8 in [8, 128]";
+  return nullptr;
+}
+bool too_many(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv) {   // waves of a launch: 31 bits
+  const int64_t most = (int64_t)1 << 31;
+  if (T > most || N > most) return true;
+  const int64_t seqs = N * heads * ((std::max(dk, dv) + 31) / 32);
+  return seqs >= most || seqs * segments_of(T, N, heads, dk, dv).n >= most;
+}
+// Inputs may repeat rows (a stride of 0); outputs hold each row once.
+bool good(const Rows& x, int64_t T, int64_t N, int64_t F, int e, bool output) {
+  if (T == 0 || N == 0) return true;
+  const int64_t per = 16 / e, most = INT64_MAX / 16;
+  if (!x.p || !ops::aligned16(x.p) || x.st < 0 || x.sn < 0 || x.st % per || x.sn % per) return false;
+  if (x.st > most / T || x.sn > most / N) return false;
+  if (!output) return true;
+  if (T > 1 && N > 1) return x.st >= x.sn ? x.sn >= F && x.st >= N * x.sn : x.st >= F && x.sn >= T * x.st;
+  return T > 1 ? x.st >= F : N > 1 ? x.sn >= F : true;
+}
+// Whether an output shares an element with another tensor; rows side by side in one buffer do not.
+bool meet(const Rows& x, int64_t Fx, const Rows& y, int64_t Fy, int64_t T, int64_t N, int e) {
+  if (!x.p || !y.p || T == 0 || N == 0) return false;
+  const uintptr_t x0 = (uintptr_t)x.p, y0 = (uintptr_t)y.p;
+  const uintptr_t x1 = x0 + ((T - 1) * x.st + (N - 1) * x.sn + Fx) * e, y1 = y0 + ((T - 1) * y.st + (N - 1) * y.sn + Fy) * e;
+  if (x0 >= y1 || y0 >= x1) return false;
+  if ((T > 1 && x.st != y.st) || (N > 1 && x.sn != y.sn)) return true;
+  const int64_t inner = T == 1 ? x.sn : N == 1 ? x.st : std::min(x.st, x.sn), outer = T == 1 || N == 1 ? inner : std::max(x.st, x.sn);
+  if ((T == 1 && N == 1) || inner == 0 || outer % inner) return true;
+  const uint64_t pitch = (uint64_t)inner * e, d = x0 >= y0 ? (x0 - y0) % pitch : (pitch - (y0 - x0) % pitch) % pitch;
+  return d < (uint64_t)Fy * e || d + (uint64_t)Fx * e > pitch;
+}
+constexpr const char* kBadRows =
+    "decay attention: tensors need a 16-byte aligned base and strides that are multiples of 16 bytes; an output's rows lie apart";
+constexpr const char* kMeet = "decay attention: outputs lie apart from the inputs and each other";
+
+}  // namespace
+}  // namespace dgc
+
+using namespace dgc;
+
+extern "C" {
+
+int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t backward) {
+  if (check(T, N, heads, dk, dv, 0) || too_many(T, N, heads, dk, dv)) return -1;
+  const Segments s = segments_of(T, N, heads, dk, dv);
+  return s.n > 1 ? 4 * (int64_t)s.n * N * heads * (dk * dv + 1) + 16 : 0;
+}
+
+static dgc_status_t decay_call(Call* c, int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, const float* decay, float scale,
+                               const int32_t* lengths, const uint8_t* reset, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (too_many(T, N, heads, dk, dv)) return ops::refuse(DGC_ERR_UNSUPPORTED, "decay attention: more sequences and heads than a launch takes");
+  if (!decay) return ops::refuse(DGC_ERR_INVALID_ARG, "decay attention: NULL decay");
+  const int64_t need = dgc_decay_attn_workspace_bytes(T, N, heads, dk, dv, 0);
+  if (need > 0 && (!workspace || !ops::aligned16(workspace) || workspace_bytes < need))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "decay attention: workspace missing, too small (dgc_decay_attn_workspace_bytes) or not 16-byte aligned");
+  *c = Call{T, N, heads, dk, dv, decay, scale, lengths, reset, segments_of(T, N, heads, dk, dv), static_cast<float*>(workspace), nullptr,
+            static_cast<hipStream_t>(stream)};
+  if (need > 0) c->factor = c->states + (int64_t)c->seg.n * N * heads * dk * dv;
+  return DGC_OK;
+}
+
+dgc_status_t dgc_decay_attn_forward(const void* q, int64_t qt, int64_t qn, const void* k, int64_t kt, int64_t kn, const void* v,
+                                    int64_t vt, int64_t vn, int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t dtype,
+                                    const float* decay, float scale, const float* s0, const int32_t* lengths, const uint8_t* reset,
+                                    void* o, int64_t ot, int64_t on, float* sn, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (const char* msg = check(T, N, heads, dk, dv, dtype)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
+  const int e = ops::elem_bytes(dtype);
+  const int64_t fk = (int64_t)heads * dk, fv = (int64_t)heads * dv;
+  const Rows Q{q, qt, qn}, K{k, kt, kn}, V{v, vt, vn}, O{o, ot, on};
+  if (!good(Q, T, N, fk, e, false) || !good(K, T, N, fk, e, false) || !good(V, T, N, fv, e, false) || !good(O, T, N, fv, e, true))
+    return ops::refuse(DGC_ERR_INVALID_ARG, kBadRows);
+  if (!ops::aligned16(s0) || !ops::aligned16(sn)) return ops::refuse(DGC_ERR_INVALID_ARG, "decay attention: states need 16-byte alignment");
+  Call c;
+  if (dgc_status_t rc = decay_call(&c, T, N, heads, dk, dv, decay, scale, lengths, reset, workspace, workspace_bytes, stream)) return rc;
+  if (meet(O, fv, Q, fk, T, N, e) || meet(O, fv, K, fk, T, N, e) || meet(O, fv, V, fv, T, N, e))
+    return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
+  if (N == 0) return DGC_OK;
+  if (dtype == DGC_DTYPE_F32) forward<float>(c, Q, K, V, O, s0, sn);
+  else forward<uint16_t>(c, Q, K, V, O, s0, sn);
+  return ops::launched("decay attention");
+}
+
+dgc_status_t dgc_decay_attn_backward(const void* q, int64_t qt, int64_t qn, const void* k, int64_t kt, int64_t kn, const void* v,
+                                     int64_t vt, int64_t vn, const void* go, int64_t gt, int64_t gn, int64_t T, int64_t N,
+                                     int32_t heads, int32_t dk, int32_t dv, int32_t dtype, const float* decay, float scale,
+                                     const float* s0, const float* dsn, const int32_t* lengths, const uint8_t* reset, void* dq,
+                                     int64_t dqt, int64_t dqn, void* dkey, int64_t dkt, int64_t dkn, void* dval, int64_t dvt,
+                                     int64_t dvn, float* ds0, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (const char* msg = check(T, N, heads, dk, dv, dtype)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
+  const int e = ops::elem_bytes(dtype);
+  const int64_t fk = (int64_t)heads * dk, fv = (int64_t)heads * dv;
+  const Rows in[4] = {{q, qt, qn}, {k, kt, kn}, {v, vt, vn}, {go, gt, gn}}, out[3] = {{dq, dqt, dqn}, {dkey, dkt, dkn}, {dval, dvt, dvn}};
+  const int64_t fi[4] = {fk, fk, fv, fv}, fo[3] = {fk, fk, fv};
+  for (int x = 0; x < 4; ++x) {
+    if (!good(in[x], T, N, fi[x], e, false)) return ops::refuse(DGC_ERR_INVALID_ARG, kBadRows);
+  }
+  for (int x = 0; x < 3; ++x) {
+    if (out[x].p && !good(out[x], T, N, fo[x], e, true)) return ops::refuse(DGC_ERR_INVALID_ARG, kBadRows);
+  }
+  if (!ops::aligned16(s0) || !ops::aligned16(dsn) || !ops::aligned16(ds0))
+    return ops::refuse(DGC_ERR_INVALID_ARG, "decay attention: states need 16-byte alignment");
+  Call c;
+  if (dgc_status_t rc = decay_call(&c, T, N, heads, dk, dv, decay, scale, lengths, reset, workspace, workspace_bytes, stream)) return rc;
+  for (int x = 0; x < 3; ++x) {
+    for (int y = 0; y < 4; ++y) {
+      if (meet(out[x], fo[x], in[y], fi[y], T, N, e)) return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
+    }
+    for (int y = 0; y < x; ++y) {
+      if (meet(out[x], fo[x], out[y], fo[y], T, N, e)) return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
+    }
+  }
+  if (N == 0) return DGC_OK;
+  if (dtype == DGC_DTYPE_F32) backward<float>(c, in[0], in[1], in[2], in[3], out[0], out[1], out[2], s0, dsn, ds0);
+  else backward<uint16_t>(c, in[0], in[1], in[2], in[3], out[0], out[1], out[2], s0, dsn, ds0);
+  return ops::launched("decay attention");
+}
+
+}  // extern "C"

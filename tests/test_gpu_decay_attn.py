@@ -1,0 +1,336 @@
+"""Linear attention with a decay per head, forward, backward, chained and token by token, against the recurrence in double.
+
+Tolerances count roundings against magnitudes: the same recurrence over absolute values.  A result of the element type
+is off by half a step of it.  Before that, fp32: each product and sum is cut off by the matrix unit at 2^-23 of its partial
+sum, at most dk/16 + 32 of them in scores, as many again in outputs, and 8 for each 32 tokens in the state, the decay's powers 2^-24
+each: (T/32 * 8 + 160) 2^-23 covers them.  bf16 kernels take scores and states in two bf16 parts in the output: 2^-16 each, 2^-15."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+def _dt(dtype):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+
+
+def _reference(q, k, v, decay, scale, s0, lengths, reset, heads, do=None, dsn=None):
+    """Outputs of the recurrence in double: (o, sn), and with do: (o, sn, dq, dk, dv, ds0).  Rows behind a sequence: zero."""
+    import torch
+    T, N = q.shape[:2]
+    Q, K, V = (x.double().reshape(T, N, heads, -1) for x in (q, k, v))
+    dk, dv = Q.shape[-1], V.shape[-1]
+    S = s0.double() if s0 is not None else torch.zeros(N, heads, dk, dv, dtype=torch.float64, device=q.device)
+    g = decay.double()[None, :, None, None]
+    n = lengths.clamp(0, T) if lengths is not None else torch.full((N,), T, device=q.device)
+    o, hist = torch.zeros_like(V), [S]
+
+    def live(t, x):
+        return (t < n).reshape(-1, *[1] * (x.dim() - 1))
+
+    def linked(t, x):
+        return x if reset is None else torch.where((reset[t] != 0)[:, None, None, None], 0.0, x)
+
+    for t in range(T):
+        new = linked(t, g * S) + K[t][..., :, None] * V[t][..., None, :]
+        S = torch.where(live(t, S), new, S)
+        o[t] = torch.where(live(t, o[t]), scale * (Q[t][..., :, None] * S).sum(-2), 0.0)
+        hist.append(S)
+    if do is None:
+        return o.reshape(T, N, -1), S
+    D = do.double().reshape(T, N, heads, -1)
+    G = dsn.double() if dsn is not None else torch.zeros_like(S)
+    dq, dkk, dvv = torch.zeros_like(Q), torch.zeros_like(K), torch.zeros_like(V)
+    for t in range(T - 1, -1, -1):
+        a = live(t, S)
+        G = torch.where(a, G + scale * Q[t][..., :, None] * D[t][..., None, :], G)
+        dq[t] = torch.where(a[..., 0], scale * (hist[t + 1] * D[t][..., None, :]).sum(-1), 0.0)
+        dkk[t] = torch.where(a[..., 0], (G * V[t][..., None, :]).sum(-1), 0.0)
+        dvv[t] = torch.where(a[..., 0], (G * K[t][..., :, None]).sum(-2), 0.0)
+        G = torch.where(a, linked(t, g * G), G)
+    return o.reshape(T, N, -1), S, dq.reshape(T, N, -1), dkk.reshape(T, N, -1), dvv.reshape(T, N, -1), G
+
+
+def _case(T, N, heads, dk, dv, dtype, seed, *, state=True, reset=0.0, ragged=False, batch_first=False, fused=False):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = _dt(dtype)
+
+    def rows(d, fill=None):
+        shape = (N, T, d + 16) if batch_first else (T, N, d + 16)      # wider rows: strides that are not the width
+        t = torch.randn(*shape, generator=g, device="cuda") if fill is None else torch.full(shape, fill, device="cuda")
+        t = t.to(dt)[..., 8:8 + d]
+        return t.transpose(0, 1) if batch_first else t
+
+    c = dict(q=rows(heads * dk), k=rows(heads * dk), v=rows(heads * dv), do=rows(heads * dv))
+    if fused:     # one buffer, as a fused product leaves it
+        x = torch.randn(T, N, heads * (2 * dk + dv), generator=g, device="cuda").to(dt)
+        c["q"], c["k"], c["v"] = x.split([heads * dk, heads * dk, heads * dv], -1)
+    c["decay"] = torch.rand(heads, generator=g, device="cuda") * 0.6 + 0.4
+    c["scale"] = dk ** -0.5
+    c["s0"] = torch.randn(N, heads, dk, dv, generator=g, device="cuda") if state else None
+    c["dsn"] = torch.randn(N, heads, dk, dv, generator=g, device="cuda") if state else None
+    c["reset"] = (torch.rand(T, N, generator=g, device="cuda") < reset).to(torch.uint8) if reset else None
+    c["lengths"] = torch.randint(-1, T + 2, (N,), generator=g, device="cuda", dtype=torch.int32) if ragged else None
+    c["rows"] = rows
+    c["dims"] = (T, N, heads, dk, dv)
+    return c
+
+
+def _workspace(binding, dims, fill=float("nan")):
+    import torch
+    n = binding.decay_attn_workspace_bytes(*dims, backward=True)
+    return torch.full((n // 4,), fill, device="cuda") if n else None
+
+
+def _run_forward(c, **kw):
+    import torch
+    from paper_2309_03523_amd import binding
+    T, N, heads, dk, dv = c["dims"]
+    o = c["rows"](heads * dv, -7.0)
+    sn = torch.full((N, heads, dk, dv), float("nan"), device="cuda")
+    binding.decay_attn_forward(c["q"], c["k"], c["v"], c["decay"], o, heads=heads, scale=c["scale"], s0=c["s0"], sn=sn, lengths=c["lengths"],
+                               reset=c["reset"], workspace=_workspace(binding, c["dims"]), **kw)
+    return o, sn
+
+
+def _run_backward(c, **kw):
+    import torch
+    from paper_2309_03523_amd import binding
+    T, N, heads, dk, dv = c["dims"]
+    dq, dkk, dvv = c["rows"](heads * dk, -7.0), c["rows"](heads * dk, -7.0), c["rows"](heads * dv, -7.0)
+    ds0 = torch.full((N, heads, dk, dv), float("nan"), device="cuda")
+    binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], dq, dkk, dvv, heads=heads, scale=c["scale"], s0=c["s0"], dsn=c["dsn"],
+                                ds0=ds0, lengths=c["lengths"], reset=c["reset"], workspace=_workspace(binding, c["dims"]), **kw)
+    return dq, dkk, dvv, ds0
+
+
+def _fp32_tol(T):
+    return (T / 32 * 8 + 160) * 2.0 ** -23
+
+
+def _absolute(c):
+    a = {k: (x.abs() if x is not None and x.is_floating_point() else x) for k, x in c.items() if k in ("q", "k", "v", "do", "s0", "dsn", "reset", "lengths", "decay")}
+    return a
+
+
+def _ref(c, back=False):
+    h = c["dims"][2]
+    a = _absolute(c)
+    more = lambda d: dict(do=d["do"], dsn=d["dsn"]) if back else {}  # noqa: E731
+    return (_reference(c["q"], c["k"], c["v"], c["decay"], c["scale"], c["s0"], c["lengths"], c["reset"], h, **more(c)),
+            _reference(a["q"], a["k"], a["v"], a["decay"], c["scale"], a["s0"], a["lengths"], a["reset"], h, **more(a)))
+
+
+def _close(got, want, mag, dtype, T, state=False):
+    tol = _fp32_tol(T) * mag + 1e-30
+    if not state:
+        tol = tol + HALF[dtype] * want.abs() + (2.0 ** -15 * mag if dtype == "bf16" else 0)
+    else:
+        tol = tol + 2.0 ** -24 * want.abs()
+    bad = ~((got.double() - want).abs() <= tol)
+    assert not bool(bad.any()), (int(bad.sum()), float(((got.double() - want).abs() / tol).nan_to_num(1e9).max()))
+
+
+def _behind(c, x):
+    """Rows behind the sequences are as they were filled."""
+    import torch
+    if c["lengths"] is None:
+        return
+    T = c["dims"][0]
+    off = torch.arange(T, device="cuda")[:, None] >= c["lengths"]
+    assert bool((x[off] == -7.0).all())
+
+
+def _live(c, x):
+    import torch
+    if c["lengths"] is None:
+        return x
+    off = torch.arange(c["dims"][0], device="cuda")[:, None] >= c["lengths"]
+    return torch.where(off[..., None], torch.zeros((), dtype=x.dtype, device="cuda"), x)
+
+
+DIMS = [(1, 1, 1, 8, 8), (1, 7, 3, 16, 24), (1, 5, 2, 128, 128), (1, 9, 2, 64, 40), (2, 3, 2, 8, 16), (16, 11, 8, 16, 16), (17, 5, 3, 16, 32), (31, 4, 1, 32, 8),
+        (32, 6, 4, 32, 32), (33, 3, 2, 40, 64), (64, 2, 2, 64, 64), (65, 3, 1, 128, 128), (100, 2, 3, 24, 128), (129, 2, 2, 64, 32), (300, 2, 2, 128, 72),
+        (1000, 1, 1, 64, 64)]
+MODES = [dict(), dict(state=False), dict(reset=0.2), dict(reset=0.2, ragged=True, batch_first=True), dict(ragged=True, state=False), dict(fused=True, reset=0.9)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dims", DIMS)
+def test_forward(dims, dtype):
+    for k, mode in enumerate(MODES):
+        c = _case(*dims, dtype, sum(dims) + k, **mode)
+        (o, sn), (mo, ms) = _ref(c)
+        got, state = _run_forward(c)
+        _behind(c, got)
+        _close(_live(c, got), o, mo, dtype, dims[0])
+        _close(state, sn, ms, dtype, dims[0], state=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dims", DIMS)
+def test_backward(dims, dtype):
+    for k, mode in enumerate(MODES):
+        c = _case(*dims, dtype, sum(dims) + 10 + k, **mode)
+        want, mag = _ref(c, back=True)
+        got = _run_backward(c)
+        for x, w, m, state in zip(got, want[2:], mag[2:], (False, False, False, True)):
+            if not state:
+                _behind(c, x)
+                x = _live(c, x)
+            _close(x, w, m, dtype, dims[0], state)
+
+
+def test_gradients_against_differences():
+    """fp32 gradients of sum(do * o) + sum(dsn * sn) against central differences of the recurrence in double."""
+    import torch
+    c = _case(40, 3, 2, 16, 24, "f32", 3, reset=0.1, ragged=True)
+    got = dict(zip(("q", "k", "v", "s0"), _run_backward(c)))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def f(**kw):
+        d = {**{k: c[k] for k in ("q", "k", "v", "s0")}, **kw}
+        o, sn = _reference(d["q"], d["k"], d["v"], c["decay"], c["scale"], d["s0"], c["lengths"], c["reset"], 2)
+        return float((o * c["do"].double()).sum() + (sn * c["dsn"].double()).sum())
+
+    h = 1e-6
+    for name, gr in got.items():
+        gr = _live(c, gr).double() if name != "s0" else gr.double()
+        e = torch.randn(gr.shape, generator=gen, device="cuda", dtype=torch.float64)
+        slope = (f(**{name: c[name].double() + h * e}) - f(**{name: c[name].double() - h * e})) / (2 * h)
+        assert abs(float((gr * e).sum()) - slope) <= 1e-5 * float((gr * e).abs().sum()), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_windows_and_single_tokens_chain(dtype):
+    """A long run, the same in windows whose states are handed on, in place, and token by token."""
+    import torch
+    from paper_2309_03523_amd import binding
+    c = _case(70, 5, 3, 32, 40, dtype, 8, reset=0.05)
+    want, sn = _run_forward(c)
+    (wo, ws_), (mo, ms) = _ref(c)
+    for cuts in ([0, 33, 34, 64, 70], list(range(71))):
+        s, o = c["s0"].clone(), torch.empty_like(want)
+        for a, b in zip(cuts, cuts[1:]):
+            binding.decay_attn_forward(c["q"][a:b], c["k"][a:b], c["v"][a:b], c["decay"], o[a:b], heads=3, scale=c["scale"], s0=s, sn=s,
+                                       reset=c["reset"][a:b])
+        _close(o, wo, mo, dtype, 70)
+        _close(s, ws_, ms, dtype, 70, state=True)
+    s = c["dsn"].clone()        # ds0 in the place of dsn
+    dq, dkk, dvv, ds0 = _run_backward(c)
+    binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], torch.empty_like(dq), torch.empty_like(dkk), torch.empty_like(dvv), heads=3,
+                                scale=c["scale"], s0=c["s0"], dsn=s, ds0=s, reset=c["reset"])
+    assert torch.equal(s, ds0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("decay", [0.0, 1.0, 1e-20])
+def test_extreme_decays(decay, dtype):
+    import torch
+    c = _case(77, 3, 2, 16, 16, dtype, 4)
+    c["decay"] = torch.full((2,), decay, device="cuda")
+    (o, sn), (mo, ms) = _ref(c)
+    got, state = _run_forward(c)
+    _close(got, o, mo, dtype, 77)
+    _close(state, sn, ms, dtype, 77, state=True)
+    want, mag = _ref(c, back=True)
+    for x, w, m, st in zip(_run_backward(c), want[2:], mag[2:], (False, False, False, True)):
+        _close(x, w, m, dtype, 77, st)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 30, 90, 600])
+def test_values_that_are_not_finite_reach_what_the_formula_lets_them(T, dtype):
+    """Behind a sequence's end anything may stand; a NaN or infinity in a live token is seen by that token and those after it up to
+    the next reset, in its own columns, and by no other sequence or head."""
+    import torch
+    c = _case(T, 4, 2, 32, 40, dtype, 6, reset=0.05)
+    c["lengths"] = torch.tensor([T, max(T - 3, 0), 0, T], dtype=torch.int32, device="cuda")
+    for x in ("q", "k", "v", "do"):
+        for i in range(4):
+            c[x][int(c["lengths"][i]):, i] = float("nan")
+    (o, sn), (mo, ms) = _ref(c)
+    got, state = _run_forward(c)
+    _behind(c, got)
+    _close(_live(c, got), o, mo, dtype, T)
+    _close(state, sn, ms, dtype, T, state=True)
+    want, mag = _ref(c, back=True)
+    for x, w, m, st in zip(_run_backward(c), want[2:], mag[2:], (False, False, False, True)):
+        _close(x if st else _live(c, x), w, m, dtype, T, st)
+    # live ones
+    c["lengths"] = None
+    for x in ("q", "k", "v", "do"):
+        c[x][:, 1:3] = 0.5
+    t = T // 2
+    c["v"][t, 0, 3], c["k"][t, 1, 5], c["v"][T - 1, 3, 79], c["s0"][2, 1, 4, 7] = float("nan"), float("inf"), float("-inf"), float("inf")
+    if T > 40:
+        c["reset"][t + 9, :2] = 1
+    (o, sn), _ = _ref(c)
+    got, state = _run_forward(c)
+    for x, w in ((got, o), (state, sn)):
+        assert torch.equal(torch.isnan(x), torch.isnan(w)) and torch.equal(torch.isinf(x), torch.isinf(w))
+        fine = torch.isfinite(w)
+        assert bool((x[fine].double() - w[fine]).abs().max() <= (0.02 if dtype == "bf16" else 1e-3) * w[fine].abs().max())
+
+
+def test_repeated_rows_and_empty_calls():
+    """An input expanded over the sequences (stride 0); no tokens; no sequences."""
+    import torch
+    from paper_2309_03523_amd import binding
+    c = _case(20, 6, 2, 16, 16, "f32", 5)
+    c["k"] = c["k"][:, :1].expand(-1, 6, -1)
+    (o, sn), (mo, ms) = _ref(c)
+    got, state = _run_forward(c)
+    _close(got, o, mo, "f32", 20)
+    _close(state, sn, ms, "f32", 20, state=True)
+    e = torch.empty(0, 6, 32, device="cuda")
+    sn = torch.empty_like(c["s0"])
+    binding.decay_attn_forward(e, e, e, c["decay"], torch.empty_like(e), heads=2, s0=c["s0"], sn=sn)
+    assert torch.equal(sn, c["s0"])
+    binding.decay_attn_backward(e, e, e, c["decay"], e, torch.empty_like(e), torch.empty_like(e), torch.empty_like(e), heads=2, dsn=c["s0"], ds0=sn)
+    assert torch.equal(sn, c["s0"])
+    e = torch.empty(5, 0, 32, device="cuda")
+    binding.decay_attn_forward(e, e, e, c["decay"], torch.empty_like(e), heads=2)
+
+
+@pytest.mark.parametrize("dims", [(33, 50, 4, 32, 32), (700, 2, 2, 64, 64)])
+def test_streams_graphs_and_repeats(dims):
+    import torch
+    from paper_2309_03523_amd import binding
+    T, N, heads, dk, dv = dims
+    c = _case(*dims, "bf16", 11, reset=0.02, ragged=True)
+
+    def room():
+        return [c["rows"](heads * dv, 0.0), torch.zeros(N, heads, dk, dv, device="cuda"), c["rows"](heads * dk, 0.0), c["rows"](heads * dk, 0.0),
+                c["rows"](heads * dv, 0.0), torch.zeros(N, heads, dk, dv, device="cuda"), _workspace(binding, dims)]
+
+    def step(r, stream=None):
+        kw = dict(heads=heads, scale=c["scale"], s0=c["s0"], lengths=c["lengths"], reset=c["reset"], workspace=r[6], stream=stream)
+        binding.decay_attn_forward(c["q"], c["k"], c["v"], c["decay"], r[0], sn=r[1], **kw)
+        binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], r[2], r[3], r[4], dsn=c["dsn"], ds0=r[5], **kw)
+
+    want, other, out = room(), room(), room()
+    step(want)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    step(other, s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want[:6], other[:6]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for k in range(3):
+        c["q"].mul_(0.5)
+        c["reset"].copy_(c["reset"].roll(1, 0))
+        step(want)
+        torch.cuda.synchronize()
+        for t in out[:6]:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want[:6], out[:6])), k

@@ -103,3 +103,39 @@ def test_linear_refusals(lib):
     for dt in (0, 1):
         sizes = [size(r, 128, 512, dt, 2) for r in (0, 1, 1000, 10 ** 6, 10 ** 8)]
         assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
+
+
+def test_decay_attention_refusals(lib):
+    D, E, F = 0x40000000, 0x50000000, 0x60000000
+    good = dict(q=A, qt=320, qn=64, k=B, kt=320, kn=64, v=C, vt=320, vn=64, T=6, N=5, heads=2, dk=32, dv=32, dtype=0, decay=D, scale=1.0, s0=None, lengths=None,
+                reset=None, o=E, ot=320, on=64, sn=None, ws=None, ws_bytes=0, stream=None)
+
+    def fwd(**kw):
+        return lib.dgc_decay_attn_forward(*{**good, **kw}.values())
+
+    for kw in (dict(q=None), dict(v=None), dict(o=None), dict(decay=None), dict(q=A + 8), dict(kt=322), dict(vn=62), dict(qt=-320), dict(T=-1), dict(N=-1),
+               dict(heads=0), dict(heads=1025), dict(dk=12), dict(dk=136), dict(dv=0), dict(dv=129), dict(dtype=2), dict(on=60), dict(ot=256), dict(on=0), dict(ot=0),
+               dict(o=A), dict(o=B + 16), dict(o=C, ot=640, on=128), dict(s0=D + 4), dict(sn=D + 8), dict(q=A, qt=640, qn=128, o=A + 128, ot=640, on=128)):
+        assert fwd(**kw) == INVALID, kw
+        assert "decay attention" in _text(lib)
+    assert fwd(N=1 << 30, qn=0, kn=0, vn=0, ot=64, on=64 * 6) == UNSUPPORTED
+    assert fwd(N=0, q=None, k=None, v=None, o=None) == OK
+    long = dict(T=4096, N=2, qt=128, kt=128, vt=128, ot=128)
+    need = lib.dgc_decay_attn_workspace_bytes(4096, 2, 2, 32, 32, 0)
+    assert need > 0 and fwd(**long) == INVALID and "workspace" in _text(lib)
+    assert fwd(**long, ws=F, ws_bytes=need - 1) == INVALID and fwd(**long, ws=F + 4, ws_bytes=need) == INVALID
+    assert lib.dgc_decay_attn_workspace_bytes(16, 100000, 8, 16, 16, 1) == 0
+    for bad in ((-1, 1, 1, 8, 8), (1, -1, 1, 8, 8), (1, 1, 0, 8, 8), (1, 1, 1, 7, 8), (1, 1, 1, 8, 200)):
+        assert lib.dgc_decay_attn_workspace_bytes(*bad, 0) < 0
+    G = [0x70000000 + (x << 24) for x in range(3)]
+    good = dict(q=A, qt=320, qn=64, k=B, kt=320, kn=64, v=C, vt=320, vn=64, go=F, gt=320, gn=64, T=6, N=5, heads=2, dk=32, dv=32, dtype=0, decay=D, scale=1.0, s0=None,
+                dsn=None, lengths=None, reset=None, dq=G[0], dqt=320, dqn=64, dk_=G[1], dkt=320, dkn=64, dv_=G[2], dvt=320, dvn=64, ds0=None, ws=None, ws_bytes=0,
+                stream=None)
+
+    def bwd(**kw):
+        return lib.dgc_decay_attn_backward(*{**good, **kw}.values())
+
+    for kw in (dict(go=None), dict(dq=A), dict(dk_=G[0]), dict(dv_=F), dict(dvn=32), dict(ds0=D + 4), dict(dsn=D + 4), dict(heads=0), dict(dtype=9),
+               dict(dv_=G[1] + 32), dict(gt=3)):
+        assert bwd(**kw) == INVALID, kw
+        assert "decay attention" in _text(lib)
