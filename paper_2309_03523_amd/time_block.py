@@ -1,0 +1,181 @@
+"""A pre-norm time block over snapshots, built of the library's operators: a trainable time encoder whose state is carried
+from window to window (as H0 / HN of the recurrent layers), to stand behind a structure encoder or another block.
+
+    n = norm1(x);  q, k, v = qkv(n);  o = linear attention with a decay per head over every vertex' sequence
+    m = x + out(o);  y = m + down(act(up(norm2(m))))
+
+x, y are [T, N, width], snapshots by vertices, float32 or bfloat16.  Every step runs in the HIP library
+(binding.norm_*, linear_*, decay_attn_*); PyTorch supplies device memory and the stream.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from . import binding
+
+NAMES = ["norm1.weight", "norm1.bias", "qkv.weight", "qkv.bias", "out.weight", "out.bias", "norm2.weight", "norm2.bias",
+         "up.weight", "up.bias", "down.weight", "down.bias"]
+
+
+class TimeBlock:
+    """width = heads * size of a head (a multiple of 8, at most 128); hidden: width between up and down.  decay: one number in
+    [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.
+
+    Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad".  A block runs one
+    call at a time.  Its buffers are made at the first call with new sizes and kept until release(), so a call may be captured
+    into a HIP graph after an eager one of the same sizes."""
+
+    def __init__(self, width: int, heads: int, hidden: int, *, dtype: str = "f32", act: str = "gelu", decay=None, eps: float = 1e-5,
+                 device="cuda:0"):
+        import torch
+        if heads < 1 or width % heads or (width // heads) % 8 or width // heads > 128:
+            raise ValueError("width must be heads times a multiple of 8 that is at most 128")
+        if hidden < 1 or act not in binding.LINEAR_ACT or dtype not in binding.DTYPE:
+            raise ValueError("unknown activation or element type, or hidden < 1")
+        self.width, self.heads, self.hidden, self.act, self.eps = width, heads, hidden, act, float(eps)
+        self.dtype_name, self.dtype = dtype, {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        g = np.asarray(decay if decay is not None else 1.0 - 2.0 ** -(2.0 + 6.0 * np.arange(heads) / heads), np.float32).reshape(-1)
+        if g.size != heads or not ((g >= 0) & (g <= 1)).all():
+            raise ValueError("decay must hold one number in [0, 1] for each head")
+        self._decay = torch.from_numpy(g).to(self.device)
+        W = width
+        self.shapes = {"norm1.weight": (W,), "norm1.bias": (W,), "qkv.weight": (3 * W, W), "qkv.bias": (3 * W,), "out.weight": (W, W),
+                       "out.bias": (W,), "norm2.weight": (W,), "norm2.bias": (W,), "up.weight": (hidden, W), "up.bias": (hidden,),
+                       "down.weight": (W, hidden), "down.bias": (W,)}
+        self._p = {n: self._room(s, self._kind(n)) for n, s in self.shapes.items()}
+        for n in ("norm1.weight", "norm2.weight"):
+            self._p[n].fill_(1.0)
+        self._g = {}
+        self._buffers = {}
+        self._last = None
+
+    def _kind(self, name: str):
+        import torch
+        return self.dtype if len(self.shapes[name]) == 2 else torch.float32
+
+    def _room(self, shape, dtype):
+        """Zeroed rows at a pitch that is a multiple of 16 bytes."""
+        import torch
+        per = 16 // torch.empty(0, dtype=dtype).element_size()
+        buf = torch.zeros(*shape[:-1], -(-shape[-1] // per) * per, dtype=dtype, device=self.device)
+        return buf[..., :shape[-1]]
+
+    # -- parameters
+    def set_param(self, name: str, value):
+        import torch
+        v = torch.from_numpy(np.ascontiguousarray(value, np.float32))
+        if tuple(v.shape) != self.shapes[name]:
+            raise ValueError(f"{name} must have shape {self.shapes[name]}")
+        self._p[name].copy_(v.to(self._p[name].dtype))
+
+    def set_params(self, params: dict):
+        for k, v in params.items():
+            self.set_param(k, v)
+
+    def get_param(self, name: str) -> np.ndarray:
+        """The parameter as the kernels use it, or "<name>.grad" after a backward, as fp32."""
+        if name.endswith(".grad"):
+            if name[:-5] not in self._g:
+                raise RuntimeError("no gradient yet: run a backward first")
+            return self._g[name[:-5]].float().cpu().numpy()
+        return self._p[name].float().cpu().numpy()
+
+    # -- memory
+    def release(self):
+        """Drops the buffers of all sizes; graphs captured before must not be replayed after it."""
+        self._buffers.clear()
+        self._last = None
+
+    def _made(self, T: int, N: int, train: bool, stream):
+        import torch
+        key = (T, N, train)
+        b = self._buffers.get(key)
+        if b is not None:
+            return b
+        W, Hd, h = self.width, self.hidden, self.heads
+        b = {"n": self._room((T, N, W), self.dtype), "qkv": self._room((T, N, 3 * W), self.dtype), "o": self._room((T, N, W), self.dtype),
+             "m": self._room((T, N, W), self.dtype), "u": self._room((T, N, Hd), self.dtype)}
+        ws = binding.decay_attn_workspace_bytes(T, N, h, W // h, W // h, backward=train)
+        if train:
+            R = T * N
+            b["n2"], b["pre"] = self._room((T, N, W), self.dtype), self._room((T, N, Hd), self.dtype)
+            for k in ("mean1", "rstd1", "mean2", "rstd2"):
+                b[k] = torch.empty(R, device=self.device)
+            b["du"], b["dw"], b["dm"] = self._room((T, N, Hd), self.dtype), self._room((T, N, W), self.dtype), self._room((T, N, W), self.dtype)
+            b["dqkv"] = self._room((T, N, 3 * W), self.dtype)
+            size = lambda k, m, act: binding.linear_workspace_bytes(R, k, m, dtype=self.dtype_name, act=act)  # noqa: E731
+            ws = max(ws, binding.norm_workspace_bytes(R, W), size(W, 3 * W, "none"), size(W, W, "none"), size(W, Hd, self.act),
+                     size(Hd, W, "none"))
+            if not self._g:
+                self._g = {n: self._room(s, self._kind(n)) for n, s in self.shapes.items()}
+        else:
+            b["n2"] = b["n"]       # nothing is read again
+        b["ws"] = torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device)
+        if stream is not None:     # the zeros above were written on the current stream
+            stream.wait_stream(torch.cuda.current_stream(self.device))
+        self._buffers[key] = b
+        return b
+
+    def _blank(self, t, lengths, stream):
+        """Rows behind the sequences hold what an earlier call left; no attention and no gradient there is zero."""
+        import torch
+        if lengths is not None:
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                t.zero_()
+
+    def _rows(self, t, name: str):
+        if t.dim() != 3 or t.shape[2] != self.width or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"{name} must be [T, N, {self.width}] of the block's element type and device")
+
+    # -- the path
+    def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, train: bool = True, stream=None):
+        """Y = block(X).  S0, SN fp32 [N, heads, d, d]: states entering and leaving the window (SN may be S0); lengths, reset as
+        binding.decay_attn_forward has them (rows behind a sequence take part in the row-wise steps alone).  train=True keeps what
+        backward reads; T = 1 with train=False is the form for one new snapshot."""
+        self._rows(X, "X")
+        self._rows(Y, "Y")
+        T, N = X.shape[:2]
+        b, p, W = self._made(T, N, train, stream), self._p, self.width
+        q, k, v = b["qkv"][..., :W], b["qkv"][..., W:2 * W], b["qkv"][..., 2 * W:]
+        binding.norm_forward(X, b["n"], gamma=p["norm1.weight"], beta=p["norm1.bias"], mean=b.get("mean1"), rstd=b.get("rstd1"), eps=self.eps,
+                             stream=stream)
+        binding.linear_forward(b["n"], p["qkv.weight"], b["qkv"], bias=p["qkv.bias"], stream=stream)
+        self._blank(b["o"], lengths, stream)
+        binding.decay_attn_forward(q, k, v, self._decay, b["o"], heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0, sn=SN, lengths=lengths,
+                                   reset=reset, workspace=b["ws"], stream=stream)
+        binding.linear_forward(b["o"], p["out.weight"], b["m"], bias=p["out.bias"], residual=X, stream=stream)
+        binding.norm_forward(b["m"], b["n2"], gamma=p["norm2.weight"], beta=p["norm2.bias"], mean=b.get("mean2"), rstd=b.get("rstd2"),
+                             eps=self.eps, stream=stream)
+        binding.linear_forward(b["n2"], p["up.weight"], b["u"], bias=p["up.bias"], act=self.act, pre=b.get("pre"), stream=stream)
+        binding.linear_forward(b["u"], p["down.weight"], Y, bias=p["down.bias"], residual=b["m"], stream=stream)
+        self._last = (b, X, S0, lengths, reset) if train else None
+        return Y
+
+    def backward(self, dY, *, dX=None, dSN=None, dS0=None, stream=None):
+        """Gradients of the last forward with train=True: of the parameters (get_param("<name>.grad")), of X into dX if given
+        (dX may be dY), and of S0 into dS0.  X, S0, lengths and reset of that forward must be unchanged."""
+        if self._last is None:
+            raise RuntimeError("backward follows a forward with train=True")
+        b, X, S0, lengths, reset = self._last
+        self._rows(dY, "dY")
+        if dY.shape != X.shape:
+            raise ValueError("dY must have the shape of the forward's X")
+        p, g, W = self._p, self._g, self.width
+        ws = b["ws"]
+        cut = lambda t: (t[..., :W], t[..., W:2 * W], t[..., 2 * W:])  # noqa: E731
+        lin = lambda dy, x, n, dx, **kw: binding.linear_backward(dy, x, p[n + ".weight"], dx=dx, dw=g[n + ".weight"], dbias=g[n + ".bias"],  # noqa: E731
+                                                                  workspace=ws, stream=stream, **kw)
+        lin(dY, b["u"], "down", b["du"])
+        lin(b["du"], b["n2"], "up", b["dw"], pre=b["pre"], act=self.act)
+        binding.norm_backward(b["dw"], b["m"], b["mean2"], b["rstd2"], b["dm"], gamma=p["norm2.weight"], add=dY, dgamma=g["norm2.weight"],
+                              dbeta=g["norm2.bias"], workspace=ws, stream=stream)
+        lin(b["dm"], b["o"], "out", b["dw"])
+        self._blank(b["dqkv"], lengths, stream)
+        binding.decay_attn_backward(*cut(b["qkv"]), self._decay, b["dw"], *cut(b["dqkv"]), heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0,
+                                    dsn=dSN, ds0=dS0, lengths=lengths, reset=reset, workspace=ws, stream=stream)
+        lin(b["dqkv"], b["n"], "qkv", b["dw"])
+        binding.norm_backward(b["dw"], X, b["mean1"], b["rstd1"], dX if dX is not None else b["dw"], gamma=p["norm1.weight"], add=b["dm"],
+                              dgamma=g["norm1.weight"], dbeta=g["norm1.bias"], workspace=ws, stream=stream)

@@ -1,0 +1,179 @@
+"""The time block: its operators run together, as they are used, against the same formulas in double with torch's gradients.
+
+Tolerances: fp32 steps are each off by under 4e-6 of the magnitudes they add up, the chain has twelve and a norm multiplies by up to
+1/std (about 1 here): 2e-4 of a tensor's largest value.  bf16 rounds the activations ten times on the way, by half a step 2^-8
+each of the value at hand: 10 * 2^-8 of the root mean square, times up to 2 where the gradients add up two branches: 0.08."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _params(block, seed):
+    rng = np.random.default_rng(seed)
+    out = {}
+    for n, s in block.shapes.items():
+        if len(s) == 2:
+            out[n] = rng.normal(0, s[1] ** -0.5, s).astype(np.float32)
+        else:
+            out[n] = ((1.0 if n.startswith("norm") and n.endswith("weight") else 0.0) + rng.normal(0, 0.2, s)).astype(np.float32)
+    block.set_params(out)
+    return {n: block.get_param(n) for n in out}      # as rounded
+
+
+def _norm(x, w, b, eps):
+    xc = x - x.mean(-1, keepdim=True)
+    return xc / (xc.square().mean(-1, keepdim=True) + eps).sqrt() * w + b
+
+
+def _formula(block, P, x, s0, lengths, reset):
+    """Output and last state in double; P: dict of double tensors."""
+    import torch
+    T, N, W = x.shape
+    h = block.heads
+    d = W // h
+    qkv = _norm(x, P["norm1.weight"], P["norm1.bias"], block.eps) @ P["qkv.weight"].t() + P["qkv.bias"]
+    q, k, v = (t.reshape(T, N, h, d) for t in qkv.split(W, -1))
+    S = s0
+    g = block._decay.double()[None, :, None, None]
+    o = []
+    for t in range(T):
+        link = g * S if reset is None else torch.where((reset[t] != 0)[:, None, None, None], 0.0, g * S)
+        new = link + k[t][..., :, None] * v[t][..., None, :]
+        on = torch.ones(N, dtype=torch.bool, device=x.device) if lengths is None else t < lengths
+        S = torch.where(on[:, None, None, None], new, S)
+        o.append(torch.where(on[:, None, None], (q[t][..., :, None] * S).sum(-2) * d ** -0.5, 0.0).reshape(N, W))
+    m = x + torch.stack(o) @ P["out.weight"].t() + P["out.bias"]
+    p = _norm(m, P["norm2.weight"], P["norm2.bias"], block.eps) @ P["up.weight"].t() + P["up.bias"]
+    u = {"gelu": p * torch.special.ndtr(p), "relu": torch.relu(p), "silu": p * torch.sigmoid(p), "none": p}[block.act]
+    return m + u @ P["down.weight"].t() + P["down.bias"], S
+
+
+def _near(got, want, dtype):
+    want = want.detach()
+    err = (got.double() - want).abs().max()
+    size = want.abs().max() if dtype == "f32" else want.square().mean().sqrt()
+    if dtype == "f32":
+        assert err <= 2e-4 * size
+    else:
+        assert (got.double() - want).square().mean().sqrt() <= 0.08 * size
+
+
+CASES = [(5, 7, 32, 2, 48, "gelu"), (33, 20, 64, 8, 100, "silu"), (16, 40, 128, 8, 256, "relu"), (300, 2, 64, 1, 64, "gelu")]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES)
+def test_forward_and_backward(case, dtype):
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W, h, hidden, act = case
+    block = TimeBlock(W, h, hidden, dtype=dtype, act=act)
+    host = _params(block, T)
+    g = torch.Generator(device="cuda").manual_seed(T + N)
+    x, dy = (torch.randn(T, N, W, generator=g, device="cuda").to(block.dtype) for _ in range(2))
+    s0, dsn = (torch.randn(N, h, W // h, W // h, generator=g, device="cuda") for _ in range(2))
+    reset = (torch.rand(T, N, generator=g, device="cuda") < 0.1).to(torch.uint8)
+    y, sn, dx, ds0 = torch.empty_like(x), torch.empty_like(s0), torch.empty_like(x), torch.empty_like(s0)
+    block.forward(x, y, S0=s0, SN=sn, reset=reset)
+    block.backward(dy, dX=dx, dSN=dsn, dS0=ds0)
+    P = {n: torch.from_numpy(a).cuda().double().requires_grad_() for n, a in host.items()}
+    X, S = x.double().requires_grad_(), s0.double().requires_grad_()
+    want, last = _formula(block, P, X, S, None, reset)
+    ((want * dy.double()).sum() + (last * dsn.double()).sum()).backward()
+    _near(y, want, dtype)
+    _near(sn, last, dtype)
+    _near(dx, X.grad, dtype)
+    _near(ds0, S.grad, dtype)
+    for n in P:
+        _near(torch.from_numpy(block.get_param(n + ".grad")).cuda(), P[n].grad, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_windows_and_snapshots_chain(dtype):
+    """One window of 40, and the same as a window of 33 and seven single snapshots with the states handed on, behind a structure encoder's
+    rows of ragged sequences."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W, h = 40, 30, 64, 4
+    block = TimeBlock(W, h, 96, dtype=dtype)
+    _params(block, 1)
+    x = torch.randn(T, N, W, device="cuda").to(block.dtype)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    sn = torch.zeros(N, h, W // h, W // h, device="cuda")
+    block.forward(x, y, SN=sn)
+    s = torch.zeros_like(sn)
+    block.forward(x[:33], z[:33], S0=s, SN=s, train=False)
+    for t in range(33, T):
+        block.forward(x[t:t + 1], z[t:t + 1], S0=s, SN=s, train=False)
+    _near(z, y.double(), dtype)
+    _near(s, sn.double(), "f32" if dtype == "f32" else dtype)
+    with pytest.raises(RuntimeError, match="train=True"):
+        block.backward(x)
+
+
+def test_behind_a_structure_encoder():
+    """A GCN layer's output goes through the block; rows behind a vertex' last snapshot keep to themselves."""
+    import torch
+    from paper_2309_03523_amd.runner import DeviceWorkload
+    from paper_2309_03523_amd.time_block import TimeBlock
+    from workloads import synth
+    wl = synth.config1(seed=0, random_bias=True)
+    wl.time_kind = "none"
+    wl.params = {k: v for k, v in wl.params.items() if k.startswith("gcn")}
+    wl.H0 = None
+    dw = DeviceWorkload(wl)
+    x = dw.forward()
+    T, N, W = x.shape
+    block = TimeBlock(W, 2, 2 * W)
+    host = _params(block, 2)
+    lengths = torch.randint(0, T + 1, (N,), device="cuda", dtype=torch.int32)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    dy = torch.randn_like(x)
+    for given in (None, lengths):      # the first call leaves its rows in the buffers
+        block.forward(x, y, lengths=given)
+        block.backward(dy, dX=dx)
+    P = {n: torch.from_numpy(a).cuda().double().requires_grad_() for n, a in host.items()}
+    X = x.double().requires_grad_()
+    want, _ = _formula(block, P, X, torch.zeros(N, 2, W // 2, W // 2, dtype=torch.float64, device="cuda"), lengths, None)
+    (want * dy.double()).sum().backward()
+    _near(y, want, "f32")
+    _near(dx, X.grad, "f32")
+    for n in P:
+        _near(torch.from_numpy(block.get_param(n + ".grad")).cuda(), P[n].grad, "f32")
+    dw.layer.destroy()
+
+
+def test_captured_step():
+    """A training step captured after an eager one, replayed with other inputs while another size runs between."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W = 12, 50, 32
+    block = TimeBlock(W, 2, 64, dtype="bf16")
+    _params(block, 3)
+    x, dy = (torch.randn(T, N, W, device="cuda").to(torch.bfloat16) for _ in range(2))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+
+    def step():
+        block.forward(x, y)
+        block.backward(dy, dX=dx)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    small = torch.randn(1, 9, W, device="cuda").to(torch.bfloat16)
+    for _ in range(3):
+        x.mul_(0.8).add_(0.1)
+        step()
+        torch.cuda.synchronize()
+        want = [y.clone(), dx.clone()] + [block.get_param(n + ".grad") for n in block.shapes]
+        block.forward(small, torch.empty_like(small), train=False)
+        y.zero_(), dx.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dx, want[1])
+        for n, a in zip(block.shapes, want[2:]):
+            np.testing.assert_array_equal(block.get_param(n + ".grad"), a)

@@ -139,3 +139,11 @@ def test_decay_attention_refusals(lib):
                dict(dv_=G[1] + 32), dict(gt=3)):
         assert bwd(**kw) == INVALID, kw
         assert "decay attention" in _text(lib)
+
+
+def test_time_block_refusals():
+    from paper_2309_03523_amd.time_block import TimeBlock
+    for kw in (dict(width=30, heads=4), dict(width=36, heads=3), dict(width=272, heads=2), dict(width=32, heads=0), dict(hidden=0), dict(act="tanh"), dict(dtype="f16"),
+               dict(decay=[0.5]), dict(decay=[0.5, 1.5])):
+        with pytest.raises(ValueError):
+            TimeBlock(**{**dict(width=32, heads=2, hidden=64, device="cuda:0"), **kw})
