@@ -18,7 +18,7 @@
 // result is rounded to bf16, three (all 24 bits) where it goes into the fp32 state; fp32 tensors always in three, six part
 // products a product.  The matrix unit cuts its sums off, so the state is carried from one 32 tokens to the next by the vector unit.
 // A zero score or weight times a value that is not finite would be NaN for tokens that do not see that value: 32 tokens with such
-// a value among k, v, their scores or the state go one by one (walk).
+// a value go one by one.
 //
 // Few long sequences are split into segments: a first pass leaves each segment's own state, a scan joins them into the states
 // that enter the segments, a second pass starts from those.  One token (serving a new snapshot) has a kernel of its own that
@@ -97,20 +97,6 @@ template <class T> struct Kind;
 template <> struct Kind<uint16_t> { static constexpr int kIn = 1, kMid = 2; };
 template <> struct Kind<float> { static constexpr int kIn = 3, kMid = 3; };
 
-// Eight numbers of a row as an operand.
-template <class T>
-__device__ __forceinline__ void load8(const T* p, bool in, uint4 (&f)[Kind<T>::kIn]) {
-  if constexpr (sizeof(T) == 2) {
-    f[0] = in ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
-  } else {
-    float x[8] = {};
-    if (in) {
-      Elem<float>::unpack(*reinterpret_cast<const uint4*>(p), x);
-      Elem<float>::unpack(*reinterpret_cast<const uint4*>(p + 4), x + 4);
-    }
-    split::split8(x, f);
-  }
-}
 template <class T> __device__ __forceinline__ float to_float(T x);
 template <> __device__ __forceinline__ float to_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ float to_float<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
@@ -125,240 +111,315 @@ __device__ __forceinline__ uint4 identity(int c, int half, int n) {   // rows 16
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ float power(float g, int64_t n) {   // g^n in double, so that far powers keep their bits
-  return n == 0 ? 1.f : (float)exp2((double)n * log2((double)g));
+__device__ __forceinline__ float power(float g, uint32_t n) {   // g^n by squaring, in double, so that far powers keep their bits
+  double r = 1., x = (double)g;
+  for (; n; n >>= 1) {
+    if (n & 1) r *= x;
+    x *= x;
+  }
+  return (float)r;
 }
 __device__ __forceinline__ void not_finite(float& t, const floatx16& x) {   // t turns NaN if one of them is not finite
 #pragma unroll
   for (int r = 0; r < 16; ++r) t = fmaf(x[r], 0.f, t);
 }
 
+// Raw fragments of a row: 8 numbers from each of a lane's places, as they lie in memory.
+template <class T> struct Raw8 { uint4 w[sizeof(T) == 2 ? 1 : 2]; };
+template <class T>
+__device__ __forceinline__ Raw8<T> fetch8(const T* p, bool in) {
+  Raw8<T> r;
+#pragma unroll
+  for (int k = 0; k < (int)(sizeof(r) / 16); ++k) r.w[k] = in ? reinterpret_cast<const uint4*>(p)[k] : make_uint4(0, 0, 0, 0);
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void operand(const Raw8<T>& r, uint4 (&f)[Kind<T>::kIn]) {
+  if constexpr (sizeof(T) == 2) {
+    f[0] = r.w[0];
+  } else {
+    float x[8];
+    Elem<float>::unpack(r.w[0], x);
+    Elem<float>::unpack(r.w[1], x + 4);
+    split::split8(x, f);
+  }
+}
+template <class T>
+__device__ __forceinline__ void store4(T* to, const float (&x)[4]) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = Elem<float>::pack(x);
+  else *reinterpret_cast<uint2*>(to) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
+}
+template <int N>
+__device__ __forceinline__ void half_parts(const floatx16& x, int k, uint4 (&p)[N]) {   // registers 8 k .. 8 k + 7
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = x[8 * k + e];
+  parts_of(y, p);
+}
+// Registers of the state: rows 32 t + 16 (r / 8) + 8 half + r % 8 of column c.
+__device__ __forceinline__ int state_row(int t, int r) { return 32 * t + 16 * (r >> 3) + (r & 7); }
+
 // KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
+// A wave goes over (unit, 32 tokens) in turn and has the next ones' rows on the way while it works.
 template <class T, int KD, bool OUT>
-__global__ __launch_bounds__(256) void k_decay(DecayArgs a) {
+__global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void k_decay(DecayArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid;
   __shared__ float pw_lds[4][kTok + 4];
   const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
-  float* pw = pw_lds[threadIdx.x >> 6];
-  const uint4 eye[2] = {identity(0, half, tok), identity(1, half, tok)};
-  const uint4 turned[2] = {identity(0, half, swap23(tok)), identity(1, half, swap23(tok))};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float* pw = pw_lds[wave];
   const uint32_t units = (uint32_t)(a.N * a.heads * a.blocks_v * a.segs);
   int last_h = -1;
   float g = 0.f, near[16], fade0 = 0.f, fade1 = 0.f;   // near: g^(i-j) of the lane's scores; fade: g^i, g^(i+1)
 #pragma unroll
   for (int r = 0; r < 16; ++r) near[r] = 0.f;
 
-  for (uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += gridDim.x * 4) {
-    const int b = unit % a.blocks_v;
+  struct Item {
+    uint32_t unit;
+    int b, h, seg;
+    int64_t i, n, p0, p_hi;
+  };
+  auto begin = [&](uint32_t unit) {
+    Item it;
+    it.unit = unit;
+    it.b = unit % a.blocks_v;
     const uint32_t ih = unit / a.blocks_v;
-    const int h = ih % a.heads;
-    const int64_t i = ih / a.heads % (uint32_t)a.N;
-    const int seg = ih / a.heads / (uint32_t)a.N;
-    if (h != last_h) {
-      last_h = h;
-      g = a.decay[h];
-      if (lane <= kTok) pw[lane] = power(g, lane);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    it.h = ih % a.heads;
+    it.i = ih / a.heads % (uint32_t)a.N;
+    it.seg = ih / a.heads / (uint32_t)a.N;
+    it.n = a.T;
+    if (a.lengths) it.n = __builtin_amdgcn_readfirstlane(min((int)min(a.T, (int64_t)INT32_MAX), max(a.lengths[it.i], 0)));
+    it.p0 = it.seg * a.seg_len;
+    it.p_hi = min(it.n, it.p0 + a.seg_len);
+    return it;
+  };
+  auto from = [&](const Rows& x, int width, const Item& it) {    // the item's first row, and from one token's row to the next
+    const int64_t t = a.reversed ? it.n - 1 - it.p0 : it.p0;
+    return static_cast<const T*>(x.p) + t * x.st + it.i * x.sn + (int64_t)it.h * width;
+  };
+  const int64_t way = a.reversed ? -1 : 1;
+  const int64_t offA = way * tok * a.A.st + 8 * half, offB = way * tok * a.B.st + 8 * half, offC = way * tok * a.C.st + 8 * half;
+  Raw8<T> rawA[KC], rawB[KC], rawC[2];
+  bool flag = false;
+  auto fetch = [&](const Item& it) {
+    const bool on = tok < it.p_hi - it.p0;
+    const T* pb = from(a.B, a.dk, it) + offB;
+    const T* pc = from(a.C, a.dv, it) + 32 * it.b + offC;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = 8 * (r >> 2) + 4 * half + (r & 3);
-        near[r] = j <= tok ? pw[max(tok - j, 0)] : 0.f;
-      }
-      fade0 = pw[tok];
-      fade1 = pw[tok + 1];
+    for (int k = 0; k < 2; ++k) rawC[k] = fetch8(pc + 16 * k, on && 32 * it.b + 16 * k + 8 * half < a.dv);
+#pragma unroll
+    for (int k = 0; k < KC; ++k) rawB[k] = fetch8(pb + 16 * k, on && 16 * k + 8 * half < a.dk);
+    if constexpr (OUT) {
+      const T* pa = from(a.A, a.dk, it) + offA;
+#pragma unroll
+      for (int k = 0; k < KC; ++k) rawA[k] = fetch8(pa + 16 * k, on && 16 * k + 8 * half < a.dk);
     }
-    const int64_t n = a.lengths ? min(a.T, (int64_t)max(a.lengths[i], 0)) : a.T;
-    const int64_t p_lo = seg * a.seg_len, p_hi = min(n, p_lo + a.seg_len);
-    const int dv0 = 32 * b;
-    const int64_t state_at = (((int64_t)seg * a.N + i) * a.heads + h) * a.dk * a.dv;
-    const int c = dv0 + tok;      // the lane's column of the state
-    floatx16 S[KT];
-#pragma unroll
-    for (int t = 0; t < KT; ++t) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
-        S[t][r] = a.s_in && row < a.dk && c < a.dv ? a.s_in[state_at + (int64_t)row * a.in_r + (int64_t)c * a.in_c] : 0.f;
-      }
+    flag = false;
+    if (a.reset && on && half == 0) {
+      const int64_t pos = it.p0 + tok;
+      if (!a.reversed) flag = a.reset[pos * a.N + it.i] != 0;
+      else if (pos > 0) flag = a.reset[(it.n - pos) * a.N + it.i] != 0;
     }
-    bool holds = a.s_in != nullptr;       // whether the state may be other than zero
-    bool cut = false;                     // whether a reset was met
-    for (int64_t p0 = p_lo; p0 < p_hi; p0 += kTok) {
-      const int m = (int)min((int64_t)kTok, p_hi - p0);
-      const bool on = tok < m;
-      const bool fresh = a.reversed && p0 == 0;     // the state that comes in is that of the first token, not of one before
-      const int64_t pos = p0 + tok, t_of = a.reversed ? n - 1 - pos : pos;
-      uint32_t resets = 0;
-      if (a.reset) {
-        bool f = false;
-        if (on && half == 0) {
-          if (!a.reversed) f = a.reset[pos * a.N + i] != 0;
-          else if (pos > 0) f = a.reset[(n - pos) * a.N + i] != 0;
-        }
-        resets = (uint32_t)__ballot(f);
-        cut |= resets != 0;
-      }
-      const T* rowA = static_cast<const T*>(a.A.p) + t_of * a.A.st + i * a.A.sn + (int64_t)h * a.dk + 8 * half;
-      const T* rowB = static_cast<const T*>(a.B.p) + t_of * a.B.st + i * a.B.sn + (int64_t)h * a.dk + 8 * half;
-      const T* rowC = static_cast<const T*>(a.C.p) + t_of * a.C.st + i * a.C.sn + (int64_t)h * a.dv + dv0 + 8 * half;
-      const bool step = !OUT || a.s_out || p0 + kTok < p_hi;   // whether the state is wanted after these tokens
+  };
 
-      floatx16 P = {}, inter = {}, Bc[KT], Cc = {};
-#pragma unroll
-      for (int t = 0; t < KT; ++t) Bc[t] = floatx16{};
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (dv0 + 16 * k < a.dv) {
-          uint4 f[IN];
-          load8(rowC + 16 * k, on && dv0 + 16 * k + 8 * half < a.dv, f);
-          mul(Cc, f, {eye[k]});
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        uint4 fa[IN], fb[IN];
-        load8(rowB + 16 * k, on && 16 * k + 8 * half < a.dk, fb);
-        if constexpr (OUT) {
-          load8(rowA + 16 * k, on && 16 * k + 8 * half < a.dk, fa);
-          mul(P, fb, fa);
-          if (holds) {
-            float x[8];
-            uint4 fs[MID];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = S[k / 2][8 * (k & 1) + e];
-            parts_of(x, fs);
-            mul(inter, fs, fa);
-          }
-        }
-        mul(Bc[k / 2], fb, {turned[k & 1]});
-      }
-      float bad = 0.f;
-      not_finite(bad, Cc);
-      if constexpr (OUT) not_finite(bad, P);
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        not_finite(bad, Bc[t]);
-        if (holds) not_finite(bad, S[t]);
-      }
-      if (__builtin_expect(__any(bad != 0.f), 0)) {
-        // one by one: the state for each token, its row's product with it
-        for (int q = 0; q < m; ++q) {
-          const int64_t at = a.reversed ? n - 1 - (p0 + q) : p0 + q;
-          const T* qa = static_cast<const T*>(a.A.p) + at * a.A.st + i * a.A.sn + (int64_t)h * a.dk;
-          const T* qb = static_cast<const T*>(a.B.p) + at * a.B.st + i * a.B.sn + (int64_t)h * a.dk;
-          const float vc = c < a.dv ? to_float((static_cast<const T*>(a.C.p) + at * a.C.st + i * a.C.sn + (int64_t)h * a.dv)[c]) : 0.f;
-          const bool zero = resets >> q & 1;
-          const float keep = fresh && q == 0 ? 1.f : g;
-          float o = 0.f;
-#pragma unroll
-          for (int t = 0; t < KT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
-              if (row < a.dk && c < a.dv) {
-                const float old = zero ? 0.f : holds || q > 0 ? keep * S[t][r] : 0.f;
-                S[t][r] = fmaf(a.beta * to_float(qb[row]), vc, old);
-                if constexpr (OUT) o = fmaf(to_float(qa[row]), S[t][r], o);
-              }
-            }
-          }
-          if constexpr (OUT) {
-            o += __shfl_xor(o, 32);
-            if (half == 0 && c < a.dv)
-              (static_cast<T*>(const_cast<void*>(a.O.p)) + at * a.O.st + i * a.O.sn + (int64_t)h * a.dv)[c] = Elem<T>::one(a.gam * o);
-          }
-        }
-        holds = true;
-        continue;
-      }
-      uint4 fc[2][IN];      // C with its tokens as the contraction
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = Cc[8 * k + e];
-        parts_of(x, fc[k]);
-      }
-      if constexpr (OUT) {
-        const uint32_t before = resets & ((2u << tok) - 1u);       // resets up to the lane's token (2 << 31 is 0: all of them)
-        const int since = before ? 31 - __clz(before) : 0;
-        floatx16 intra = {};
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (16 * k < m) {
-            float x[8];
-            uint4 fp[MID];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int r = 8 * k + e, j = 8 * (r >> 2) + 4 * half + (r & 3);
-              x[e] = j >= since ? P[r] * near[r] : 0.f;
-            }
-            parts_of(x, fp);
-            mul(intra, fc[k], fp);
-          }
-        }
-        const float f = before || !holds ? 0.f : a.gam * (fresh ? fade0 : fade1);
-        T* out = static_cast<T*>(const_cast<void*>(a.O.p)) + t_of * a.O.st + i * a.O.sn + (int64_t)h * a.dv;
-        if (on) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int col = dv0 + 8 * q + 4 * half;
-            if (col < a.dv) {
-              float x[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = fmaf(a.alpha, intra[4 * q + e], f * inter[4 * q + e]);
-              if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(out + col) = Elem<float>::pack(x);
-              else *reinterpret_cast<uint2*>(out + col) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
-            }
-          }
-        }
-      }
-      if (step) {
-        const int last = resets ? 31 - __clz(resets) : 0;
-        const float keep = resets ? 0.f : pw[m - (fresh ? 1 : 0)];
-        float w[16];
+  const uint32_t first = blockIdx.x * 4 + wave, stride = gridDim.x * 4;
+  if (first >= units) return;
+  Item it = begin(first);
+  fetch(it);
+  floatx16 S[KT];
+  bool holds = false, cut = false, fresh_unit = true;    // holds: the state may be other than zero; cut: a reset was met
+  while (true) {
+    const int dv0 = 32 * it.b, c = dv0 + tok;            // c: the lane's column of the state
+    const int64_t state_at = (((int64_t)it.seg * a.N + it.i) * a.heads + it.h) * a.dk * a.dv;
+    if (fresh_unit) {
+      if (it.h != last_h) {
+        last_h = it.h;
+        g = a.decay[it.h];
+        if (lane <= kTok) pw[lane] = power(g, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int j = 8 * (r >> 2) + 4 * half + (r & 3);
-          w[r] = j < m && j >= last ? a.beta * pw[max(m - 1 - j, 0)] : 0.f;
+          near[r] = j <= tok ? pw[max(tok - j, 0)] : 0.f;
         }
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          floatx16 U = {};
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (16 * k < m) {
-              float x[8];
-              uint4 fb[3];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = Bc[t][8 * k + e] * w[8 * k + e];
-              parts_of(x, fb);
-              mul(U, fb, fc[k]);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) S[t][r] = holds ? fmaf(keep, S[t][r], U[r]) : U[r];
-        }
-        holds = true;
+        fade0 = pw[tok];
+        fade1 = pw[tok + 1];
       }
-    }
-    if (a.s_out) {
-      float f = 1.f;
-      if (a.out_link && n > 0) f = a.reset && a.reset[i] ? 0.f : g;
+      const float* in = a.s_in + state_at + 8 * half * a.in_r + c * a.in_c;
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = 32 * t + swap23(8 * (r >> 2) + 4 * half + (r & 3));
-          if (row < a.dk && c < a.dv)
-            a.s_out[state_at + (int64_t)row * a.out_r + (int64_t)c * a.out_c] = f == 0.f && g != 0.f ? 0.f : f * S[t][r];
-        }
+        for (int r = 0; r < 16; ++r)
+          S[t][r] = a.s_in && state_row(t, r) + 8 * half < a.dk && c < a.dv ? in[state_row(t, r) * a.in_r] : 0.f;
+      }
+      holds = a.s_in != nullptr;
+      cut = false;
+    }
+    const int64_t p0 = it.p0, n = it.n;
+    const int m = (int)min((int64_t)kTok, it.p_hi - p0);      // may be none
+    const bool on = tok < m;
+    const bool fresh = a.reversed && p0 == 0;     // the state that comes in is that of the first token, not of one before
+    const bool unit_ends = p0 + kTok >= it.p_hi;
+    const bool step = !OUT || a.s_out || !unit_ends;          // whether the state is wanted after these tokens
+    uint32_t resets = 0;
+    if (a.reset) {
+      resets = (uint32_t)__ballot(flag);
+      cut |= resets != 0;
+    }
+    floatx16 P = {}, inter = {}, Bc[KT], Cc = {};
+#pragma unroll
+    for (int t = 0; t < KT; ++t) Bc[t] = floatx16{};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (dv0 + 16 * k < a.dv) {
+        uint4 f[IN];
+        operand(rawC[k], f);
+        mul(Cc, f, {identity(k, half, tok)});
       }
     }
-    if (!OUT && a.factor && b == 0 && lane == 0) {
-      const int64_t len = max(p_hi - p_lo, (int64_t)0);
-      a.factor[((int64_t)seg * a.N + i) * a.heads + h] = cut ? -1.f : power(g, len - (a.reversed && seg == 0 && len > 0 ? 1 : 0));
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      uint4 fb[IN];
+      operand(rawB[k], fb);
+      if constexpr (OUT) {
+        uint4 fa[IN];
+        operand(rawA[k], fa);
+        mul(P, fb, fa);
+        if (holds) {
+          uint4 fs[MID];
+          half_parts(S[k / 2], k & 1, fs);
+          mul(inter, fs, fa);
+        }
+      }
+      if (step) mul(Bc[k / 2], fb, {identity(k & 1, half, swap23(tok))});
     }
+    // the next rows, on their way from here on
+    Item next = it;
+    next.p0 += kTok;
+    if (unit_ends && it.unit + stride < units) next = begin(it.unit + stride);
+    const bool more = !unit_ends || it.unit + stride < units;
+    if (more) fetch(next);
+
+    uint4 fc[2][IN];      // C with its tokens as the contraction
+#pragma unroll
+    for (int k = 0; k < 2; ++k) half_parts(Cc, k, fc[k]);
+    float bad = 0.f;
+    if constexpr (OUT) {
+      const uint32_t before = resets & ((2u << tok) - 1u);       // resets up to the lane's token (2 << 31 is 0: all of them)
+      floatx16 intra = {};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) P[r] = near[r] != 0.f ? P[r] * near[r] : 0.f;
+      if (resets) {
+        const int since = before ? 31 - __clz(before) : 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) P[r] = 8 * (r >> 2) + 4 * half + (r & 3) >= since ? P[r] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (16 * k < m) {
+          uint4 fp[MID];
+          half_parts(P, k, fp);
+          mul(intra, fc[k], fp);
+        }
+      }
+      const float f = a.gam * (fresh ? fade0 : fade1);
+      const bool sees = holds && !before;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        P[r] = fmaf(a.alpha, intra[r], sees ? f * inter[r] : 0.f);
+        bad = fmaf(P[r], 0.f, bad);
+      }
+      if (on) {
+        T* out = static_cast<T*>(const_cast<void*>(a.O.p)) + (from(a.O, a.dv, it) - static_cast<const T*>(a.O.p)) + way * tok * a.O.st + dv0 + 4 * half;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float x[4] = {P[4 * q], P[4 * q + 1], P[4 * q + 2], P[4 * q + 3]};
+          if (dv0 + 8 * q + 4 * half < a.dv) store4(out + 8 * q, x);
+        }
+      }
+    } else {
+      not_finite(bad, Cc);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) { not_finite(bad, Bc[t]); not_finite(bad, S[t]); }
+    }
+    if (__builtin_expect(__any(bad != 0.f), 0)) {
+      // One by one, over what was stored: the state for each token, its row's product with it.  (An output is not finite
+      // wherever a value among the tokens or in the state is not.)
+      for (int q = 0; q < m; ++q) {
+        const int64_t at = a.reversed ? n - 1 - (p0 + q) : p0 + q;
+        const T* qa = static_cast<const T*>(a.A.p) + at * a.A.st + it.i * a.A.sn + (int64_t)it.h * a.dk + 8 * half;
+        const T* qb = static_cast<const T*>(a.B.p) + at * a.B.st + it.i * a.B.sn + (int64_t)it.h * a.dk + 8 * half;
+        const float vc = c < a.dv ? to_float((static_cast<const T*>(a.C.p) + at * a.C.st + it.i * a.C.sn + (int64_t)it.h * a.dv)[c]) : 0.f;
+        const bool zero = resets >> q & 1;
+        const float keep = fresh && q == 0 ? 1.f : g;
+        float o = 0.f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (state_row(t, r) + 8 * half < a.dk && c < a.dv) {
+              const float old = zero ? 0.f : holds || q > 0 ? keep * S[t][r] : 0.f;
+              S[t][r] = fmaf(a.beta * to_float(qb[state_row(t, r)]), vc, old);
+              if constexpr (OUT) o = fmaf(to_float(qa[state_row(t, r)]), S[t][r], o);
+            }
+          }
+        }
+        if constexpr (OUT) {
+          o += __shfl_xor(o, 32);
+          if (half == 0 && c < a.dv)
+            (static_cast<T*>(const_cast<void*>(a.O.p)) + at * a.O.st + it.i * a.O.sn + (int64_t)it.h * a.dv)[c] = Elem<T>::one(a.gam * o);
+        }
+      }
+      holds |= m > 0;
+    } else if (step && m > 0) {
+      const int last = resets ? 31 - __clz(resets) : 0;
+      const float keep = resets ? 0.f : pw[m - (fresh ? 1 : 0)];
+      float w[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = 8 * (r >> 2) + 4 * half + (r & 3);
+        w[r] = j < m && j >= last ? a.beta * pw[max(m - 1 - j, 0)] : 0.f;
+      }
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        floatx16 U = {};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) Bc[t][r] *= w[r];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (16 * k < m) {
+            uint4 fb[3];
+            half_parts(Bc[t], k, fb);
+            mul(U, fb, fc[k]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[t][r] = holds && !resets ? fmaf(keep, S[t][r], U[r]) : U[r];
+      }
+      holds = true;
+    }
+    if (unit_ends) {
+      if (a.s_out) {
+        float f = 1.f;
+        const bool drop = a.out_link && n > 0 && a.reset && a.reset[it.i];
+        if (a.out_link && n > 0) f = g;
+        float* out = a.s_out + state_at + 8 * half * a.out_r + c * a.out_c;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (state_row(t, r) + 8 * half < a.dk && c < a.dv) out[state_row(t, r) * a.out_r] = drop ? 0.f : f * S[t][r];
+          }
+        }
+      }
+      if (!OUT && a.factor && it.b == 0 && lane == 0) {
+        const int64_t len = max(it.p_hi - it.seg * a.seg_len, (int64_t)0);
+        a.factor[((int64_t)it.seg * a.N + it.i) * a.heads + it.h] = cut ? -1.f : power(g, (uint32_t)(len - (a.reversed && it.seg == 0 && len > 0 ? 1 : 0)));
+      }
+    }
+    if (!more) return;
+    fresh_unit = unit_ends;
+    it = next;
   }
 }
 
