@@ -39,6 +39,7 @@ constexpr int kMaxHeads = 1024, kMaxDim = 128;
 constexpr int kTok = 32;               // tokens at a time
 constexpr int64_t kFillWaves = 2048;   // two a SIMD
 constexpr int64_t kSegTokens = 128;    // tokens of a segment at least
+constexpr int64_t kRun = 8;            // rows that a wave takes in turn
 
 struct Rows {          // row (t, i) at p + t st + i sn, in elements
   const void* p;
@@ -63,6 +64,7 @@ struct DecayArgs {
   float* factor;                // first pass: what a segment keeps of the state entering it, [seg][N][heads]; -1: cut off by a reset
   int32_t segs;
   int64_t seg_len;
+  uint32_t run;                 // sequences (or pairs, or segments) that a wave takes one after the other
 };
 
 // The product of operands in parts, those below 2^-24 left out, the smallest first.
@@ -159,6 +161,21 @@ __device__ __forceinline__ void half_parts(const floatx16& x, int k, uint4 (&p)[
 // Registers of the state: rows 32 t + 16 (r / 8) + 8 half + r % 8 of column c.
 __device__ __forceinline__ int state_row(int t, int r) { return 32 * t + 16 * (r >> 3) + (r & 7); }
 
+// The decays between a lane's token and the others of its window: g^|x - tok| for the 16 others x = 8 (r / 4) + 4 half + r % 4, of those up
+// to it (ahead = false) or from it on; of its own half of the 32 only where two sequences share them.
+template <bool PAIR>
+__device__ __forceinline__ void decays(const float* pw, int tok, int half, bool ahead, float (&out)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int x = 8 * (r >> 2) + 4 * half + (r & 3), d = ahead ? x - tok : tok - x;
+    out[r] = d >= 0 && !(PAIR && (x ^ tok) & 16) ? pw[max(d, 0)] : 0.f;
+  }
+}
+__device__ __forceinline__ void powers_of(float g, float* pw, int lane) {
+  if (lane <= kTok) pw[lane] = power(g, lane);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
 // A wave goes over (unit, 32 tokens) in turn and has the next ones' rows on the way while it works.
 template <class T, int KD, bool OUT>
@@ -168,25 +185,26 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
   const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float* pw = pw_lds[wave];
-  const uint32_t units = (uint32_t)(a.N * a.heads * a.blocks_v * a.segs);
-  int last_h = -1;
-  float g = 0.f, near[16], fade0 = 0.f, fade1 = 0.f;   // near: g^(i-j) of the lane's scores; fade: g^i, g^(i+1)
-#pragma unroll
-  for (int r = 0; r < 16; ++r) near[r] = 0.f;
+  // a wave keeps to one head and block of columns and takes sequences (of a segment) that lie side by side
+  const uint32_t line = blockIdx.x * 4 + wave, across = (uint32_t)(a.heads * a.blocks_v), rows = (uint32_t)(a.N * a.segs);
+  const int h = line % across / a.blocks_v, b = line % a.blocks_v;
+  uint32_t row = line / across * a.run;
+  const uint32_t row_end = min(rows, row + a.run);
+  if (row >= rows) return;
+  const float g = a.decay[h];
+  powers_of(g, pw, lane);
+  float near[16];                                                // g^(i-j) of the lane's scores
+  decays<false>(pw, tok, half, false, near);
+  const float fade0 = pw[tok], fade1 = pw[tok + 1];              // g^i, g^(i+1)
 
   struct Item {
-    uint32_t unit;
-    int b, h, seg;
+    int seg;
     int64_t i, n, p0, p_hi;
   };
-  auto begin = [&](uint32_t unit) {
+  auto begin = [&](uint32_t row) {
     Item it;
-    it.unit = unit;
-    it.b = unit % a.blocks_v;
-    const uint32_t ih = unit / a.blocks_v;
-    it.h = ih % a.heads;
-    it.i = ih / a.heads % (uint32_t)a.N;
-    it.seg = ih / a.heads / (uint32_t)a.N;
+    it.i = row % (uint32_t)a.N;
+    it.seg = row / (uint32_t)a.N;
     it.n = a.T;
     if (a.lengths) it.n = __builtin_amdgcn_readfirstlane(min((int)min(a.T, (int64_t)INT32_MAX), max(a.lengths[it.i], 0)));
     it.p0 = it.seg * a.seg_len;
@@ -195,7 +213,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
   };
   auto from = [&](const Rows& x, int width, const Item& it) {    // the item's first row, and from one token's row to the next
     const int64_t t = a.reversed ? it.n - 1 - it.p0 : it.p0;
-    return static_cast<const T*>(x.p) + t * x.st + it.i * x.sn + (int64_t)it.h * width;
+    return static_cast<const T*>(x.p) + t * x.st + it.i * x.sn + (int64_t)h * width;
   };
   const int64_t way = a.reversed ? -1 : 1;
   const int64_t offA = way * tok * a.A.st + 8 * half, offB = way * tok * a.B.st + 8 * half, offC = way * tok * a.C.st + 8 * half;
@@ -204,9 +222,9 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
   auto fetch = [&](const Item& it) {
     const bool on = tok < it.p_hi - it.p0;
     const T* pb = from(a.B, a.dk, it) + offB;
-    const T* pc = from(a.C, a.dv, it) + 32 * it.b + offC;
+    const T* pc = from(a.C, a.dv, it) + 32 * b + offC;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) rawC[k] = fetch8(pc + 16 * k, on && 32 * it.b + 16 * k + 8 * half < a.dv);
+    for (int k = 0; k < 2; ++k) rawC[k] = fetch8(pc + 16 * k, on && 32 * b + 16 * k + 8 * half < a.dv);
 #pragma unroll
     for (int k = 0; k < KC; ++k) rawB[k] = fetch8(pb + 16 * k, on && 16 * k + 8 * half < a.dk);
     if constexpr (OUT) {
@@ -222,29 +240,14 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
     }
   };
 
-  const uint32_t first = blockIdx.x * 4 + wave, stride = gridDim.x * 4;
-  if (first >= units) return;
-  Item it = begin(first);
+  Item it = begin(row);
   fetch(it);
   floatx16 S[KT];
   bool holds = false, cut = false, fresh_unit = true;    // holds: the state may be other than zero; cut: a reset was met
   while (true) {
-    const int dv0 = 32 * it.b, c = dv0 + tok;            // c: the lane's column of the state
-    const int64_t state_at = (((int64_t)it.seg * a.N + it.i) * a.heads + it.h) * a.dk * a.dv;
+    const int dv0 = 32 * b, c = dv0 + tok;            // c: the lane's column of the state
+    const int64_t state_at = (((int64_t)it.seg * a.N + it.i) * a.heads + h) * a.dk * a.dv;
     if (fresh_unit) {
-      if (it.h != last_h) {
-        last_h = it.h;
-        g = a.decay[it.h];
-        if (lane <= kTok) pw[lane] = power(g, lane);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = 8 * (r >> 2) + 4 * half + (r & 3);
-          near[r] = j <= tok ? pw[max(tok - j, 0)] : 0.f;
-        }
-        fade0 = pw[tok];
-        fade1 = pw[tok + 1];
-      }
       const float* in = a.s_in + state_at + 8 * half * a.in_r + c * a.in_c;
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
@@ -296,8 +299,9 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
     // the next rows, on their way from here on
     Item next = it;
     next.p0 += kTok;
-    if (unit_ends && it.unit + stride < units) next = begin(it.unit + stride);
-    const bool more = !unit_ends || it.unit + stride < units;
+    if (unit_ends) ++row;
+    const bool more = !unit_ends || row < row_end;
+    if (unit_ends && more) next = begin(row);
     if (more) fetch(next);
 
     uint4 fc[2][IN];      // C with its tokens as the contraction
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
       const uint32_t before = resets & ((2u << tok) - 1u);       // resets up to the lane's token (2 << 31 is 0: all of them)
       floatx16 intra = {};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) P[r] = near[r] != 0.f ? P[r] * near[r] : 0.f;
+      for (int r = 0; r < 16; ++r) P[r] *= near[r];    // a score that is not finite leaves an output that is not
       if (resets) {
         const int since = before ? 31 - __clz(before) : 0;
 #pragma unroll
@@ -347,9 +351,9 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
       // wherever a value among the tokens or in the state is not.)
       for (int q = 0; q < m; ++q) {
         const int64_t at = a.reversed ? n - 1 - (p0 + q) : p0 + q;
-        const T* qa = static_cast<const T*>(a.A.p) + at * a.A.st + it.i * a.A.sn + (int64_t)it.h * a.dk + 8 * half;
-        const T* qb = static_cast<const T*>(a.B.p) + at * a.B.st + it.i * a.B.sn + (int64_t)it.h * a.dk + 8 * half;
-        const float vc = c < a.dv ? to_float((static_cast<const T*>(a.C.p) + at * a.C.st + it.i * a.C.sn + (int64_t)it.h * a.dv)[c]) : 0.f;
+        const T* qa = static_cast<const T*>(a.A.p) + at * a.A.st + it.i * a.A.sn + (int64_t)h * a.dk + 8 * half;
+        const T* qb = static_cast<const T*>(a.B.p) + at * a.B.st + it.i * a.B.sn + (int64_t)h * a.dk + 8 * half;
+        const float vc = c < a.dv ? to_float((static_cast<const T*>(a.C.p) + at * a.C.st + it.i * a.C.sn + (int64_t)h * a.dv)[c]) : 0.f;
         const bool zero = resets >> q & 1;
         const float keep = fresh && q == 0 ? 1.f : g;
         float o = 0.f;
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
         if constexpr (OUT) {
           o += __shfl_xor(o, 32);
           if (half == 0 && c < a.dv)
-            (static_cast<T*>(const_cast<void*>(a.O.p)) + at * a.O.st + it.i * a.O.sn + (int64_t)it.h * a.dv)[c] = Elem<T>::one(a.gam * o);
+            (static_cast<T*>(const_cast<void*>(a.O.p)) + at * a.O.st + it.i * a.O.sn + (int64_t)h * a.dv)[c] = Elem<T>::one(a.gam * o);
         }
       }
       holds |= m > 0;
@@ -412,14 +416,482 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
           }
         }
       }
-      if (!OUT && a.factor && it.b == 0 && lane == 0) {
+      if (!OUT && a.factor && b == 0 && lane == 0) {
         const int64_t len = max(it.p_hi - it.seg * a.seg_len, (int64_t)0);
-        a.factor[((int64_t)it.seg * a.N + it.i) * a.heads + it.h] = cut ? -1.f : power(g, (uint32_t)(len - (a.reversed && it.seg == 0 && len > 0 ? 1 : 0)));
+        a.factor[((int64_t)it.seg * a.N + it.i) * a.heads + h] = cut ? -1.f : power(g, (uint32_t)(len - (a.reversed && it.seg == 0 && len > 0 ? 1 : 0)));
       }
     }
     if (!more) return;
     fresh_unit = unit_ends;
     it = next;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- windows of up to 32 tokens
+
+// A window's outputs one row of the state after the other: what is done where a value is not finite.  acc: [32][64] floats of the wave.
+template <class T>
+struct Walk {
+  const T* A; const T* B; const T* C; T* O;     // the sequence's and head's first rows
+  int64_t sa, sb, sc, so;                       // from token to token
+  int n, da, dc;
+  bool reversed;
+  float g, beta, gam;
+  const uint8_t* reset; int64_t reset_st;       // the sequence's first flag
+  const float* in; int in_r, in_c;
+  float* out;                                   // [da][dc]: the last state times l_0 g
+};
+template <class T>
+__device__ void walk_window(const Walk<T>& w, float* acc) {
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  for (int b = 0; b < w.dc; b += 32) {
+    const int c = b + (lane & 31);
+    const bool have = c < w.dc;
+    for (int p = 0; p < w.n; ++p) acc[p * 64 + lane] = 0.f;
+    for (int r = half; r < w.da; r += 2) {
+      float s = w.in && have ? w.in[r * w.in_r + c * w.in_c] : 0.f;
+      for (int p = 0; p < w.n; ++p) {
+        const int64_t t = w.reversed ? w.n - 1 - p : p;
+        if (p > 0 || !w.reversed) {
+          const bool cut = w.reset && w.reset[(w.reversed ? t + 1 : t) * w.reset_st];
+          s = cut || (p == 0 && !w.in) ? 0.f : w.g * s;
+        }
+        if (have) {
+          s = fmaf(w.beta * to_float(w.B[t * w.sb + r]), to_float(w.C[t * w.sc + c]), s);
+          acc[p * 64 + lane] = fmaf(to_float(w.A[t * w.sa + r]), s, acc[p * 64 + lane]);
+        }
+      }
+      if (w.out && have) w.out[r * w.dc + c] = w.n == 0 ? s : w.reset && w.reset[0] ? 0.f : w.g * s;
+    }
+    if (!w.O) continue;
+    for (int p = 0; p < w.n; ++p) {
+      const float o = acc[p * 64 + lane] + __shfl_xor(acc[p * 64 + lane], 32);
+      const int64_t t = w.reversed ? w.n - 1 - p : p;
+      if (have && half == 0) w.O[t * w.so + c] = Elem<T>::one(w.gam * o);
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ bool store_rows(T* out, const floatx16& x, int width, int half, bool on) {   // whether all were finite
+  float bad = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) bad = fmaf(x[r], 0.f, bad);
+  if (on) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float y[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+      if (8 * q + 4 * half < width) store4(out + 8 * q + 4 * half, y);
+    }
+  }
+  return !__any(bad != 0.f);
+}
+
+// The forward pass of windows of up to 32 tokens from zero states, the states not wanted: nothing is carried.  Two sequences
+// of up to 16 tokens share the 32 of a wave (PAIR).
+template <class T, int KD, bool PAIR>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 64 ? 2 : 1)) void k_decay_window(DecayArgs a) {
+  constexpr int KC = KD / 16, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
+  __shared__ float pw_lds[4][kTok + 4];
+  __shared__ float walk_lds[4][32 * 64];
+  const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slot = PAIR ? tok >> 4 : 0, pos = PAIR ? tok & 15 : tok;
+  float* pw = pw_lds[wave];
+  const uint32_t line = blockIdx.x * 4 + wave, across = (uint32_t)(a.heads * a.blocks_v), rows = (uint32_t)((a.N + PER - 1) / PER);
+  const int h = line % across / a.blocks_v, dv0 = 32 * (line % a.blocks_v);
+  uint32_t row = line / across * a.run;
+  const uint32_t row_end = min(rows, row + a.run);
+  if (row >= rows) return;
+  // Narrow heads share cache lines with their neighbours, which the workgroup's other waves read: where all four take the same rows
+  // they fetch in step, and each line comes into the L1 cache once (100 000 windows of 16, 8 heads of 16: 451 us apart, 410 in step).
+  const bool together = (across & 3) == 0;
+  const int64_t offA = slot * a.A.sn + pos * a.A.st + 8 * half, offB = slot * a.B.sn + pos * a.B.st + 8 * half;
+  const int64_t offC = slot * a.C.sn + pos * a.C.st + 8 * half, offO = slot * a.O.sn + pos * a.O.st;
+  const float g = a.decay[h];
+  powers_of(g, pw, lane);
+  float near[16];
+  decays<PAIR>(pw, tok, half, false, near);
+  auto tokens = [&](uint32_t row) {      // of the lane's sequence
+    const int64_t i = (int64_t)row * PER + slot;
+    if (i >= a.N) return 0;
+    return a.lengths ? min((int)a.T, max(a.lengths[i], 0)) : (int)a.T;
+  };
+  Raw8<T> rawA[KC], rawB[KC], rawC[2];
+  bool flag = false;
+  auto fetch = [&](uint32_t row, int n) {
+    const bool on = pos < n;
+    const int64_t i = (int64_t)row * PER;
+    const T* pa = static_cast<const T*>(a.A.p) + i * a.A.sn + (int64_t)h * a.dk + offA;
+    const T* pb = static_cast<const T*>(a.B.p) + i * a.B.sn + (int64_t)h * a.dk + offB;
+    const T* pc = static_cast<const T*>(a.C.p) + i * a.C.sn + (int64_t)h * a.dv + dv0 + offC;
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      rawB[k] = fetch8(pb + 16 * k, on && 16 * k + 8 * half < a.dk);
+      rawA[k] = fetch8(pa + 16 * k, on && 16 * k + 8 * half < a.dk);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) rawC[k] = fetch8(pc + 16 * k, on && dv0 + 16 * k + 8 * half < a.dv);
+    flag = a.reset && on && half == 0 && a.reset[pos * a.N + i + slot] != 0;
+  };
+
+  int n_next = tokens(row);
+  int n = n_next;
+  fetch(row, n);
+  n_next = row + 1 < row_end ? tokens(row + 1) : 0;
+  while (true) {
+    const int64_t i0 = (int64_t)row * PER;
+    const bool on = pos < n;
+    const uint32_t resets = a.reset ? (uint32_t)__ballot(flag) : 0;
+    floatx16 P = {}, Cc = {}, out = {};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (dv0 + 16 * k < a.dv) {
+        uint4 f[IN];
+        operand(rawC[k], f);
+        mul(Cc, f, {identity(k, half, tok)});
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      uint4 fa[IN], fb[IN];
+      operand(rawA[k], fa);
+      operand(rawB[k], fb);
+      mul(P, fb, fa);
+    }
+    const int n_this = n;
+    if (together) __builtin_amdgcn_s_barrier();
+    if (++row < row_end) {
+      fetch(row, n_next);
+      n = n_next;
+      n_next = row + 1 < row_end ? tokens(row + 1) : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) P[r] *= near[r];    // a score that is not finite leaves an output that is not
+    if (resets) {
+      const uint32_t before = resets & ((2u << tok) - 1u) & (PAIR ? 0xffffu << (16 * slot) : ~0u);
+      const int since = before ? 31 - __clz(before) : 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) P[r] = 8 * (r >> 2) + 4 * half + (r & 3) >= since ? P[r] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint4 fc[IN], fp[MID];
+      half_parts(Cc, k, fc);
+      half_parts(P, k, fp);
+      mul(out, fc, fp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[r] *= a.alpha;
+    T* O = static_cast<T*>(const_cast<void*>(a.O.p));
+    const int64_t at = i0 * a.O.sn + (int64_t)h * a.dv;
+    if (__builtin_expect(!store_rows(O + at + offO + dv0, out, a.dv - dv0, half, on), 0)) {
+      for (int q = 0; q < PER; ++q) {
+        const int64_t i = i0 + q;
+        const int live = __builtin_amdgcn_readlane(n_this, 16 * q);
+        const T *A = static_cast<const T*>(a.A.p), *B = static_cast<const T*>(a.B.p), *C = static_cast<const T*>(a.C.p);
+        const Walk<T> w{A + i * a.A.sn + h * a.dk, B + i * a.B.sn + h * a.dk, C + i * a.C.sn + h * a.dv + dv0, O + i * a.O.sn + h * a.dv + dv0,
+                        a.A.st, a.B.st, a.C.st, a.O.st, live, a.dk, min(32, a.dv - dv0), false, g, a.beta, a.gam,
+                        a.reset ? a.reset + i : nullptr, a.N, nullptr, 0, 0, nullptr};
+        if (live > 0) walk_window(w, walk_lds[wave]);
+      }
+    }
+    if (row >= row_end) return;
+  }
+}
+
+struct BackArgs {
+  Rows q, k, v, go, dq, dkey, dval;
+  int64_t T, N;
+  int32_t heads, dk, dv;
+  const float* decay;
+  float scale;
+  const float* s0;
+  const float* dsn;
+  float* ds0;
+  const int32_t* lengths;
+  const uint8_t* reset;
+  uint32_t run;
+};
+
+// All gradients of windows of up to 32 tokens, every tensor read once: dk, dv up to KD.  States (not with PAIR) are read and written as
+// they are needed: nothing is carried.
+template <class T, int KD, bool PAIR>
+__global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void k_decay_window_back(BackArgs a) {
+  constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
+  __shared__ float pw_lds[4][kTok + 4];
+  __shared__ float walk_lds[4][32 * 64];
+  const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slot = PAIR ? tok >> 4 : 0, pos = PAIR ? tok & 15 : tok;
+  float* pw = pw_lds[wave];
+  const uint32_t line = blockIdx.x * 4 + wave, rows = (uint32_t)((a.N + PER - 1) / PER);
+  const int h = line % a.heads;
+  uint32_t row = line / a.heads * a.run;
+  const uint32_t row_end = min(rows, row + a.run);
+  if (row >= rows) return;
+  const float g = a.decay[h];
+  powers_of(g, pw, lane);
+  const bool together = (a.heads & 3) == 0;      // as above
+  auto tokens = [&](uint32_t row) {
+    const int64_t i = (int64_t)row * PER + slot;
+    if (i >= a.N) return 0;
+    return a.lengths ? min((int)a.T, max(a.lengths[i], 0)) : (int)a.T;
+  };
+  auto place = [&](const Rows& x, int width, uint32_t row) {   // the lane's row
+    return static_cast<const T*>(x.p) + ((int64_t)row * PER + slot) * x.sn + pos * x.st + (int64_t)h * width;
+  };
+  Raw8<T> rawq[KC], rawk[KC], rawv[KC], rawd[KC];
+  bool flag = false;
+  auto fetch = [&](uint32_t row, int n) {
+    const bool on = pos < n;
+    const T *pq = place(a.q, a.dk, row) + 8 * half, *pk = place(a.k, a.dk, row) + 8 * half;
+    const T *pv = place(a.v, a.dv, row) + 8 * half, *pd = place(a.go, a.dv, row) + 8 * half;
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      const bool ink = on && 16 * k + 8 * half < a.dk, inv = on && 16 * k + 8 * half < a.dv;
+      rawq[k] = fetch8(pq + 16 * k, ink);
+      rawk[k] = fetch8(pk + 16 * k, ink);
+      rawv[k] = fetch8(pv + 16 * k, inv);
+      rawd[k] = fetch8(pd + 16 * k, inv);
+    }
+    flag = a.reset && on && half == 0 && a.reset[pos * a.N + (int64_t)row * PER + slot] != 0;
+  };
+
+  int n = tokens(row), n_next = row + 1 < row_end ? tokens(row + 1) : 0;
+  fetch(row, n);
+  while (true) {
+    const uint32_t this_row = row;
+    const int64_t i0 = (int64_t)row * PER, state = (i0 * a.heads + h) * a.dk * a.dv;
+    const bool on = pos < n;
+    const uint32_t resets = a.reset ? (uint32_t)__ballot(flag) : 0;
+    const uint32_t own = PAIR ? 0xffffu << (16 * slot) : ~0u;
+    const uint32_t before = resets & ((2u << tok) - 1u) & own, after = resets & ~((2u << tok) - 1u) & own;
+    const float *s0 = a.s0 + state, *dsn = a.dsn + state;
+    // eight numbers of a state for the lane's output column: along row r of it, or down column c
+    auto along = [&](const float* s, int r, int c, float (&x)[8]) {
+      const bool in = s && r < a.dk && c < a.dv;
+      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f), *at = reinterpret_cast<const float4*>(s + r * a.dv + c);
+      const float4 lo = in ? at[0] : none, hi = in ? at[1] : none;
+      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+    };
+    auto down = [&](const float* s, int r, int c, float (&x)[8]) {
+      const bool in = s && r < a.dk && c < a.dv;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = in ? s[(r + e) * a.dv + c] : 0.f;
+    };
+    // states that fit the registers come while the scores are worked out: one wait instead of four
+    constexpr bool EARLY = !PAIR && KT == 1;
+    float s0_row[EARLY ? KC : 1][8], dsn_row[EARLY ? KC : 1][8], dsn_col[EARLY ? KC : 1][8];
+    if constexpr (EARLY) {
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        along(a.s0 ? s0 : nullptr, tok, 16 * k + 8 * half, s0_row[k]);
+        along(a.dsn ? dsn : nullptr, tok, 16 * k + 8 * half, dsn_row[k]);
+        down(a.dsn ? dsn : nullptr, 16 * k + 8 * half, tok, dsn_col[k]);
+      }
+    }
+    uint4 fq[KC][IN], fk[KC][IN], fv[KC][IN], fd[KC][IN];
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+      operand(rawq[k], fq[k]);
+      operand(rawk[k], fk[k]);
+      operand(rawv[k], fv[k]);
+      operand(rawd[k], fd[k]);
+    }
+    const int n_this = n;
+    if (together) __builtin_amdgcn_s_barrier();
+    if (++row < row_end) {
+      fetch(row, n_next);
+      n = n_next;
+      n_next = row + 1 < row_end ? tokens(row + 1) : 0;
+    }
+    // scores: do . v of the lane's token as the one that reads (dq) and as the one that is read (dk), q . k as the latter (dv)
+    uint4 sdq[2][MID], sdk[2][MID], sdv[2][MID];
+    {
+      floatx16 x = {}, y = {}, z = {};
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        mul(x, fv[k], fd[k]);
+        mul(y, fd[k], fv[k]);
+        mul(z, fq[k], fk[k]);
+      }
+      float w[16];
+      decays<PAIR>(pw, tok, half, false, w);
+      const int since = before ? 31 - __clz(before) : 0, until = after ? __ffs(after) - 1 : 32;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= w[r];
+      decays<PAIR>(pw, tok, half, true, w);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { y[r] *= w[r]; z[r] *= w[r]; }
+      if (resets) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int o = 8 * (r >> 2) + 4 * half + (r & 3);
+          x[r] = o >= since ? x[r] : 0.f;
+          y[r] = o < until ? y[r] : 0.f;
+          z[r] = o < until ? z[r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        half_parts(x, k, sdq[k]);
+        half_parts(y, k, sdk[k]);
+        half_parts(z, k, sdv[k]);
+      }
+    }
+    // a tensor's 32 columns with its tokens as the contraction
+    auto columns = [&](const uint4 (&f)[KC][IN], int t, floatx16& x, int order) {
+      x = floatx16{};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (2 * t + k < KC) mul(x, f[2 * t + k < KC ? 2 * t + k : 0], {identity(k, half, order)});
+      }
+    };
+    auto sums = [&](const floatx16& x, const uint4 (&score)[2][MID], floatx16& out) {
+      out = floatx16{};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint4 f[IN];
+        half_parts(x, k, f);
+        mul(out, f, score[k]);
+      }
+    };
+    const int n0 = PAIR ? 0 : __builtin_amdgcn_readfirstlane(n_this);
+    const int last = resets ? 31 - __clz(resets) : 0;
+    const float fade = before ? 0.f : a.scale * pw[tok + 1];                                        // of S0 in the lane's token
+    const float keep = !PAIR && tok < n0 && tok >= last ? pw[max(n0 - 1 - tok, 0)] : 0.f;           // of the token in the last state
+    bool fine = true;
+    auto leave = [&](const Rows& out, int width, int t, const floatx16& sum, const floatx16& far, float weight) {
+      floatx16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = a.scale * sum[r] + (!PAIR && weight != 0.f ? weight * far[r] : 0.f);
+      fine &= store_rows(const_cast<T*>(place(out, width, this_row)) + 32 * t, x, width - 32 * t, half, on && out.p);
+    };
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      if (32 * t >= a.dk) break;
+      floatx16 x, out, far = {};
+      columns(fk, t, x, tok);
+      sums(x, sdq, out);
+      if (!PAIR && a.s0) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          uint4 f[MID];
+          if constexpr (EARLY) {
+            parts_of(s0_row[k], f);
+          } else {
+            float y[8];
+            along(s0, 32 * t + tok, 16 * k + 8 * half, y);
+            parts_of(y, f);
+          }
+          mul(far, f, fd[k]);
+        }
+      }
+      leave(a.dq, a.dk, t, out, far, a.s0 ? fade : 0.f);
+      columns(fq, t, x, tok);
+      sums(x, sdk, out);
+      far = floatx16{};
+      if (!PAIR && a.dsn) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          uint4 f[MID];
+          if constexpr (EARLY) {
+            parts_of(dsn_row[k], f);
+          } else {
+            float y[8];
+            along(dsn, 32 * t + tok, 16 * k + 8 * half, y);
+            parts_of(y, f);
+          }
+          mul(far, f, fv[k]);
+        }
+      }
+      leave(a.dkey, a.dk, t, out, far, a.dsn ? keep : 0.f);
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      if (32 * t >= a.dv) break;
+      floatx16 x, out, far = {};
+      columns(fd, t, x, tok);
+      sums(x, sdv, out);
+      if (!PAIR && a.dsn) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          uint4 f[MID];
+          if constexpr (EARLY) {
+            parts_of(dsn_col[k], f);
+          } else {
+            float y[8];
+            down(dsn, 16 * k + 8 * half, 32 * t + tok, y);
+            parts_of(y, f);
+          }
+          mul(far, f, fk[k]);
+        }
+      }
+      leave(a.dval, a.dv, t, out, far, a.dsn ? keep : 0.f);
+    }
+    if (__builtin_expect(!fine, 0)) {
+      for (int q = 0; q < PER; ++q) {
+        const int64_t i = i0 + q;
+        const int live = __builtin_amdgcn_readlane(n_this, 16 * q);
+        auto at = [&](const Rows& x, int width) { return x.p ? static_cast<T*>(const_cast<void*>(x.p)) + i * x.sn + (int64_t)h * width : nullptr; };
+        const uint8_t* reset = a.reset ? a.reset + i : nullptr;
+        const int m = a.dk, c = a.dv;
+        if (PAIR && live == 0) continue;
+        walk_window(Walk<T>{at(a.go, c), at(a.v, c), at(a.k, m), at(a.dq, m), a.go.st, a.v.st, a.k.st, a.dq.st, live, c, m, false, g, 1.f, a.scale, reset, a.N,
+                            !PAIR && a.s0 ? s0 : nullptr, 1, c, nullptr}, walk_lds[wave]);
+        walk_window(Walk<T>{at(a.v, c), at(a.go, c), at(a.q, m), at(a.dkey, m), a.v.st, a.go.st, a.q.st, a.dkey.st, live, c, m, true, g, a.scale, 1.f, reset, a.N,
+                            !PAIR && a.dsn ? dsn : nullptr, 1, c, nullptr}, walk_lds[wave]);
+        walk_window(Walk<T>{at(a.k, m), at(a.q, m), at(a.go, c), at(a.dval, c), a.k.st, a.q.st, a.go.st, a.dval.st, live, m, c, true, g, a.scale, 1.f, reset, a.N,
+                            !PAIR && a.dsn ? dsn : nullptr, c, 1, !PAIR && a.ds0 ? a.ds0 + state : nullptr}, walk_lds[wave]);
+      }
+    } else if (!PAIR && a.ds0) {      // after all that reads dsn, which may be in its place
+      const int until = resets ? __ffs(resets) - 1 : 32;        // the tokens that S0 reaches are those before it
+      const float pass = pw[n0];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        if (32 * t >= a.dv) break;
+        floatx16 x;
+        columns(fd, t, x, tok);
+        uint4 fx[2][IN];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) half_parts(x, k, fx[k]);
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+          if (32 * u >= a.dk) break;
+          floatx16 y, S = {};
+          columns(fq, u, y, swap23(tok));     // dS0's rows in the order of `down`
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int o = 8 * (r >> 2) + 4 * half + (r & 3);
+            y[r] = o < until ? y[r] * (a.scale * pw[o + 1]) : 0.f;
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            uint4 f[3];
+            half_parts(y, k, f);
+            mul(S, f, fx[k]);
+          }
+          const int c = 32 * t + tok;
+          float* to = a.ds0 + state + (int64_t)(32 * u + 8 * half) * a.dv + c;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float in[8];
+            if constexpr (EARLY) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) in[e] = dsn_col[k < KC ? k : 0][e];
+            } else {
+              down(a.dsn ? dsn : nullptr, 32 * u + 16 * k + 8 * half, c, in);
+            }
+            if (32 * u + 16 * k + 8 * half < a.dk && c < a.dv) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) to[(16 * k + e) * a.dv] = a.dsn && !resets ? fmaf(pass, in[e], S[8 * k + e]) : S[8 * k + e];
+            }
+          }
+        }
+      }
+    }
+    if (row >= row_end) return;
   }
 }
 
@@ -540,24 +1012,52 @@ Segments segments_of(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv
   return {(int32_t)((T + len - 1) / len), len};
 }
 
+// How many rows (sequences, pairs or segments) a wave takes, and the workgroups for it: `across` waves side by side, one for each
+// head and block of columns, on the same rows.  Waves that take neighbouring rows keep the memory that is open at a time together: taking
+// every so manieth instead read the same bytes at two thirds of the rate.
+unsigned runs_of(int64_t rows, int64_t across, uint32_t* run) {
+  *run = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(kRun, rows * across / (kFillWaves * 4)));
+  return (unsigned)(((rows + *run - 1) / *run * across + 3) / 4);
+}
+
 template <class T, bool OUT>
 void launch(DecayArgs a, hipStream_t st) {
   a.blocks_v = (a.dv + 31) / 32;
-  const int64_t units = a.N * a.heads * a.blocks_v * a.segs;
-  // Waves walk the units in steps of the grid: a grid that holds whole sequences keeps each wave at one head and its powers.
-  const int64_t seq = (int64_t)a.heads * a.blocks_v;
-  int64_t grid = (units + 3) / 4;
-  const int64_t most = 256 * 8 * 2;
-  if (grid > most) {
-    int64_t step = seq;
-    while (step % 4) step += seq;               // whole sequences and whole workgroups
-    grid = std::max<int64_t>(1, most * 4 / step) * step / 4;
-  }
-#define DGC_DECAY(KD) hipLaunchKernelGGL((k_decay<T, KD, OUT>), (unsigned)grid, 256, 0, st, a)
+  const unsigned grid = runs_of(a.N * a.segs, (int64_t)a.heads * a.blocks_v, &a.run);
+#define DGC_DECAY(KD) hipLaunchKernelGGL((k_decay<T, KD, OUT>), grid, 256, 0, st, a)
   if (a.dk <= 16) DGC_DECAY(16);
   else if (a.dk <= 32) DGC_DECAY(32);
   else if (a.dk <= 64) DGC_DECAY(64);
   else DGC_DECAY(128);
+#undef DGC_DECAY
+}
+
+template <class T>
+void launch_window(DecayArgs a, hipStream_t st) {
+  a.blocks_v = (a.dv + 31) / 32;
+  const bool pair = a.T <= kTok / 2;
+  const unsigned grid = runs_of(pair ? (a.N + 1) / 2 : a.N, (int64_t)a.heads * a.blocks_v, &a.run);
+#define DGC_DECAY(KD)                                                                                          \
+  if (pair) hipLaunchKernelGGL((k_decay_window<T, KD, true>), grid, 256, 0, st, a);   \
+  else hipLaunchKernelGGL((k_decay_window<T, KD, false>), grid, 256, 0, st, a)
+  if (a.dk <= 16) { DGC_DECAY(16); }
+  else if (a.dk <= 32) { DGC_DECAY(32); }
+  else if (a.dk <= 64) { DGC_DECAY(64); }
+  else { DGC_DECAY(128); }
+#undef DGC_DECAY
+}
+
+template <class T>
+void launch_window_back(BackArgs a, hipStream_t st) {
+  const bool pair = a.T <= kTok / 2 && !a.s0 && !a.dsn && !a.ds0;
+  const unsigned grid = runs_of(pair ? (a.N + 1) / 2 : a.N, a.heads, &a.run);
+  const int most = std::max(a.dk, a.dv);
+#define DGC_DECAY(KD)                                                                                \
+  if (pair) hipLaunchKernelGGL((k_decay_window_back<T, KD, true>), grid, 256, 0, st, a);             \
+  else hipLaunchKernelGGL((k_decay_window_back<T, KD, false>), grid, 256, 0, st, a)
+  if (most <= 16) { DGC_DECAY(16); }
+  else if (most <= 32) { DGC_DECAY(32); }
+  else { DGC_DECAY(64); }
 #undef DGC_DECAY
 }
 
@@ -606,6 +1106,10 @@ void forward(const Call& c, const Rows& q, const Rows& k, const Rows& v, const R
     hipLaunchKernelGGL(k_decay_step<T>, (unsigned)std::min<int64_t>((c.N * c.heads + 3) / 4, 256 * 32), 256, 0, c.st, a);
     return;
   }
+  if (c.T <= kTok && !s0 && !sn) {
+    launch_window<T>(a, c.st);
+    return;
+  }
   if (c.seg.n > 1) {
     join_segments<T>(c, a, s0, sn, false);
     a.s_in = c.states; a.s_out = nullptr;
@@ -616,6 +1120,10 @@ void forward(const Call& c, const Rows& q, const Rows& k, const Rows& v, const R
 template <class T>
 void backward(const Call& c, const Rows& q, const Rows& k, const Rows& v, const Rows& go, const Rows& dq, const Rows& dk, const Rows& dv,
               const float* s0, const float* dsn, float* ds0) {
+  if (c.T <= kTok && std::max(c.dk, c.dv) <= 64) {
+    launch_window_back<T>({q, k, v, go, dq, dk, dv, c.T, c.N, c.heads, c.dk, c.dv, c.decay, c.scale, s0, dsn, ds0, c.lengths, c.reset, 0}, c.st);
+    return;
+  }
   const bool split = c.seg.n > 1;
   if (dq.p) {
     DecayArgs a = args_of(c, go, v, k, dq, c.dv, c.dk);

@@ -185,6 +185,47 @@ def test_backward(dims, dtype):
             _close(x, w, m, dtype, dims[0], state)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dims", [(2, 3, 2, 8, 16), (5, 1, 1, 64, 64), (15, 8, 3, 32, 40), (16, 7, 8, 16, 16), (16, 6, 2, 128, 24), (17, 5, 3, 24, 96), (32, 9, 4, 32, 32),
+                                  (32, 3, 1, 128, 128), (9, 20000, 8, 16, 16)])
+def test_windows_from_zero_states(dims, dtype):
+    """No state is given and none wanted: windows that share a wave, an odd one out, more of them than waves at once."""
+    import torch
+    from paper_2309_03523_amd import binding
+    T, N, heads, dk, dv = dims
+    for k, mode in enumerate([dict(), dict(reset=0.3), dict(reset=0.1, ragged=True, batch_first=True)]):
+        c = _case(*dims, dtype, sum(dims) + k, state=False, **mode)
+        want, mag = _ref(c, back=True)
+        o, dq, dkk, dvv = (c["rows"](heads * d, -7.0) for d in (dv, dk, dk, dv))
+        kw = dict(heads=heads, scale=c["scale"], lengths=c["lengths"], reset=c["reset"])
+        binding.decay_attn_forward(c["q"], c["k"], c["v"], c["decay"], o, **kw)
+        binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], dq, dkk, dvv, **kw)
+        for x, w, m in zip((o, dq, dkk, dvv), (want[0], *want[2:5]), (mag[0], *mag[2:5])):
+            _behind(c, x)
+            _close(_live(c, x), w, m, dtype, T)
+        for skip in range(3):       # a gradient that is not wanted
+            again = [c["rows"](heads * d, -7.0) for d in (dk, dk, dv)]
+            binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], *[None if x == skip else t for x, t in enumerate(again)], **kw)
+            assert all(torch.equal(t, x) for y, (t, x) in enumerate(zip(again, (dq, dkk, dvv))) if y != skip)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [7, 16, 25])
+def test_windows_with_values_that_are_not_finite(T, dtype):
+    import torch
+    from paper_2309_03523_amd import binding
+    c = _case(T, 5, 2, 32, 40, dtype, 60, state=False, reset=0.15)
+    c["k"][2, 1, 4], c["v"][T // 2, 2, 41], c["q"][1, 4, 9], c["do"][3, 3, 50] = float("inf"), float("nan"), float("-inf"), float("nan")
+    want, _ = _ref(c, back=True)
+    o, dq, dkk, dvv = (c["rows"](2 * d, -7.0) for d in (40, 32, 32, 40))
+    binding.decay_attn_forward(c["q"], c["k"], c["v"], c["decay"], o, heads=2, scale=c["scale"], reset=c["reset"])
+    binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], dq, dkk, dvv, heads=2, scale=c["scale"], reset=c["reset"])
+    for x, w in zip((o, dq, dkk, dvv), (want[0], *want[2:5])):
+        assert torch.equal(torch.isnan(x), torch.isnan(w)) and torch.equal(torch.isinf(x), torch.isinf(w))
+        fine = torch.isfinite(w)
+        assert bool((x[fine].double() - w[fine]).abs().max() <= (0.02 if dtype == "bf16" else 1e-3) * w[fine].abs().max())
+
+
 def test_gradients_against_differences():
     """fp32 gradients of sum(do * o) + sum(dsn * sn) against central differences of the recurrence in double."""
     import torch
