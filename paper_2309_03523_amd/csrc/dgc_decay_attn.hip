@@ -667,30 +667,6 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     const uint32_t resets = a.reset ? (uint32_t)__ballot(flag) : 0;
     const uint32_t own = PAIR ? 0xffffu << (16 * slot) : ~0u;
     const uint32_t before = resets & ((2u << tok) - 1u) & own, after = resets & ~((2u << tok) - 1u) & own;
-    const float *s0 = a.s0 + state, *dsn = a.dsn + state;
-    // eight numbers of a state for the lane's output column: along row r of it, or down column c
-    auto along = [&](const float* s, int r, int c, float (&x)[8]) {
-      const bool in = s && r < a.dk && c < a.dv;
-      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f), *at = reinterpret_cast<const float4*>(s + r * a.dv + c);
-      const float4 lo = in ? at[0] : none, hi = in ? at[1] : none;
-      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
-    };
-    auto down = [&](const float* s, int r, int c, float (&x)[8]) {
-      const bool in = s && r < a.dk && c < a.dv;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = in ? s[(r + e) * a.dv + c] : 0.f;
-    };
-    // states that fit the registers come while the scores are worked out: one wait instead of four
-    constexpr bool EARLY = !PAIR && KT == 1;
-    float s0_row[EARLY ? KC : 1][8], dsn_row[EARLY ? KC : 1][8], dsn_col[EARLY ? KC : 1][8];
-    if constexpr (EARLY) {
-#pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        along(a.s0 ? s0 : nullptr, tok, 16 * k + 8 * half, s0_row[k]);
-        along(a.dsn ? dsn : nullptr, tok, 16 * k + 8 * half, dsn_row[k]);
-        down(a.dsn ? dsn : nullptr, 16 * k + 8 * half, tok, dsn_col[k]);
-      }
-    }
     uint4 fq[KC][IN], fk[KC][IN], fv[KC][IN], fd[KC][IN];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
@@ -741,11 +717,11 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
       }
     }
     // a tensor's 32 columns with its tokens as the contraction
-    auto columns = [&](const uint4 (&f)[KC][IN], int t, floatx16& x, int order) {
+    auto columns = [&](const uint4 (&f)[KC][IN], int t, floatx16& x) {
       x = floatx16{};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if (2 * t + k < KC) mul(x, f[2 * t + k < KC ? 2 * t + k : 0], {identity(k, half, order)});
+        if (2 * t + k < KC) mul(x, f[2 * t + k < KC ? 2 * t + k : 0], {identity(k, half, tok)});
       }
     };
     auto sums = [&](const floatx16& x, const uint4 (&score)[2][MID], floatx16& out) {
@@ -757,10 +733,27 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         mul(out, f, score[k]);
       }
     };
+    // eight numbers of a state with the lane's column: along a row of it (r: the row), or down a column
+    auto state_part = [&](const float* s, int r, int c, bool down, uint4 (&f)[MID]) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      if (r < a.dk && c < a.dv) {
+        if (down) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = s[(int64_t)(r + e) * a.dv + c];
+        } else {
+          const float4 lo = *reinterpret_cast<const float4*>(s + r * a.dv + c), hi = *reinterpret_cast<const float4*>(s + r * a.dv + c + 4);
+          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+        }
+      }
+      parts_of(x, f);
+    };
     const int n0 = PAIR ? 0 : __builtin_amdgcn_readfirstlane(n_this);
     const int last = resets ? 31 - __clz(resets) : 0;
     const float fade = before ? 0.f : a.scale * pw[tok + 1];                                        // of S0 in the lane's token
     const float keep = !PAIR && tok < n0 && tok >= last ? pw[max(n0 - 1 - tok, 0)] : 0.f;           // of the token in the last state
+    const float *s0 = a.s0 + state, *dsn = a.dsn + state;
     bool fine = true;
     auto leave = [&](const Rows& out, int width, int t, const floatx16& sum, const floatx16& far, float weight) {
       floatx16 x;
@@ -772,37 +765,25 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     for (int t = 0; t < KT; ++t) {
       if (32 * t >= a.dk) break;
       floatx16 x, out, far = {};
-      columns(fk, t, x, tok);
+      columns(fk, t, x);
       sums(x, sdq, out);
       if (!PAIR && a.s0) {
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
           uint4 f[MID];
-          if constexpr (EARLY) {
-            parts_of(s0_row[k], f);
-          } else {
-            float y[8];
-            along(s0, 32 * t + tok, 16 * k + 8 * half, y);
-            parts_of(y, f);
-          }
+          state_part(s0, 32 * t + tok, 16 * k + 8 * half, false, f);
           mul(far, f, fd[k]);
         }
       }
       leave(a.dq, a.dk, t, out, far, a.s0 ? fade : 0.f);
-      columns(fq, t, x, tok);
+      columns(fq, t, x);
       sums(x, sdk, out);
       far = floatx16{};
       if (!PAIR && a.dsn) {
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
           uint4 f[MID];
-          if constexpr (EARLY) {
-            parts_of(dsn_row[k], f);
-          } else {
-            float y[8];
-            along(dsn, 32 * t + tok, 16 * k + 8 * half, y);
-            parts_of(y, f);
-          }
+          state_part(dsn, 32 * t + tok, 16 * k + 8 * half, false, f);
           mul(far, f, fv[k]);
         }
       }
@@ -812,19 +793,13 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     for (int t = 0; t < KT; ++t) {
       if (32 * t >= a.dv) break;
       floatx16 x, out, far = {};
-      columns(fd, t, x, tok);
+      columns(fd, t, x);
       sums(x, sdv, out);
       if (!PAIR && a.dsn) {
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
           uint4 f[MID];
-          if constexpr (EARLY) {
-            parts_of(dsn_col[k], f);
-          } else {
-            float y[8];
-            down(dsn, 16 * k + 8 * half, 32 * t + tok, y);
-            parts_of(y, f);
-          }
+          state_part(dsn, 16 * k + 8 * half, 32 * t + tok, true, f);
           mul(far, f, fk[k]);
         }
       }
@@ -852,7 +827,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
       for (int t = 0; t < KT; ++t) {
         if (32 * t >= a.dv) break;
         floatx16 x;
-        columns(fd, t, x, tok);
+        columns(fd, t, x);
         uint4 fx[2][IN];
 #pragma unroll
         for (int k = 0; k < 2; ++k) half_parts(x, k, fx[k]);
@@ -860,7 +835,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         for (int u = 0; u < KT; ++u) {
           if (32 * u >= a.dk) break;
           floatx16 y, S = {};
-          columns(fq, u, y, swap23(tok));     // dS0's rows in the order of `down`
+          columns(fq, u, y);
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int o = 8 * (r >> 2) + 4 * half + (r & 3);
@@ -873,20 +848,12 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
             mul(S, f, fx[k]);
           }
           const int c = 32 * t + tok;
-          float* to = a.ds0 + state + (int64_t)(32 * u + 8 * half) * a.dv + c;
+          float* to = a.ds0 + state + (int64_t)(32 * u + 4 * half) * a.dv + c;
+          const float* from = dsn + (int64_t)(32 * u + 4 * half) * a.dv + c;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float in[8];
-            if constexpr (EARLY) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) in[e] = dsn_col[k < KC ? k : 0][e];
-            } else {
-              down(a.dsn ? dsn : nullptr, 32 * u + 16 * k + 8 * half, c, in);
-            }
-            if (32 * u + 16 * k + 8 * half < a.dk && c < a.dv) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) to[(16 * k + e) * a.dv] = a.dsn && !resets ? fmaf(pass, in[e], S[8 * k + e]) : S[8 * k + e];
-            }
+          for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r >> 2) + (r & 3);
+            if (32 * u + row + 4 * half < a.dk && c < a.dv) to[row * a.dv] = a.dsn && !resets ? fmaf(pass, from[row * a.dv], S[r]) : S[r];
           }
         }
       }
