@@ -12,7 +12,7 @@
 //    is rotated by the row, so that neither the fragments' reads nor the writes of turned pieces meet in a bank.
 //  - bf16 numbers are taken as they are and summed in fp32.  An fp32 number is split into three bf16 parts, which hold it exactly
 //    (dgc_split_dev.h), and a product is the sum of the six part products above 2^-24 of it.  The matrix unit cuts its sums off,
-//    so for fp32 those of 32 terms are added up by the vector unit, which rounds: errors as of an fp32 product, 2e-7.
+//    so for fp32 those of 16 terms are added up by the vector unit, which rounds: errors as of an fp32 product, 2e-7.
 //  - dw is a sum over all rows with a small result: the rows are split over workgroups, each writes an fp32 partial, and a
 //    second kernel adds them in order.  No atomics: the same inputs give the same bits.
 //  - Up to 32 rows (a few vertices served at once) read every weight once and multiply little: a workgroup takes 32 output
@@ -32,8 +32,10 @@ using split::floatx16;
 
 constexpr int kMaxDim = 65536;      // K, M
 constexpr int kFewRows = 32;
+constexpr int64_t kNear = 1 << 23;        // pitches below it: a tile's rows are within 32 bits of each other
 constexpr int64_t kMostTiles = 1 << 20;   // workgroups of one launch; more tiles are taken in turns
-constexpr int kSplitBlocks = 1024;  // workgroups that dw is split over, about
+constexpr int64_t kRowTiles = 16;         // tiles of 32 rows that a wave takes in turn (8: 514 us, 16: 512, 4: 536 for 800 000 rows 128 -> 512)
+constexpr int kSplitBlocks = 512;  // workgroups that dw is split over, about
 constexpr int kSplitRows = 512;     // rows of a share of dw at least
 constexpr int kSumBlocks = 1024, kMostSums = 512;   // as for the norm's weight gradients
 
@@ -122,6 +124,11 @@ __device__ __forceinline__ void load_unit(const float* p, int64_t k, int64_t K, 
   ops::load_vec(p + k, 0, (int)min((int64_t)8, K - k), x);
   ops::load_vec(p + k, 4, (int)min((int64_t)8, K - k), x + 4);
 }
+__device__ __forceinline__ void take_unit(const char* p, uint4& u) { u = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void take_unit(const char* p, float (&x)[8]) {
+  Elem<float>::unpack(reinterpret_cast<const uint4*>(p)[0], x);
+  Elem<float>::unpack(reinterpret_cast<const uint4*>(p)[1], x + 4);
+}
 __device__ __forceinline__ void zero_unit(uint4& u) { u = make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ void zero_unit(float (&x)[8]) {
 #pragma unroll
@@ -144,6 +151,12 @@ template <class T, int BX> struct Stage<T, BX, false> {   // the contraction lie
       if (x < X && k < K) load_unit(base + x * ld, k, K, unit[i]);
       else zero_unit(unit[i]);
     }
+  }
+  // A tile that lies inside the tensor: a 32-bit offset for each lane from addresses that are the same for all.
+  __device__ __forceinline__ void load_whole(const T* base, int64_t ld, int64_t x0, int64_t k0) {
+    const uint32_t off = (threadIdx.x / UK * (uint32_t)ld + threadIdx.x % UK * 8) * sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N; ++i) take_unit(reinterpret_cast<const char*>(base + (x0 + i * (256 / UK)) * ld + k0) + off, unit[i]);
   }
   __device__ __forceinline__ void store(uint4* lds) const {
 #pragma unroll
@@ -192,6 +205,17 @@ template <class T, int BX> struct Stage<T, BX, true> {    // the contraction goe
   }
 };
 
+// (The second way to read a tile pays for units along the rows; for pieces across them it takes more registers than there are.)
+template <class T, int BX>
+__device__ __forceinline__ void fetch_stage(Stage<T, BX, false>& s, const T* base, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t K) {
+  if (k0 + Stage<T, BX, false>::BK <= K && x0 + BX <= X && ld < kNear) s.load_whole(base, ld, x0, k0);
+  else s.load(base, ld, x0, X, k0, K);
+}
+template <class T, int BX>
+__device__ __forceinline__ void fetch_stage(Stage<T, BX, true>& s, const T* base, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t K) {
+  s.load(base, ld, x0, X, k0, K);
+}
+
 // ---------------------------------------------------------------------------------------------- the tile kernel
 
 struct LinearArgs {
@@ -208,83 +232,135 @@ struct LinearArgs {
   float* partial;                           // [parts][NQ][NP rounded up to 4]
 };
 
-// Four outputs of one row from column p (a multiple of 4) on: bias, pre-activation, activation, residual.
-template <class T>
-__device__ __forceinline__ void finish4(const LinearArgs& a, int64_t q, int64_t p, float (&v)[4]) {
-  typedef typename std::conditional<sizeof(T) == 4, uint4, uint2>::type Pack;
-  const int n = (int)min((int64_t)4, a.NP - p);
-  auto store = [&](void* base, int64_t ld, const float (&x)[4]) {
-    T* to = static_cast<T*>(base) + q * ld + p;
-    if (n == 4) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<Pack*>(to) = Elem<float>::pack(x);
-      else *reinterpret_cast<Pack*>(to) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
-    } else {
+// N numbers of a row from column `col` (a multiple of N) on, 4 or 8 of them; nothing is read or written from column F on but
+// what a vector of the pitch brings along.
+template <class T, int N>
+__device__ __forceinline__ void load_n(const T* row, int64_t col, int64_t F, float (&x)[N]) {
+  const int left = (int)min((int64_t)N, F - col);
+  if constexpr (N * sizeof(T) >= 16) {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) { if (i < n) to[i] = Elem<T>::one(x[i]); }
-    }
+    for (int i = 0; i < N; i += Elem<T>::kPer) ops::load_vec(row + col, i, left, x + i);
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(row + col);
+    x[0] = split::bf_lo(u.x); x[1] = split::bf_hi(u.x); x[2] = split::bf_lo(u.y); x[3] = split::bf_hi(u.y);
+  }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_n(T* row, int64_t col, int64_t F, const float (&x)[N]) {
+  const int left = (int)min((int64_t)N, F - col);
+  if constexpr (N * sizeof(T) >= 16) {
+#pragma unroll
+    for (int i = 0; i < N; i += Elem<T>::kPer) ops::store_vec(row + col, i, left, x + i);
+  } else if (left >= 4) {
+    *reinterpret_cast<uint2*>(row + col) = make_uint2(Elem<uint16_t>::pack2(x[0], x[1]), Elem<uint16_t>::pack2(x[2], x[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) { if (i < left) row[col + i] = Elem<T>::one(x[i]); }
+  }
+}
+// N outputs of row q from column p on: bias, pre-activation, activation, residual.
+template <class T, int N>
+__device__ __forceinline__ void finish(const LinearArgs& a, int64_t q, int64_t p, const float (&bias)[N], float (&v)[N]) {
+  if (a.bias) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += bias[i];
+  }
+  if (a.pre) store_n<T, N>(static_cast<T*>(a.pre) + q * a.ldpre, p, a.NP, v);
+  if (a.act != DGC_LINEAR_NONE) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = activate<T>(v[i], a.act);
+  }
+  if (a.residual) {
+    float x[N];
+    load_n<T, N>(static_cast<const T*>(a.residual) + q * a.ldr, p, a.NP, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += x[i];
+  }
+  store_n<T, N>(static_cast<T*>(a.out) + q * a.ldo, p, a.NP, v);
+}
+// The same for eight outputs inside the tensor: row q + r, column p + c, q and p the same for all lanes.
+template <class T>
+__device__ __forceinline__ void finish_whole(const LinearArgs& a, int64_t q, uint32_t r, int64_t p, uint32_t c, const float (&bias)[8], float (&v)[8]) {
+  auto place = [&](auto* base, int64_t ld) { return base + q * ld + p + (r * (uint32_t)ld + c); };
+  auto store = [&](void* base, int64_t ld) {
+    T* to = place(static_cast<T*>(base), ld);
+#pragma unroll
+    for (int i = 0; i < 8; i += Elem<T>::kPer) *reinterpret_cast<uint4*>(to + i) = Elem<T>::pack(v + i);
   };
   if (a.bias) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += i < n ? a.bias[p + i] : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
   }
-  if (a.pre) store(a.pre, a.ldpre, v);
+  if (a.pre) store(a.pre, a.ldpre);
   if (a.act != DGC_LINEAR_NONE) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = activate<T>(v[i], a.act);
+    for (int i = 0; i < 8; ++i) v[i] = activate<T>(v[i], a.act);
   }
   if (a.residual) {
-    const T* from = static_cast<const T*>(a.residual) + q * a.ldr + p;    // four of a row's pitch, at least one of them below NP
-    float r[4];
-    if constexpr (sizeof(T) == 4) {
-      Elem<float>::unpack(*reinterpret_cast<const uint4*>(from), r);
-    } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(from);
-      r[0] = split::bf_lo(u.x); r[1] = split::bf_hi(u.x); r[2] = split::bf_lo(u.y); r[3] = split::bf_hi(u.y);
-    }
+    const T* from = place(static_cast<const T*>(a.residual), a.ldr);
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += r[i];
+    for (int i = 0; i < 8; i += Elem<T>::kPer) Elem<T>::unpack(*reinterpret_cast<const uint4*>(from + i), x + i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
   }
-  store(a.out, a.ldo, v);
+  store(a.out, a.ldo);
+}
+template <int N>
+__device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t p, float (&bias)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) bias[i] = a.bias && p + i < a.NP ? a.bias[p + i] : 0.f;
 }
 
 // BP x BQ outputs a workgroup, a quarter of them a wave.
 template <class T, int BP, int BQ, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
-__global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) {
   constexpr int BK = Kind<T>::kBK, UK = BK / 8, PARTS = Kind<T>::kParts, FP = BP / 64, FQ = BQ / 64;
-  __shared__ uint4 lds_p[PARTS * BP * UK];
-  __shared__ uint4 lds_q[PARTS * BQ * UK];
+  __shared__ uint4 lds[PARTS * (BP + BQ) * UK];
+  uint4 *lds_p = lds, *lds_q = lds + PARTS * BP * UK;
+  static_assert(BQ / 2 * BP / 4 <= PARTS * (BP + BQ) * UK, "half of the outputs fit where the operands were");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const int wp = (wave & 1) * (BP / 2), wq = (wave >> 1) * (BQ / 2);
   const int64_t np = (a.NP + BP - 1) / BP, nq = (a.NQ + BQ - 1) / BQ, tiles = np * nq * a.parts;
   // Workgroups go round the 8 XCDs: neighbours in the list of tiles, which share rows of Q, stay on one of them and its L2.
   const int64_t per = (tiles + 7) / 8;
-  for (int64_t local = blockIdx.x >> 3; local < per; local += gridDim.x >> 3) {
+  struct Tile { int64_t p0, q0, c0, c1; int part; };
+  auto tile_of = [&](int64_t local) {
     const int64_t id = (int64_t)(blockIdx.x & 7) * per + local;
-    if (id >= tiles) break;
-    const int64_t p0 = id % np * BP, q0 = id / np % nq * BQ;
-    const int part = (int)(id / (np * nq));
-    const int64_t c0 = (int64_t)part * a.share, c1 = min(a.C, c0 + a.share);
-    const T* P = static_cast<const T*>(a.P);
-    const T* Q = static_cast<const T*>(a.Q);
-    Stage<T, BP, ACROSS_P> sp;
-    Stage<T, BQ, ACROSS_Q> sq;
+    Tile t;
+    t.part = local < per && id < tiles ? (int)(id / (np * nq)) : -1;      // none left: -1
+    t.p0 = id % np * BP;
+    t.q0 = id / np % nq * BQ;
+    t.c0 = (int64_t)t.part * a.share;
+    t.c1 = min(a.C, t.c0 + a.share);
+    return t;
+  };
+  const T* P = static_cast<const T*>(a.P);
+  const T* Q = static_cast<const T*>(a.Q);
+  Stage<T, BP, ACROSS_P> sp;
+  Stage<T, BQ, ACROSS_Q> sq;
+  auto fetch = [&](const Tile& t, int64_t c) {
+    fetch_stage(sp, P, a.ldp, t.p0, a.NP, c, t.c1);
+    fetch_stage(sq, Q, a.ldq, t.q0, a.NQ, c, t.c1);
+  };
+  for (int64_t local = blockIdx.x >> 3; local < per; local += gridDim.x >> 3) {
+    const Tile tile = tile_of(local);
+    if (tile.part < 0) return;
+    fetch(tile, tile.c0);
+    const int64_t p0 = tile.p0, q0 = tile.q0, c0 = tile.c0, c1 = tile.c1;
+    const int part = tile.part;
     floatx16 acc[FP][FQ];
 #pragma unroll
     for (int i = 0; i < FP; ++i) {
 #pragma unroll
       for (int j = 0; j < FQ; ++j) acc[i][j] = floatx16{};
     }
-    sp.load(P, a.ldp, p0, a.NP, c0, c1);
-    sq.load(Q, a.ldq, q0, a.NQ, c0, c1);
     for (int64_t c = c0; c < c1; c += BK) {
       __syncthreads();
       sp.store(lds_p);
       sq.store(lds_q);
       __syncthreads();
-      if (c + BK < c1) {
-        sp.load(P, a.ldp, p0, a.NP, c + BK, c1);
-        sq.load(Q, a.ldq, q0, a.NQ, c + BK, c1);
-      }
+      if (c + BK < c1) fetch(tile, c + BK);
       if constexpr (PARTS == 1) {
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
@@ -300,12 +376,6 @@ __global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
           }
         }
       } else {
-        floatx16 sum[FP][FQ];
-#pragma unroll
-        for (int i = 0; i < FP; ++i) {
-#pragma unroll
-          for (int j = 0; j < FQ; ++j) sum[i][j] = floatx16{};
-        }
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
           uint4 fp[FP][3], fq[FQ][3];
@@ -319,36 +389,133 @@ __global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
 #pragma unroll
           for (int i = 0; i < FP; ++i) {
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) split::six(sum[i][j], sum[i][j], fp[i], fq[j]);
+            for (int j = 0; j < FQ; ++j) {
+              floatx16 sum = {};
+              split::six(sum, sum, fp[i], fq[j]);
+              acc[i][j] += sum;
+            }
           }
-        }
-#pragma unroll
-        for (int i = 0; i < FP; ++i) {
-#pragma unroll
-          for (int j = 0; j < FQ; ++j) acc[i][j] += sum[i][j];
         }
       }
     }
+    // Outputs go through LDS, half of the rows at a time, so that 16 or 8 threads finish a row's columns side by side: stored from
+    // the registers as they are, each instruction touched 32 rows and the stores took longer than the products.
+    constexpr int UR = BP / 4, CG = BP / 8, PASS = 256 / CG;     // 16-byte units of a row of sums; threads a row; rows at a time
+    const int col = threadIdx.x % CG * 8;
+    float bias[8];
+    load_bias(a, p0 + col, bias);
+    const bool whole = p0 + BP <= a.NP && q0 + BQ <= a.NQ && (PARTIAL ? a.NP % 4 == 0 : a.ldo < kNear && a.ldr < kNear && a.ldpre < kNear);
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int64_t q = q0 + wq + 32 * j + (lane & 31);
-      if (q >= a.NQ) continue;
+    for (int ph = 0; ph < 2; ++ph) {
+      __syncthreads();
+      if ((wave >> 1) == ph) {
 #pragma unroll
-      for (int i = 0; i < FP; ++i) {
+        for (int j = 0; j < FQ; ++j) {
+          const int row = 32 * j + (lane & 31);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int64_t p = p0 + wp + 32 * i + 8 * g + 4 * half;
-          if (p >= a.NP) continue;
-          float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          for (int i = 0; i < FP; ++i) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const int u = (wp + 32 * i + 8 * g + 4 * half) / 4;
+              const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+              lds[row * UR + (u ^ (row & (UR - 1)))] = Elem<float>::pack(v);
+            }
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < BQ / 2 / PASS; ++k) {
+        const int row = k * PASS + threadIdx.x / CG;
+        const int64_t q = q0 + ph * (BQ / 2) + row, p = p0 + col;
+        float v[8];
+        Elem<float>::unpack(lds[row * UR + (col / 4 ^ (row & (UR - 1)))], v);
+        Elem<float>::unpack(lds[row * UR + ((col / 4 + 1) ^ (row & (UR - 1)))], v + 4);
+        if (whole) {
+          if constexpr (PARTIAL) {
+            float* to = a.partial + ((int64_t)part * a.NQ + q0 + ph * (BQ / 2) + k * PASS) * a.NP + p0;
+            to += threadIdx.x / CG * (uint32_t)a.NP + col;
+            *reinterpret_cast<uint4*>(to) = Elem<float>::pack(v);
+            *reinterpret_cast<uint4*>(to + 4) = Elem<float>::pack(v + 4);
+          } else {
+            finish_whole<T>(a, q0 + ph * (BQ / 2) + k * PASS, threadIdx.x / CG, p0, col, bias, v);
+          }
+        } else if (q < a.NQ && p < a.NP) {
           if constexpr (PARTIAL) {
             const int64_t pitch = (a.NP + 3) / 4 * 4;
-            *reinterpret_cast<uint4*>(a.partial + ((int64_t)part * a.NQ + q) * pitch + p) = Elem<float>::pack(v);
+            store_n<float, 8>(a.partial + ((int64_t)part * a.NQ + q) * pitch, p, pitch, v);
           } else {
-            finish4<T>(a, q, p, v);
+            finish<T, 8>(a, q, p, bias, v);
           }
         }
       }
     }
+  }
+}
+
+// bf16 rows of 16 KF numbers, short enough for the weights to stay in registers: a wave holds 64 columns of them and takes 32 rows after
+// 32 rows, which it reads as fragments straight from memory.  No wave waits for another, so products, epilogue and traffic of
+// different waves overlap.
+template <int KF>
+__global__ __launch_bounds__(256, KF <= 4 ? 4 : 3) void k_linear_rows(LinearArgs a) {
+  typedef uint16_t T;
+  constexpr int UR = 16;                     // 16-byte units of a row of 64 sums
+  __shared__ uint4 lds[4][32 * UR];
+  const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint4* mine = lds[wave];
+  // workgroups go round the 8 XCDs: those that read the same rows stay on one
+  const uint32_t group = gridDim.x / 8, block = blockIdx.x < group * 8 ? blockIdx.x % 8 * group + blockIdx.x / 8 : blockIdx.x;
+  const uint32_t line = block * 4 + wave, across = (uint32_t)(a.NP / 64), tiles = (uint32_t)((a.NQ + 31) / 32);
+  const int64_t p0 = (int64_t)(line % across) * 64;
+  uint32_t tile = line / across * (uint32_t)a.share;
+  const uint32_t end = min(tiles, tile + (uint32_t)a.share);
+  if (tile >= tiles) return;
+  const T* Q = static_cast<const T*>(a.Q);
+  bf16x8 fp[2][KF];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const T* P = static_cast<const T*>(a.P) + (p0 + 32 * i) * a.ldp + (tok * (uint32_t)a.ldp + 8 * half);
+#pragma unroll
+    for (int k = 0; k < KF; ++k) fp[i][k] = as_frag(*reinterpret_cast<const uint4*>(P + 16 * k));
+  }
+  const uint32_t col = lane % 8 * 8;
+  float bias[8];
+  load_bias(a, p0 + col, bias);
+  uint4 raw[KF];
+  auto fetch = [&](uint32_t t) {
+    const uint32_t r = min((uint32_t)tok, (uint32_t)min(a.NQ - 1 - (int64_t)t * 32, (int64_t)31));  // rows behind the last are not kept
+    const T* row = Q + (int64_t)t * 32 * a.ldq + (r * (uint32_t)a.ldq + 8 * half);
+#pragma unroll
+    for (int k = 0; k < KF; ++k) raw[k] = *reinterpret_cast<const uint4*>(row + 16 * k);
+  };
+  fetch(tile);
+  for (; tile < end; ++tile) {
+    floatx16 acc[2] = {};
+#pragma unroll
+    for (int k = 0; k < KF; ++k) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i][k], as_frag(raw[k]), acc[i], 0, 0, 0);
+    }
+    if (tile + 1 < end) fetch(tile + 1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float v[4] = {acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+        mine[tok * UR + ((8 * i + 2 * g + half) ^ (tok & 15))] = Elem<float>::pack(v);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+    for (int k = 0; k < 4; ++k) {
+      const int row = 8 * k + lane / 8;
+      float v[8];
+      Elem<float>::unpack(mine[row * UR + (col / 4 ^ (row & 15))], v);
+      Elem<float>::unpack(mine[row * UR + ((col / 4 + 1) ^ (row & 15))], v + 4);
+      if ((int64_t)tile * 32 + row < a.NQ) finish_whole<T>(a, (int64_t)tile * 32 + 8 * k, lane / 8, p0, col, bias, v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
@@ -402,24 +569,43 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += joined[w][4 * g + e][lane];
     }
-    if (q < a.NQ && col < a.NP) finish4<T>(a, q, col, v);
+    if (q < a.NQ && col < a.NP) {
+      float bias[4];
+      load_bias(a, col, bias);
+      finish<T, 4>(a, q, col, bias, v);
+    }
   }
 }
 
-// The partial sums of dw, in the order of the rows.
+// The partial sums of dw: 16 units of four columns a workgroup, 16 parts at a time.
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
-  const int64_t pitch = (a.NP + 3) / 4, n = a.NQ * pitch;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t q = i / pitch, p = i % pitch * 4;
-    float v[4] = {};
-    for (int part = 0; part < a.parts; ++part) {
-      float x[4];
-      Elem<float>::unpack(*reinterpret_cast<const uint4*>(a.partial + (part * n + i) * 4), x);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += x[e];
+  __shared__ float4 lds[16][16];
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int64_t pitch = (a.NP + 3) / 4, n = a.NQ * pitch, unit = (int64_t)blockIdx.x * 16 + c;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (unit < n) {
+#pragma unroll 4
+    for (int part = g; part < a.parts; part += 16) {
+      const float4 x = *reinterpret_cast<const float4*>(a.partial + (part * n + unit) * 4);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
-    finish4<T>(a, q, p, v);
+  }
+  lds[g][c] = v;
+  __syncthreads();
+#pragma unroll
+  for (int m = 8; m >= 1; m >>= 1) {
+    if (g < m) {
+      const float4 x = lds[g + m][c];
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      lds[g][c] = v;
+    }
+    __syncthreads();
+  }
+  if (g == 0 && unit < n) {
+    float y[4] = {v.x, v.y, v.z, v.w};
+    const float none[4] = {};
+    finish<T, 4>(a, unit / pitch, unit % pitch * 4, none, y);
   }
 }
 
@@ -504,7 +690,11 @@ void launch_slope(const SlopeArgs& a, int64_t blocks, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------- host
 
 // 128 x 128 outputs a workgroup; 64 x 64 where that leaves compute units without work, or the output is that narrow.
-bool small_tiles(int64_t NP, int64_t NQ) { return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < 256; }
+// (100 000 rows 172 -> 128 in fp32, 782 large tiles: 59 us in small ones, 65 in large.)
+template <class T>
+bool small_tiles(int64_t NP, int64_t NQ) {
+  return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < (sizeof(T) == 4 ? 1024 : 256);
+}
 
 template <class T, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
 void launch_tiles(const LinearArgs& a, bool small, hipStream_t st) {
@@ -512,6 +702,23 @@ void launch_tiles(const LinearArgs& a, bool small, hipStream_t st) {
   const unsigned grid = (unsigned)(std::min<int64_t>((tiles + 7) / 8, kMostTiles / 8) * 8);
   if (small) hipLaunchKernelGGL((k_linear<T, 64, 64, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
   else hipLaunchKernelGGL((k_linear<T, 128, 128, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
+}
+
+// The kernel for short rows takes these (the largest pitch that is not there is 0).
+bool short_rows(const LinearArgs& a, int32_t dtype) {
+  return dtype == DGC_DTYPE_BF16 && a.C <= 128 && a.C % 32 == 0 && a.NP % 64 == 0 && (a.NQ + 31) / 32 * (a.NP / 64) < ((int64_t)1 << 31) &&
+         std::max({a.ldp, a.ldq, a.ldo, a.ldr, a.ldpre}) < kNear;
+}
+// Tiles of 32 rows that a wave takes one after the other, enough waves to fill the chip first.
+void launch_rows(LinearArgs a, hipStream_t st) {
+  const int64_t across = a.NP / 64, tiles = (a.NQ + 31) / 32;
+  a.share = std::max<int64_t>(1, std::min<int64_t>(kRowTiles, tiles * across / (256 * 4 * 3)));
+  const int64_t waves = (tiles + a.share - 1) / a.share * across;
+  const unsigned grid = (unsigned)((waves + 3) / 4);
+  if (a.C == 32) hipLaunchKernelGGL(k_linear_rows<2>, grid, 256, 0, st, a);
+  else if (a.C == 64) hipLaunchKernelGGL(k_linear_rows<4>, grid, 256, 0, st, a);
+  else if (a.C == 96) hipLaunchKernelGGL(k_linear_rows<6>, grid, 256, 0, st, a);
+  else hipLaunchKernelGGL(k_linear_rows<8>, grid, 256, 0, st, a);
 }
 
 // How dw's rows are split: enough shares to fill the chip, none below kSplitRows.
@@ -587,14 +794,14 @@ void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const vo
     } else {
       launch_tiles<T, true, true, true>(a, s.small, st);
       const int64_t n = (int64_t)M * ((K + 3) / 4);
-      hipLaunchKernelGGL(k_linear_join<T>, (unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, st, a);
+      hipLaunchKernelGGL(k_linear_join<T>, (unsigned)((n + 15) / 16), 256, 0, st, a);
     }
   }
   if (dx && R > 0) {
     LinearArgs a{};
     a.P = w; a.ldp = ldw; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
     a.out = dx; a.ldo = lddx;
-    launch_tiles<T, true, false, false>(a, small_tiles(a.NP, a.NQ), st);
+    launch_tiles<T, true, false, false>(a, small_tiles<T>(a.NP, a.NQ), st);
   }
 }
 
@@ -640,10 +847,12 @@ dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64
     const unsigned grid = (unsigned)((M + 31) / 32);
     if (dtype == DGC_DTYPE_F32) hipLaunchKernelGGL(k_linear_few<float>, grid, 512, 0, st, a);
     else hipLaunchKernelGGL(k_linear_few<uint16_t>, grid, 512, 0, st, a);
+  } else if (short_rows(a, dtype)) {
+    launch_rows(a, st);
   } else if (dtype == DGC_DTYPE_F32) {
-    launch_tiles<float, false, false, false>(a, small_tiles(M, R), st);
+    launch_tiles<float, false, false, false>(a, small_tiles<float>(M, R), st);
   } else {
-    launch_tiles<uint16_t, false, false, false>(a, small_tiles(M, R), st);
+    launch_tiles<uint16_t, false, false, false>(a, small_tiles<uint16_t>(M, R), st);
   }
   return ops::launched("linear");
 }
