@@ -420,70 +420,99 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
 # enqueued on `stream` (default: the current stream of the tensors' device).
 
 
-def _op_dtype(t, name: str) -> int:
+_torch = None
+_raw_stream = None      # device index -> the current stream's handle
+
+
+def _op_init():
+    global _torch, _raw_stream
     import torch
-    if t.dtype == torch.bfloat16:
-        return 1
-    if t.dtype == torch.float32:
-        return 0
-    raise ValueError(f"{name} must be float32 or bfloat16")
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _torch = torch
+    return load()
 
 
-def _op_rows(t, name: str, like=None, shape=None):
-    """(address, pitch) of [..., F] rows at one pitch; `like`: a tensor of the same element type and device; `shape`: (R, F)."""
+def _op_first(t, name: str):
+    """(library, element type, device index) of a call's first tensor."""
+    lib = _lib if _torch is not None and _lib is not None else _op_init()
+    dt = t.dtype
+    if dt is _torch.bfloat16:
+        code = 1
+    elif dt is _torch.float32:
+        code = 0
+    else:
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    return lib, code, dev
+
+
+def _op_rows(t, name: str, dtype=None, dev=None, shape=None):
+    """(address, pitch) of [..., F] rows at one pitch; dtype, dev: what the first tensor has; shape: (R, F)."""
     if t is None:
         return None, 0
     st, sh = t.stride(), t.shape
     n = len(sh)
-    if n < 2 or (sh[-1] != 1 and st[-1] != 1):
+    if n < 2 or (st[-1] != 1 and sh[-1] != 1):
         raise ValueError(f"{name} must be rows [..., F] with a contiguous last dimension")
-    for d in range(n - 2):
-        inner = sh[d + 1] * st[d + 1]
-        if sh[d] != 1 and st[d] != inner and t.numel():
-            raise ValueError(f"{name}: its rows must lie at one pitch")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+    if dtype is not None and (t.dtype is not dtype or t.get_device() != dev):
         raise ValueError(f"{name} has another element type or device than the first tensor")
-    if shape is not None and (sh[-1] != shape[1] or t.numel() != shape[0] * shape[1]):
+    F, rows, pitch = sh[-1], sh[-2], st[-2]
+    if n > 2:
+        step = pitch
+        for d in range(n - 3, -1, -1):
+            if sh[d] != 1:
+                if rows == 1:
+                    step = pitch = st[d]     # leading sizes of 1 leave their strides free
+                elif st[d] != rows * step and rows and sh[d]:
+                    raise ValueError(f"{name}: its rows must lie at one pitch")
+                rows *= sh[d]
+    if rows <= 1:
+        pitch = -(-F // 8) * 8
+    if shape is not None and (F != shape[1] or rows != shape[0]):
         raise ValueError(f"{name} must hold {shape[0]} rows of {shape[1]}, not {tuple(sh)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    per = 16 // t.element_size()
-    pitch = st[-2] if sh[-2] != 1 else (st[-3] if n > 2 and t.numel() > sh[-1] else -(-sh[-1] // per) * per)
-    if n > 2 and sh[-2] == 1:       # leading sizes of 1 leave their strides free: the pitch is that of the first longer one
-        pitch = next((st[d] for d in range(n - 3, -1, -1) if sh[d] != 1), pitch)
     return t.data_ptr(), pitch
 
 
-def _op_flat(t, name: str, numel: int, like, dtype=None):
+def _op_count(t) -> int:
+    """Rows of a [..., F] tensor."""
+    n = 1
+    for x in t.shape[:-1]:
+        n *= x
+    return n
+
+
+def _op_flat(t, name: str, numel: int, dev: int, dtype=None):
     """Address of a contiguous device tensor of `numel` elements (fp32 unless `dtype` says otherwise), or None."""
-    import torch
     if t is None:
         return None
-    if t.dtype != (dtype or torch.float32) or not t.is_contiguous() or t.numel() != numel or t.device != like.device:
-        raise ValueError(f"{name} must be a contiguous {str(dtype or torch.float32)[6:]} tensor of {numel} elements on the first tensor's device")
+    if t.dtype is not (dtype or _torch.float32) or t.numel() != numel or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {str(dtype or _torch.float32)[6:]} tensor of {numel} elements on the first tensor's device")
     return t.data_ptr()
 
 
-def _op_workspace(t, like):
+def _op_workspace(t, dev: int):
     if t is None:
         return None, 0
-    if not t.is_contiguous() or t.device != like.device:
+    if t.get_device() != dev or not t.is_contiguous():
         raise ValueError("workspace must be contiguous and on the first tensor's device")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _op_call(fn, like, stream, *args):
+def _op_call(fn, dev: int, stream, *args):
     """Calls fn(*args, stream) with the tensors' device current."""
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream(like.device)
-    elif stream.device != like.device:
-        raise ValueError("stream belongs to another device than the tensors")
-    if torch.cuda.current_device() == like.device.index:
-        rc = fn(*args, stream.cuda_stream)
+        handle = _raw_stream(dev)
     else:
-        with torch.cuda.device(like.device):
-            rc = fn(*args, stream.cuda_stream)
+        if stream.device.index != dev:
+            raise ValueError("stream belongs to another device than the tensors")
+        handle = stream.cuda_stream
+    if _torch.cuda.current_device() == dev:
+        rc = fn(*args, handle)
+    else:
+        with _torch.cuda.device(dev):
+            rc = fn(*args, handle)
     if rc:
         raise DgcError(rc, _lib.dgc_last_error(None).decode())
 
@@ -495,32 +524,30 @@ def norm_workspace_bytes(R: int, F: int) -> int:
 def norm_forward(x, y, *, gamma=None, beta=None, mean=None, rstd=None, eps: float = 1e-5, stream=None):
     """dgc_norm_forward: y = layer norm of the rows of x [..., F] (y may be x); gamma, beta fp32 [F] or None (1, 0);
     mean, rstd fp32, one entry a row, written if given."""
-    lib = load()
-    dt = _op_dtype(x, "x")
+    lib, code, dev = _op_first(x, "x")
+    dt = x.dtype
     px, ldx = _op_rows(x, "x")
-    F = x.shape[-1]
-    R = x.numel() // F if F else 0
-    py, ldy = _op_rows(y, "y", x, (R, F))
-    _op_call(lib.dgc_norm_forward, x, stream, px, ldx, R, F, dt, _op_flat(gamma, "gamma", F, x), _op_flat(beta, "beta", F, x),
-             float(eps), py, ldy, _op_flat(mean, "mean", R, x), _op_flat(rstd, "rstd", R, x))
+    F, R = x.shape[-1], _op_count(x)
+    py, ldy = _op_rows(y, "y", dt, dev, (R, F))
+    _op_call(lib.dgc_norm_forward, dev, stream, px, ldx, R, F, code, _op_flat(gamma, "gamma", F, dev), _op_flat(beta, "beta", F, dev),
+             float(eps), py, ldy, _op_flat(mean, "mean", R, dev), _op_flat(rstd, "rstd", R, dev))
     return y
 
 
 def norm_backward(dy, x, mean, rstd, dx, *, gamma=None, add=None, dgamma=None, dbeta=None, workspace=None, stream=None):
     """dgc_norm_backward: dx = gradient of x, plus `add` if given (dx may be dy, x or add); dgamma, dbeta fp32 [F], written if
     given (they need `workspace`, norm_workspace_bytes(R, F) device bytes)."""
-    lib = load()
-    dt = _op_dtype(x, "x")
+    lib, code, dev = _op_first(x, "x")
+    dt = x.dtype
     px, ldx = _op_rows(x, "x")
-    F = x.shape[-1]
-    R = x.numel() // F if F else 0
-    pdy, lddy = _op_rows(dy, "dy", x, (R, F))
-    padd, ldadd = _op_rows(add, "add", x, (R, F))
-    pdx, lddx = _op_rows(dx, "dx", x, (R, F))
-    ws, ws_bytes = _op_workspace(workspace, x)
-    _op_call(lib.dgc_norm_backward, x, stream, pdy, lddy, px, ldx, _op_flat(mean, "mean", R, x), _op_flat(rstd, "rstd", R, x), R, F,
-             dt, _op_flat(gamma, "gamma", F, x), padd, ldadd, pdx, lddx, _op_flat(dgamma, "dgamma", F, x),
-             _op_flat(dbeta, "dbeta", F, x), ws, ws_bytes)
+    F, R = x.shape[-1], _op_count(x)
+    pdy, lddy = _op_rows(dy, "dy", dt, dev, (R, F))
+    padd, ldadd = _op_rows(add, "add", dt, dev, (R, F))
+    pdx, lddx = _op_rows(dx, "dx", dt, dev, (R, F))
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_norm_backward, dev, stream, pdy, lddy, px, ldx, _op_flat(mean, "mean", R, dev), _op_flat(rstd, "rstd", R, dev), R, F,
+             code, _op_flat(gamma, "gamma", F, dev), padd, ldadd, pdx, lddx, _op_flat(dgamma, "dgamma", F, dev),
+             _op_flat(dbeta, "dbeta", F, dev), ws, ws_bytes)
     return dx
 
 
@@ -532,17 +559,15 @@ def linear_workspace_bytes(R: int, K: int, M: int, *, dtype: str = "f32", act: s
 def linear_forward(x, w, y, *, bias=None, act: str = "none", residual=None, pre=None, stream=None):
     """dgc_linear_forward: y = act(x w^T + bias) + residual for rows x [..., K], w [M, K] (out, in), y [..., M] of one element
     type; bias fp32 [M]; pre [..., M] receives the activation's argument; y may be residual itself."""
-    lib = load()
-    dt = _op_dtype(x, "x")
+    lib, code, dev = _op_first(x, "x")
+    dt = x.dtype
     px, ldx = _op_rows(x, "x")
-    K = x.shape[-1]
-    R = x.numel() // K if K else 0
-    M = w.shape[0]
-    pw, ldw = _op_rows(w, "w", x, (M, K))
-    py, ldy = _op_rows(y, "y", x, (R, M))
-    pr, ldr = _op_rows(residual, "residual", x, (R, M))
-    pp, ldp = _op_rows(pre, "pre", x, (R, M))
-    _op_call(lib.dgc_linear_forward, x, stream, px, ldx, pw, ldw, R, K, M, dt, _op_flat(bias, "bias", M, x), LINEAR_ACT[act], pr, ldr,
+    K, R, M = x.shape[-1], _op_count(x), w.shape[0]
+    pw, ldw = _op_rows(w, "w", dt, dev, (M, K))
+    py, ldy = _op_rows(y, "y", dt, dev, (R, M))
+    pr, ldr = _op_rows(residual, "residual", dt, dev, (R, M))
+    pp, ldp = _op_rows(pre, "pre", dt, dev, (R, M))
+    _op_call(lib.dgc_linear_forward, dev, stream, px, ldx, pw, ldw, R, K, M, code, _op_flat(bias, "bias", M, dev), LINEAR_ACT[act], pr, ldr,
              py, ldy, pp, ldp)
     return y
 
@@ -550,20 +575,18 @@ def linear_forward(x, w, y, *, bias=None, act: str = "none", residual=None, pre=
 def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, dbias=None, workspace, stream=None):
     """dgc_linear_backward: the wanted ones of dx [..., K], dw [M, K] and dbias fp32 [M] from dy [..., M]; `pre`: what
     linear_forward left, needed with an activation; workspace: linear_workspace_bytes device bytes."""
-    lib = load()
-    dt = _op_dtype(x, "x")
+    lib, code, dev = _op_first(x, "x")
+    dt = x.dtype
     px, ldx = _op_rows(x, "x")
-    K = x.shape[-1]
-    R = x.numel() // K if K else 0
-    M = w.shape[0]
-    pw, ldw = _op_rows(w, "w", x, (M, K))
-    pdy, lddy = _op_rows(dy, "dy", x, (R, M))
-    pp, ldp = _op_rows(pre, "pre", x, (R, M))
-    pdx, lddx = _op_rows(dx, "dx", x, (R, K))
-    pdw, lddw = _op_rows(dw, "dw", x, (M, K))
-    ws, ws_bytes = _op_workspace(workspace, x)
-    _op_call(lib.dgc_linear_backward, x, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, dt, pp, ldp, LINEAR_ACT[act], pdx, lddx, pdw, lddw,
-             _op_flat(dbias, "dbias", M, x), ws, ws_bytes)
+    K, R, M = x.shape[-1], _op_count(x), w.shape[0]
+    pw, ldw = _op_rows(w, "w", dt, dev, (M, K))
+    pdy, lddy = _op_rows(dy, "dy", dt, dev, (R, M))
+    pp, ldp = _op_rows(pre, "pre", dt, dev, (R, M))
+    pdx, lddx = _op_rows(dx, "dx", dt, dev, (R, K))
+    pdw, lddw = _op_rows(dw, "dw", dt, dev, (M, K))
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_linear_backward, dev, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, code, pp, ldp, LINEAR_ACT[act], pdx, lddx, pdw, lddw,
+             _op_flat(dbias, "dbias", M, dev), ws, ws_bytes)
 
 
 def decay_attn_workspace_bytes(T: int, N: int, heads: int, dk: int, dv: int, *, backward: bool = False) -> int:
@@ -571,15 +594,16 @@ def decay_attn_workspace_bytes(T: int, N: int, heads: int, dk: int, dv: int, *, 
     return int(load().dgc_decay_attn_workspace_bytes(int(T), int(N), int(heads), int(dk), int(dv), int(backward)))
 
 
-def _op_seq(t, name: str, like, T: int, N: int, F: int):
+def _op_seq(t, name: str, dtype, dev: int, T: int, N: int, F: int):
     """(address, stride of t, stride of i) of rows (t, i) in a [T, N, F] tensor or view."""
     if t is None:
         return None, 0, 0
-    if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
+    if t.dtype is not dtype or t.get_device() != dev:
         raise ValueError(f"{name} must be a device tensor of the first tensor's element type and device")
-    if tuple(t.shape) != (T, N, F) or t.stride(2) != 1:
+    st = t.stride()
+    if tuple(t.shape) != (T, N, F) or st[2] != 1:
         raise ValueError(f"{name} must be [{T}, {N}, {F}] with a contiguous last dimension")
-    return t.data_ptr(), (t.stride(0) if T > 1 else 0), (t.stride(1) if N > 1 else 0)
+    return t.data_ptr(), (st[0] if T > 1 else 0), (st[1] if N > 1 else 0)
 
 
 def _decay_sizes(q, v, heads: int):
@@ -595,16 +619,15 @@ def decay_attn_forward(q, k, v, decay, o, *, heads: int, scale: float = 1.0, s0=
     fine); decay fp32 [heads], each in [0, 1]; s0, sn fp32 [N, heads, dk, dv] or None (sn may be s0); lengths int32 [N]: tokens
     of each sequence, rows behind them are not written; reset uint8 [T, N]: a non-zero byte drops the state entering (t, i).
     workspace: decay_attn_workspace_bytes device bytes, None where that is 0.  T = 1 is the form for one new snapshot."""
-    import torch
-    lib = load()
-    dt = _op_dtype(q, "q")
+    lib, code, dev = _op_first(q, "q")
+    dt = q.dtype
     T, N, dk, dv = _decay_sizes(q, v, heads)
     n_state = N * heads * dk * dv
-    ws, ws_bytes = _op_workspace(workspace, q)
-    _op_call(lib.dgc_decay_attn_forward, q, stream, *_op_seq(q, "q", q, T, N, heads * dk), *_op_seq(k, "k", q, T, N, heads * dk),
-             *_op_seq(v, "v", q, T, N, heads * dv), T, N, heads, dk, dv, dt, _op_flat(decay, "decay", heads, q), float(scale),
-             _op_flat(s0, "s0", n_state, q), _op_flat(lengths, "lengths", N, q, torch.int32), _op_flat(reset, "reset", T * N, q, torch.uint8),
-             *_op_seq(o, "o", q, T, N, heads * dv), _op_flat(sn, "sn", n_state, q), ws, ws_bytes)
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_decay_attn_forward, dev, stream, *_op_seq(q, "q", dt, dev, T, N, heads * dk), *_op_seq(k, "k", dt, dev, T, N, heads * dk),
+             *_op_seq(v, "v", dt, dev, T, N, heads * dv), T, N, heads, dk, dv, code, _op_flat(decay, "decay", heads, dev), float(scale),
+             _op_flat(s0, "s0", n_state, dev), _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_flat(reset, "reset", T * N, dev, _torch.uint8),
+             *_op_seq(o, "o", dt, dev, T, N, heads * dv), _op_flat(sn, "sn", n_state, dev), ws, ws_bytes)
     return o
 
 
@@ -612,15 +635,14 @@ def decay_attn_backward(q, k, v, decay, do, dq, dk, dv, *, heads: int, scale: fl
                         reset=None, workspace=None, stream=None):
     """dgc_decay_attn_backward: the gradients of decay_attn_forward's q, k, v (each may be None: not wanted) and s0 (ds0) from
     do and the last state's gradient dsn (None: zero); ds0 may be dsn.  decay is a constant."""
-    import torch
-    lib = load()
-    dt = _op_dtype(q, "q")
+    lib, code, dev = _op_first(q, "q")
+    dt = q.dtype
     T, N, nk, nv = _decay_sizes(q, v, heads)
     n_state = N * heads * nk * nv
-    ws, ws_bytes = _op_workspace(workspace, q)
-    _op_call(lib.dgc_decay_attn_backward, q, stream, *_op_seq(q, "q", q, T, N, heads * nk), *_op_seq(k, "k", q, T, N, heads * nk),
-             *_op_seq(v, "v", q, T, N, heads * nv), *_op_seq(do, "do", q, T, N, heads * nv), T, N, heads, nk, nv, dt,
-             _op_flat(decay, "decay", heads, q), float(scale), _op_flat(s0, "s0", n_state, q), _op_flat(dsn, "dsn", n_state, q),
-             _op_flat(lengths, "lengths", N, q, torch.int32), _op_flat(reset, "reset", T * N, q, torch.uint8),
-             *_op_seq(dq, "dq", q, T, N, heads * nk), *_op_seq(dk, "dk", q, T, N, heads * nk), *_op_seq(dv, "dv", q, T, N, heads * nv),
-             _op_flat(ds0, "ds0", n_state, q), ws, ws_bytes)
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_decay_attn_backward, dev, stream, *_op_seq(q, "q", dt, dev, T, N, heads * nk), *_op_seq(k, "k", dt, dev, T, N, heads * nk),
+             *_op_seq(v, "v", dt, dev, T, N, heads * nv), *_op_seq(do, "do", dt, dev, T, N, heads * nv), T, N, heads, nk, nv, code,
+             _op_flat(decay, "decay", heads, dev), float(scale), _op_flat(s0, "s0", n_state, dev), _op_flat(dsn, "dsn", n_state, dev),
+             _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_flat(reset, "reset", T * N, dev, _torch.uint8),
+             *_op_seq(dq, "dq", dt, dev, T, N, heads * nk), *_op_seq(dk, "dk", dt, dev, T, N, heads * nk), *_op_seq(dv, "dv", dt, dev, T, N, heads * nv),
+             _op_flat(ds0, "ds0", n_state, dev), ws, ws_bytes)

@@ -71,6 +71,10 @@ def test_binding_refusals():
         binding._op_rows(torch.zeros(32, 4).t(), "x")
     with pytest.raises(ValueError, match="one pitch"):
         binding._op_rows(torch.zeros(4, 5, 8)[:, :3], "x")
+    for t, pitch in ((torch.zeros(6, 8)[:, :5], 8), (torch.zeros(2, 3, 16)[..., :5], 16), (torch.zeros(4, 1, 3, 8), 8), (torch.zeros(5, 8)[::2], 16), (torch.zeros(1, 7, 24), 24),
+                     (torch.zeros(5, 1, 16)[:, :, :3], 16), (torch.zeros(3, 4, 8)[:, :1], 32)):
+        assert binding._op_rows(t, "x") == (t.data_ptr(), pitch)
+    assert binding._op_rows(torch.zeros(1, 5), "x")[1] == 8 and binding._op_rows(torch.zeros(1, 1, 3), "x")[1] == 8
 
 
 def test_linear_refusals(lib):
