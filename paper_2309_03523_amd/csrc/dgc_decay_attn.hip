@@ -379,10 +379,15 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
       const int last = resets ? 31 - __clz(resets) : 0;
       const float keep = resets ? 0.f : pw[m - (fresh ? 1 : 0)];
       float w[16];
+      if (m == kTok && !resets) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = 8 * (r >> 2) + 4 * half + (r & 3);
-        w[r] = j < m && j >= last ? a.beta * pw[max(m - 1 - j, 0)] : 0.f;
+        for (int r = 0; r < 16; ++r) w[r] = a.beta * pw[kTok - 1 - (8 * (r >> 2) + 4 * half + (r & 3))];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 8 * (r >> 2) + 4 * half + (r & 3);
+          w[r] = j < m && j >= last ? a.beta * pw[max(m - 1 - j, 0)] : 0.f;
+        }
       }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
@@ -398,7 +403,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
           }
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[t][r] = holds && !resets ? fmaf(keep, S[t][r], U[r]) : U[r];
+        for (int r = 0; r < 16; ++r) S[t][r] = fmaf(resets ? 0.f : S[t][r], keep, U[r]);   // what a reset drops may be infinite
       }
       holds = true;
     }
@@ -881,12 +886,23 @@ __global__ __launch_bounds__(256) void k_decay_scan(ScanArgs a) {
     const int64_t ih = e / a.size;
     const float g = a.decay[ih % a.heads];
     float s = a.s_in ? a.s_in[e] : 0.f;
-    for (int seg = 0; seg < a.segs; ++seg) {
-      const float f = a.factor[seg * seqs + ih], own = a.states[seg * all + e];
-      a.states[seg * all + e] = s;
-      // a power that is zero only in fp32 leaves an infinity what it is
-      if (f == 0.f && g != 0.f) s = fabsf(s) <= 3.4028235e38f ? own : s + own;
-      else s = f < 0.f ? own : fmaf(f, s, own);
+    for (int base = 0; base < a.segs; base += 8) {       // eight on their way at a time
+      float own[8], f[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool in = base + k < a.segs;
+        f[k] = in ? a.factor[(base + k) * seqs + ih] : 1.f;
+        own[k] = in ? a.states[(base + k) * all + e] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (base + k < a.segs) {
+          a.states[(base + k) * all + e] = s;
+          // a power that is zero only in fp32 leaves an infinity what it is
+          if (f[k] == 0.f && g != 0.f) s = fabsf(s) <= 3.4028235e38f ? own[k] : s + own[k];
+          else s = f[k] < 0.f ? own[k] : fmaf(f[k], s, own[k]);
+        }
+      }
     }
     if (a.s_out) {
       const int64_t i = ih / a.heads;

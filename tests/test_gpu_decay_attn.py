@@ -318,6 +318,27 @@ def test_values_that_are_not_finite_reach_what_the_formula_lets_them(T, dtype):
         assert bool((x[fine].double() - w[fine]).abs().max() <= (0.02 if dtype == "bf16" else 1e-3) * w[fine].abs().max())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [70, 600])
+def test_a_reset_drops_a_state_that_is_not_finite(T, dtype):
+    """An infinity before a reset that falls on the first of 32 tokens, where no token sees the old state."""
+    import torch
+    c = _case(T, 2, 2, 32, 32, dtype, 77)
+    c["reset"] = torch.zeros(T, 2, dtype=torch.uint8, device="cuda")
+    c["reset"][32] = 1
+    c["v"][3, 0, 0], c["s0"][1, 0, 5, 6] = float("inf"), float("nan")
+    (o, sn), (mo, ms) = _ref(c)
+    got, state = _run_forward(c)
+    assert torch.isfinite(o[32:]).all() and torch.isfinite(sn).all()
+    _close(got[32:], o[32:], mo[32:].nan_to_num(), dtype, T)
+    _close(state, sn, ms.nan_to_num(), dtype, T, state=True)
+    assert torch.equal(torch.isfinite(got[:32]), torch.isfinite(o[:32]))
+    c["do"][40, 1, 3] = float("inf")        # the gradients go the other way: nothing before the reset sees it
+    want, _ = _ref(c, back=True)
+    for x, w in zip(_run_backward(c), want[2:]):
+        assert torch.equal(torch.isfinite(x), torch.isfinite(w))
+
+
 def test_repeated_rows_and_empty_calls():
     """An input expanded over the sequences (stride 0); no tokens; no sequences."""
     import torch
