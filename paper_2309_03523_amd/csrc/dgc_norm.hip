@@ -261,8 +261,10 @@ Shape shape_of(int32_t F, int per) {
   while (lpr < vecs && lpr < 64) lpr *= 2;
   if (vecs <= 64) return {lpr, 1, 4};
   if (vecs <= 128) return {64, 2, 2};
+  if (vecs <= 192) return {64, 3, 1};
   if (vecs <= 256) return {64, 4, 1};
   if (vecs <= 512) return {256, 2, 1};
+  if (vecs <= 768) return {256, 3, 1};
   if (vecs <= 1024) return {256, 4, 1};
   return {256, 8, 1};
 }
@@ -271,7 +273,10 @@ Shape shape_of(int32_t F, int per) {
 int64_t sum_blocks(int64_t R, int32_t F, int per) {
   const Shape s = shape_of(F, per);
   const int64_t rows = (int64_t)(256 / s.lpr) * s.u, turns = (R + rows - 1) / rows;
-  return std::max(std::min<int64_t>(turns, kSumBlocks), (turns * s.u + kMostSums - 1) / kMostSums);
+  // Of wide rows, fewer: their partial rows are traffic (868 rows of 6417 fp32: 78 us with as many as 1024, 41 with 256), but two vectors a
+  // lane leave registers for more waves (30 000 rows of 4096 bf16: 241 us with 512, 393 with 256).
+  const int64_t fill = s.lpr < 256 ? kSumBlocks : s.nv == 2 ? kSumBlocks / 2 : kSumBlocks / 4;
+  return std::max(std::min<int64_t>(turns, fill), (turns * s.u + kMostSums - 1) / kMostSums);
 }
 
 template <class T, bool BACK>
@@ -289,8 +294,10 @@ void launch(const NormArgs& a, int64_t blocks, hipStream_t st) {
   DGC_NORM(32, 1, 4);
   DGC_NORM(64, 1, 4);
   DGC_NORM(64, 2, 2);
+  DGC_NORM(64, 3, 1);
   DGC_NORM(64, 4, 1);
   DGC_NORM(256, 2, 1);
+  DGC_NORM(256, 3, 1);
   DGC_NORM(256, 4, 1);
   if constexpr (Elem<T>::kPer == 4) DGC_NORM(256, 8, 1);
 #undef DGC_NORM
