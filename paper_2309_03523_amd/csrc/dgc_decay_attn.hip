@@ -176,12 +176,42 @@ __device__ __forceinline__ void powers_of(float g, float* pw, int lane) {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// 32 columns of the wave's 32 rows go out through LDS (`room`: 32 rows of kRoom units): a row's lanes then store it side by side, 16 bytes
+// each, where the registers as they are would leave 16-byte pieces of 32 rows with each instruction, four times as many requests.
+// base: the rows' first column; n0, n1: tokens of the first and, with PAIR, the second sequence.  Returns whether all were finite.
+template <class T> constexpr int kRoom = 2 * (int)sizeof(T) + 1;
+template <class T, bool PAIR>
+__device__ __forceinline__ bool store_rows(T* base, int64_t st, int64_t sn, const floatx16& x, int width, int n0, int n1, bool wanted, uint4* room) {
+  constexpr int PER = Elem<T>::kPer, UNITS = 32 / PER;
+  const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
+  float bad = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) bad = fmaf(x[r], 0.f, bad);
+  T* mine = reinterpret_cast<T*>(room + tok * kRoom<T>) + 4 * half;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float y[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    store4(mine + 8 * q, y);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int u = lane % UNITS;
+#pragma unroll
+  for (int i = 0; i < 32 * UNITS / 64; ++i) {
+    const int row = i * (64 / UNITS) + lane / UNITS, pos = PAIR ? row & 15 : row, slot = PAIR ? row >> 4 : 0;
+    const uint4 v = room[row * kRoom<T> + u];
+    if (wanted && u * PER < width && pos < (slot ? n1 : n0)) *reinterpret_cast<uint4*>(base + slot * sn + pos * st + u * PER) = v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return !__any(bad != 0.f);
+}
+
 // KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
 // A wave goes over (unit, 32 tokens) in turn and has the next ones' rows on the way while it works.
 template <class T, int KD, bool OUT>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void k_decay(DecayArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid;
   __shared__ float pw_lds[4][kTok + 4];
+  __shared__ uint4 room_lds[OUT ? 4 : 1][32 * kRoom<T>];
   const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float* pw = pw_lds[wave];
@@ -260,7 +290,6 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
     }
     const int64_t p0 = it.p0, n = it.n;
     const int m = (int)min((int64_t)kTok, it.p_hi - p0);      // may be none
-    const bool on = tok < m;
     const bool fresh = a.reversed && p0 == 0;     // the state that comes in is that of the first token, not of one before
     const bool unit_ends = p0 + kTok >= it.p_hi;
     const bool step = !OUT || a.s_out || !unit_ends;          // whether the state is wanted after these tokens
@@ -329,18 +358,8 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
       const float f = a.gam * (fresh ? fade0 : fade1);
       const bool sees = holds && !before;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        P[r] = fmaf(a.alpha, intra[r], sees ? f * inter[r] : 0.f);
-        bad = fmaf(P[r], 0.f, bad);
-      }
-      if (on) {
-        T* out = static_cast<T*>(const_cast<void*>(a.O.p)) + (from(a.O, a.dv, it) - static_cast<const T*>(a.O.p)) + way * tok * a.O.st + dv0 + 4 * half;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float x[4] = {P[4 * q], P[4 * q + 1], P[4 * q + 2], P[4 * q + 3]};
-          if (dv0 + 8 * q + 4 * half < a.dv) store4(out + 8 * q, x);
-        }
-      }
+      for (int r = 0; r < 16; ++r) P[r] = fmaf(a.alpha, intra[r], sees ? f * inter[r] : 0.f);
+      bad = store_rows<T, false>(const_cast<T*>(from(a.O, a.dv, it)) + dv0, way * a.O.st, 0, P, a.dv - dv0, m, 0, true, room_lds[wave]) ? 0.f : 1.f;
     } else {
       not_finite(bad, Cc);
 #pragma unroll
@@ -477,28 +496,13 @@ __device__ void walk_window(const Walk<T>& w, float* acc) {
   }
 }
 
-template <class T>
-__device__ __forceinline__ bool store_rows(T* out, const floatx16& x, int width, int half, bool on) {   // whether all were finite
-  float bad = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) bad = fmaf(x[r], 0.f, bad);
-  if (on) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float y[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-      if (8 * q + 4 * half < width) store4(out + 8 * q + 4 * half, y);
-    }
-  }
-  return !__any(bad != 0.f);
-}
-
 // The forward pass of windows of up to 32 tokens from zero states, the states not wanted: nothing is carried.  Two sequences
 // of up to 16 tokens share the 32 of a wave (PAIR).
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 64 ? 2 : 1)) void k_decay_window(DecayArgs a) {
   constexpr int KC = KD / 16, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
   __shared__ float pw_lds[4][kTok + 4];
-  __shared__ float walk_lds[4][32 * 64];
+  __shared__ __align__(16) float walk_lds[4][32 * 64];
   const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int slot = PAIR ? tok >> 4 : 0, pos = PAIR ? tok & 15 : tok;
@@ -512,7 +516,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 6
   // they fetch in step, and each line comes into the L1 cache once (100 000 windows of 16, 8 heads of 16: 451 us apart, 410 in step).
   const bool together = (across & 3) == 0;
   const int64_t offA = slot * a.A.sn + pos * a.A.st + 8 * half, offB = slot * a.B.sn + pos * a.B.st + 8 * half;
-  const int64_t offC = slot * a.C.sn + pos * a.C.st + 8 * half, offO = slot * a.O.sn + pos * a.O.st;
+  const int64_t offC = slot * a.C.sn + pos * a.C.st + 8 * half;
   const float g = a.decay[h];
   powers_of(g, pw, lane);
   float near[16];
@@ -546,7 +550,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 6
   n_next = row + 1 < row_end ? tokens(row + 1) : 0;
   while (true) {
     const int64_t i0 = (int64_t)row * PER;
-    const bool on = pos < n;
     const uint32_t resets = a.reset ? (uint32_t)__ballot(flag) : 0;
     floatx16 P = {}, Cc = {}, out = {};
 #pragma unroll
@@ -590,10 +593,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 6
     for (int r = 0; r < 16; ++r) out[r] *= a.alpha;
     T* O = static_cast<T*>(const_cast<void*>(a.O.p));
     const int64_t at = i0 * a.O.sn + (int64_t)h * a.dv;
-    if (__builtin_expect(!store_rows(O + at + offO + dv0, out, a.dv - dv0, half, on), 0)) {
+    const int n0 = __builtin_amdgcn_readfirstlane(n_this), n1 = PAIR ? __builtin_amdgcn_readlane(n_this, 16) : 0;
+    if (__builtin_expect(!store_rows<T, PAIR>(O + at + dv0, a.O.st, a.O.sn, out, a.dv - dv0, n0, n1, true, reinterpret_cast<uint4*>(walk_lds[wave])), 0)) {
       for (int q = 0; q < PER; ++q) {
         const int64_t i = i0 + q;
-        const int live = __builtin_amdgcn_readlane(n_this, 16 * q);
+        const int live = q ? n1 : n0;
         const T *A = static_cast<const T*>(a.A.p), *B = static_cast<const T*>(a.B.p), *C = static_cast<const T*>(a.C.p);
         const Walk<T> w{A + i * a.A.sn + h * a.dk, B + i * a.B.sn + h * a.dk, C + i * a.C.sn + h * a.dv + dv0, O + i * a.O.sn + h * a.dv + dv0,
                         a.A.st, a.B.st, a.C.st, a.O.st, live, a.dk, min(32, a.dv - dv0), false, g, a.beta, a.gam,
@@ -625,7 +629,8 @@ template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void k_decay_window_back(BackArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
   __shared__ float pw_lds[4][kTok + 4];
-  __shared__ float walk_lds[4][32 * 64];
+  __shared__ __align__(16) float walk_lds[4][32 * 64];
+  __shared__ uint4 room_lds[4][32 * kRoom<T>];
   const int lane = threadIdx.x & 63, half = lane >> 5, tok = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int slot = PAIR ? tok >> 4 : 0, pos = PAIR ? tok & 15 : tok;
@@ -637,7 +642,15 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
   if (row >= rows) return;
   const float g = a.decay[h];
   powers_of(g, pw, lane);
-  const bool together = (a.heads & 3) == 0;      // as above
+  // [32 rows][8 units] each; what the walk sums in takes the same place
+  uint4 *s0_lds = reinterpret_cast<uint4*>(walk_lds[wave]), *dsn_lds = s0_lds + 256;
+  const int state_units = a.dk * a.dv / 4;
+  int unit_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = 64 * i + lane, r = n / (a.dv / 4), u = n % (a.dv / 4);
+    unit_at[i] = r * 8 + (u ^ (r & 7));
+  }
   auto tokens = [&](uint32_t row) {
     const int64_t i = (int64_t)row * PER + slot;
     if (i >= a.N) return 0;
@@ -663,15 +676,50 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     flag = a.reset && on && half == 0 && a.reset[pos * a.N + (int64_t)row * PER + slot] != 0;
   };
 
+  if constexpr (!PAIR && KT == 1) {       // what lies behind a narrower state stays zero
+    for (int i = lane; i < 512; i += 64) s0_lds[i] = make_uint4(0, 0, 0, 0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
   int n = tokens(row), n_next = row + 1 < row_end ? tokens(row + 1) : 0;
   fetch(row, n);
   while (true) {
-    const uint32_t this_row = row;
     const int64_t i0 = (int64_t)row * PER, state = (i0 * a.heads + h) * a.dk * a.dv;
-    const bool on = pos < n;
     const uint32_t resets = a.reset ? (uint32_t)__ballot(flag) : 0;
     const uint32_t own = PAIR ? 0xffffu << (16 * slot) : ~0u;
     const uint32_t before = resets & ((2u << tok) - 1u) & own, after = resets & ~((2u << tok) - 1u) & own;
+    const float *s0 = a.s0 + state, *dsn = a.dsn + state;
+    // eight numbers of a state for the lane's output column: along row r of it, or down column c
+    auto along = [&](const float* s, int r, int c, float (&x)[8]) {
+      const bool in = s && r < a.dk && c < a.dv;
+      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f), *at = reinterpret_cast<const float4*>(s + r * a.dv + c);
+      const float4 lo = in ? at[0] : none, hi = in ? at[1] : none;
+      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+    };
+    auto down = [&](const float* s, int r, int c, float (&x)[8]) {
+      const bool in = s && r < a.dk && c < a.dv;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = in ? s[(r + e) * a.dv + c] : 0.f;
+    };
+    // States of up to 32 x 32 go through LDS, on their way there while the first scores are worked out: their rows and columns are then
+    // at hand for all that reads them.  A 16-byte unit's place in its row is turned by the row, so that neither way meets in a bank.
+    constexpr bool STAGED = !PAIR && KT == 1;
+    Raw8<uint16_t> s0_raw[4], dsn_raw[4];
+    if constexpr (STAGED) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = 64 * i + lane < state_units;
+        s0_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(s0 + 4 * (64 * i + lane)), a.s0 && in);
+        dsn_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(dsn + 4 * (64 * i + lane)), a.dsn && in);
+      }
+    }
+    auto staged_row = [&](const uint4* s, int r, int c, float (&x)[8]) {
+      Elem<float>::unpack(s[r * 8 + (c / 4 ^ (r & 7))], x);
+      Elem<float>::unpack(s[r * 8 + ((c / 4 + 1) ^ (r & 7))], x + 4);
+    };
+    auto staged_col = [&](const uint4* s, int r, int c, float (&x)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = reinterpret_cast<const float*>(s)[((r + e) * 8 + (c / 4 ^ ((r + e) & 7))) * 4 + (c & 3)];
+    };
     uint4 fq[KC][IN], fk[KC][IN], fv[KC][IN], fd[KC][IN];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
@@ -681,52 +729,37 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
       operand(rawd[k], fd[k]);
     }
     const int n_this = n;
-    if (together) __builtin_amdgcn_s_barrier();
     if (++row < row_end) {
       fetch(row, n_next);
       n = n_next;
       n_next = row + 1 < row_end ? tokens(row + 1) : 0;
     }
-    // scores: do . v of the lane's token as the one that reads (dq) and as the one that is read (dk), q . k as the latter (dv)
-    uint4 sdq[2][MID], sdk[2][MID], sdv[2][MID];
-    {
-      floatx16 x = {}, y = {}, z = {};
+    // the lane's token as the one that reads (the others before it) or that is read (from it on), with what lies between
+    auto scores = [&](const uint4 (&f)[KC][IN], const uint4 (&own)[KC][IN], bool ahead, uint4 (&score)[2][MID]) {
+      floatx16 x = {};
 #pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        mul(x, fv[k], fd[k]);
-        mul(y, fd[k], fv[k]);
-        mul(z, fq[k], fk[k]);
-      }
+      for (int k = 0; k < KC; ++k) mul(x, f[k], own[k]);
       float w[16];
-      decays<PAIR>(pw, tok, half, false, w);
+      decays<PAIR>(pw, tok, half, ahead, w);
       const int since = before ? 31 - __clz(before) : 0, until = after ? __ffs(after) - 1 : 32;
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] *= w[r];
-      decays<PAIR>(pw, tok, half, true, w);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) { y[r] *= w[r]; z[r] *= w[r]; }
       if (resets) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int o = 8 * (r >> 2) + 4 * half + (r & 3);
-          x[r] = o >= since ? x[r] : 0.f;
-          y[r] = o < until ? y[r] : 0.f;
-          z[r] = o < until ? z[r] : 0.f;
+          x[r] = (ahead ? o < until : o >= since) ? x[r] : 0.f;
         }
       }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        half_parts(x, k, sdq[k]);
-        half_parts(y, k, sdk[k]);
-        half_parts(z, k, sdv[k]);
-      }
-    }
+      for (int k = 0; k < 2; ++k) half_parts(x, k, score[k]);
+    };
     // a tensor's 32 columns with its tokens as the contraction
-    auto columns = [&](const uint4 (&f)[KC][IN], int t, floatx16& x) {
+    auto columns = [&](const uint4 (&f)[KC][IN], int t, floatx16& x, int order) {
       x = floatx16{};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if (2 * t + k < KC) mul(x, f[2 * t + k < KC ? 2 * t + k : 0], {identity(k, half, tok)});
+        if (2 * t + k < KC) mul(x, f[2 * t + k < KC ? 2 * t + k : 0], {identity(k, half, order)});
       }
     };
     auto sums = [&](const floatx16& x, const uint4 (&score)[2][MID], floatx16& out) {
@@ -738,82 +771,120 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         mul(out, f, score[k]);
       }
     };
-    // eight numbers of a state with the lane's column: along a row of it (r: the row), or down a column
-    auto state_part = [&](const float* s, int r, int c, bool down, uint4 (&f)[MID]) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      if (r < a.dk && c < a.dv) {
-        if (down) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = s[(int64_t)(r + e) * a.dv + c];
-        } else {
-          const float4 lo = *reinterpret_cast<const float4*>(s + r * a.dv + c), hi = *reinterpret_cast<const float4*>(s + r * a.dv + c + 4);
-          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
-        }
-      }
-      parts_of(x, f);
-    };
-    const int n0 = PAIR ? 0 : __builtin_amdgcn_readfirstlane(n_this);
+    const int live0 = __builtin_amdgcn_readfirstlane(n_this), live1 = PAIR ? __builtin_amdgcn_readlane(n_this, 16) : 0;
+    const int n0 = PAIR ? 0 : live0;
     const int last = resets ? 31 - __clz(resets) : 0;
     const float fade = before ? 0.f : a.scale * pw[tok + 1];                                        // of S0 in the lane's token
     const float keep = !PAIR && tok < n0 && tok >= last ? pw[max(n0 - 1 - tok, 0)] : 0.f;           // of the token in the last state
-    const float *s0 = a.s0 + state, *dsn = a.dsn + state;
     bool fine = true;
     auto leave = [&](const Rows& out, int width, int t, const floatx16& sum, const floatx16& far, float weight) {
       floatx16 x;
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = a.scale * sum[r] + (!PAIR && weight != 0.f ? weight * far[r] : 0.f);
-      fine &= store_rows(const_cast<T*>(place(out, width, this_row)) + 32 * t, x, width - 32 * t, half, on && out.p);
+      T* base = static_cast<T*>(const_cast<void*>(out.p)) + i0 * out.sn + (int64_t)h * width + 32 * t;
+      fine &= store_rows<T, PAIR>(base, out.st, out.sn, x, width - 32 * t, live0, live1, out.p != nullptr, room_lds[wave]);
     };
+    {   // dq
+      uint4 score[2][MID];
+      scores(fv, fd, false, score);
+      if constexpr (STAGED) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      if (32 * t >= a.dk) break;
-      floatx16 x, out, far = {};
-      columns(fk, t, x);
-      sums(x, sdq, out);
-      if (!PAIR && a.s0) {
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          uint4 f[MID];
-          state_part(s0, 32 * t + tok, 16 * k + 8 * half, false, f);
-          mul(far, f, fd[k]);
+        for (int i = 0; i < 4; ++i) {
+          if (64 * i + lane < state_units) {
+            s0_lds[unit_at[i]] = s0_raw[i].w[0];
+            dsn_lds[unit_at[i]] = dsn_raw[i].w[0];
+          }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
-      leave(a.dq, a.dk, t, out, far, a.s0 ? fade : 0.f);
-      columns(fq, t, x);
-      sums(x, sdk, out);
-      far = floatx16{};
-      if (!PAIR && a.dsn) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          uint4 f[MID];
-          state_part(dsn, 32 * t + tok, 16 * k + 8 * half, false, f);
-          mul(far, f, fv[k]);
+      for (int t = 0; t < KT; ++t) {
+        if (32 * t >= a.dk) break;
+        floatx16 x, out, far = {};
+        columns(fk, t, x, tok);
+        sums(x, score, out);
+        if (!PAIR && a.s0) {
+#pragma unroll
+          for (int k = 0; k < KC; ++k) {
+            uint4 f[MID];
+            if constexpr (STAGED) {
+              float y[8];
+              staged_row(s0_lds, tok, 16 * k + 8 * half, y);
+              parts_of(y, f);
+            } else {
+              float y[8];
+              along(s0, 32 * t + tok, 16 * k + 8 * half, y);
+              parts_of(y, f);
+            }
+            mul(far, f, fd[k]);
+          }
         }
+        leave(a.dq, a.dk, t, out, far, a.s0 ? fade : 0.f);
       }
-      leave(a.dkey, a.dk, t, out, far, a.dsn ? keep : 0.f);
     }
+    __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
+    {   // dk
+      uint4 score[2][MID];
+      scores(fd, fv, true, score);
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      if (32 * t >= a.dv) break;
-      floatx16 x, out, far = {};
-      columns(fd, t, x);
-      sums(x, sdv, out);
-      if (!PAIR && a.dsn) {
+      for (int t = 0; t < KT; ++t) {
+        if (32 * t >= a.dk) break;
+        floatx16 x, out, far = {};
+        columns(fq, t, x, tok);
+        sums(x, score, out);
+        if (!PAIR && a.dsn) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          uint4 f[MID];
-          state_part(dsn, 16 * k + 8 * half, 32 * t + tok, true, f);
-          mul(far, f, fk[k]);
+          for (int k = 0; k < KC; ++k) {
+            uint4 f[MID];
+            if constexpr (STAGED) {
+              float y[8];
+              staged_row(dsn_lds, tok, 16 * k + 8 * half, y);
+              parts_of(y, f);
+            } else {
+              float y[8];
+              along(dsn, 32 * t + tok, 16 * k + 8 * half, y);
+              parts_of(y, f);
+            }
+            mul(far, f, fv[k]);
+          }
         }
+        leave(a.dkey, a.dk, t, out, far, a.dsn ? keep : 0.f);
       }
-      leave(a.dval, a.dv, t, out, far, a.dsn ? keep : 0.f);
     }
+    __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
+    {   // dv
+      uint4 score[2][MID];
+      scores(fq, fk, true, score);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        if (32 * t >= a.dv) break;
+        floatx16 x, out, far = {};
+        columns(fd, t, x, tok);
+        sums(x, score, out);
+        if (!PAIR && a.dsn) {
+#pragma unroll
+          for (int k = 0; k < KC; ++k) {
+            uint4 f[MID];
+            if constexpr (STAGED) {
+              float y[8];
+              staged_col(dsn_lds, 16 * k + 8 * half, tok, y);
+              parts_of(y, f);
+            } else {
+              float y[8];
+              down(dsn, 16 * k + 8 * half, 32 * t + tok, y);
+              parts_of(y, f);
+            }
+            mul(far, f, fk[k]);
+          }
+        }
+        leave(a.dval, a.dv, t, out, far, a.dsn ? keep : 0.f);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
     if (__builtin_expect(!fine, 0)) {
       for (int q = 0; q < PER; ++q) {
         const int64_t i = i0 + q;
-        const int live = __builtin_amdgcn_readlane(n_this, 16 * q);
+        const int live = q ? live1 : live0;
         auto at = [&](const Rows& x, int width) { return x.p ? static_cast<T*>(const_cast<void*>(x.p)) + i * x.sn + (int64_t)h * width : nullptr; };
         const uint8_t* reset = a.reset ? a.reset + i : nullptr;
         const int m = a.dk, c = a.dv;
@@ -832,7 +903,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
       for (int t = 0; t < KT; ++t) {
         if (32 * t >= a.dv) break;
         floatx16 x;
-        columns(fd, t, x);
+        columns(fd, t, x, tok);
         uint4 fx[2][IN];
 #pragma unroll
         for (int k = 0; k < 2; ++k) half_parts(x, k, fx[k]);
@@ -840,7 +911,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         for (int u = 0; u < KT; ++u) {
           if (32 * u >= a.dk) break;
           floatx16 y, S = {};
-          columns(fq, u, y);
+          columns(fq, u, y, swap23(tok));     // dS0's rows in the order of `down`
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int o = 8 * (r >> 2) + 4 * half + (r & 3);
@@ -853,12 +924,16 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
             mul(S, f, fx[k]);
           }
           const int c = 32 * t + tok;
-          float* to = a.ds0 + state + (int64_t)(32 * u + 4 * half) * a.dv + c;
-          const float* from = dsn + (int64_t)(32 * u + 4 * half) * a.dv + c;
+          float* to = a.ds0 + state + (int64_t)(32 * u + 8 * half) * a.dv + c;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int row = 8 * (r >> 2) + (r & 3);
-            if (32 * u + row + 4 * half < a.dk && c < a.dv) to[row * a.dv] = a.dsn && !resets ? fmaf(pass, from[row * a.dv], S[r]) : S[r];
+          for (int k = 0; k < 2; ++k) {
+            float in[8];
+            if constexpr (STAGED) staged_col(dsn_lds, 16 * k + 8 * half, tok, in);
+            else down(a.dsn ? dsn : nullptr, 32 * u + 16 * k + 8 * half, c, in);
+            if (32 * u + 16 * k + 8 * half < a.dk && c < a.dv) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) to[(16 * k + e) * a.dv] = a.dsn && !resets ? fmaf(pass, in[e], S[8 * k + e]) : S[8 * k + e];
+            }
           }
         }
       }
