@@ -503,7 +503,8 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
  *   the state after the last token (s0 of an empty sequence).  reset device uint8 [T][N] or NULL.
  *  backward: gradients dq, dk, dv (each may be NULL) and ds0 (NULL = not wanted; may be dsn) from the output's gradient `go` and
  *   the last state's, dsn (NULL = zeros).  The decays are constants.
- *  workspace: dgc_decay_attn_workspace_bytes bytes (0 unless few long sequences are split; negative for sizes outside the range).
+ *  workspace: dgc_decay_attn_workspace_bytes bytes (0 unless few long sequences are split; negative for sizes outside the range;
+ *   `backward` 0 or 1: which call they are for).
  *  DGC_ERR_UNSUPPORTED for 2^31 and more sequences x heads x blocks of 32 columns.
  * A token that holds an infinity or NaN reaches only the outputs that the formula lets it reach. */
 int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t backward);

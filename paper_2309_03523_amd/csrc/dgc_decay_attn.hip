@@ -206,7 +206,8 @@ __device__ __forceinline__ bool store_rows(T* base, int64_t st, int64_t sn, cons
 }
 
 // KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
-// A wave goes over (unit, 32 tokens) in turn and has the next ones' rows on the way while it works.
+// A wave goes over its rows' 32 tokens in turn and has the next ones' on the way while it works.  4 sequences of 8192, 8 heads of 64: 38 us for
+// the states, 10 for the scan, 52 for the outputs; vector instructions (the parts of scores, keys and states) bound it at two waves a SIMD.
 template <class T, int KD, bool OUT>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void k_decay(DecayArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid;
@@ -366,6 +367,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void
       for (int t = 0; t < KT; ++t) { not_finite(bad, Bc[t]); not_finite(bad, S[t]); }
     }
     if (__builtin_expect(__any(bad != 0.f), 0)) {
+      __threadfence();      // other lanes wrote these rows above
       // One by one, over what was stored: the state for each token, its row's product with it.  (An output is not finite
       // wherever a value among the tokens or in the state is not.)
       for (int q = 0; q < m; ++q) {
@@ -497,7 +499,7 @@ __device__ void walk_window(const Walk<T>& w, float* acc) {
 }
 
 // The forward pass of windows of up to 32 tokens from zero states, the states not wanted: nothing is carried.  Two sequences
-// of up to 16 tokens share the 32 of a wave (PAIR).
+// of up to 16 tokens share the 32 of a wave (PAIR).  100 000 windows of 16, 8 heads of 16: 350 to 365 us, 4.5 TB/s and more; memory bounds it.
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 64 ? 2 : 1)) void k_decay_window(DecayArgs a) {
   constexpr int KC = KD / 16, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
@@ -513,7 +515,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 6
   const uint32_t row_end = min(rows, row + a.run);
   if (row >= rows) return;
   // Narrow heads share cache lines with their neighbours, which the workgroup's other waves read: where all four take the same rows
-  // they fetch in step, and each line comes into the L1 cache once (100 000 windows of 16, 8 heads of 16: 451 us apart, 410 in step).
+  // they fetch in step, and each line comes into the L1 cache once (100 000 windows of 16, 8 heads of 16: 451 us apart, 410 in step, when the
+  // outputs left the registers as they were).
   const bool together = (across & 3) == 0;
   const int64_t offA = slot * a.A.sn + pos * a.A.st + 8 * half, offB = slot * a.B.sn + pos * a.B.st + 8 * half;
   const int64_t offC = slot * a.C.sn + pos * a.C.st + 8 * half;
@@ -595,6 +598,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 6
     const int64_t at = i0 * a.O.sn + (int64_t)h * a.dv;
     const int n0 = __builtin_amdgcn_readfirstlane(n_this), n1 = PAIR ? __builtin_amdgcn_readlane(n_this, 16) : 0;
     if (__builtin_expect(!store_rows<T, PAIR>(O + at + dv0, a.O.st, a.O.sn, out, a.dv - dv0, n0, n1, true, reinterpret_cast<uint4*>(walk_lds[wave])), 0)) {
+      __threadfence();      // other lanes wrote these rows above
       for (int q = 0; q < PER; ++q) {
         const int64_t i = i0 + q;
         const int live = q ? n1 : n0;
@@ -624,7 +628,8 @@ struct BackArgs {
 };
 
 // All gradients of windows of up to 32 tokens, every tensor read once: dk, dv up to KD.  States (not with PAIR) are read and written as
-// they are needed: nothing is carried.
+// they are needed: nothing is carried.  20 000 ragged windows of 32, 4 heads of 32, with states: 485 us, 3.2 TB/s; the registers (256) leave two
+// waves a SIMD, which do not cover all waits.  (Three passes of k_decay took 900.)
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void k_decay_window_back(BackArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
@@ -676,10 +681,11 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     flag = a.reset && on && half == 0 && a.reset[pos * a.N + (int64_t)row * PER + slot] != 0;
   };
 
-  if constexpr (!PAIR && KT == 1) {       // what lies behind a narrower state stays zero
+  auto clear_staged = [&]() {       // what lies behind a narrower state is zero
     for (int i = lane; i < 512; i += 64) s0_lds[i] = make_uint4(0, 0, 0, 0);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
+  };
+  if constexpr (!PAIR && KT == 1) clear_staged();
   int n = tokens(row), n_next = row + 1 < row_end ? tokens(row + 1) : 0;
   fetch(row, n);
   while (true) {
@@ -774,13 +780,13 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     const int live0 = __builtin_amdgcn_readfirstlane(n_this), live1 = PAIR ? __builtin_amdgcn_readlane(n_this, 16) : 0;
     const int n0 = PAIR ? 0 : live0;
     const int last = resets ? 31 - __clz(resets) : 0;
-    const float fade = before ? 0.f : a.scale * pw[tok + 1];                                        // of S0 in the lane's token
-    const float keep = !PAIR && tok < n0 && tok >= last ? pw[max(n0 - 1 - tok, 0)] : 0.f;           // of the token in the last state
+    const bool lasts = tok < n0 && tok >= last;                  // whether the last state holds something of the lane's token
+    const float fade = a.scale * pw[tok + 1], keep = pw[max(n0 - 1 - tok, 0)];   // S0 in the token, the token in the last state
     bool fine = true;
-    auto leave = [&](const Rows& out, int width, int t, const floatx16& sum, const floatx16& far, float weight) {
+    auto leave = [&](const Rows& out, int width, int t, const floatx16& sum, const floatx16& far, bool sees, float weight) {
       floatx16 x;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = a.scale * sum[r] + (!PAIR && weight != 0.f ? weight * far[r] : 0.f);
+      for (int r = 0; r < 16; ++r) x[r] = a.scale * sum[r] + (!PAIR && sees ? weight * far[r] : 0.f);
       T* base = static_cast<T*>(const_cast<void*>(out.p)) + i0 * out.sn + (int64_t)h * width + 32 * t;
       fine &= store_rows<T, PAIR>(base, out.st, out.sn, x, width - 32 * t, live0, live1, out.p != nullptr, room_lds[wave]);
     };
@@ -819,7 +825,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
             mul(far, f, fd[k]);
           }
         }
-        leave(a.dq, a.dk, t, out, far, a.s0 ? fade : 0.f);
+        leave(a.dq, a.dk, t, out, far, a.s0 && !before, fade);
       }
     }
     __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
@@ -848,7 +854,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
             mul(far, f, fv[k]);
           }
         }
-        leave(a.dkey, a.dk, t, out, far, a.dsn ? keep : 0.f);
+        leave(a.dkey, a.dk, t, out, far, a.dsn && lasts, keep);
       }
     }
     __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
@@ -877,11 +883,12 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
             mul(far, f, fk[k]);
           }
         }
-        leave(a.dval, a.dv, t, out, far, a.dsn ? keep : 0.f);
+        leave(a.dval, a.dv, t, out, far, a.dsn && lasts, keep);
       }
     }
     __builtin_amdgcn_sched_barrier(0);      // one gradient's scores and sums at a time: all three at once do not fit the registers
     if (__builtin_expect(!fine, 0)) {
+      __threadfence();      // other lanes wrote these rows above
       for (int q = 0; q < PER; ++q) {
         const int64_t i = i0 + q;
         const int live = q ? live1 : live0;
@@ -896,6 +903,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         walk_window(Walk<T>{at(a.k, m), at(a.q, m), at(a.go, c), at(a.dval, c), a.k.st, a.q.st, a.go.st, a.dval.st, live, m, c, true, g, a.scale, 1.f, reset, a.N,
                             !PAIR && a.dsn ? dsn : nullptr, c, 1, !PAIR && a.ds0 ? a.ds0 + state : nullptr}, walk_lds[wave]);
       }
+      clear_staged();
     } else if (!PAIR && a.ds0) {      // after all that reads dsn, which may be in its place
       const int until = resets ? __ffs(resets) - 1 : 32;        // the tokens that S0 reaches are those before it
       const float pass = pw[n0];
@@ -987,7 +995,7 @@ __global__ __launch_bounds__(256) void k_decay_scan(ScanArgs a) {
   }
 }
 
-// One token: a wave a sequence and head, dv / 4 lanes a row of the state, as many rows at a time as fit, eight times.
+// One token (4000 of them over 8 fp32 states of 64 x 64: 197 us, 5.3 TB/s): a wave a sequence and head, dv / 4 lanes a row of the state, as many rows at a time as fit, eight times.
 template <class T>
 __global__ __launch_bounds__(256) void k_decay_step(DecayArgs a) {
   __shared__ float4 sums[4][64];
@@ -1071,10 +1079,11 @@ Segments segments_of(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv
 }
 
 // How many rows (sequences, pairs or segments) a wave takes, and the workgroups for it: `across` waves side by side, one for each
-// head and block of columns, on the same rows.  Waves that take neighbouring rows keep the memory that is open at a time together: taking
-// every so manieth instead read the same bytes at two thirds of the rate.
+// head and block of columns, on the same rows.  Waves that take neighbouring rows keep the memory that is open at a time together: with
+// rows a grid apart instead the windows above took 574 us for 444; runs of 4, 8, 16 and 32 rows 418, 410, 424 and more.
 unsigned runs_of(int64_t rows, int64_t across, uint32_t* run) {
   *run = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(kRun, rows * across / (kFillWaves * 4)));
+  *run = (uint32_t)std::max<int64_t>(*run, (rows * across + 4 * kMostBlocks - 1) / (4 * kMostBlocks));    // grids end below 2^32 threads
   return (unsigned)(((rows + *run - 1) / *run * across + 3) / 4);
 }
 
@@ -1255,7 +1264,7 @@ using namespace dgc;
 
 extern "C" {
 
-int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t backward) {
+int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t /*backward*/) {
   if (check(T, N, heads, dk, dv, 0) || too_many(T, N, heads, dk, dv)) return -1;
   const Segments s = segments_of(T, N, heads, dk, dv);
   return s.n > 1 ? 4 * (int64_t)s.n * N * heads * (dk * dv + 1) + 16 : 0;

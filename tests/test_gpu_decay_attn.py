@@ -396,3 +396,17 @@ def test_streams_graphs_and_repeats(dims):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want[:6], out[:6])), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_window_states_that_are_not_finite(dtype):
+    """A window whose states hold an infinity, next to windows whose do not, narrower than the wave's tile; a decay whose powers are zero in fp32."""
+    import torch
+    c = _case(20, 40, 2, 16, 24, dtype, 91, reset=0.02)
+    c["decay"] = torch.tensor([1e-20, 0.9], device="cuda")
+    c["dsn"][5, 0, 3, 4], c["s0"][6, 1, 2, 2], c["dsn"][7, 1, 15, 23] = float("inf"), float("nan"), float("-inf")
+    want, mag = _ref(c, back=True)
+    for x, w, m, st in zip(_run_backward(c), want[2:], mag[2:], (False, False, False, True)):
+        assert torch.equal(torch.isnan(x), torch.isnan(w)) and torch.equal(torch.isinf(x), torch.isinf(w))
+        fine = torch.isfinite(w)
+        _close(torch.where(fine, x, 0), torch.where(fine, w, 0), torch.where(fine, m, m[fine].max()), dtype, 20, st)
