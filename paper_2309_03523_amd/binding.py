@@ -422,11 +422,13 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
 
 _torch = None
 _raw_stream = None      # device index -> the current stream's handle
+_device = None          # () -> the current device's index
 
 
 def _op_init():
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _device
     import torch
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     _torch = torch
     return load()
@@ -508,7 +510,7 @@ def _op_call(fn, dev: int, stream, *args):
         if stream.device.index != dev:
             raise ValueError("stream belongs to another device than the tensors")
         handle = stream.cuda_stream
-    if _torch.cuda.current_device() == dev:
+    if _device() == dev:
         rc = fn(*args, handle)
     else:
         with _torch.cuda.device(dev):
