@@ -15,8 +15,9 @@
 //    so for fp32 those of 16 terms are added up by the vector unit, which rounds: errors as of an fp32 product, 2e-7.
 //  - dw is a sum over all rows with a small result: the rows are split over workgroups, each writes an fp32 partial, and a
 //    second kernel adds them in order.  No atomics: the same inputs give the same bits.
-//  - Up to 32 rows (a few vertices served at once) read every weight once and multiply little: a workgroup takes 32 output
-//    columns, its 8 waves a share of the contraction each, and fragments come straight from memory.
+//  - Up to 32 rows (a few vertices served at once) read every weight once and multiply little, and a few tiles with a long contraction
+//    would keep a few compute units for long: a workgroup takes 32 x 32 outputs, its 8 waves a share of the contraction each, and
+//    fragments come straight from memory.
 #include <algorithm>
 
 #include "dgc_ops.h"
@@ -32,6 +33,7 @@ using split::floatx16;
 
 constexpr int kMaxDim = 65536;      // K, M
 constexpr int kFewRows = 32;
+constexpr int64_t kFewLong = 256, kFewTiles = 64;   // contraction at least, tiles of 64 x 64 at most
 constexpr int64_t kNear = 1 << 23;        // pitches below it: a tile's rows are within 32 bits of each other
 constexpr int64_t kMostTiles = 1 << 20;   // workgroups of one launch; more tiles are taken in turns
 constexpr int64_t kRowTiles = 16;         // tiles of 32 rows that a wave takes in turn (8: 514 us, 16: 512, 4: 536 for 800 000 rows 128 -> 512)
@@ -128,6 +130,13 @@ __device__ __forceinline__ void take_unit(const char* p, uint4& u) { u = *reinte
 __device__ __forceinline__ void take_unit(const char* p, float (&x)[8]) {
   Elem<float>::unpack(reinterpret_cast<const uint4*>(p)[0], x);
   Elem<float>::unpack(reinterpret_cast<const uint4*>(p)[1], x + 4);
+}
+__device__ __forceinline__ void gather_unit(const uint16_t (&x)[8], uint4& u) {
+  u = make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+}
+__device__ __forceinline__ void gather_unit(const float (&x)[8], float (&u)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u[i] = x[i];
 }
 __device__ __forceinline__ void zero_unit(uint4& u) { u = make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ void zero_unit(float (&x)[8]) {
@@ -522,14 +531,14 @@ __global__ __launch_bounds__(256, KF <= 4 ? 4 : 3) void k_linear_rows(LinearArgs
   }
 }
 
-// Up to 32 rows of Q: 32 columns a workgroup, 8 waves that take 64 of the contraction at a time in turn.  8 rows 1024 -> 4096: 6 us, one round
-// of loads and the join; 8 MB of weights are 1.7 us.
-template <class T>
+// Few outputs, or few rows: 32 rows by 32 columns a workgroup, 8 waves that take 64 of the contraction at a time in turn.  8 rows 1024 -> 4096:
+// 6 us, one round of loads and the join; 8 MB of weights are 1.7 us.
+template <class T, bool ACROSS_P>
 __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
   __shared__ float joined[8][16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int64_t p0 = (int64_t)blockIdx.x * 32, p = p0 + (lane & 31), q = lane & 31;
-  const T* P = static_cast<const T*>(a.P) + p * a.ldp;
+  const int64_t p0 = (int64_t)blockIdx.x * 32, p = p0 + (lane & 31), q = (int64_t)blockIdx.y * 32 + (lane & 31);
+  const T* P = static_cast<const T*>(a.P) + (ACROSS_P ? p : p * a.ldp);
   const T* Q = static_cast<const T*>(a.Q) + q * a.ldq;
   floatx16 acc = floatx16{};
   for (int64_t c = wave * 64; c < a.C; c += 8 * 64) {
@@ -537,8 +546,15 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const int64_t k = c + 16 * s + 8 * half;
-      if (p < a.NP && k < a.C) load_unit(P, k, a.C, up[s]);
-      else zero_unit(up[s]);
+      if constexpr (ACROSS_P) {
+        T x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p < a.NP && k + e < a.C ? P[(k + e) * a.ldp] : T(0);
+        gather_unit(x, up[s]);
+      } else {
+        if (p < a.NP && k < a.C) load_unit(P, k, a.C, up[s]);
+        else zero_unit(up[s]);
+      }
       if (q < a.NQ && k < a.C) load_unit(Q, k, a.C, uq[s]);
       else zero_unit(uq[s]);
     }
@@ -547,15 +563,12 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
       for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(up[s]), as_frag(uq[s]), acc, 0, 0, 0);
     } else {
 #pragma unroll
-      for (int s = 0; s < 4; s += 2) {
+      for (int s = 0; s < 4; ++s) {
+        uint4 fp[3], fq[3];
+        split::split8(up[s], fp);
+        split::split8(uq[s], fq);
         floatx16 sum = floatx16{};
-#pragma unroll
-        for (int t = s; t < s + 2; ++t) {
-          uint4 fp[3], fq[3];
-          split::split8(up[t], fp);
-          split::split8(uq[t], fq);
-          split::six(sum, sum, fp, fq);
-        }
+        split::six(sum, sum, fp, fq);
         acc += sum;
       }
     }
@@ -700,6 +713,16 @@ bool small_tiles(int64_t NP, int64_t NQ) {
   return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < (sizeof(T) == 4 ? 1024 : 256);
 }
 
+// Up to 32 rows, or so few tiles with so long a contraction that it is better split over the waves of more workgroups: bf16 100 x 4000 -> 50
+// 12 us for 48 in tiles, 200 x 2000 -> 200 8 for 23; fp32 500 x 300 -> 500 8 for 16, 100 x 4000 -> 50 42 for 159.
+bool few_outputs(int64_t NP, int64_t NQ, int64_t C) {
+  return NQ <= kFewRows || (C >= kFewLong && ((NP + 63) / 64) * ((NQ + 63) / 64) <= kFewTiles);
+}
+template <class T, bool ACROSS_P>
+void launch_few(const LinearArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_linear_few<T, ACROSS_P>), dim3((unsigned)((a.NP + 31) / 32), (unsigned)((a.NQ + 31) / 32)), 512, 0, st, a);
+}
+
 template <class T, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
 void launch_tiles(const LinearArgs& a, bool small, hipStream_t st) {
   const int64_t b = small ? 64 : 128, tiles = ((a.NP + b - 1) / b) * ((a.NQ + b - 1) / b) * a.parts;
@@ -806,7 +829,8 @@ void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const vo
     LinearArgs a{};
     a.P = w; a.ldp = ldw; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
     a.out = dx; a.ldo = lddx;
-    launch_tiles<T, true, false, false>(a, small_tiles<T>(a.NP, a.NQ), st);
+    if (few_outputs(a.NP, a.NQ, a.C)) launch_few<T, true>(a, st);
+    else launch_tiles<T, true, false, false>(a, small_tiles<T>(a.NP, a.NQ), st);
   }
 }
 
@@ -848,10 +872,9 @@ dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64
   a.P = w; a.ldp = ldw; a.NP = M; a.Q = x; a.ldq = ldx; a.NQ = R; a.C = K; a.share = (K + 63) / 64 * 64; a.parts = 1; a.act = act;
   a.out = y; a.ldo = ldy; a.bias = bias; a.residual = residual; a.ldr = ldr; a.pre = pre; a.ldpre = ldpre;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (R <= kFewRows) {
-    const unsigned grid = (unsigned)((M + 31) / 32);
-    if (dtype == DGC_DTYPE_F32) hipLaunchKernelGGL(k_linear_few<float>, grid, 512, 0, st, a);
-    else hipLaunchKernelGGL(k_linear_few<uint16_t>, grid, 512, 0, st, a);
+  if (few_outputs(M, R, K)) {
+    if (dtype == DGC_DTYPE_F32) launch_few<float, false>(a, st);
+    else launch_few<uint16_t, false>(a, st);
   } else if (short_rows(a, dtype)) {
     launch_rows(a, st);
   } else if (dtype == DGC_DTYPE_F32) {

@@ -45,7 +45,8 @@ def _sum_tol(n):
 
 SHAPES = [(1, 1, 1), (1, 1024, 40), (8, 64, 96), (17, 513, 300), (32, 100, 33), (33, 100, 33), (64, 64, 64), (65, 63, 65),
           (200, 172, 128), (129, 129, 257), (1000, 40, 8), (300, 520, 520), (33000, 70, 130), (32900, 130, 129),
-          (33, 32, 64), (100, 96, 192), (4097, 128, 128), (50001, 64, 64)]
+          (33, 32, 64), (100, 96, 192), (4097, 128, 128), (50001, 64, 64),
+          (100, 600, 70), (70, 40, 600), (33, 260, 33), (1, 42, 1152)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
