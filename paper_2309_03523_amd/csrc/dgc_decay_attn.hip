@@ -628,7 +628,7 @@ struct BackArgs {
 };
 
 // All gradients of windows of up to 32 tokens, every tensor read once: dk, dv up to KD.  States (not with PAIR) are read and written as
-// they are needed: nothing is carried.  20 000 ragged windows of 32, 4 heads of 32, with states: 485 us, 3.2 TB/s; the registers (256) leave two
+// they are needed: nothing is carried.  20 000 ragged windows of 32, 4 heads of 32, with states: 457 us, 3.4 TB/s; the registers (256) leave two
 // waves a SIMD, which do not cover all waits.  (Three passes of k_decay took 900.)
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void k_decay_window_back(BackArgs a) {
@@ -649,13 +649,7 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
   powers_of(g, pw, lane);
   // [32 rows][8 units] each; what the walk sums in takes the same place
   uint4 *s0_lds = reinterpret_cast<uint4*>(walk_lds[wave]), *dsn_lds = s0_lds + 256;
-  const int state_units = a.dk * a.dv / 4;
-  int unit_at[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = 64 * i + lane, r = n / (a.dv / 4), u = n % (a.dv / 4);
-    unit_at[i] = r * 8 + (u ^ (r & 7));
-  }
+  const int part_row = lane / 8, part_unit = lane % 8, part_at = 8 * part_row + (part_unit ^ part_row);    // the lane's unit of 8 rows
   auto tokens = [&](uint32_t row) {
     const int64_t i = (int64_t)row * PER + slot;
     if (i >= a.N) return 0;
@@ -681,11 +675,6 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     flag = a.reset && on && half == 0 && a.reset[pos * a.N + (int64_t)row * PER + slot] != 0;
   };
 
-  auto clear_staged = [&]() {       // what lies behind a narrower state is zero
-    for (int i = lane; i < 512; i += 64) s0_lds[i] = make_uint4(0, 0, 0, 0);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  };
-  if constexpr (!PAIR && KT == 1) clear_staged();
   int n = tokens(row), n_next = row + 1 < row_end ? tokens(row + 1) : 0;
   fetch(row, n);
   while (true) {
@@ -713,9 +702,10 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
     if constexpr (STAGED) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool in = 64 * i + lane < state_units;
-        s0_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(s0 + 4 * (64 * i + lane)), a.s0 && in);
-        dsn_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(dsn + 4 * (64 * i + lane)), a.dsn && in);
+        const int r = 8 * i + part_row;
+        const bool in = r < a.dk && 4 * part_unit < a.dv;      // zeros behind a narrower state
+        s0_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(s0 + r * a.dv + 4 * part_unit), a.s0 && in);
+        dsn_raw[i] = fetch8(reinterpret_cast<const uint16_t*>(dsn + r * a.dv + 4 * part_unit), a.dsn && in);
       }
     }
     auto staged_row = [&](const uint4* s, int r, int c, float (&x)[8]) {
@@ -796,10 +786,8 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
       if constexpr (STAGED) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (64 * i + lane < state_units) {
-            s0_lds[unit_at[i]] = s0_raw[i].w[0];
-            dsn_lds[unit_at[i]] = dsn_raw[i].w[0];
-          }
+          s0_lds[64 * i + part_at] = s0_raw[i].w[0];
+          dsn_lds[64 * i + part_at] = dsn_raw[i].w[0];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
@@ -903,7 +891,6 @@ __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void
         walk_window(Walk<T>{at(a.k, m), at(a.q, m), at(a.go, c), at(a.dval, c), a.k.st, a.q.st, a.go.st, a.dval.st, live, m, c, true, g, a.scale, 1.f, reset, a.N,
                             !PAIR && a.dsn ? dsn : nullptr, c, 1, !PAIR && a.ds0 ? a.ds0 + state : nullptr}, walk_lds[wave]);
       }
-      clear_staged();
     } else if (!PAIR && a.ds0) {      // after all that reads dsn, which may be in its place
       const int until = resets ? __ffs(resets) - 1 : 32;        // the tokens that S0 reaches are those before it
       const float pass = pw[n0];
