@@ -466,8 +466,8 @@ __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) 
 
 // bf16 rows of 16 KF numbers, short enough for the weights to stay in registers: a wave holds 64 columns of them and takes 32 rows after
 // 32 rows, which it reads as fragments straight from memory.  No wave waits for another, so products, epilogue and traffic of
-// different waves overlap.  800 000 rows 128 -> 512 with GELU and the pre-activation 513 us (the tile kernel: 720), with neither 335:
-// vector instructions of GELU beside 3.6 TB/s.
+// different waves overlap.  800 000 rows 128 -> 512 with GELU and the pre-activation 513 us (the tile kernel: 720), with neither 335: at
+// three waves a SIMD (the weights' registers) a wave's own chain of loads, products, LDS and stores, at 3.1 to 3.6 TB/s.
 template <int KF>
 __global__ __launch_bounds__(256, KF <= 4 ? 4 : 3) void k_linear_rows(LinearArgs a) {
   typedef uint16_t T;
