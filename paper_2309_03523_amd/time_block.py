@@ -95,6 +95,8 @@ class TimeBlock:
         b = self._buffers.get(key)
         if b is not None:
             return b
+        if torch.cuda.is_current_stream_capturing():      # memory made now would belong to the graph
+            raise RuntimeError("these sizes are new to the block: make one eager call of them before the captured one")
         W, Hd, h = self.width, self.hidden, self.heads
         b = {"n": self._room((T, N, W), self.dtype), "qkv": self._room((T, N, 3 * W), self.dtype), "o": self._room((T, N, W), self.dtype),
              "m": self._room((T, N, W), self.dtype), "u": self._room((T, N, Hd), self.dtype)}

@@ -159,6 +159,11 @@ def test_captured_step():
         block.backward(dy, dX=dx)
 
     step()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):        # sizes that no eager call has had are refused
+        y.mul_(1.0)
+        with pytest.raises(RuntimeError, match="eager call"):
+            block.forward(x[:3], y[:3])
     graph = torch.cuda.CUDAGraph()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):
