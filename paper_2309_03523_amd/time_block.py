@@ -121,6 +121,21 @@ class TimeBlock:
         self._buffers[key] = b
         return b
 
+    def _kept(self, b, S0, stream):
+        """A copy of the first state, which the call is about to overwrite, for backward."""
+        import torch
+        shape = (b["m"].shape[1], self.heads, self.width // self.heads, self.width // self.heads)
+        if S0.shape != shape or S0.dtype != torch.float32 or S0.device != self.device:
+            raise ValueError(f"S0 must be float32 {list(shape)} on the block's device")
+        on = stream if stream is not None else torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(on):
+            if "s0" not in b:
+                if torch.cuda.is_current_stream_capturing():      # memory made now would belong to the graph
+                    raise RuntimeError("a state in place is new to these sizes: make one eager call of it before the captured one")
+                b["s0"] = torch.empty(shape, device=self.device)
+            b["s0"].copy_(S0)
+        return b["s0"]
+
     def _blank(self, t, lengths, stream):
         """Rows behind the sequences hold what an earlier call left; no attention and no gradient there is zero."""
         import torch
@@ -128,19 +143,36 @@ class TimeBlock:
             with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
                 t.zero_()
 
+    @staticmethod
+    def _overlap(a, b) -> bool:
+        """Whether two tensors share memory; rows side by side in one buffer do not."""
+        if a is None or b is None or not a.numel() or not b.numel():
+            return False
+        size = lambda t: t.element_size()  # noqa: E731
+        last = lambda t: t.data_ptr() + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * size(t)  # noqa: E731
+        if a.data_ptr() >= last(b) or b.data_ptr() >= last(a):
+            return False
+        rows = [s for n, s in zip(a.shape[:-1], a.stride()) if n > 1]
+        if not rows or a.stride() != b.stride() or a.shape[:-1] != b.shape[:-1] or size(a) != size(b) or not min(rows) or any(s % min(rows) for s in rows):
+            return True
+        pitch, first = min(rows) * size(a), b.data_ptr() - a.data_ptr()
+        return not a.shape[-1] * size(a) <= first % pitch <= pitch - b.shape[-1] * size(b)
+
     def _rows(self, t, name: str):
         if t.dim() != 3 or t.shape[2] != self.width or t.dtype != self.dtype or t.device != self.device:
             raise ValueError(f"{name} must be [T, N, {self.width}] of the block's element type and device")
 
     # -- the path
     def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, train: bool = True, stream=None):
-        """Y = block(X).  S0, SN fp32 [N, heads, d, d]: states entering and leaving the window (SN may be S0); lengths, reset as
-        binding.decay_attn_forward has them (rows behind a sequence take part in the row-wise steps alone).  train=True keeps what
-        backward reads; T = 1 with train=False is the form for one new snapshot."""
+        """Y = block(X).  S0, SN fp32 [N, heads, d, d]: states entering and leaving the window (SN may be S0, of which train=True then
+        keeps a copy); lengths, reset as binding.decay_attn_forward has them (rows behind a sequence take part in the row-wise steps
+        alone).  train=True keeps what backward reads; T = 1 with train=False is the form for one new snapshot."""
         self._rows(X, "X")
         self._rows(Y, "Y")
         T, N = X.shape[:2]
         b, p, W = self._made(T, N, train, stream), self._p, self.width
+        if train and self._overlap(S0, SN):
+            S0 = self._kept(b, S0, stream)
         q, k, v = b["qkv"][..., :W], b["qkv"][..., W:2 * W], b["qkv"][..., 2 * W:]
         binding.norm_forward(X, b["n"], gamma=p["norm1.weight"], beta=p["norm1.bias"], mean=b.get("mean1"), rstd=b.get("rstd1"), eps=self.eps,
                              stream=stream)

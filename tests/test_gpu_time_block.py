@@ -182,3 +182,61 @@ def test_captured_step():
         assert torch.equal(y, want[0]) and torch.equal(dx, want[1])
         for n, a in zip(block.shapes, want[2:]):
             np.testing.assert_array_equal(block.get_param(n + ".grad"), a)
+
+
+@pytest.mark.parametrize("T", [1, 9, 40])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_training_with_the_state_in_place(T, dtype):
+    """SN given as S0 itself: the same output, state and gradients, bit for bit, as with states of their own."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    N, W, h = 13, 32, 2
+    block = TimeBlock(W, h, 40, dtype=dtype)
+    _params(block, 4)
+    x, dy = (torch.randn(T, N, W, device="cuda").to(block.dtype) for _ in range(2))
+    s0, dsn = (torch.randn(N, h, W // h, W // h, device="cuda") for _ in range(2))
+    state = s0.clone()
+    for turn in range(2):      # the second call finds the copy's place made
+        out = []
+        for given, left in ((s0, torch.empty_like(s0)), (state, state)):
+            y, dx, ds0 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(s0)
+            block.forward(x, y, S0=given, SN=left)
+            block.backward(dy, dX=dx, dSN=dsn, dS0=ds0)
+            out.append([y, left.clone(), dx, ds0] + [torch.from_numpy(block.get_param(n + ".grad")) for n in block.shapes])
+        assert all(torch.equal(a, b) for a, b in zip(*out))
+        s0.copy_(state)
+
+
+def test_a_captured_training_step_with_the_state_in_place():
+    """Truncated back-propagation through time: each replay starts from the state that the one before left."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W, h = 6, 21, 32, 4
+    block = TimeBlock(W, h, 64)
+    _params(block, 5)
+    x, dy = torch.randn(T, N, W, device="cuda"), torch.randn(T, N, W, device="cuda")
+    y, dx, s = torch.empty_like(x), torch.empty_like(x), torch.zeros(N, h, W // h, W // h, device="cuda")
+
+    def step():
+        block.forward(x, y, S0=s, SN=s)
+        block.backward(dy, dX=dx)
+
+    want, first = [], s.clone()
+    for _ in range(4):       # with states of their own
+        left = torch.empty_like(s)
+        block.forward(x, y, S0=first, SN=left)
+        block.backward(dy, dX=dx)
+        want.append([t.clone() for t in (y, dx, left)])
+        first = left
+    step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    s.zero_()
+    for turn in range(4):
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((y, dx, s), want[turn]))
+        block.forward(x[:2], y[:2].clone(), train=False)
