@@ -166,9 +166,13 @@ class TimeBlock:
     def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, train: bool = True, stream=None):
         """Y = block(X).  S0, SN fp32 [N, heads, d, d]: states entering and leaving the window (SN may be S0, of which train=True then
         keeps a copy); lengths, reset as binding.decay_attn_forward has them (rows behind a sequence take part in the row-wise steps
-        alone).  train=True keeps what backward reads; T = 1 with train=False is the form for one new snapshot."""
+        alone).  train=True keeps what backward reads, X and S0 among it, so Y must lie apart from X; with train=False Y may be X.
+        T = 1 with train=False is the form for one new snapshot."""
+        self._last = None
         self._rows(X, "X")
         self._rows(Y, "Y")
+        if train and self._overlap(X, Y):
+            raise ValueError("with train=True Y must lie apart from X, which backward reads")
         T, N = X.shape[:2]
         b, p, W = self._made(T, N, train, stream), self._p, self.width
         if train and self._overlap(S0, SN):

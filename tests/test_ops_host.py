@@ -151,3 +151,29 @@ def test_time_block_refusals():
                dict(decay=[0.5]), dict(decay=[0.5, 1.5])):
         with pytest.raises(ValueError):
             TimeBlock(**{**dict(width=32, heads=2, hidden=64, device="cuda:0"), **kw})
+
+
+def _host_block():
+    """A block without a device: what it refuses before it needs one."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    block = object.__new__(TimeBlock)
+    block.width, block.heads, block.dtype, block.device, block._last = 32, 2, torch.float32, torch.device("cpu"), None
+    return block
+
+
+def test_time_block_refuses_a_training_output_over_its_input():
+    import torch
+    block = _host_block()
+    buf = torch.zeros(6, 5, 96)
+    x = buf[..., :32]
+    for y in (x, buf[..., 16:48], buf[1:, :, :32][:, :, :], torch.as_strided(buf, (6, 5, 32), (480, 96, 1), 8)):
+        block._last = "an earlier call"
+        with pytest.raises(ValueError, match="apart from X"):
+            block.forward(x[:y.shape[0]], y)
+        assert block._last is None      # a call that fails leaves no half of another to backward
+    assert not block._overlap(x, buf[..., 32:64]) and not block._overlap(buf[..., 64:], x) and not block._overlap(x, torch.zeros(6, 5, 32))
+    assert not block._overlap(buf[:, :1, :32], buf[:, 1:2, :32]) and block._overlap(buf[:, :1, :32], buf[:, :1, 31:63])
+    assert not block._overlap(x, None) and not block._overlap(torch.zeros(0, 5, 32), x)
+    s = torch.zeros(4, 2, 16, 16)
+    assert block._overlap(s, s) and block._overlap(s[1:], s[:3]) and not block._overlap(s[2:], s[:2])
