@@ -21,8 +21,8 @@ class TimeBlock:
     """width = heads * size of a head (a multiple of 8, at most 128); hidden: width between up and down.  decay: one number in
     [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.
 
-    Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad".  A block runs one
-    call at a time.  Its buffers are made at the first call with new sizes and kept until release(), so a call may be captured
+    Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad": they and release()
+    wait for the device, forward and backward only enqueue.  A block runs one call at a time.  Its buffers are made at the first call with new sizes and kept until release(), so a call may be captured
     into a HIP graph after an eager one of the same sizes."""
 
     def __init__(self, width: int, heads: int, hidden: int, *, dtype: str = "f32", act: str = "gelu", decay=None, eps: float = 1e-5,
@@ -51,6 +51,7 @@ class TimeBlock:
         self._g = {}
         self._buffers = {}
         self._last = None
+        self._settle()
 
     def _kind(self, name: str):
         import torch
@@ -63,13 +64,20 @@ class TimeBlock:
         buf = torch.zeros(*shape[:-1], -(-shape[-1] // per) * per, dtype=dtype, device=self.device)
         return buf[..., :shape[-1]]
 
-    # -- parameters
+    def _settle(self):
+        """Waits for the device: calls that were given other streams and replayed graphs read and write what the block holds."""
+        import torch
+        torch.cuda.synchronize(self.device)
+
+    # -- parameters (these calls synchronise, as those of a layer do)
     def set_param(self, name: str, value):
         import torch
         v = torch.from_numpy(np.ascontiguousarray(value, np.float32))
         if tuple(v.shape) != self.shapes[name]:
             raise ValueError(f"{name} must have shape {self.shapes[name]}")
+        self._settle()
         self._p[name].copy_(v.to(self._p[name].dtype))
+        self._settle()
 
     def set_params(self, params: dict):
         for k, v in params.items():
@@ -80,12 +88,15 @@ class TimeBlock:
         if name.endswith(".grad"):
             if name[:-5] not in self._g:
                 raise RuntimeError("no gradient yet: run a backward first")
+            self._settle()
             return self._g[name[:-5]].float().cpu().numpy()
+        self._settle()
         return self._p[name].float().cpu().numpy()
 
     # -- memory
     def release(self):
-        """Drops the buffers of all sizes; graphs captured before must not be replayed after it."""
+        """Drops the buffers of all sizes once the device has done with them; graphs captured before must not be replayed after it."""
+        self._settle()
         self._buffers.clear()
         self._last = None
 

@@ -240,3 +240,57 @@ def test_a_captured_training_step_with_the_state_in_place():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, s), want[turn]))
         block.forward(x[:2], y[:2].clone(), train=False)
+
+
+def _busy(stream):
+    """Some 50 ms of work ahead of what is enqueued on the stream next."""
+    import torch
+    with torch.cuda.stream(stream):
+        a = torch.zeros(8192, 8192, device="cuda")
+        for _ in range(6):
+            a = a @ a
+
+
+@pytest.mark.parametrize("hidden", [64, 100])      # a pitch of its own, and rows inside a wider one
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_calls_on_another_stream(dtype, hidden):
+    """Parameters, gradients and buffers follow the stream that a call was given: nothing here waits but the block itself."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W = 10, 300, 64
+    g = torch.Generator(device="cuda").manual_seed(6)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x, dy = (torch.randn(T, N, W, generator=g, device="cuda").to(dt) for _ in range(2))
+
+    def results(stream):
+        block = TimeBlock(W, 4, hidden, dtype=dtype)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        out = []
+        for seed in (7, 8):
+            _params(block, seed)
+            if stream is not None:
+                _busy(stream)
+            block.forward(x, y, stream=stream)
+            block.backward(dy, dX=dx, stream=stream)
+            out += [block.get_param(n + ".grad") for n in block.shapes]
+            if stream is not None:
+                _busy(stream)
+            z = torch.empty_like(x)
+            block.forward(x, z, train=False, stream=stream)
+            block.set_param("qkv.weight", np.zeros(block.shapes["qkv.weight"], np.float32))      # not before that call has read it
+            out += [t.float().cpu().numpy() for t in (y, dx, z)]
+            if stream is not None:
+                _busy(stream)
+            block.forward(x, z, train=False, stream=stream)
+            block.release()
+            used = [torch.full((T, N, k * W), float("nan"), device="cuda").to(dt) for k in (1, 1, 1, 3)]      # memory that was dropped
+            torch.cuda.synchronize()
+            out.append(z.float().cpu().numpy())
+            del used
+        return out
+
+    want = results(None)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    got = results(stream)
+    assert all(np.array_equal(a, b) for a, b in zip(want, got)), [bool(np.array_equal(a, b)) for a, b in zip(want, got)]
