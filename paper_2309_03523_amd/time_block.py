@@ -100,13 +100,24 @@ class TimeBlock:
         self._buffers.clear()
         self._last = None
 
+    def _capturing(self, stream) -> bool:
+        """Whether the call's stream, or the current one of the block's device, is being captured."""
+        import torch
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                return True
+        if stream is None:
+            return False
+        with torch.cuda.stream(stream):
+            return torch.cuda.is_current_stream_capturing()
+
     def _made(self, T: int, N: int, train: bool, stream):
         import torch
         key = (T, N, train)
         b = self._buffers.get(key)
         if b is not None:
             return b
-        if torch.cuda.is_current_stream_capturing():      # memory made now would belong to the graph
+        if self._capturing(stream):      # memory made now would belong to the graph, and be cleared in it
             raise RuntimeError("these sizes are new to the block: make one eager call of them before the captured one")
         W, Hd, h = self.width, self.hidden, self.heads
         b = {"n": self._room((T, N, W), self.dtype), "qkv": self._room((T, N, 3 * W), self.dtype), "o": self._room((T, N, W), self.dtype),
@@ -138,12 +149,11 @@ class TimeBlock:
         shape = (b["m"].shape[1], self.heads, self.width // self.heads, self.width // self.heads)
         if S0.shape != shape or S0.dtype != torch.float32 or S0.device != self.device:
             raise ValueError(f"S0 must be float32 {list(shape)} on the block's device")
-        on = stream if stream is not None else torch.cuda.current_stream(self.device)
-        with torch.cuda.stream(on):
-            if "s0" not in b:
-                if torch.cuda.is_current_stream_capturing():      # memory made now would belong to the graph
-                    raise RuntimeError("a state in place is new to these sizes: make one eager call of it before the captured one")
-                b["s0"] = torch.empty(shape, device=self.device)
+        if "s0" not in b:
+            if self._capturing(stream):
+                raise RuntimeError("a state in place is new to these sizes: make one eager call of it before the captured one")
+            b["s0"] = torch.empty(shape, device=self.device)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             b["s0"].copy_(S0)
         return b["s0"]
 

@@ -294,3 +294,28 @@ def test_calls_on_another_stream(dtype, hidden):
     stream = torch.cuda.Stream()
     got = results(stream)
     assert all(np.array_equal(a, b) for a, b in zip(want, got)), [bool(np.array_equal(a, b)) for a, b in zip(want, got)]
+
+
+def test_new_sizes_are_refused_on_a_capturing_stream_that_is_not_the_current_one():
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    block = TimeBlock(32, 2, 64)
+    x = torch.randn(4, 9, 32, device="cuda")
+    y, s0 = torch.empty_like(x), torch.zeros(9, 2, 16, 16, device="cuda")
+    block.forward(x, y, S0=s0, SN=torch.empty_like(s0))
+    want, aside, graph = y.clone(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        on = torch.cuda.current_stream()
+        with torch.cuda.stream(aside):
+            with pytest.raises(RuntimeError, match="eager call"):
+                block.forward(x[:3], y[:3], stream=on)
+            with pytest.raises(RuntimeError, match="eager call"):
+                block.forward(x, y, S0=s0, SN=s0, stream=on)
+            block.forward(x, y, S0=s0, stream=on)
+    for _ in range(2):
+        y.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
