@@ -494,6 +494,15 @@ def _op_flat(t, name: str, numel: int, dev: int, dtype=None):
     return t.data_ptr()
 
 
+def _op_shape(t, name: str, shape, dev: int, dtype=None):
+    """Address of a contiguous device tensor of just this shape (fp32 unless `dtype` says otherwise), or None."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    return _op_flat(t, name, t.numel(), dev, dtype)
+
+
 def _op_workspace(t, dev: int):
     if t is None:
         return None, 0
@@ -624,12 +633,12 @@ def decay_attn_forward(q, k, v, decay, o, *, heads: int, scale: float = 1.0, s0=
     lib, code, dev = _op_first(q, "q")
     dt = q.dtype
     T, N, dk, dv = _decay_sizes(q, v, heads)
-    n_state = N * heads * dk * dv
+    state = (N, heads, dk, dv)
     ws, ws_bytes = _op_workspace(workspace, dev)
     _op_call(lib.dgc_decay_attn_forward, dev, stream, *_op_seq(q, "q", dt, dev, T, N, heads * dk), *_op_seq(k, "k", dt, dev, T, N, heads * dk),
              *_op_seq(v, "v", dt, dev, T, N, heads * dv), T, N, heads, dk, dv, code, _op_flat(decay, "decay", heads, dev), float(scale),
-             _op_flat(s0, "s0", n_state, dev), _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_flat(reset, "reset", T * N, dev, _torch.uint8),
-             *_op_seq(o, "o", dt, dev, T, N, heads * dv), _op_flat(sn, "sn", n_state, dev), ws, ws_bytes)
+             _op_shape(s0, "s0", state, dev), _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_shape(reset, "reset", (T, N), dev, _torch.uint8),
+             *_op_seq(o, "o", dt, dev, T, N, heads * dv), _op_shape(sn, "sn", state, dev), ws, ws_bytes)
     return o
 
 
@@ -640,11 +649,11 @@ def decay_attn_backward(q, k, v, decay, do, dq, dk, dv, *, heads: int, scale: fl
     lib, code, dev = _op_first(q, "q")
     dt = q.dtype
     T, N, nk, nv = _decay_sizes(q, v, heads)
-    n_state = N * heads * nk * nv
+    state = (N, heads, nk, nv)
     ws, ws_bytes = _op_workspace(workspace, dev)
     _op_call(lib.dgc_decay_attn_backward, dev, stream, *_op_seq(q, "q", dt, dev, T, N, heads * nk), *_op_seq(k, "k", dt, dev, T, N, heads * nk),
              *_op_seq(v, "v", dt, dev, T, N, heads * nv), *_op_seq(do, "do", dt, dev, T, N, heads * nv), T, N, heads, nk, nv, code,
-             _op_flat(decay, "decay", heads, dev), float(scale), _op_flat(s0, "s0", n_state, dev), _op_flat(dsn, "dsn", n_state, dev),
-             _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_flat(reset, "reset", T * N, dev, _torch.uint8),
+             _op_flat(decay, "decay", heads, dev), float(scale), _op_shape(s0, "s0", state, dev), _op_shape(dsn, "dsn", state, dev),
+             _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_shape(reset, "reset", (T, N), dev, _torch.uint8),
              *_op_seq(dq, "dq", dt, dev, T, N, heads * nk), *_op_seq(dk, "dk", dt, dev, T, N, heads * nk), *_op_seq(dv, "dv", dt, dev, T, N, heads * nv),
-             _op_flat(ds0, "ds0", n_state, dev), ws, ws_bytes)
+             _op_shape(ds0, "ds0", state, dev), ws, ws_bytes)

@@ -177,3 +177,35 @@ def test_time_block_refuses_a_training_output_over_its_input():
     assert not block._overlap(x, None) and not block._overlap(torch.zeros(0, 5, 32), x)
     s = torch.zeros(4, 2, 16, 16)
     assert block._overlap(s, s) and block._overlap(s[1:], s[:3]) and not block._overlap(s[2:], s[:2])
+
+
+def test_states_and_flags_have_their_shapes(monkeypatch):
+    """As many elements in another order are refused: flags laid out [N, T], states [N, heads, dv, dk] or flat."""
+    import torch
+    T, N, h, dk, dv = 6, 4, 2, 8, 16
+    binding._op_init()
+    monkeypatch.setattr(binding, "_op_first", lambda t, name: (binding.load(), 0, -1))      # host tensors stand for device ones: -1
+    reached = []
+    monkeypatch.setattr(binding, "_op_call", lambda *args: reached.append(1))
+    q, k, v = torch.zeros(T, N, h * dk), torch.zeros(T, N, h * dk), torch.zeros(T, N, h * dv)
+    decay, state, turned = torch.ones(h), torch.zeros(N, h, dk, dv), torch.zeros(N, h, dv, dk)
+    flags = torch.zeros(T, N, dtype=torch.uint8)
+
+    def forward(**kw):
+        binding.decay_attn_forward(q, k, v, decay, torch.zeros_like(v), heads=h, **kw)
+
+    def backward(**kw):
+        binding.decay_attn_backward(q, k, v, decay, torch.zeros_like(v), None, None, None, heads=h, **kw)
+
+    forward(s0=state, sn=state, reset=flags)
+    backward(s0=state, dsn=state, ds0=state, reset=flags)
+    assert len(reached) == 2
+    for call, kw in [(forward, dict(s0=turned)), (forward, dict(sn=turned)), (forward, dict(s0=state.reshape(-1))), (forward, dict(reset=flags.t().contiguous())),
+                     (forward, dict(reset=flags.reshape(-1))), (backward, dict(s0=turned)), (backward, dict(dsn=turned)), (backward, dict(ds0=state[None])),
+                     (backward, dict(reset=torch.zeros(N, T, dtype=torch.uint8)))]:
+        with pytest.raises(ValueError, match="must be "):
+            call(**kw)
+    for kw in (dict(s0=state.double()), dict(reset=flags.int()), dict(s0=torch.zeros(N, h, dv, dk).transpose(2, 3))):
+        with pytest.raises(ValueError, match="contiguous"):
+            forward(**kw)
+    assert len(reached) == 2
