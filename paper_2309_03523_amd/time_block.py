@@ -179,9 +179,11 @@ class TimeBlock:
         pitch, first = min(rows) * size(a), b.data_ptr() - a.data_ptr()
         return not a.shape[-1] * size(a) <= first % pitch <= pitch - b.shape[-1] * size(b)
 
-    def _rows(self, t, name: str):
+    def _rows(self, t, name: str, like=None):
         if t.dim() != 3 or t.shape[2] != self.width or t.dtype != self.dtype or t.device != self.device:
             raise ValueError(f"{name} must be [T, N, {self.width}] of the block's element type and device")
+        if like is not None and t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape of X, {list(like.shape)}, not {list(t.shape)}")
 
     # -- the path
     def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, train: bool = True, stream=None):
@@ -191,7 +193,7 @@ class TimeBlock:
         T = 1 with train=False is the form for one new snapshot."""
         self._last = None
         self._rows(X, "X")
-        self._rows(Y, "Y")
+        self._rows(Y, "Y", X)
         if train and self._overlap(X, Y):
             raise ValueError("with train=True Y must lie apart from X, which backward reads")
         T, N = X.shape[:2]
@@ -219,9 +221,9 @@ class TimeBlock:
         if self._last is None:
             raise RuntimeError("backward follows a forward with train=True")
         b, X, S0, lengths, reset = self._last
-        self._rows(dY, "dY")
-        if dY.shape != X.shape:
-            raise ValueError("dY must have the shape of the forward's X")
+        self._rows(dY, "dY", X)
+        if dX is not None:
+            self._rows(dX, "dX", X)
         p, g, W = self._p, self._g, self.width
         ws = b["ws"]
         cut = lambda t: (t[..., :W], t[..., W:2 * W], t[..., 2 * W:])  # noqa: E731

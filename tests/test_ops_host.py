@@ -167,7 +167,7 @@ def test_time_block_refuses_a_training_output_over_its_input():
     block = _host_block()
     buf = torch.zeros(6, 5, 96)
     x = buf[..., :32]
-    for y in (x, buf[..., 16:48], buf[1:, :, :32][:, :, :], torch.as_strided(buf, (6, 5, 32), (480, 96, 1), 8)):
+    for y in (x, buf[..., 16:48], buf[1:, :, :32], torch.as_strided(buf, (6, 5, 32), (480, 96, 1), 8)):
         block._last = "an earlier call"
         with pytest.raises(ValueError, match="apart from X"):
             block.forward(x[:y.shape[0]], y)
@@ -209,3 +209,21 @@ def test_states_and_flags_have_their_shapes(monkeypatch):
         with pytest.raises(ValueError, match="contiguous"):
             forward(**kw)
     assert len(reached) == 2
+
+
+def test_time_block_refuses_rows_of_another_shape():
+    """As many rows in another order: a [N, T, width] output or gradient, or fewer tokens."""
+    import torch
+    block = _host_block()
+    x, turned = torch.zeros(6, 4, 32), torch.zeros(4, 6, 32)
+    for y in (turned, torch.zeros(5, 4, 32), torch.zeros(24, 1, 32)):
+        for train in (True, False):
+            with pytest.raises(ValueError, match="shape of X"):
+                block.forward(x, y, train=train)
+    for kw in (dict(dY=turned), dict(dY=torch.zeros_like(x), dX=turned), dict(dY=torch.zeros_like(x), dX=torch.zeros(1, 24, 32))):
+        block._last = ({}, x, None, None, None)
+        with pytest.raises(ValueError, match="shape of X"):
+            block.backward(**kw)
+    block._last = ({}, x, None, None, None)
+    with pytest.raises(ValueError, match="element type"):
+        block.backward(torch.zeros_like(x), dX=x.double())
