@@ -498,10 +498,11 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
  *   heads side by side: [heads][dk] or [heads][dv].  Inputs may repeat rows (a stride of 0).  An output's rows
  *   lie apart, and outputs lie apart from inputs and each other (side by side in rows of one buffer is apart).
  *  T, N: tokens and sequences; heads in [1, 1024]; dk, dv multiples of 8 in [8, 128].  decay device fp32 [heads], in [0, 1].
- *  s0, sn device fp32 [N][heads][dk][dv], NULL = zeros, not wanted; sn may be s0.  lengths device int32 [N] or NULL (all
+ *  s0, sn device fp32 [N][heads][dk][dv], NULL = zeros, not wanted; sn may be s0, and lies
+ *   apart from all else.  lengths device int32 [N] or NULL (all
  *   T): sequence i has its first lengths[i] tokens (clamped to [0, T]); rows behind them are neither read nor written, and sn is
  *   the state after the last token (s0 of an empty sequence).  reset device uint8 [T][N] or NULL.
- *  backward: gradients dq, dk, dv (each may be NULL) and ds0 (NULL = not wanted; may be dsn) from the output's gradient `go` and
+ *  backward: gradients dq, dk, dv (each may be NULL) and ds0 (NULL = not wanted; may be dsn or s0, else apart) from the output's gradient `go` and
  *   the last state's, dsn (NULL = zeros).  The decays are constants.
  *  workspace: dgc_decay_attn_workspace_bytes bytes (0 unless few long sequences are split; negative for sizes outside the range;
  *   `backward` 0 or 1: which call they are for).

@@ -1240,9 +1240,22 @@ bool meet(const Rows& x, int64_t Fx, const Rows& y, int64_t Fy, int64_t T, int64
   const uint64_t pitch = (uint64_t)inner * e, d = x0 >= y0 ? (x0 - y0) % pitch : (pitch - (y0 - x0) % pitch) % pitch;
   return d < (uint64_t)Fy * e || d + (uint64_t)Fx * e > pitch;
 }
+// Whether a state lies over a tensor of rows, by their spans, or over another state (`same`: it may be that state itself).
+bool state_meets(const float* s, const Rows& x, int64_t F, int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int e) {
+  if (!s || !x.p || T == 0 || N == 0) return false;
+  const uintptr_t s0 = (uintptr_t)s, x0 = (uintptr_t)x.p;
+  return s0 < x0 + ((T - 1) * x.st + (N - 1) * x.sn + F) * e && x0 < s0 + N * heads * dk * dv * (int64_t)sizeof(float);
+}
+bool states_meet(const float* a, const float* b, bool same, int64_t N, int32_t heads, int32_t dk, int32_t dv) {
+  if (!a || !b || N == 0 || (same && a == b)) return false;
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  const uint64_t bytes = (uint64_t)N * heads * dk * dv * sizeof(float);
+  return a0 < b0 + bytes && b0 < a0 + bytes;
+}
 constexpr const char* kBadRows =
     "decay attention: tensors need a 16-byte aligned base and strides that are multiples of 16 bytes; an output's rows lie apart";
 constexpr const char* kMeet = "decay attention: outputs lie apart from the inputs and each other";
+constexpr const char* kStates = "decay attention: a state lies apart from the tensors of rows and the other states, or (sn: s0; ds0: dsn or s0) is one of them itself";
 
 }  // namespace
 }  // namespace dgc
@@ -1285,6 +1298,9 @@ dgc_status_t dgc_decay_attn_forward(const void* q, int64_t qt, int64_t qn, const
   if (dgc_status_t rc = decay_call(&c, T, N, heads, dk, dv, decay, scale, lengths, reset, workspace, workspace_bytes, stream)) return rc;
   if (meet(O, fv, Q, fk, T, N, e) || meet(O, fv, K, fk, T, N, e) || meet(O, fv, V, fv, T, N, e))
     return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
+  if (states_meet(sn, s0, true, N, heads, dk, dv) || state_meets(s0, O, fv, T, N, heads, dk, dv, e) || state_meets(sn, O, fv, T, N, heads, dk, dv, e) ||
+      state_meets(sn, Q, fk, T, N, heads, dk, dv, e) || state_meets(sn, K, fk, T, N, heads, dk, dv, e) || state_meets(sn, V, fv, T, N, heads, dk, dv, e))
+    return ops::refuse(DGC_ERR_INVALID_ARG, kStates);
   if (N == 0) return DGC_OK;
   if (dtype == DGC_DTYPE_F32) forward<float>(c, Q, K, V, O, s0, sn);
   else forward<uint16_t>(c, Q, K, V, O, s0, sn);
@@ -1320,6 +1336,12 @@ dgc_status_t dgc_decay_attn_backward(const void* q, int64_t qt, int64_t qn, cons
       if (meet(out[x], fo[x], out[y], fo[y], T, N, e)) return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
     }
   }
+  bool meets = states_meet(ds0, dsn, true, N, heads, dk, dv) || states_meet(ds0, s0, true, N, heads, dk, dv);
+  for (int x = 0; x < 4; ++x) meets = meets || state_meets(ds0, in[x], fi[x], T, N, heads, dk, dv, e);
+  for (int x = 0; x < 3; ++x) {
+    for (const float* s : {s0, dsn, static_cast<const float*>(ds0)}) meets = meets || state_meets(s, out[x], fo[x], T, N, heads, dk, dv, e);
+  }
+  if (meets) return ops::refuse(DGC_ERR_INVALID_ARG, kStates);
   if (N == 0) return DGC_OK;
   if (dtype == DGC_DTYPE_F32) backward<float>(c, in[0], in[1], in[2], in[3], out[0], out[1], out[2], s0, dsn, ds0);
   else backward<uint16_t>(c, in[0], in[1], in[2], in[3], out[0], out[1], out[2], s0, dsn, ds0);

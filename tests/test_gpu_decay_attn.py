@@ -410,3 +410,23 @@ def test_window_states_that_are_not_finite(dtype):
         assert torch.equal(torch.isnan(x), torch.isnan(w)) and torch.equal(torch.isinf(x), torch.isinf(w))
         fine = torch.isfinite(w)
         _close(torch.where(fine, x, 0), torch.where(fine, w, 0), torch.where(fine, m, m[fine].max()), dtype, 20, st)
+
+
+@pytest.mark.parametrize("dims", [(1, 6, 2, 16, 16), (20, 9, 2, 32, 32), (20, 5, 2, 64, 40), (20, 3, 1, 128, 72), (70, 5, 3, 32, 40), (700, 2, 2, 64, 64)])
+def test_states_in_place(dims):
+    """sn over s0, ds0 over dsn and ds0 over s0: the bits of separate ones, where segments, windows or single tokens are walked."""
+    import torch
+    from paper_2309_03523_amd import binding
+    T, N, heads, dk, dv = dims
+    c = _case(*dims, "bf16", 15, reset=0.1, ragged=True)
+    kw = dict(heads=heads, scale=c["scale"], lengths=c["lengths"], reset=c["reset"], workspace=_workspace(binding, dims))
+    o, sn = _run_forward(c)
+    s, again = c["s0"].clone(), c["rows"](heads * dv, -7.0)
+    binding.decay_attn_forward(c["q"], c["k"], c["v"], c["decay"], again, s0=s, sn=s, **kw)
+    assert torch.equal(s, sn) and torch.equal(again, o)
+    want = _run_backward(c)
+    for over in ("s0", "dsn"):
+        states = {"s0": c["s0"], "dsn": c["dsn"], over: c[over].clone()}
+        got = [c["rows"](heads * d, -7.0) for d in (dk, dk, dv)]
+        binding.decay_attn_backward(c["q"], c["k"], c["v"], c["decay"], c["do"], *got, ds0=states[over], **states, **kw)
+        assert all(torch.equal(a, b) for a, b in zip((*got, states[over]), want)), over

@@ -227,3 +227,31 @@ def test_time_block_refuses_rows_of_another_shape():
     block._last = ({}, x, None, None, None)
     with pytest.raises(ValueError, match="element type"):
         block.backward(torch.zeros_like(x), dX=x.double())
+
+
+def test_decay_attention_refuses_states_over_other_tensors(lib):
+    """A state of 5 sequences x 2 heads x 32 x 32 (40960 bytes) partly over another one, or over rows that are read or written."""
+    D, E, F = 0x40000000, 0x50000000, 0x60000000
+    size = 5 * 2 * 32 * 32 * 4
+    good = dict(q=A, qt=320, qn=64, k=B, kt=320, kn=64, v=C, vt=320, vn=64, T=6, N=5, heads=2, dk=32, dv=32, dtype=0, decay=D, scale=1.0, s0=F, lengths=None,
+                reset=None, o=E, ot=320, on=64, sn=None, ws=None, ws_bytes=0, stream=None)
+
+    def fwd(**kw):
+        return lib.dgc_decay_attn_forward(*{**good, **kw}.values())
+
+    rows = (5 * 320 + 4 * 64 + 64) * 4
+    for kw in (dict(sn=F + 16), dict(sn=F - size + 16), dict(s0=E), dict(s0=E + rows - 16), dict(sn=E - size + 16), dict(sn=A), dict(sn=B + 1024), dict(sn=C - 16)):
+        assert fwd(**kw) == INVALID, kw
+        assert "state" in _text(lib)
+    G = [0x70000000 + (x << 24) for x in range(3)]
+    S, D0 = 0x80000000, 0x90000000
+    good = dict(q=A, qt=320, qn=64, k=B, kt=320, kn=64, v=C, vt=320, vn=64, go=F, gt=320, gn=64, T=6, N=5, heads=2, dk=32, dv=32, dtype=0, decay=D, scale=1.0, s0=S,
+                dsn=D0, lengths=None, reset=None, dq=G[0], dqt=320, dqn=64, dk_=G[1], dkt=320, dkn=64, dv_=G[2], dvt=320, dvn=64, ds0=None, ws=None, ws_bytes=0,
+                stream=None)
+
+    def bwd(**kw):
+        return lib.dgc_decay_attn_backward(*{**good, **kw}.values())
+
+    for kw in (dict(ds0=S + 16), dict(ds0=D0 - 16), dict(ds0=A), dict(ds0=F + 64), dict(ds0=G[2]), dict(s0=G[0]), dict(dsn=G[1] + rows - 16), dict(ds0=G[0] - size + 16)):
+        assert bwd(**kw) == INVALID, kw
+        assert "state" in _text(lib)
