@@ -22,8 +22,11 @@ class TimeBlock:
     [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.
 
     Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad": they and release()
-    wait for the device, forward and backward only enqueue.  A block runs one call at a time.  Its buffers are made at the first call with new sizes and kept until release(), so a call may be captured
-    into a HIP graph after an eager one of the same sizes."""
+    wait for the device, forward and backward only enqueue.  A block runs one call at a time.  Its buffers are made at the first call
+    with new sizes, so a call may be captured into a HIP graph after an eager one of the same sizes.  Those of the last SIZES sizes
+    and all that a captured call uses are kept until release()."""
+
+    SIZES = 8      # a program trains, evaluates and steps at a few sizes; the vertices of a served graph change in number for ever
 
     def __init__(self, width: int, heads: int, hidden: int, *, dtype: str = "f32", act: str = "gelu", decay=None, eps: float = 1e-5,
                  device="cuda:0"):
@@ -103,9 +106,13 @@ class TimeBlock:
     def _capturing(self, stream) -> bool:
         """Whether the call's stream, or the current one of the block's device, is being captured."""
         import torch
-        with torch.cuda.device(self.device):
+        if torch.cuda.current_device() == self.device.index:
             if torch.cuda.is_current_stream_capturing():
                 return True
+        else:
+            with torch.cuda.device(self.device):
+                if torch.cuda.is_current_stream_capturing():
+                    return True
         if stream is None:
             return False
         with torch.cuda.stream(stream):
@@ -114,8 +121,9 @@ class TimeBlock:
     def _made(self, T: int, N: int, train: bool, stream):
         import torch
         key = (T, N, train)
-        b = self._buffers.get(key)
+        b = self._buffers.pop(key, None)
         if b is not None:
+            self._buffers[key] = b      # the last to go
             return b
         if self._capturing(stream):      # memory made now would belong to the graph, and be cleared in it
             raise RuntimeError("these sizes are new to the block: make one eager call of them before the captured one")
@@ -140,8 +148,25 @@ class TimeBlock:
         b["ws"] = torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device)
         if stream is not None:     # the zeros above were written on the current stream
             stream.wait_stream(torch.cuda.current_stream(self.device))
+        b["on"], b["captured"] = set(), False
         self._buffers[key] = b
+        old = [k for k, s in self._buffers.items() if not s["captured"]][:-self.SIZES]
+        for k in old:
+            self._drop(self._buffers.pop(k))
         return b
+
+    def _used(self, b, stream):
+        """Notes where a call runs that uses a set of buffers."""
+        import torch
+        b["on"].add(stream if stream is not None else torch.cuda.current_stream(self.device))
+        b["captured"] |= self._capturing(stream)
+
+    @staticmethod
+    def _drop(b):
+        """Leaves a set of buffers to the allocator, which is told of the streams that may still use them."""
+        for t in b.values():
+            for stream in b["on"] if hasattr(t, "record_stream") else ():
+                t.record_stream(stream)
 
     def _kept(self, b, S0, stream):
         """A copy of the first state, which the call is about to overwrite, for backward."""
@@ -198,6 +223,7 @@ class TimeBlock:
             raise ValueError("with train=True Y must lie apart from X, which backward reads")
         T, N = X.shape[:2]
         b, p, W = self._made(T, N, train, stream), self._p, self.width
+        self._used(b, stream)
         if train and self._overlap(S0, SN):
             S0 = self._kept(b, S0, stream)
         q, k, v = b["qkv"][..., :W], b["qkv"][..., W:2 * W], b["qkv"][..., 2 * W:]
@@ -225,6 +251,7 @@ class TimeBlock:
         if dX is not None:
             self._rows(dX, "dX", X)
         p, g, W = self._p, self._g, self.width
+        self._used(b, stream)
         ws = b["ws"]
         cut = lambda t: (t[..., :W], t[..., W:2 * W], t[..., 2 * W:])  # noqa: E731
         lin = lambda dy, x, n, dx, **kw: binding.linear_backward(dy, x, p[n + ".weight"], dx=dx, dw=g[n + ".weight"], dbias=g[n + ".bias"],  # noqa: E731

@@ -319,3 +319,44 @@ def test_new_sizes_are_refused_on_a_capturing_stream_that_is_not_the_current_one
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+def test_buffers_of_many_sizes():
+    """A graph whose vertices come and go: what the block holds stays that of a few sizes, a captured size outlives them all, and memory
+    that is let go under a queue of work is not given away early."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    W, h = 64, 4
+    block = TimeBlock(W, h, 128)
+    _params(block, 9)
+    x = torch.randn(1, 4200, W, device="cuda")
+    y = torch.empty_like(x)
+    block.forward(x, y, train=False)
+    want = y.clone()
+    graph, z = torch.cuda.CUDAGraph(), torch.empty_like(x[:, :700])
+    block.forward(x[:, :700], z, train=False)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        block.forward(x[:, :700], z, train=False)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for n in range(4000, 4060):
+        block.forward(x[:, :n], y[:, :n], train=False)
+        assert torch.equal(y[:, :n], want[:, :n])
+    rows = 4200 * W * 4 * (1 + 3 + 1 + 1 + 2)      # n, qkv, o, m, u
+    assert torch.cuda.memory_allocated() - before <= (block.SIZES + 1) * (rows + (1 << 16))
+    for _ in range(2):
+        z.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(z, want[:, :700])
+    stream = torch.cuda.Stream()
+    _busy(stream)
+    out = [torch.empty(1, n, W, device="cuda") for n in range(3000, 3000 + 3 * block.SIZES)]
+    for o in out:
+        block.forward(x[:, :o.shape[1]], o, train=False, stream=stream)
+    used = [torch.full((1, 3000, k * W), float("nan"), device="cuda") for k in (1, 3, 1, 1, 2) * 3 * block.SIZES]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[:, :o.shape[1]]) for o in out)
+    del used
