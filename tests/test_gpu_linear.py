@@ -238,3 +238,30 @@ def test_streams_graphs_and_repeats():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(want[:5], out[:5])), k
+
+
+def test_activations_far_below_zero():
+    """There GELU and SiLU are small multiples of p, and their slopes too: each is still off by no more than its rounding.
+
+    The arguments p are bf16 numbers and the weight is 1, so the products are exact.  Half a bf16 step is 2^-8 of the value; before it,
+    e^-x is off by 2^-23 of its exponent (at most 128: 1.6e-5) and the tail's formula by 1.4e-6, over values that are a few times as large as
+    their difference in the slopes' (p^2 against 1): 2e-5, and 1e-4 for slopes, whose zeros near -0.75 and -1.28 are left out."""
+    import torch
+    from paper_2309_03523_amd import binding
+    for act, least in (("gelu", -12.9), ("silu", -86.0)):
+        p = torch.linspace(least, 0, 40000, device="cuda").to(torch.bfloat16)[:, None]
+        x = torch.zeros(p.shape[0], 8, dtype=torch.bfloat16, device="cuda")[:, :1].copy_(p)
+        w = torch.ones(8, 8, dtype=torch.bfloat16, device="cuda")[:1, :1]
+        room = lambda: torch.zeros(p.shape[0], 8, dtype=torch.bfloat16, device="cuda")[:, :1]  # noqa: E731
+        y, dx, dy = room(), room(), room().fill_(1)
+        binding.linear_forward(x, w, y, act=act)
+        P = x.double().requires_grad_()
+        want = 0.5 * P * torch.special.erfc(-P * 0.5 ** 0.5) if act == "gelu" else P / (1 + torch.exp(-P))
+        rel = ((y.double() - want) / want).detach()[P != 0]
+        assert float(rel.abs().max()) <= 2.0 ** -8 + 2e-5, act
+        slope, = torch.autograd.grad(want.sum(), P)
+        ws = torch.empty(binding.linear_workspace_bytes(p.shape[0], 1, 1, dtype="bf16", act=act), dtype=torch.uint8, device="cuda")
+        binding.linear_backward(dy, x, w, pre=x, act=act, dx=dx, workspace=ws)
+        far = (P < -2) | (P > -0.5)
+        rel = ((dx.double() - slope) / slope).detach()[far]
+        assert float(rel.abs().max()) <= 2.0 ** -8 + 1e-4, act
