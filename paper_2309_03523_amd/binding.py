@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libdgc.so")
 TIME_KIND = {"none": 0, "gru": 1, "lstm": 2, "self_attn": 3}
 ACT = {"none": 0, "relu": 1}
 LINEAR_ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+LINEAR_EXACT = 16       # added to an activation in the backward calls
 GATHER = {"in_place": 0, "staged": 1}
 DENSE = {"auto": 0, "tile": 1, "wave": 2}
 AGG = {"table": 0, "walk": 1}
@@ -562,9 +563,9 @@ def norm_backward(dy, x, mean, rstd, dx, *, gamma=None, add=None, dgamma=None, d
     return dx
 
 
-def linear_workspace_bytes(R: int, K: int, M: int, *, dtype: str = "f32", act: str = "gelu") -> int:
-    """Bytes that linear_backward needs; without an activation it needs less."""
-    return int(load().dgc_linear_workspace_bytes(int(R), int(K), int(M), DTYPE[dtype], LINEAR_ACT[act]))
+def linear_workspace_bytes(R: int, K: int, M: int, *, dtype: str = "f32", act: str = "gelu", exact: bool = False) -> int:
+    """Bytes that linear_backward needs; without an activation it needs less, with exact=True more."""
+    return int(load().dgc_linear_workspace_bytes(int(R), int(K), int(M), DTYPE[dtype], LINEAR_ACT[act] + LINEAR_EXACT * bool(exact)))
 
 
 def linear_forward(x, w, y, *, bias=None, act: str = "none", residual=None, pre=None, stream=None):
@@ -583,9 +584,11 @@ def linear_forward(x, w, y, *, bias=None, act: str = "none", residual=None, pre=
     return y
 
 
-def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, dbias=None, workspace, stream=None):
+def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, dbias=None, workspace, exact: bool = False,
+                    stream=None):
     """dgc_linear_backward: the wanted ones of dx [..., K], dw [M, K] and dbias fp32 [M] from dy [..., M]; `pre`: what
-    linear_forward left, needed with an activation; workspace: linear_workspace_bytes device bytes."""
+    linear_forward left, needed with an activation; workspace: linear_workspace_bytes device bytes.  exact=True: bfloat16's dy act'(pre)
+    is not rounded to bfloat16 before it is multiplied."""
     lib, code, dev = _op_first(x, "x")
     dt = x.dtype
     px, ldx = _op_rows(x, "x")
@@ -596,7 +599,7 @@ def linear_backward(dy, x, w, *, pre=None, act: str = "none", dx=None, dw=None, 
     pdx, lddx = _op_rows(dx, "dx", dt, dev, (R, K))
     pdw, lddw = _op_rows(dw, "dw", dt, dev, (M, K))
     ws, ws_bytes = _op_workspace(workspace, dev)
-    _op_call(lib.dgc_linear_backward, dev, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, code, pp, ldp, LINEAR_ACT[act], pdx, lddx, pdw, lddw,
+    _op_call(lib.dgc_linear_backward, dev, stream, pdy, lddy, px, ldx, pw, ldw, R, K, M, code, pp, ldp, LINEAR_ACT[act] + (LINEAR_EXACT if exact else 0), pdx, lddx, pdw, lddw,
              _op_flat(dbias, "dbias", M, dev), ws, ws_bytes)
 
 

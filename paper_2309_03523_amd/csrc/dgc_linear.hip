@@ -41,6 +41,12 @@ constexpr int kSplitBlocks = 512;  // workgroups that dw is split over, about
 constexpr int kSplitRows = 512;     // rows of a share of dw at least
 constexpr int kSumBlocks = 1024, kMostSums = 512;   // as for the norm's weight gradients
 
+// Whether dp takes two parts (at two_parts).  act: an activation, plus DGC_LINEAR_EXACT where the caller asks for them.
+bool parted(int32_t dtype, int32_t act) {
+  return dtype == DGC_DTYPE_BF16 && (act == DGC_LINEAR_EXACT + DGC_LINEAR_GELU || act == DGC_LINEAR_EXACT + DGC_LINEAR_SILU);
+}
+int32_t activation_of(int32_t act) { return act >= DGC_LINEAR_EXACT ? act - DGC_LINEAR_EXACT : act; }
+
 // ---------------------------------------------------------------------------------------------- activations
 // erfc(z) exp(z^2) for z >= 0 as t times a polynomial of t = 1 / (1 + 0.38 z), fitted so that the largest relative error over z in [0, 14] is
 // least: 1.0e-6, 1.4e-6 in fp32.  Relative, since GELU far below zero is this tail and little else.  A fifth of the library call's
@@ -233,6 +239,7 @@ __device__ __forceinline__ void fetch_stage(Stage<T, BX, true>& s, const T* base
 struct LinearArgs {
   const void* P; int64_t ldp; int64_t NP;   // NP columns of the output
   const void* Q; int64_t ldq; int64_t NQ;   // NQ rows of it
+  int64_t q_low;                            // two parts: where Q's low part lies, elements from Q (0: Q is as it is)
   int64_t C;                                // contraction
   int64_t share;                            // contraction of one part (a multiple of kBK); parts > 1: partial sums
   int32_t parts;
@@ -327,7 +334,7 @@ __device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t p, float 
 // BP x BQ outputs a workgroup, a quarter of them a wave.  Measured: bf16 8192 x 4096 x 4096 366 us (750 TFLOP/s), fp32 8192 x 2048 x
 // 2048 411 us (167 of its own, 1000 of the part products); one tile's loads, products and epilogue follow each other, and two
 // workgroups a CU (registers) cover part of that.
-template <class T, int BP, int BQ, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
+template <class T, int BP, int BQ, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL, bool LOW>
 __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) {
   constexpr int BK = Kind<T>::kBK, UK = BK / 8, PARTS = Kind<T>::kParts, FP = BP / 64, FQ = BQ / 64;
   __shared__ uint4 lds[PARTS * (BP + BQ) * UK];
@@ -353,14 +360,13 @@ __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) 
   const T* Q = static_cast<const T*>(a.Q);
   Stage<T, BP, ACROSS_P> sp;
   Stage<T, BQ, ACROSS_Q> sq;
-  auto fetch = [&](const Tile& t, int64_t c) {
-    fetch_stage(sp, P, a.ldp, t.p0, a.NP, c, t.c1);
-    fetch_stage(sq, Q, a.ldq, t.q0, a.NQ, c, t.c1);
-  };
+  auto fetch_p = [&](const Tile& t, int64_t c) { fetch_stage(sp, P, a.ldp, t.p0, a.NP, c, t.c1); };
+  auto fetch_q = [&](const Tile& t, int64_t c, bool low) { fetch_stage(sq, LOW && low ? Q + a.q_low : Q, a.ldq, t.q0, a.NQ, c, t.c1); };
   for (int64_t local = blockIdx.x >> 3; local < per; local += gridDim.x >> 3) {
     const Tile tile = tile_of(local);
     if (tile.part < 0) return;
-    fetch(tile, tile.c0);
+    fetch_p(tile, tile.c0);
+    fetch_q(tile, tile.c0, true);
     const int64_t p0 = tile.p0, q0 = tile.q0, c0 = tile.c0, c1 = tile.c1;
     const int part = tile.part;
     floatx16 acc[FP][FQ];
@@ -369,12 +375,7 @@ __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) 
 #pragma unroll
       for (int j = 0; j < FQ; ++j) acc[i][j] = floatx16{};
     }
-    for (int64_t c = c0; c < c1; c += BK) {
-      __syncthreads();
-      sp.store(lds_p);
-      sq.store(lds_q);
-      __syncthreads();
-      if (c + BK < c1) fetch(tile, c + BK);
+    auto multiply = [&]() {
       if constexpr (PARTS == 1) {
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
@@ -411,6 +412,25 @@ __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) 
           }
         }
       }
+    };
+    for (int64_t c = c0; c < c1; c += BK) {
+      if constexpr (LOW) {      // Q's low part over the same tile of P first
+        __syncthreads();
+        sp.store(lds_p);
+        sq.store(lds_q);
+        __syncthreads();
+        fetch_q(tile, c, false);
+        multiply();
+      }
+      __syncthreads();
+      if constexpr (!LOW) sp.store(lds_p);
+      sq.store(lds_q);
+      __syncthreads();
+      if (c + BK < c1) {
+        fetch_p(tile, c + BK);
+        fetch_q(tile, c + BK, true);
+      }
+      multiply();
     }
     // Outputs go through LDS, half of the rows at a time, so that 16 or 8 threads finish a row's columns side by side: stored from
     // the registers as they are, each instruction touched 32 rows and the stores took longer than the products.
@@ -536,7 +556,7 @@ __global__ __launch_bounds__(256, KF <= 4 ? 4 : 3) void k_linear_rows(LinearArgs
 
 // Few outputs, or few rows: 32 rows by 32 columns a workgroup, 8 waves that take 64 of the contraction at a time in turn.  8 rows 1024 -> 4096:
 // 6 us, one round of loads and the join; 8 MB of weights are 1.7 us.
-template <class T, bool ACROSS_P>
+template <class T, bool ACROSS_P, bool LOW>
 __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
   __shared__ float joined[8][16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -545,7 +565,7 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
   const T* Q = static_cast<const T*>(a.Q) + q * a.ldq;
   floatx16 acc = floatx16{};
   for (int64_t c = wave * 64; c < a.C; c += 8 * 64) {
-    typename UnitOf<T>::type up[4], uq[4];
+    typename UnitOf<T>::type up[4], uq[4], ul[LOW ? 4 : 1];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const int64_t k = c + 16 * s + 8 * half;
@@ -560,10 +580,17 @@ __global__ __launch_bounds__(512) void k_linear_few(LinearArgs a) {
       }
       if (q < a.NQ && k < a.C) load_unit(Q, k, a.C, uq[s]);
       else zero_unit(uq[s]);
+      if constexpr (LOW) {
+        if (q < a.NQ && k < a.C) load_unit(Q + a.q_low, k, a.C, ul[s]);
+        else zero_unit(ul[s]);
+      }
     }
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(up[s]), as_frag(uq[s]), acc, 0, 0, 0);
+      for (int s = 0; s < 4; ++s) {
+        if constexpr (LOW) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(up[s]), as_frag(ul[s]), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(up[s]), as_frag(uq[s]), acc, 0, 0, 0);
+      }
     } else {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
@@ -635,14 +662,26 @@ struct SlopeArgs {
   const void* dy; int64_t lddy;
   const void* pre; int64_t ldpre;
   void* dp; int64_t lddp;        // nullptr: act is none, dp is dy itself
+  int64_t low;                   // two parts: where the low one lies, elements from dp (0: one part)
   float* partial;                // [workgroups][M], or nullptr
   int64_t R;
   int32_t M;
   int32_t act;
 };
 
+// The matrix unit takes bf16.  dp rounded to one such number, 2^-8, adds as much to the error of dx and dw as their own rounding does
+// (2.3e-3 of their norm for 1.7e-3), and is what a training step in bf16 takes by default: in two parts, 2^-16, dp is twice the traffic and the products are
+// twice the matrix work (400 000 rows 128 -> 512 with GELU 510 us and 915, 8192 rows 4096 -> 4096 810 us and 1430).  So that is the caller's
+// choice, DGC_LINEAR_EXACT, for GELU and SILU: RELU's dp is dy or 0, one bf16 number.  Both parts have dp's sign, the high one by cutting off
+// and the low one by never being zero where dp (from 2^-109 on) is not, so that dp times an infinity is that infinity.
+__device__ __forceinline__ void two_parts(float dp, float& high, float& low) {
+  high = dp == dp ? split::cut(dp) : dp;
+  const float rest = dp - high;
+  low = fabsf(rest) >= 0x1p-126f || fabsf(dp) < 0x1p-109f ? rest : copysignf(0x1p-126f, dp);
+}
+
 // 400 000 x 512 bf16 with GELU: 260 us, 4.7 TB/s of dy, pre and dp.  LPR lanes a row, 256 / LPR rows at a time; blockIdx.y: which LPR vectors of a wide row.
-template <class T, int LPR>
+template <class T, int LPR, bool LOW>
 __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs a) {
   constexpr int VN = Elem<T>::kPer, GROUPS = 256 / LPR, U = 4;
   __shared__ float joined[256 * VN];
@@ -663,8 +702,18 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs a) {
       if (a.dp) {
 #pragma unroll
         for (int i = 0; i < VN; ++i) dy[u][i] = slope_times<T>(dy[u][i], p[u][i], a.act);
-        // dp is rounded to the element type, the form in which the matrix unit takes it; dbias sums what it was before
-        if (r < a.R && col < a.M) *reinterpret_cast<uint4*>(static_cast<T*>(a.dp) + r * a.lddp + col) = Elem<T>::pack(dy[u]);
+        if (r < a.R && col < a.M) {
+          T* to = static_cast<T*>(a.dp) + r * a.lddp + col;
+          if constexpr (LOW) {
+            float high[VN], low[VN];
+#pragma unroll
+            for (int i = 0; i < VN; ++i) two_parts(dy[u][i], high[i], low[i]);
+            *reinterpret_cast<uint4*>(to) = Elem<T>::pack(high);
+            *reinterpret_cast<uint4*>(to + a.low) = Elem<T>::pack(low);
+          } else {
+            *reinterpret_cast<uint4*>(to) = Elem<T>::pack(dy[u]);
+          }
+        }
       }
 #pragma unroll
       for (int i = 0; i < VN; ++i) sum[i] += dy[u][i];
@@ -695,16 +744,16 @@ int64_t slope_blocks(int64_t R, int32_t M, int per) {
   return std::max<int64_t>(std::min<int64_t>(turns, std::max<int64_t>(kSumBlocks / wide, 64)), (turns * 4 + kMostSums - 1) / kMostSums);
 }
 
-template <class T>
+template <class T, bool LOW>
 void launch_slope(const SlopeArgs& a, int64_t blocks, hipStream_t st) {
   const int per = Elem<T>::kPer, lpr = slope_lanes(a.M, per), vecs = (a.M + per - 1) / per;
   const dim3 grid((unsigned)blocks, (unsigned)((vecs + lpr - 1) / lpr));
-  if (lpr == 8) hipLaunchKernelGGL((k_linear_slope<T, 8>), grid, 256, 0, st, a);
-  else if (lpr == 16) hipLaunchKernelGGL((k_linear_slope<T, 16>), grid, 256, 0, st, a);
-  else if (lpr == 32) hipLaunchKernelGGL((k_linear_slope<T, 32>), grid, 256, 0, st, a);
-  else if (lpr == 64) hipLaunchKernelGGL((k_linear_slope<T, 64>), grid, 256, 0, st, a);
-  else if (lpr == 128) hipLaunchKernelGGL((k_linear_slope<T, 128>), grid, 256, 0, st, a);
-  else hipLaunchKernelGGL((k_linear_slope<T, 256>), grid, 256, 0, st, a);
+  if (lpr == 8) hipLaunchKernelGGL((k_linear_slope<T, 8, LOW>), grid, 256, 0, st, a);
+  else if (lpr == 16) hipLaunchKernelGGL((k_linear_slope<T, 16, LOW>), grid, 256, 0, st, a);
+  else if (lpr == 32) hipLaunchKernelGGL((k_linear_slope<T, 32, LOW>), grid, 256, 0, st, a);
+  else if (lpr == 64) hipLaunchKernelGGL((k_linear_slope<T, 64, LOW>), grid, 256, 0, st, a);
+  else if (lpr == 128) hipLaunchKernelGGL((k_linear_slope<T, 128, LOW>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_linear_slope<T, 256, LOW>), grid, 256, 0, st, a);
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -721,17 +770,17 @@ bool small_tiles(int64_t NP, int64_t NQ) {
 bool few_outputs(int64_t NP, int64_t NQ, int64_t C) {
   return NQ <= kFewRows || (C >= kFewLong && ((NP + 63) / 64) * ((NQ + 63) / 64) <= kFewTiles);
 }
-template <class T, bool ACROSS_P>
+template <class T, bool ACROSS_P, bool LOW>
 void launch_few(const LinearArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_linear_few<T, ACROSS_P>), dim3((unsigned)((a.NP + 31) / 32), (unsigned)((a.NQ + 31) / 32)), 512, 0, st, a);
+  hipLaunchKernelGGL((k_linear_few<T, ACROSS_P, LOW>), dim3((unsigned)((a.NP + 31) / 32), (unsigned)((a.NQ + 31) / 32)), 512, 0, st, a);
 }
 
-template <class T, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL>
+template <class T, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL, bool LOW>
 void launch_tiles(const LinearArgs& a, bool small, hipStream_t st) {
   const int64_t b = small ? 64 : 128, tiles = ((a.NP + b - 1) / b) * ((a.NQ + b - 1) / b) * a.parts;
   const unsigned grid = (unsigned)(std::min<int64_t>((tiles + 7) / 8, kMostTiles / 8) * 8);
-  if (small) hipLaunchKernelGGL((k_linear<T, 64, 64, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
-  else hipLaunchKernelGGL((k_linear<T, 128, 128, ACROSS_P, ACROSS_Q, PARTIAL>), grid, 256, 0, st, a);
+  if (small) hipLaunchKernelGGL((k_linear<T, 64, 64, ACROSS_P, ACROSS_Q, PARTIAL, LOW>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_linear<T, 128, 128, ACROSS_P, ACROSS_Q, PARTIAL, LOW>), grid, 256, 0, st, a);
 }
 
 // The kernel for short rows takes these (the largest pitch that is not there is 0).
@@ -770,7 +819,7 @@ Room room_of(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
   const Split s = split_of(R, K, M);
   Room r;
   r.dp = 0;
-  r.sums = act == DGC_LINEAR_NONE ? 0 : R * ((M + per - 1) / per * per) * e;
+  r.sums = activation_of(act) == DGC_LINEAR_NONE ? 0 : R * ((M + per - 1) / per * per) * e * (parted(dtype, act) ? 2 : 1);
   r.partial = r.sums + (slope_blocks(R, M, per) * M + 3) / 4 * 16;
   r.all = r.partial + (s.parts > 1 ? 4 * (int64_t)s.parts * M * ((K + 3) / 4 * 4) : 0) + 16;
   return r;
@@ -795,14 +844,40 @@ __global__ __launch_bounds__(1024) void k_linear_dbias(const float* partial, int
   if (p == 0 && col < M) dbias[col] = (float)lds[0][c];
 }
 
+// dx and dw from dp, whose low part lies `low` elements behind it (LOW).
+template <class T, bool LOW>
+void products(const void* dp, int64_t lddp, int64_t low, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
+              void* dx, int64_t lddx, void* dw, int64_t lddw, float* partial, hipStream_t st) {
+  LinearArgs a{};
+  a.Q = dp; a.ldq = lddp; a.q_low = low; a.NP = K;
+  if (dw) {
+    const Split s = split_of(R, K, M);
+    a.P = x; a.ldp = ldx; a.NQ = M; a.C = R; a.share = s.share; a.parts = s.parts;
+    a.out = dw; a.ldo = lddw; a.partial = partial;
+    if (s.parts == 1) {
+      launch_tiles<T, true, true, false, LOW>(a, s.small, st);
+    } else {
+      launch_tiles<T, true, true, true, LOW>(a, s.small, st);
+      const int64_t n = (int64_t)M * ((K + 3) / 4);
+      hipLaunchKernelGGL(k_linear_join<T>, (unsigned)((n + 15) / 16), 256, 0, st, a);
+    }
+  }
+  if (dx && R > 0) {
+    a.P = w; a.ldp = ldw; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
+    a.out = dx; a.ldo = lddx; a.partial = nullptr;
+    if (few_outputs(a.NP, a.NQ, a.C)) launch_few<T, true, LOW>(a, st);
+    else launch_tiles<T, true, false, false, LOW>(a, small_tiles<T>(a.NP, a.NQ), st);
+  }
+}
+
 template <class T>
 void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
-              const void* pre, int64_t ldpre, int32_t act, void* dx, int64_t lddx, void* dw, int64_t lddw, float* dbias,
+              const void* pre, int64_t ldpre, int32_t act, bool two, void* dx, int64_t lddx, void* dw, int64_t lddw, float* dbias,
               char* workspace, const Room& room, hipStream_t st) {
   const void* dp = dy;
-  int64_t lddp = lddy;
+  int64_t lddp = lddy, low = 0;
   const int64_t blocks = slope_blocks(R, M, Elem<T>::kPer);
-  float* sums = reinterpret_cast<float*>(workspace + room.sums);
+  float *sums = reinterpret_cast<float*>(workspace + room.sums), *partial = reinterpret_cast<float*>(workspace + room.partial);
   if (R > 0 && (dbias || act != DGC_LINEAR_NONE)) {
     SlopeArgs s{};
     s.dy = dy; s.lddy = lddy; s.pre = pre; s.ldpre = ldpre; s.R = R; s.M = M; s.act = act;
@@ -810,31 +885,18 @@ void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const vo
     if (act != DGC_LINEAR_NONE) {
       s.dp = workspace + room.dp;
       s.lddp = (M + Elem<T>::kPer - 1) / Elem<T>::kPer * Elem<T>::kPer;
+      if (two) {      // a row's low parts behind its high ones
+        s.low = low = s.lddp;
+        s.lddp *= 2;
+      }
       dp = s.dp; lddp = s.lddp;
     }
-    launch_slope<T>(s, blocks, st);
+    if (two && s.dp) launch_slope<T, sizeof(T) == 2>(s, blocks, st);
+    else launch_slope<T, false>(s, blocks, st);
   }
   if (dbias) hipLaunchKernelGGL(k_linear_dbias, (unsigned)((M + 15) / 16), 1024, 0, st, sums, R > 0 ? blocks : 0, M, dbias);
-  if (dw) {
-    const Split s = split_of(R, K, M);
-    LinearArgs a{};
-    a.P = x; a.ldp = ldx; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = M; a.C = R; a.share = s.share; a.parts = s.parts;
-    a.out = dw; a.ldo = lddw; a.partial = reinterpret_cast<float*>(workspace + room.partial);
-    if (s.parts == 1) {
-      launch_tiles<T, true, true, false>(a, s.small, st);
-    } else {
-      launch_tiles<T, true, true, true>(a, s.small, st);
-      const int64_t n = (int64_t)M * ((K + 3) / 4);
-      hipLaunchKernelGGL(k_linear_join<T>, (unsigned)((n + 15) / 16), 256, 0, st, a);
-    }
-  }
-  if (dx && R > 0) {
-    LinearArgs a{};
-    a.P = w; a.ldp = ldw; a.NP = K; a.Q = dp; a.ldq = lddp; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
-    a.out = dx; a.ldo = lddx;
-    if (few_outputs(a.NP, a.NQ, a.C)) launch_few<T, true>(a, st);
-    else launch_tiles<T, true, false, false>(a, small_tiles<T>(a.NP, a.NQ), st);
-  }
+  if (two && low > 0) products<T, sizeof(T) == 2>(dp, lddp, low, x, ldx, w, ldw, R, K, M, dx, lddx, dw, lddw, partial, st);
+  else products<T, false>(dp, lddp, 0, x, ldx, w, ldw, R, K, M, dx, lddx, dw, lddw, partial, st);
 }
 
 const char* check(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
@@ -853,7 +915,7 @@ using namespace dgc;
 extern "C" {
 
 int64_t dgc_linear_workspace_bytes(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
-  if (check(R, K, M, dtype, act)) return -1;
+  if (check(R, K, M, dtype, activation_of(act))) return -1;
   return room_of(R, K, M, dtype, act).all;
 }
 
@@ -876,14 +938,14 @@ dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64
   a.out = y; a.ldo = ldy; a.bias = bias; a.residual = residual; a.ldr = ldr; a.pre = pre; a.ldpre = ldpre;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (few_outputs(M, R, K)) {
-    if (dtype == DGC_DTYPE_F32) launch_few<float, false>(a, st);
-    else launch_few<uint16_t, false>(a, st);
+    if (dtype == DGC_DTYPE_F32) launch_few<float, false, false>(a, st);
+    else launch_few<uint16_t, false, false>(a, st);
   } else if (short_rows(a, dtype)) {
     launch_rows(a, st);
   } else if (dtype == DGC_DTYPE_F32) {
-    launch_tiles<float, false, false, false>(a, small_tiles<float>(M, R), st);
+    launch_tiles<float, false, false, false, false>(a, small_tiles<float>(M, R), st);
   } else {
-    launch_tiles<uint16_t, false, false, false>(a, small_tiles<uint16_t>(M, R), st);
+    launch_tiles<uint16_t, false, false, false, false>(a, small_tiles<uint16_t>(M, R), st);
   }
   return ops::launched("linear");
 }
@@ -892,9 +954,11 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
                                  int32_t K, int32_t M, int32_t dtype, const void* pre, int64_t ldpre, int32_t act, void* dx,
                                  int64_t lddx, void* dw, int64_t lddw, float* dbias, void* workspace, int64_t workspace_bytes,
                                  void* stream) {
-  if (const char* msg = check(R, K, M, dtype, act)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
+  const bool two = parted(dtype, act);
+  const int32_t f = activation_of(act);
+  if (const char* msg = check(R, K, M, dtype, f)) return ops::refuse(DGC_ERR_INVALID_ARG, msg);
   const int e = ops::elem_bytes(dtype);
-  const bool pre_used = act != DGC_LINEAR_NONE;
+  const bool pre_used = f != DGC_LINEAR_NONE;
   if (!ops::good_rows(dy, R, M, lddy, e) || (dw && !ops::good_rows(x, R, K, ldx, e)) || (dx && !ops::good_rows(w, M, K, ldw, e)) ||
       (pre_used && !ops::good_rows(pre, R, M, ldpre, e)) || (dx && !ops::good_rows(dx, R, K, lddx, e)) ||
       (dw && !ops::good_rows(dw, M, K, lddw, e)))
@@ -914,9 +978,9 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   if (dtype == DGC_DTYPE_F32)
-    backward<float>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, act, dx, lddx, dw, lddw, dbias, ws, room, st);
+    backward<float>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, f, false, dx, lddx, dw, lddw, dbias, ws, room, st);
   else
-    backward<uint16_t>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, act, dx, lddx, dw, lddw, dbias, ws, room, st);
+    backward<uint16_t>(dy, lddy, x, ldx, w, ldw, R, K, M, pre, ldpre, f, two, dx, lddx, dw, lddw, dbias, ws, room, st);
   return ops::launched("linear");
 }
 

@@ -19,7 +19,8 @@ NAMES = ["norm1.weight", "norm1.bias", "qkv.weight", "qkv.bias", "out.weight", "
 
 class TimeBlock:
     """width = heads * size of a head (a multiple of 8, at most 128); hidden: width between up and down.  decay: one number in
-    [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.
+    [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.  exact: binding.linear_backward's, for
+    the gradients behind the activation.
 
     Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad": they and release()
     wait for the device, forward and backward only enqueue.  A block runs one call at a time.  Its buffers are made at the first call
@@ -29,13 +30,13 @@ class TimeBlock:
     SIZES = 8      # a program trains, evaluates and steps at a few sizes; the vertices of a served graph change in number for ever
 
     def __init__(self, width: int, heads: int, hidden: int, *, dtype: str = "f32", act: str = "gelu", decay=None, eps: float = 1e-5,
-                 device="cuda:0"):
+                 exact: bool = False, device="cuda:0"):
         import torch
         if heads < 1 or width % heads or (width // heads) % 8 or width // heads > 128:
             raise ValueError("width must be heads times a multiple of 8 that is at most 128")
         if hidden < 1 or act not in binding.LINEAR_ACT or dtype not in binding.DTYPE:
             raise ValueError("unknown activation or element type, or hidden < 1")
-        self.width, self.heads, self.hidden, self.act, self.eps = width, heads, hidden, act, float(eps)
+        self.width, self.heads, self.hidden, self.act, self.eps, self.exact = width, heads, hidden, act, float(eps), bool(exact)
         self.dtype_name, self.dtype = dtype, {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.device = torch.device(device)
         if self.device.index is None:
@@ -138,7 +139,7 @@ class TimeBlock:
                 b[k] = torch.empty(R, device=self.device)
             b["du"], b["dw"], b["dm"] = self._room((T, N, Hd), self.dtype), self._room((T, N, W), self.dtype), self._room((T, N, W), self.dtype)
             b["dqkv"] = self._room((T, N, 3 * W), self.dtype)
-            size = lambda k, m, act: binding.linear_workspace_bytes(R, k, m, dtype=self.dtype_name, act=act)  # noqa: E731
+            size = lambda k, m, act: binding.linear_workspace_bytes(R, k, m, dtype=self.dtype_name, act=act, exact=self.exact)  # noqa: E731
             ws = max(ws, binding.norm_workspace_bytes(R, W), size(W, 3 * W, "none"), size(W, W, "none"), size(W, Hd, self.act),
                      size(Hd, W, "none"))
             if not self._g:
@@ -257,7 +258,7 @@ class TimeBlock:
         lin = lambda dy, x, n, dx, **kw: binding.linear_backward(dy, x, p[n + ".weight"], dx=dx, dw=g[n + ".weight"], dbias=g[n + ".bias"],  # noqa: E731
                                                                   workspace=ws, stream=stream, **kw)
         lin(dY, b["u"], "down", b["du"])
-        lin(b["du"], b["n2"], "up", b["dw"], pre=b["pre"], act=self.act)
+        lin(b["du"], b["n2"], "up", b["dw"], pre=b["pre"], act=self.act, exact=self.exact)
         binding.norm_backward(b["dw"], b["m"], b["mean2"], b["rstd2"], b["dm"], gamma=p["norm2.weight"], add=dY, dgamma=g["norm2.weight"],
                               dbeta=g["norm2.bias"], workspace=ws, stream=stream)
         lin(b["dm"], b["o"], "out", b["dw"])

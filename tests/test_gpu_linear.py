@@ -265,3 +265,82 @@ def test_activations_far_below_zero():
         far = (P < -2) | (P > -0.5)
         rel = ((dx.double() - slope) / slope).detach()[far]
         assert float(rel.abs().max()) <= 2.0 ** -8 + 1e-4, act
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_backward_with_dp_in_two_parts(shape):
+    """exact=True: dp is off by 2^-16 of itself, not by a bf16 rounding; else the tolerances of test_backward.  Without a GELU or SILU it changes nothing."""
+    import torch
+    from paper_2309_03523_amd import binding
+    R, K, M = shape
+    g = torch.Generator(device="cuda").manual_seed(R + K + M + 2)
+    _, x = _rows(g, R, K, "bf16", extra=1)
+    _, w = _rows(g, M, K, "bf16", K ** -0.5, extra=R % 2)
+    _, dy = _rows(g, R, M, "bf16", extra=1)
+    _, pre = _rows(g, R, M, "bf16", 1.5)
+    for k, act in enumerate(ACTS):
+        out = []
+        for exact in (True, False):
+            bufx, dx = _rows(g, R, K, "bf16", extra=k)
+            bufw, dw = _rows(g, M, K, "bf16", extra=1)
+            db = torch.empty(M, device="cuda")
+            n = binding.linear_workspace_bytes(R, K, M, dtype="bf16", act=act, exact=exact)
+            ws = torch.full((n // 4 + 1,), float("nan"), device="cuda")
+            binding.linear_backward(dy, x, w, pre=pre, act=act, dx=dx, dw=dw, dbias=db, workspace=ws, exact=exact)
+            assert bool(torch.isnan(bufx[:, K:]).all()) and bool(torch.isnan(bufw[:, K:]).all())
+            out.append((dx, dw, db))
+        (dx, dw, db), rounded = out
+        assert torch.equal(db, rounded[2])
+        if act in ("none", "relu"):
+            assert torch.equal(dx, rounded[0]) and torch.equal(dw, rounded[1])
+            continue
+        p = pre.double().requires_grad_()
+        dp, = torch.autograd.grad(_act(p, act), p, dy.double())
+        slack = 4e-6 * dy.double().abs()
+        for got, a, b, n in ((dx, dp, w.double(), M), (dw, dp.t(), x.double(), R)):
+            want, mag = _mm(a, b), _mm(a.abs(), b.abs())
+            extra = _mm(slack if a is dp else slack.t(), b.abs())
+            tol = HALF["bf16"] * want.abs() + (_sum_tol(min(n, 4096)) + 2.0 ** -16 + 2.0 ** -20) * mag + extra
+            assert bool(((got.double() - want).abs() <= tol).all()), (act, n)
+
+
+@pytest.mark.parametrize("exact", [False, True])
+@pytest.mark.parametrize("R", [20, 300])
+def test_gradients_that_are_not_finite_stay_where_they_belong(R, exact):
+    """An infinity or NaN in dy, x or w reaches the gradients that the formula lets it reach, with its sign, in one part or two."""
+    import torch
+    from paper_2309_03523_amd import binding
+    g = torch.Generator(device="cuda").manual_seed(R)
+    (x, w, dy, pre) = (torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16) for s in ((R, 72), (88, 72), (R, 88), (R, 88)))
+    pre[5, :8] = 30.0        # dp is dy there: its low part is nothing
+    w[3, 7], x[5, 9], dy[11, 20], dy[13, 30], w[60, 70] = float("inf"), float("-inf"), float("inf"), float("nan"), float("-inf")
+    for act in ("gelu", "silu"):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        ws = torch.empty(binding.linear_workspace_bytes(R, 72, 88, dtype="bf16", act=act, exact=exact), dtype=torch.uint8, device="cuda")
+        binding.linear_backward(dy, x, w, pre=pre, act=act, dx=dx, dw=dw, workspace=ws, exact=exact)
+        p = pre.double().requires_grad_()
+        slope, = torch.autograd.grad(_act(p, act).sum(), p)
+        dp = slope * dy.double()
+        for got, want in ((dx, _mm(dp, w.double())), (dw, _mm(dp.t(), x.double()))):
+            assert torch.equal(torch.isnan(got), torch.isnan(want)), act
+            infinite = torch.isinf(want)
+            assert torch.equal(torch.isinf(got), infinite) and torch.equal(got[infinite].double(), want[infinite]), act
+
+
+def test_the_error_of_gradients_with_and_without_two_parts():
+    """Rounding errors of one bf16 number spread over +-2^-9 to 2^-8 of the value: 1.7e-3 of the norm.  dp's own, of the same size, comes on top
+    (root of the sum of squares: 2.3e-3) unless it enters in two parts."""
+    import torch
+    from paper_2309_03523_amd import binding
+    g = torch.Generator(device="cuda").manual_seed(3)
+    R, K, M = 5000, 128, 512
+    x, w, dy, pre = (torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16) for s in ((R, K), (M, K), (R, M), (R, M)))
+    p = pre.double().requires_grad_()
+    dp, = torch.autograd.grad(_act(p, "gelu"), p, dy.double())
+    for exact in (True, False):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        ws = torch.empty(binding.linear_workspace_bytes(R, K, M, dtype="bf16", act="gelu", exact=exact), dtype=torch.uint8, device="cuda")
+        binding.linear_backward(dy, x, w, pre=pre, act="gelu", dx=dx, dw=dw, workspace=ws, exact=exact)
+        for got, want in ((dx, _mm(dp, w.double())), (dw, _mm(dp.t(), x.double()))):
+            off = float((got.double() - want).norm() / want.norm())
+            assert (off <= 1.75e-3) == exact and off <= 2.6e-3, off

@@ -360,3 +360,31 @@ def test_buffers_of_many_sizes():
     torch.cuda.synchronize()
     assert all(torch.equal(o, want[:, :o.shape[1]]) for o in out)
     del used
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu"])
+def test_gradients_behind_the_activation_in_two_parts(act):
+    """exact=True: the gradients that a rounded dy act'(p) reaches (up, its bias not, and what lies before it) come closer to the formula's, the others
+    are the same bits; with RELU all are."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W = 11, 60, 64
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x, dy = (torch.randn(T, N, W, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    grads = []
+    for exact in (False, True):
+        block = TimeBlock(W, 4, 200, dtype="bf16", act=act, exact=exact)
+        host = _params(block, 12)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        block.forward(x, y)
+        block.backward(dy, dX=dx)
+        grads.append({"x": dx.float().cpu().numpy(), **{n: block.get_param(n + ".grad") for n in block.shapes}})
+    same = {n for n in grads[0] if np.array_equal(grads[0][n], grads[1][n])}
+    assert same == (set(grads[0]) if act == "relu" else {"up.bias", "down.weight", "down.bias"})
+    P = {n: torch.from_numpy(a).cuda().double().requires_grad_() for n, a in host.items()}
+    X = x.double().requires_grad_()
+    want, _ = _formula(block, P, X, torch.zeros(N, 4, 16, 16, dtype=torch.float64, device="cuda"), None, None)
+    (want * dy.double()).sum().backward()
+    for n in ("x", "up.weight"):
+        w = X.grad if n == "x" else P[n].grad
+        _near(torch.from_numpy(grads[1][n]).cuda(), w, "bf16")

@@ -255,3 +255,17 @@ def test_decay_attention_refuses_states_over_other_tensors(lib):
     for kw in (dict(ds0=S + 16), dict(ds0=D0 - 16), dict(ds0=A), dict(ds0=F + 64), dict(ds0=G[2]), dict(s0=G[0]), dict(dsn=G[1] + rows - 16), dict(ds0=G[0] - size + 16)):
         assert bwd(**kw) == INVALID, kw
         assert "state" in _text(lib)
+
+
+def test_two_parts_ask_for_more_workspace(lib):
+    """DGC_LINEAR_EXACT (16) with an activation, in the backward calls alone; it needs room where dp takes two parts."""
+    size = lib.dgc_linear_workspace_bytes
+    for act in range(4):
+        assert size(1000, 64, 96, 0, 16 + act) == size(1000, 64, 96, 0, act)
+        more = size(1000, 64, 96, 1, 16 + act) - size(1000, 64, 96, 1, act)
+        assert more == (1000 * 96 * 2 if act in (2, 3) else 0)
+    assert all(size(10, 8, 8, 1, act) < 0 for act in (-1, 4, 15, 20, 32))
+    assert lib.dgc_linear_forward(A, 32, B, 32, 10, 30, 20, 1, None, 18, None, 0, C, 24, None, 0, None) == INVALID and "activation" in _text(lib)
+    need = size(10, 32, 24, 1, 2)
+    args = (C, 24, A, 32, B, 32, 10, 32, 24, 1, 0x40000000, 24, 18, 0x50000000, 32, 0x60000000, 32, None, 0x70000000, need, None)
+    assert lib.dgc_linear_backward(*args) == INVALID and "workspace" in _text(lib)
