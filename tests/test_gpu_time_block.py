@@ -388,3 +388,61 @@ def test_gradients_behind_the_activation_in_two_parts(act):
     for n in ("x", "up.weight"):
         w = X.grad if n == "x" else P[n].grad
         _near(torch.from_numpy(grads[1][n]).cuda(), w, "bf16")
+
+
+def _near_in_rows(got, want, limit, name):
+    """Every row's error within `limit` of the tensor's root mean square, every element's within five times that.
+
+    An activation's rounding is off by at most half a step, 2^-8 of it.  From X to Y there are seven of them (n, q/k/v, o, m, n2, u, Y), ten
+    with the gradients' way back, doubled where two branches add up: 0.08, as for the whole tensor.  Of a row that is a bound as well: the
+    products' rows have norms near 1, so a row's error is a sum of as many roundings.  A row's elements scatter about it: five deviations hold
+    a hundred thousand of them.  States are sums of k and v, two roundings each (n, then the product's): 4 * 2^-8 = 0.016, rounded up to 0.02; the first state's
+    gradient is one of q (2) and of o's gradient (du, n2's, m's, o's and Y's own twice over the branches): 10 * 2^-8 = 0.04."""
+    want = want.detach()
+    rms = want.square().mean().sqrt()
+    err = got.double() - want
+    row = err.square().mean(-1).sqrt() if want.dim() > 1 else err.abs() / 5
+    assert bool((row <= limit * rms).all()), (name, float(row.max() / rms))
+    assert bool((err.abs() <= 5 * limit * rms).all()), (name, float(err.abs().max() / rms))
+
+
+def _formula_with_sides(block, P, x, s0, lengths, reset, above):
+    """_formula with RELU's side of zero given: the slope there is a step, so an argument that a rounding carries over zero, one in a hundred
+    of them, changes its gradient by all of it (two in a hundred of the squares: 0.1 to 0.2 of the root mean square)."""
+    import torch
+    nothing = {k: torch.zeros_like(P[k]) for k in ("down.weight", "down.bias")}
+    m, S = _formula(block, {**P, **nothing}, x, s0, lengths, reset)
+    p = _norm(m, P["norm2.weight"], P["norm2.bias"], block.eps) @ P["up.weight"].t() + P["up.bias"]
+    return m + torch.where(above, p, 0.0) @ P["down.weight"].t() + P["down.bias"], S
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("case", CASES + [(130, 33, 96, 12, 200, "silu"), (32, 70, 128, 4, 512, "gelu")])
+def test_bf16_row_by_row(case, ragged):
+    """A defect in one token, one sequence or the last tile shows, where the whole tensor's mean hides it."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W, h, hidden, act = case
+    block = TimeBlock(W, h, hidden, dtype="bf16", act=act)
+    host = _params(block, T + 1)
+    g = torch.Generator(device="cuda").manual_seed(T * N)
+    x, dy = (torch.randn(T, N, W, generator=g, device="cuda").to(block.dtype) for _ in range(2))
+    s0, dsn = (torch.randn(N, h, W // h, W // h, generator=g, device="cuda") for _ in range(2))
+    reset = (torch.rand(T, N, generator=g, device="cuda") < 0.05).to(torch.uint8)
+    lengths = torch.randint(0, T + 1, (N,), generator=g, device="cuda", dtype=torch.int32) if ragged else None
+    y, sn, dx, ds0 = torch.empty_like(x), torch.empty_like(s0), torch.empty_like(x), torch.empty_like(s0)
+    block.forward(x, y, S0=s0, SN=sn, reset=reset, lengths=lengths)
+    block.backward(dy, dX=dx, dSN=dsn, dS0=ds0)
+    P = {n: torch.from_numpy(a).cuda().double().requires_grad_() for n, a in host.items()}
+    X, S = x.double().requires_grad_(), s0.double().requires_grad_()
+    if act == "relu":
+        want, last = _formula_with_sides(block, P, X, S, lengths, reset, block._buffers[T, N, True]["pre"] > 0)
+    else:
+        want, last = _formula(block, P, X, S, lengths, reset)
+    ((want * dy.double()).sum() + (last * dsn.double()).sum()).backward()
+    _near_in_rows(y, want, 0.08, "y")
+    _near_in_rows(dx, X.grad, 0.08, "dx")
+    _near_in_rows(sn.flatten(2), last.flatten(2), 0.02, "sn")
+    _near_in_rows(ds0.flatten(2), S.grad.flatten(2), 0.04, "ds0")
+    for n in P:
+        _near_in_rows(torch.from_numpy(block.get_param(n + ".grad")).cuda(), P[n].grad, 0.08, n)
