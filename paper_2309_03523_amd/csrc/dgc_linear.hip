@@ -20,6 +20,7 @@
 //    fragments come straight from memory.
 #include <algorithm>
 
+#include "dgc_join.h"
 #include "dgc_ops.h"
 #include "dgc_split_dev.h"
 
@@ -825,25 +826,6 @@ Room room_of(int64_t R, int32_t K, int32_t M, int32_t dtype, int32_t act) {
   return r;
 }
 
-// Partial rows of dbias [parts][M] -> dbias, in double: 16 columns a workgroup, 64 partial rows at a time.
-__global__ __launch_bounds__(1024) void k_linear_dbias(const float* partial, int64_t parts, int32_t M, float* dbias) {
-  __shared__ double lds[64][16];
-  const int c = threadIdx.x & 15, p = threadIdx.x >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 16 + c;
-  double s = 0.;
-  if (col < M) {
-    for (int64_t k = p; k < parts; k += 64) s += (double)partial[k * M + col];
-  }
-  lds[p][c] = s;
-  __syncthreads();
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    if (p < m) lds[p][c] += lds[p + m][c];
-    __syncthreads();
-  }
-  if (p == 0 && col < M) dbias[col] = (float)lds[0][c];
-}
-
 // dx and dw from dp, whose low part lies `low` elements behind it (LOW).
 template <class T, bool LOW>
 void products(const void* dp, int64_t lddp, int64_t low, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t R, int32_t K, int32_t M,
@@ -894,7 +876,7 @@ void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const vo
     if (two && s.dp) launch_slope<T, sizeof(T) == 2>(s, blocks, st);
     else launch_slope<T, false>(s, blocks, st);
   }
-  if (dbias) hipLaunchKernelGGL(k_linear_dbias, (unsigned)((M + 15) / 16), 1024, 0, st, sums, R > 0 ? blocks : 0, M, dbias);
+  if (dbias) join_columns(sums, R > 0 ? blocks : 0, M, M, dbias, nullptr, st);
   if (two && low > 0) products<T, sizeof(T) == 2>(dp, lddp, low, x, ldx, w, ldw, R, K, M, dx, lddx, dw, lddw, partial, st);
   else products<T, false>(dp, lddp, 0, x, ldx, w, ldw, R, K, M, dx, lddx, dw, lddw, partial, st);
 }

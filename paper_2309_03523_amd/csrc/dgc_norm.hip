@@ -13,6 +13,7 @@
 // 1000 rows of 172 fp32 5.5 us, two dependent reductions behind one load.
 #include <algorithm>
 
+#include "dgc_join.h"
 #include "dgc_ops.h"
 
 namespace dgc {
@@ -232,28 +233,6 @@ __global__ __launch_bounds__(256) void k_norm_backward(NormArgs a) {
   }
 }
 
-// Sixteen of the 2 F columns a workgroup, 64 partial rows at a time; the sums in double.
-__global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int64_t parts, int32_t F, float* dgamma, float* dbeta) {
-  __shared__ double lds[64][16];
-  const int c = threadIdx.x & 15, p = threadIdx.x >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 16 + c;
-  double s = 0.;
-  if (col < 2 * F) {
-    for (int64_t k = p; k < parts; k += 64) s += (double)partial[k * 2 * F + col];
-  }
-  lds[p][c] = s;
-  __syncthreads();
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    if (p < m) lds[p][c] += lds[p + m][c];
-    __syncthreads();
-  }
-  if (p == 0 && col < 2 * F) {
-    float* to = col < F ? dgamma : dbeta;
-    if (to) to[col < F ? col : col - F] = (float)lds[0][c];
-  }
-}
-
 struct Shape { int lpr, nv, u; };   // lanes a row, vectors a lane, rows in flight
 
 // As few lanes a row as hold it in one vector each, up to a wave; then up to four vectors a lane; then a workgroup a row.
@@ -371,7 +350,7 @@ dgc_status_t dgc_norm_backward(const void* dy, int64_t lddy, const void* x, int6
     if (dtype == DGC_DTYPE_F32) launch<float, true>(a, blocks, st);
     else launch<uint16_t, true>(a, blocks, st);
   }
-  if (sums) hipLaunchKernelGGL(k_norm_join, (unsigned)((2 * F + 15) / 16), 1024, 0, st, a.partial, R > 0 ? blocks : 0, F, dgamma, dbeta);
+  if (sums) join_columns(a.partial, R > 0 ? blocks : 0, 2 * F, F, dgamma, dbeta, st);
   return ops::launched("norm");
 }
 
