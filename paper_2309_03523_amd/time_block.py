@@ -149,25 +149,23 @@ class TimeBlock:
         b["ws"] = torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device)
         if stream is not None:     # the zeros above were written on the current stream
             stream.wait_stream(torch.cuda.current_stream(self.device))
-        b["on"], b["captured"] = set(), False
+        b["home"], b["done"], b["captured"] = torch.cuda.current_stream(self.device), None, False
         self._buffers[key] = b
-        old = [k for k, s in self._buffers.items() if not s["captured"]][:-self.SIZES]
-        for k in old:
-            self._drop(self._buffers.pop(k))
+        for k in [k for k, s in self._buffers.items() if not s["captured"]][:-self.SIZES]:
+            old = self._buffers.pop(k)
+            if old["done"] is not None:      # the allocator hands its memory to what is enqueued on that stream from here on
+                old["home"].wait_event(old["done"])
         return b
 
     def _used(self, b, stream):
-        """Notes where a call runs that uses a set of buffers."""
+        """Notes where a call ran that uses a set of buffers: in a graph, or, for the stream that they were made on, on another one."""
         import torch
-        b["on"].add(stream if stream is not None else torch.cuda.current_stream(self.device))
-        b["captured"] |= self._capturing(stream)
-
-    @staticmethod
-    def _drop(b):
-        """Leaves a set of buffers to the allocator, which is told of the streams that may still use them."""
-        for t in b.values():
-            for stream in b["on"] if hasattr(t, "record_stream") else ():
-                t.record_stream(stream)
+        on = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if self._capturing(stream):
+            b["captured"] = True
+        elif on != b["home"]:
+            b["done"] = b["done"] or torch.cuda.Event()
+            b["done"].record(on)
 
     def _kept(self, b, S0, stream):
         """A copy of the first state, which the call is about to overwrite, for backward."""
@@ -178,7 +176,10 @@ class TimeBlock:
         if "s0" not in b:
             if self._capturing(stream):
                 raise RuntimeError("a state in place is new to these sizes: make one eager call of it before the captured one")
-            b["s0"] = torch.empty(shape, device=self.device)
+            with torch.cuda.stream(b["home"]):
+                b["s0"] = torch.empty(shape, device=self.device)
+            if stream is not None:
+                stream.wait_stream(b["home"])
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             b["s0"].copy_(S0)
         return b["s0"]
@@ -223,10 +224,18 @@ class TimeBlock:
         if train and self._overlap(X, Y):
             raise ValueError("with train=True Y must lie apart from X, which backward reads")
         T, N = X.shape[:2]
-        b, p, W = self._made(T, N, train, stream), self._p, self.width
-        self._used(b, stream)
-        if train and self._overlap(S0, SN):
-            S0 = self._kept(b, S0, stream)
+        b = self._made(T, N, train, stream)
+        try:
+            if train and self._overlap(S0, SN):
+                S0 = self._kept(b, S0, stream)
+            self._forward(b, X, Y, S0, SN, lengths, reset, stream)
+        finally:
+            self._used(b, stream)
+        self._last = (b, X, S0, lengths, reset) if train else None
+        return Y
+
+    def _forward(self, b, X, Y, S0, SN, lengths, reset, stream):
+        p, W = self._p, self.width
         q, k, v = b["qkv"][..., :W], b["qkv"][..., W:2 * W], b["qkv"][..., 2 * W:]
         binding.norm_forward(X, b["n"], gamma=p["norm1.weight"], beta=p["norm1.bias"], mean=b.get("mean1"), rstd=b.get("rstd1"), eps=self.eps,
                              stream=stream)
@@ -239,8 +248,6 @@ class TimeBlock:
                              eps=self.eps, stream=stream)
         binding.linear_forward(b["n2"], p["up.weight"], b["u"], bias=p["up.bias"], act=self.act, pre=b.get("pre"), stream=stream)
         binding.linear_forward(b["u"], p["down.weight"], Y, bias=p["down.bias"], residual=b["m"], stream=stream)
-        self._last = (b, X, S0, lengths, reset) if train else None
-        return Y
 
     def backward(self, dY, *, dX=None, dSN=None, dS0=None, stream=None):
         """Gradients of the last forward with train=True: of the parameters (get_param("<name>.grad")), of X into dX if given
@@ -251,9 +258,13 @@ class TimeBlock:
         self._rows(dY, "dY", X)
         if dX is not None:
             self._rows(dX, "dX", X)
-        p, g, W = self._p, self._g, self.width
-        self._used(b, stream)
-        ws = b["ws"]
+        try:
+            self._backward(b, X, S0, lengths, reset, dY, dX, dSN, dS0, stream)
+        finally:
+            self._used(b, stream)
+
+    def _backward(self, b, X, S0, lengths, reset, dY, dX, dSN, dS0, stream):
+        p, g, W, ws = self._p, self._g, self.width, b["ws"]
         cut = lambda t: (t[..., :W], t[..., W:2 * W], t[..., 2 * W:])  # noqa: E731
         lin = lambda dy, x, n, dx, **kw: binding.linear_backward(dy, x, p[n + ".weight"], dx=dx, dw=g[n + ".weight"], dbias=g[n + ".bias"],  # noqa: E731
                                                                   workspace=ws, stream=stream, **kw)

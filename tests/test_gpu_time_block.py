@@ -446,3 +446,28 @@ def test_bf16_row_by_row(case, ragged):
     _near_in_rows(ds0.flatten(2), S.grad.flatten(2), 0.04, "ds0")
     for n in P:
         _near_in_rows(torch.from_numpy(block.get_param(n + ".grad")).cuda(), P[n].grad, 0.08, n)
+
+
+def test_a_state_in_place_on_another_stream():
+    """The copy of the first state is made, and used, on the call's stream."""
+    import torch
+    from paper_2309_03523_amd.time_block import TimeBlock
+    T, N, W, h = 6, 400, 64, 4
+    block = TimeBlock(W, h, 64)
+    _params(block, 14)
+    x, dy = torch.randn(T, N, W, device="cuda"), torch.randn(T, N, W, device="cuda")
+    first = torch.randn(N, h, W // h, W // h, device="cuda")
+    y, dx, s = torch.empty_like(x), torch.empty_like(x), torch.empty_like(first)
+    block.forward(x, y, S0=first, SN=s)
+    block.backward(dy, dX=dx)
+    want = [t.clone() for t in (y, dx, s)]
+    s.copy_(first)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    _busy(stream)
+    block.forward(x, y, S0=s, SN=s, stream=stream)
+    block.backward(dy, dX=dx, stream=stream)
+    used = [torch.full_like(first, float("nan")) for _ in range(4)]
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((y, dx, s), want))
+    del used
