@@ -760,10 +760,12 @@ void launch_slope(const SlopeArgs& a, int64_t blocks, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------- host
 
 // 128 x 128 outputs a workgroup; 64 x 64 where that leaves compute units without work, or the output is that narrow.
-// (100 000 rows 172 -> 128 in fp32, 782 large tiles: 59 us in small ones, 65 in large.)
-template <class T>
+// fp32 forward, small against large tiles, us: 100 000 rows 172 -> 128 (782 large tiles) 52, 56; 40 000 256 -> 256 (626) 49, 56; 120 000 128 -> 128 (938) 42, 43;
+// 25 000 512 -> 512 (784) 113, 106.  fp32 dx, where a tile's weights are turned and split, too, so that small tiles repeat more: 60 001 256 -> 256 (938) 85, 72; 25 000
+// 512 -> 512 (784) 134, 114; 120 000 128 -> 128 (938) 50, 46; 40 000 256 -> 256 (626) 58, 62; 4000 1024 -> 1024 (256) 101, 92.
+template <class T, bool ACROSS_P>
 bool small_tiles(int64_t NP, int64_t NQ) {
-  return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < (sizeof(T) == 4 ? 1024 : 256);
+  return NP <= 64 || NQ <= 64 || ((NP + 127) / 128) * ((NQ + 127) / 128) < (sizeof(T) == 4 && !ACROSS_P ? 1024 : 256);
 }
 
 // Up to 32 rows, or so few tiles with so long a contraction that it is better split over the waves of more workgroups: bf16 100 x 4000 -> 50
@@ -848,7 +850,7 @@ void products(const void* dp, int64_t lddp, int64_t low, const void* x, int64_t 
     a.P = w; a.ldp = ldw; a.NQ = R; a.C = M; a.share = (M + 63) / 64 * 64; a.parts = 1;
     a.out = dx; a.ldo = lddx; a.partial = nullptr;
     if (few_outputs(a.NP, a.NQ, a.C)) launch_few<T, true, LOW>(a, st);
-    else launch_tiles<T, true, false, false, LOW>(a, small_tiles<T>(a.NP, a.NQ), st);
+    else launch_tiles<T, true, false, false, LOW>(a, small_tiles<T, true>(a.NP, a.NQ), st);
   }
 }
 
@@ -925,9 +927,9 @@ dgc_status_t dgc_linear_forward(const void* x, int64_t ldx, const void* w, int64
   } else if (short_rows(a, dtype)) {
     launch_rows(a, st);
   } else if (dtype == DGC_DTYPE_F32) {
-    launch_tiles<float, false, false, false, false>(a, small_tiles<float>(M, R), st);
+    launch_tiles<float, false, false, false, false>(a, small_tiles<float, false>(M, R), st);
   } else {
-    launch_tiles<uint16_t, false, false, false, false>(a, small_tiles<uint16_t>(M, R), st);
+    launch_tiles<uint16_t, false, false, false, false>(a, small_tiles<uint16_t, false>(M, R), st);
   }
   return ops::launched("linear");
 }
