@@ -173,14 +173,14 @@ class TimeBlock:
         shape = (b["m"].shape[1], self.heads, self.width // self.heads, self.width // self.heads)
         if S0.shape != shape or S0.dtype != torch.float32 or S0.device != self.device:
             raise ValueError(f"S0 must be float32 {list(shape)} on the block's device")
+        on = stream if stream is not None else torch.cuda.current_stream(self.device)
         if "s0" not in b:
             if self._capturing(stream):
                 raise RuntimeError("a state in place is new to these sizes: make one eager call of it before the captured one")
             with torch.cuda.stream(b["home"]):
                 b["s0"] = torch.empty(shape, device=self.device)
-            if stream is not None:
-                stream.wait_stream(b["home"])
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            on.wait_stream(b["home"])
+        with torch.cuda.stream(on):
             b["s0"].copy_(S0)
         return b["s0"]
 
