@@ -9,7 +9,8 @@
 //   dv: A, B, C = k, q, do and dk: A, B, C = v, do, q from dS_N (not decayed) and its transpose;   dS_0 = l_0 g G_0.
 //
 // A wave takes 32 tokens of one sequence and head and 32 columns of C at a time and keeps its part of S in registers from one
-// 32 to the next.  All products run on v_mfma_f32_32x32x16_bf16, operands and results in registers, none in LDS:
+// 32 to the next.  All products run on v_mfma_f32_32x32x16_bf16, operands and results in registers (LDS holds outputs on their way to memory,
+// and in k_decay_window_back states of up to 32 x 32 on theirs from it):
 //  - scores D[j][i] = B_j . A_i leave lane i with 16 scores of its own token i in just the order in which a product that sums over
 //    j takes them; C, and B for the state, come into that order by a product with the identity, which is exact;
 //  - the state's rows are kept in the order that makes its registers the operand of A S: row 8g + 4(l/32) + e of a tile is
@@ -206,8 +207,11 @@ __device__ __forceinline__ bool store_rows(T* base, int64_t st, int64_t sn, cons
 }
 
 // KD: dk rounded up to 16, 32, 64 or 128.  OUT: outputs are computed, else states alone.
-// A wave goes over its rows' 32 tokens in turn and has the next ones' on the way while it works.  4 sequences of 8192, 8 heads of 64: 38 us for
-// the states, 10 for the scan, 52 for the outputs; vector instructions (the parts of scores, keys and states) bound it at two waves a SIMD.
+// A wave goes over its rows' 32 tokens in turn and has the next ones' on the way while it works.  4 sequences of 8192, 8 heads of 64, bf16: 32 us
+// for the states, 10 for the scan, 47 for the outputs; vector instructions (the parts of scores, keys and states) bound it at two waves a
+// SIMD, whose 256 registers the outputs' kernel passes by 4, spilled.  In fp32 (211 us in all) a head of 64 takes one wave a SIMD; heads up to 16
+// spill 4, up to 32 18, up to 128 6.  50 000 windows of 16, 8 heads of 16, states in and out: bf16 897 us, fp32 1184, half the wave's
+// tokens idle and a window's states asked for when the one before has ended; 20 000 windows of 32, 4 heads of 32: 282 and 459 us.
 template <class T, int KD, bool OUT>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 64 : 32) ? 2 : 1) void k_decay(DecayArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid;
@@ -499,7 +503,7 @@ __device__ void walk_window(const Walk<T>& w, float* acc) {
 }
 
 // The forward pass of windows of up to 32 tokens from zero states, the states not wanted: nothing is carried.  Two sequences
-// of up to 16 tokens share the 32 of a wave (PAIR).  100 000 windows of 16, 8 heads of 16: 350 to 365 us, 4.5 TB/s and more; memory bounds it.
+// of up to 16 tokens share the 32 of a wave (PAIR).  100 000 windows of 16, 8 heads of 16: 365 us, 4.5 TB/s; memory bounds it (fp32, 50 000: 404).
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (KD <= 32 ? 3 : 2) : (KD <= 64 ? 2 : 1)) void k_decay_window(DecayArgs a) {
   constexpr int KC = KD / 16, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;
@@ -628,8 +632,9 @@ struct BackArgs {
 };
 
 // All gradients of windows of up to 32 tokens, every tensor read once: dk, dv up to KD.  States (not with PAIR) are read and written as
-// they are needed: nothing is carried.  20 000 ragged windows of 32, 4 heads of 32, with states: 457 us, 3.4 TB/s; the registers (256) leave two
-// waves a SIMD, which do not cover all waits.  (Three passes of k_decay took 900.)
+// they are needed: nothing is carried.  20 000 ragged windows of 32, 4 heads of 32, with states: 457 us, 3.4 TB/s; the registers (256, and
+// nine spilled) leave two waves a SIMD, which do not cover all waits.  In fp32 that takes 1338 us at one wave a SIMD; fp32 heads up to 16 with states
+// spill 60 registers, up to 64 134 (4000 windows of 16, 8 heads of 64: 2863 us, bf16 1276).  (Three passes of k_decay took 900.)
 template <class T, int KD, bool PAIR>
 __global__ __launch_bounds__(256, KD <= (sizeof(T) == 2 ? 32 : 16) ? 2 : 1) void k_decay_window_back(BackArgs a) {
   constexpr int KC = KD / 16, KT = (KD + 31) / 32, IN = Kind<T>::kIn, MID = Kind<T>::kMid, PER = PAIR ? 2 : 1;

@@ -332,8 +332,8 @@ __device__ __forceinline__ void load_bias(const LinearArgs& a, int64_t p, float 
   for (int i = 0; i < N; ++i) bias[i] = a.bias && p + i < a.NP ? a.bias[p + i] : 0.f;
 }
 
-// BP x BQ outputs a workgroup, a quarter of them a wave.  Measured: bf16 8192 x 4096 x 4096 366 us (750 TFLOP/s), fp32 8192 x 2048 x
-// 2048 411 us (167 of its own, 1000 of the part products); one tile's loads, products and epilogue follow each other, and two
+// BP x BQ outputs a workgroup, a quarter of them a wave.  Measured: bf16 8192 x 4096 x 4096 355 to 390 us (740 TFLOP/s), fp32 8192 x 2048 x
+// 2048 417 us (165 of its own, 990 of the part products); one tile's loads, products and epilogue follow each other, and two
 // workgroups a CU (registers) cover part of that.
 template <class T, int BP, int BQ, bool ACROSS_P, bool ACROSS_Q, bool PARTIAL, bool LOW>
 __global__ __launch_bounds__(256, BP == 64 ? 3 : 2) void k_linear(LinearArgs a) {
@@ -681,7 +681,7 @@ __device__ __forceinline__ void two_parts(float dp, float& high, float& low) {
   low = fabsf(rest) >= 0x1p-126f || fabsf(dp) < 0x1p-109f ? rest : copysignf(0x1p-126f, dp);
 }
 
-// 400 000 x 512 bf16 with GELU: 260 us, 4.7 TB/s of dy, pre and dp.  LPR lanes a row, 256 / LPR rows at a time; blockIdx.y: which LPR vectors of a wide row.
+// 400 000 x 512 bf16 with GELU: 245 us, 5 TB/s of dy, pre and dp.  LPR lanes a row, 256 / LPR rows at a time; blockIdx.y: which LPR vectors of a wide row.
 template <class T, int LPR, bool LOW>
 __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs a) {
   constexpr int VN = Elem<T>::kPer, GROUPS = 256 / LPR, U = 4;
