@@ -509,6 +509,8 @@ dgc_status_t dgc_linear_backward(const void* dy, int64_t lddy, const void* x, in
  *  workspace: dgc_decay_attn_workspace_bytes bytes (0 unless few long sequences are split; negative for sizes outside the range;
  *   `backward` 0 or 1: which call they are for).
  *  DGC_ERR_UNSUPPORTED for 2^31 and more sequences x heads x blocks of 32 columns.
+ * States are fp32 throughout.  Outputs and gradients in bf16 come of scores and states taken to 2^-16 of themselves and are rounded once; with fp32
+ * all is as exact as fp32 arithmetic.
  * A token that holds an infinity or NaN reaches only the outputs that the formula lets it reach. */
 int64_t dgc_decay_attn_workspace_bytes(int64_t T, int64_t N, int32_t heads, int32_t dk, int32_t dv, int32_t backward);
 dgc_status_t dgc_decay_attn_forward(const void* q, int64_t q_stride_t, int64_t q_stride_n, const void* k, int64_t k_stride_t,
