@@ -76,10 +76,11 @@ def draw(rng):
     d = rng.choice([8, 16, 16, 24, 32, 40, 64, 64, 96, 128])
     kind = rng.choice(["window", "window", "long", "long", "step"])
     way = "forward" if kind == "step" else rng.choice(["forward", "backward"])
-    # A row with one key has no gradient but its rounding's: backward windows are not as short as that.
-    T = {"window": _log_int(rng, 1 if way == "forward" else 6, 64), "long": _log_int(rng, 65, 8192), "step": _log_int(rng, 2, 65536)}[kind]
-    rows = 1 if kind == "step" else T
     pairs = (3e9 if dtype == "bf16" else 3e8) * 16 / (d + 16) / (2.5 if way == "backward" else 1)
+    # A row with one key has no gradient but its rounding's: backward windows are not as short as that.
+    T = {"window": _log_int(rng, 1 if way == "forward" else 6, 64), "long": _log_int(rng, 65, min(8192, (pairs / heads) ** 0.5)),
+         "step": _log_int(rng, 2, 65536)}[kind]
+    rows = 1 if kind == "step" else T
     most = min(100000, pairs / (heads * rows * T), 8e7 / (heads * rows * d), 1.3e8 / (kv_heads * T * d))
     N = _log_int(rng, 1 if way == "forward" or kind == "long" else min(8, most), max(1, most))
     buckets = rng.choice([0, 8, 16, 32, 64])
