@@ -528,6 +528,49 @@ dgc_status_t dgc_decay_attn_backward(const void* q, int64_t q_stride_t, int64_t 
                                      int64_t dk_stride_n, void* dval, int64_t dv_stride_t, int64_t dv_stride_n,
                                      float* ds0, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Softmax attention over the tokens of N sequences (vertices), with a learned bias by buckets of distance: windows of snapshots, long
+ * histories, and single new snapshots against the keys and values that are kept.  Query i of sequence n stands at position
+ * p = first[n] + i (first NULL: Tk - Tq + i), key j at position j.  For head h, which reads key head h / (heads / kv_heads):
+ *   s_j = scale q_i . k_j + bias[h][map[p - j]],   lse_i = log sum e^s_j,   o_i = sum e^(s_j - lse_i) v_j
+ * over the keys that it sees: j < lengths[n] (NULL: Tk; clamped to [0, Tk]), keep[j][n] not 0, and with `causal` j <= p.
+ *  Queries whose position is not in [0, lengths[n]), and keys from lengths[n] on, belong to no token: their rows, and entries of lse, are neither
+ *   read nor written.  A query that sees no key, or only scores of -inf, has o = 0 and lse = -inf, and gives and has no gradient.
+ *   Keys that keep masks get gradients of 0.  What a masked row holds, infinities and NaN included, reaches nothing.
+ *  q, o [heads][d], k, v [kv_heads][d] a row: row (t, n) at base + t * stride_t + n * stride_n elements (both multiples of 16 bytes, bases aligned to
+ *   16).  Inputs may repeat rows (a stride of 0); an output's rows lie apart, and outputs lie apart from inputs and each other
+ *   (side by side in rows of one buffer is apart).
+ *  0 <= Tq <= Tk <= 2^30; heads in [1, 1024], a multiple of kv_heads; d a multiple of 8 in [8, 128].
+ *  first, lengths device int32 [N]; keep device uint8 [Tk][N]; each may be NULL.
+ *  bias device fp32 [heads][buckets] (NULL: none, with buckets = reach = 0), buckets at most 256; map device uint8 [2 reach + 1]: entry c + reach is the bucket
+ *   of distance c = p - j, and distances beyond reach (at most 1024) have the last entries' (numbers from buckets on count as buckets - 1).
+ *  lse device fp32 [N][heads][Tq], NULL = not wanted in the forward pass.
+ *  backward: the wanted ones of dq, dk, dv and dbias (fp32 [heads][buckets], sums over all sequences) from the output's gradient `go`;
+ *   o and lse as the forward pass left them.
+ *  workspace: dgc_attn_workspace_bytes bytes (negative for sizes outside the range; `backward` 0 or 1: which call they are for).
+ *  DGC_ERR_UNSUPPORTED for about 2^24 and more sequences x heads x blocks of 64 tokens.
+ * Scores, weights, their sums and the gradients of scores are fp32; with bf16, weights and gradients of scores are rounded to bf16 (2^-9 of themselves) for the
+ * products that sum them, o and the gradients are rounded once more, and dbias is summed from what is not rounded.  With fp32 all is as exact as fp32 arithmetic.
+ *
+ * dgc_attn_buckets (host arithmetic) fills a map of the usual kind: of the buckets (causal), or of half of them a side (then even; keys
+ *   behind the query have the lower half), the first half holds one distance each, and bucket b of the rest, of n, begins at half (reach / half)^((b - half) / n). */
+dgc_status_t dgc_attn_buckets(int32_t buckets, int32_t reach, int32_t causal, uint8_t* host_out);
+int64_t dgc_attn_workspace_bytes(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal,
+                                 int32_t buckets, int32_t reach, int32_t backward);
+dgc_status_t dgc_attn_forward(const void* q, int64_t q_stride_t, int64_t q_stride_n, const void* k, int64_t k_stride_t,
+                              int64_t k_stride_n, const void* v, int64_t v_stride_t, int64_t v_stride_n, int64_t Tq, int64_t Tk, int64_t N,
+                              int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal, float scale, const int32_t* first,
+                              const int32_t* lengths, const uint8_t* keep, const float* bias, const uint8_t* bias_map, int32_t buckets,
+                              int32_t reach, void* o, int64_t o_stride_t, int64_t o_stride_n, float* lse, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+dgc_status_t dgc_attn_backward(const void* q, int64_t q_stride_t, int64_t q_stride_n, const void* k, int64_t k_stride_t,
+                               int64_t k_stride_n, const void* v, int64_t v_stride_t, int64_t v_stride_n, const void* o, int64_t o_stride_t,
+                               int64_t o_stride_n, const float* lse, const void* go, int64_t go_stride_t, int64_t go_stride_n, int64_t Tq,
+                               int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal, float scale,
+                               const int32_t* first, const int32_t* lengths, const uint8_t* keep, const float* bias, const uint8_t* bias_map,
+                               int32_t buckets, int32_t reach, void* dq, int64_t dq_stride_t, int64_t dq_stride_n, void* dkey,
+                               int64_t dk_stride_t, int64_t dk_stride_n, void* dval, int64_t dv_stride_t, int64_t dv_stride_n, float* dbias,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Text of the last error on this layer, or (layer = NULL) of the last failed create or layer-less
  * call on the calling thread.  Never NULL; valid until the next call on the same layer / thread. */
 const char* dgc_last_error(const dgc_layer_t* layer);

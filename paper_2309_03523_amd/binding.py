@@ -36,7 +36,8 @@ EXPORTS = ["dgc_layer_create", "dgc_layer_destroy", "dgc_layer_set_param", "dgc_
            "dgc_layer_shared_rows", "dgc_fusion_select", "dgc_chunk_assign", "dgc_chunk_generate",
            "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward",
            "dgc_linear_workspace_bytes", "dgc_linear_forward", "dgc_linear_backward",
-           "dgc_decay_attn_workspace_bytes", "dgc_decay_attn_forward", "dgc_decay_attn_backward"]
+           "dgc_decay_attn_workspace_bytes", "dgc_decay_attn_forward", "dgc_decay_attn_backward",
+           "dgc_attn_buckets", "dgc_attn_workspace_bytes", "dgc_attn_forward", "dgc_attn_backward"]
 THETA_VARIANT = {"printed": 0, "sigmoid": 1}
 N_STAGES = 13
 
@@ -118,7 +119,12 @@ def load() -> ct.CDLL:
     dims = [i64, i64, i32, i32, i32, i32]
     lib.dgc_decay_attn_forward.argtypes = seq * 3 + dims + [vp, f32, vp, vp, vp] + seq + [vp, vp, i64, vp]
     lib.dgc_decay_attn_backward.argtypes = seq * 4 + dims + [vp, f32, vp, vp, vp, vp] + seq * 3 + [vp, vp, i64, vp]
-    sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes", "dgc_decay_attn_workspace_bytes")
+    lib.dgc_attn_buckets.argtypes = [i32, i32, i32, vp]
+    lib.dgc_attn_workspace_bytes.argtypes = [i64] * 3 + [i32] * 8
+    dims = [i64] * 3 + [i32] * 5 + [f32] + [vp] * 5 + [i32] * 2
+    lib.dgc_attn_forward.argtypes = seq * 3 + dims + seq + [vp, vp, i64, vp]
+    lib.dgc_attn_backward.argtypes = seq * 4 + [vp] + seq + dims + seq * 3 + [vp, vp, i64, vp]
+    sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes", "dgc_decay_attn_workspace_bytes", "dgc_attn_workspace_bytes")
     for name in sizes:
         getattr(lib, name).restype = i64
     for name in EXPORTS:
@@ -660,3 +666,69 @@ def decay_attn_backward(q, k, v, decay, do, dq, dk, dv, *, heads: int, scale: fl
              _op_flat(lengths, "lengths", N, dev, _torch.int32), _op_shape(reset, "reset", (T, N), dev, _torch.uint8),
              *_op_seq(dq, "dq", dt, dev, T, N, heads * nk), *_op_seq(dk, "dk", dt, dev, T, N, heads * nk), *_op_seq(dv, "dv", dt, dev, T, N, heads * nv),
              _op_shape(ds0, "ds0", state, dev), ws, ws_bytes)
+
+
+def attn_buckets(buckets: int, reach: int, *, causal: bool = True) -> np.ndarray:
+    """dgc_attn_buckets: the bucket of each distance -reach .. reach (query's position minus key's), uint8 [2 reach + 1]: single distances, then growing ones."""
+    out = np.zeros(2 * max(int(reach), 0) + 1, np.uint8)
+    lib = load()
+    rc = lib.dgc_attn_buckets(int(buckets), int(reach), int(causal), out.ctypes.data_as(ct.c_void_p))
+    if rc:
+        raise DgcError(rc, lib.dgc_last_error(None).decode())
+    return out
+
+
+def attn_workspace_bytes(Tq: int, Tk: int, N: int, heads: int, d: int, *, kv_heads: Optional[int] = None, dtype: str = "f32", causal: bool = True,
+                         buckets: int = 0, reach: int = 0, backward: bool = False) -> int:
+    """Bytes that attn_forward (few queries against many keys; else none) or attn_backward needs."""
+    return int(load().dgc_attn_workspace_bytes(int(Tq), int(Tk), int(N), int(heads), int(kv_heads or heads), int(d), DTYPE[dtype], int(causal), int(buckets),
+                                               int(reach), int(backward)))
+
+
+def _attn_args(q, k, heads, kv_heads, code, dev, causal, scale, first, lengths, keep, bias, bias_map):
+    """(Tq, Tk, N, width of q, width of k, the calls' common arguments)."""
+    kv = heads if kv_heads is None else kv_heads
+    if q.dim() != 3 or k.dim() != 3 or heads < 1 or kv < 1 or q.shape[2] % heads or k.shape[2] % kv or q.shape[2] // heads != k.shape[2] // kv:
+        raise ValueError("q must be [Tq, N, heads * d], k and v [Tk, N, kv_heads * d]")
+    if (bias is None) != (bias_map is None):
+        raise ValueError("bias and bias_map go together")
+    (Tq, N, fq), (Tk, _, fk) = q.shape, k.shape
+    buckets = reach = 0
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[0] != heads or bias_map.dim() != 1 or bias_map.shape[0] % 2 == 0:
+            raise ValueError("bias must be [heads, buckets] and bias_map [2 reach + 1]")
+        buckets, reach = bias.shape[1], bias_map.shape[0] // 2
+    return Tq, Tk, N, fq, fk, (Tq, Tk, N, heads, kv, fq // heads, code, 1 if causal else 0, float(scale), _op_shape(first, "first", (N,), dev, _torch.int32),
+                               _op_shape(lengths, "lengths", (N,), dev, _torch.int32), _op_shape(keep, "keep", (Tk, N), dev, _torch.uint8),
+                               _op_flat(bias, "bias", heads * buckets, dev), _op_flat(bias_map, "bias_map", 2 * reach + 1, dev, _torch.uint8), buckets, reach)
+
+
+def attn_forward(q, k, v, o, *, heads: int, kv_heads: Optional[int] = None, scale: float = 1.0, causal: bool = True, first=None, lengths=None, keep=None,
+                 bias=None, bias_map=None, lse=None, workspace=None, stream=None):
+    """dgc_attn_forward: o_i = softmax_j(scale q_i . k_j + bias[h][bias_map[p - j]]) v_j for query i, at position p = first[n] + i (None: Tk - Tq + i), of
+    every sequence n and head h, over the keys j < lengths[n] with keep[j, n] != 0 and, with causal, j <= p.  q, o [Tq, N, heads * d], k, v [Tk, N,
+    kv_heads * d], float32 or bfloat16, with any strides of the first two (a transposed [N, T, .] tensor is fine); heads / kv_heads heads share a key
+    head.  first, lengths int32 [N], keep uint8 [Tk, N], bias fp32 [heads, buckets], bias_map uint8 [2 reach + 1] (attn_buckets); lse fp32 [N, heads, Tq]
+    is written if given, attn_backward reads it.  Rows of no token are not written; o is 0 and lse -inf where a query sees nothing.  workspace:
+    attn_workspace_bytes device bytes, None where that is 0.  Tq = 1 is the form for one new snapshot against the keys and values kept so far."""
+    lib, code, dev = _op_first(q, "q")
+    dt = q.dtype
+    Tq, Tk, N, fq, fk, args = _attn_args(q, k, heads, kv_heads, code, dev, causal, scale, first, lengths, keep, bias, bias_map)
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_attn_forward, dev, stream, *_op_seq(q, "q", dt, dev, Tq, N, fq), *_op_seq(k, "k", dt, dev, Tk, N, fk), *_op_seq(v, "v", dt, dev, Tk, N, fk),
+             *args, *_op_seq(o, "o", dt, dev, Tq, N, fq), _op_shape(lse, "lse", (N, heads, Tq), dev), ws, ws_bytes)
+    return o
+
+
+def attn_backward(q, k, v, o, lse, do, dq, dk, dv, *, heads: int, kv_heads: Optional[int] = None, scale: float = 1.0, causal: bool = True, first=None, lengths=None,
+                  keep=None, bias=None, bias_map=None, dbias=None, workspace=None, stream=None):
+    """dgc_attn_backward: the gradients of attn_forward's q, k, v (each may be None: not wanted) and bias (dbias fp32 [heads, buckets]) from do, with that call's
+    o and lse and the same other arguments.  workspace: attn_workspace_bytes(..., backward=True) device bytes."""
+    lib, code, dev = _op_first(q, "q")
+    dt = q.dtype
+    Tq, Tk, N, fq, fk, args = _attn_args(q, k, heads, kv_heads, code, dev, causal, scale, first, lengths, keep, bias, bias_map)
+    ws, ws_bytes = _op_workspace(workspace, dev)
+    _op_call(lib.dgc_attn_backward, dev, stream, *_op_seq(q, "q", dt, dev, Tq, N, fq), *_op_seq(k, "k", dt, dev, Tk, N, fk), *_op_seq(v, "v", dt, dev, Tk, N, fk),
+             *_op_seq(o, "o", dt, dev, Tq, N, fq), _op_shape(lse, "lse", (N, heads, Tq), dev), *_op_seq(do, "do", dt, dev, Tq, N, fq), *args,
+             *_op_seq(dq, "dq", dt, dev, Tq, N, fq), *_op_seq(dk, "dk", dt, dev, Tk, N, fk), *_op_seq(dv, "dv", dt, dev, Tk, N, fk),
+             _op_shape(dbias, "dbias", (heads, args[-2]), dev), ws, ws_bytes)

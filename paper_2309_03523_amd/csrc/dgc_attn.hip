@@ -1,0 +1,522 @@
+// Softmax attention over the tokens of sequences, forward.  For query i of sequence n, at position p = at + i, and head h:
+//
+//   s_j = scale q_i . k_j + bias[h][map[p - j]]  over the keys that it sees,  lse = log sum e^s_j,  o = sum e^(s_j - lse) v_j
+//
+// Scores are formed turned, keys in rows and queries in columns: a lane then holds scores of one query, the running maximum and sum of
+// its softmax are two registers, and the probabilities are the right operand of the product with the values as they stand.
+// Rounding: bf16 tensors enter products as they are; scores, exponents, maxima and sums are fp32; probabilities are rounded
+// to bf16 (2^-9 of themselves) for their product with the values, which is summed in fp32.  fp32 tensors: fp32 throughout.
+//
+// Kernels: k_attn_window (up to 64 keys: a wave a sequence and head), k_attn_few (up to 16 queries: the keys are split among lanes, waves and
+// workgroups, and joined), k_attn_forward (the rest).
+#include <algorithm>
+
+#include "dgc_attn_dev.h"
+
+namespace dgc {
+namespace attn {
+namespace {
+
+constexpr int kKeys = kTile;
+
+// ---------------------------------------------------------------------------------------------------- long sequences
+//
+// A workgroup takes 4 M queries of one sequence and head, a wave M of them, and walks over the keys in tiles of 64 that lie in LDS once for
+// all four; the next tile's rows are on their way in registers meanwhile.
+template <class Tl, int KS>
+__global__ __launch_bounds__(256) void k_attn_forward(Args a) {
+  typedef typename Tl::E E;
+  constexpr int M = Tl::M, NT = kKeys / M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  __shared__ __attribute__((aligned(16))) E sk[kKeys * P], sv[kKeys * P];
+  __shared__ float seen[kKeys];          // 0 where a key is masked
+  extern __shared__ float table[];       // bias by distance, from 0 or -reach to reach
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = Tl::col(lane), sub = Tl::sub(lane);
+  const uint32_t pairs = (uint32_t)(a.N * a.heads), blocks = (uint32_t)((a.Tq + 4 * M - 1) / (4 * M));
+  // The workgroups of a sequence and head lie `pairs` apart: on one chiplet's L2 where pairs are a multiple of 8.  The longest walks first.
+  const uint32_t pair = blockIdx.x % pairs;
+  const int64_t n = pair / a.heads;
+  const int h = pair % a.heads, y = h / a.group;
+  const int i0 = (int)(blocks - 1 - blockIdx.x / pairs) * 4 * M;
+  const Seq q(a, n);
+  if (i0 >= q.hi || i0 + 4 * M <= q.lo) return;
+  const int least = max(i0, q.lo), most = min(i0 + 4 * M, q.hi) - 1;      // live queries of the workgroup
+  const int kend = a.causal ? (int)min((int64_t)q.len, q.at + most + 1) : q.len;
+  const int mine = i0 + wave * M, i = mine + col;
+  const bool live = i >= q.lo && i < q.hi;
+  // The positions of this wave's first and last live query, and the lane's own; where none is live, as of a query that sees nothing.
+  const bool some = max(mine, q.lo) < min(mine + M, q.hi);
+  const int p0 = some ? (int)(q.at + max(mine, q.lo)) : -1, p1 = some ? (int)(q.at + min(mine + M, q.hi) - 1) : -1, p = live ? (int)(q.at + i) : -1;
+
+  const int from = a.causal ? 0 : -a.reach;
+  if (a.bias) {
+    for (int x = threadIdx.x; x <= a.reach - from; x += 256) table[x] = bias_at(a, h, from + x);
+  }
+  typename Tl::Frag fq[KS];
+  {
+    const E* row = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = 16 * s + Tl::KE * sub;
+      fq[s] = live && c < a.d ? *reinterpret_cast<const typename Tl::Frag*>(row + c) : Tl::zero();
+    }
+  }
+  const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d;
+  const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d;
+  auto there = [&](int j) { return j < kend && (!a.keep || a.keep[(int64_t)j * a.N + n]); };
+  Stage<E, kKeys, KS> nk, nv;
+  nk.fetch(kbase, a.k.st, 0, a.d, there);
+  nv.fetch(vbase, a.v.st, 0, a.d, there);
+  typename Tl::Acc o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = (typename Tl::Acc)(0.f);
+  float m = -__builtin_inff(), l = 0.f;
+
+  for (int j0 = 0; j0 < kend; j0 += kKeys) {
+    __syncthreads();      // the tile before has been read
+    nk.put(sk, P);
+    nv.put(sv, P);
+    const bool edge = a.causal && j0 + kKeys - 1 > q.at + least;          // some query does not see some key of it
+    const bool masked = a.keep || j0 + kKeys > kend;
+    if (masked && threadIdx.x < kKeys) seen[threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
+    const bool slow = edge ? __syncthreads_or(nv.template odd<Tl>()) : (__syncthreads(), false);
+    if (j0 + kKeys < kend) {
+      nk.fetch(kbase, a.k.st, j0 + kKeys, a.d, there);
+      nv.fetch(vbase, a.v.st, j0 + kKeys, a.d, there);
+    }
+    if (!some || (a.causal && j0 > p1)) continue;      // nothing that this wave's queries see
+    typename Tl::Acc x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      x[t] = (typename Tl::Acc)(0.f);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[t] = Tl::mma(Tl::rows(sk + t * M * P, P, s, lane), fq[s], x[t]);
+    }
+    if (!a.bias) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) x[t] *= a.scale;
+    } else if (p0 - (j0 + kKeys - 1) >= a.reach) {      // all far behind
+      const float b = table[a.reach - from];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) x[t] = x[t] * a.scale + b;
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) {
+          const int away = min(max(p - (j0 + t * M + Tl::row(r, lane)), from), a.reach);
+          x[t][r] = fmaf(x[t][r], a.scale, table[away - from]);
+        }
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = seen[t * M + Tl::row(r, lane)] == 0.f ? -__builtin_inff() : x[t][r];
+      }
+    }
+    if (a.causal && j0 + kKeys - 1 > p0) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = j0 + t * M + Tl::row(r, lane) > p ? -__builtin_inff() : x[t][r];
+      }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int r = 0; r < Tl::NR; ++r) top = fmaxf(top, x[t][r]);
+    }
+    top = fmaxf(m, column_max<Tl::SUBS>(top));
+    const float off = top == -__builtin_inff() ? 0.f : top, off2 = off * kLog2e;        // no key seen so far: all terms are zero
+    const float keepf = exp2_((m - off) * kLog2e);
+    const bool exact = Tl::kExact || __any(far_off(off));
+    m = top;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int r = 0; r < Tl::NR; ++r) {
+        x[t][r] = weight(x[t][r], off, off2, exact);
+        sum += x[t][r];
+      }
+    }
+    l = fmaf(l, keepf, sum);
+    if (__any(keepf != 1.f)) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= keepf;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int first = j0 + t * M;
+      gather<Tl, DT>(o, sv + t * M * P, P, Packed<Tl>(x[t]), lane, slow, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
+    }
+  }
+  l = column_sum<Tl::SUBS>(l);
+  if (!live) return;
+  E* row = static_cast<E*>(const_cast<void*>(a.o.p)) + (int64_t)i * a.o.st + n * a.o.sn + h * a.d;
+  store_column<Tl, DT>(row, o, l == 0.f ? 0.f : 1.f / l, a.d, lane);
+  if (a.lse && sub == 0) a.lse[(n * a.heads + h) * a.Tq + i] = log_sum(m, l);
+}
+
+// ---------------------------------------------------------------------------------------------------- windows
+//
+// Up to 16 NT keys and queries: a wave takes one sequence and head after the other, of one head, so that the table of
+// its bias stays.  Queries and keys go from memory into operands; only the values pass through LDS, in the wave's own part: no wave waits for another.
+template <class Tl, int NT, int KS>
+__global__ __launch_bounds__(256) void k_attn_window(Args a) {
+  typedef typename Tl::E E;
+  typedef typename Tl::Frag Frag;
+  constexpr int DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P, W = 16 * NT;
+  __shared__ __attribute__((aligned(16))) E values[4][W * P];
+  __shared__ float tables[4][2 * W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, sub = lane >> 4;
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  const int h = (int)(id % a.heads), y = h / a.group;
+  int64_t n = id / a.heads;
+  if (n >= a.slots) return;
+  E* sv = values[wave];
+  float* table = tables[wave];        // of distance at - W + 1 + x
+  for (bool begun = false; n < a.N; n += a.slots) {
+    const Seq q(a, n);
+    if (a.bias && (a.first || !begun)) {
+      for (int x = lane; x < 2 * W - 1; x += 64) table[x] = bias_at(a, h, q.at - W + 1 + x);
+    }
+    begun = true;
+    if (q.lo >= q.hi) continue;
+    const bool there = lane < q.len && (!a.keep || a.keep[(int64_t)lane * a.N + n]);
+    const uint64_t keys = __ballot(there);
+    Frag fk[NT][KS];
+    bool bad = false;
+    const E* qbase = static_cast<const E*>(a.q.p) + n * a.q.sn + h * a.d;
+    const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d;
+    const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int j = 16 * t + col;
+      const bool in = keys >> j & 1;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int c = 16 * s + 4 * sub;
+        const bool ok = in && c < a.d;
+        fk[t][s] = ok ? Tl::load(kbase + j * a.k.st + c) : Tl::zero();
+        const Frag fv = ok ? Tl::load(vbase + j * a.v.st + c) : Tl::zero();
+        bad = bad || Tl::odd(fv);
+        Tl::store(sv + j * P + c, fv);
+      }
+    }
+    wave_fence();
+    const bool slow = a.causal && __any(bad);
+    for (int i0 = 0; i0 < q.hi; i0 += 16) {
+      if (i0 + 16 <= q.lo) continue;
+      const int i = i0 + col;
+      const bool live = i >= q.lo && i < q.hi;
+      const int p = live ? (int)(q.at + i) : -1;
+      const int last = a.causal ? (int)(q.at + min(i0 + 16, q.hi) - 1) : q.len - 1;     // the last key that one of them sees
+      // The keys that this lane's query sees, one bit each.
+      const uint64_t mine = !live ? 0 : a.causal && p < 63 ? keys & ((2ull << p) - 1) : keys;
+      Frag fq[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int c = 16 * s + 4 * sub;
+        fq[s] = live && c < a.d ? Tl::load(qbase + i * a.q.st + c) : Tl::zero();
+      }
+      floatx4 x[NT];
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (16 * t > last) break;
+        x[t] = (floatx4)(0.f);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) x[t] = Tl::mma(fk[t][s], fq[s], x[t]);
+        const uint32_t bits = (uint32_t)(mine >> (16 * t + 4 * sub));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = 16 * t + 4 * sub + r;
+          float v = x[t][r] * a.scale;
+          if (a.bias) v = fmaf(x[t][r], a.scale, table[i - j + W - 1]);
+          x[t][r] = bits >> r & 1 ? v : -__builtin_inff();
+          top = fmaxf(top, x[t][r]);
+        }
+      }
+      top = column_max<4>(top);
+      float l = 0.f;
+      floatx4 o[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = (floatx4)(0.f);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (16 * t > last) break;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[t][r] = weight_of(x[t][r], top);
+          l += x[t][r];
+        }
+        gather<Tl, DT>(o, sv + 16 * t * P, P, Packed<Tl>(x[t]), lane, slow, [](int) { return 0; }, [&](int c) { return (int)(q.at + i0 + c) - 16 * t; });
+      }
+      l = column_sum<4>(l);
+      if (!live) continue;
+      E* row = static_cast<E*>(const_cast<void*>(a.o.p)) + (int64_t)i * a.o.st + n * a.o.sn + h * a.d;
+      store_column<Tl, DT>(row, o, l == 0.f ? 0.f : 1.f / l, a.d, lane);
+      if (a.lse && sub == 0) a.lse[(n * a.heads + h) * a.Tq + i] = log_sum(top, l);
+    }
+    wave_fence();
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- few queries
+//
+// Up to 16 queries (one: a new snapshot) against many keys.  The rows of a key head, its heads' queries, are taken R at a time; a key's row is
+// read by LPK lanes, 16 bytes each, by each of the wave's 64 / LPK groups another key, four keys of a group at a time.  Every group has a
+// softmax of its own, over its own keys; they are joined at the end, in the wave, in the workgroup, and by k_attn_join where the keys
+// are split among workgroups.
+template <int LPK>
+__device__ __forceinline__ float lanes_sum(float x) {      // over LPK neighbouring lanes
+  if constexpr (LPK >= 2) x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xB1, 0xf, 0xf, true));       // quad_perm 1 0 3 2
+  if constexpr (LPK >= 4) x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x4E, 0xf, 0xf, true));       // quad_perm 2 3 0 1
+  if constexpr (LPK >= 8) x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x141, 0xf, 0xf, true));      // row_half_mirror
+  if constexpr (LPK >= 16) x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x140, 0xf, 0xf, true));     // row_mirror
+  if constexpr (LPK >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  return x;
+}
+
+template <class E, int LPK, int R>
+__global__ __launch_bounds__(256) void k_attn_few(Args a) {
+  constexpr int PER = ops::Elem<E>::kPer, KW = 64 / LPK, U = 4, STEP = 4 * KW * U;      // keys of a workgroup's step
+  constexpr int ROOM = R * (LPK * PER + 2);
+  __shared__ float joined[4][ROOM];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (lane % LPK) * PER, g = lane / LPK;
+  const int rows = a.group * a.Tq, blocks = (rows + R - 1) / R, kvs = a.heads / a.group;
+  const uint32_t part = blockIdx.x % a.splits;
+  uint32_t rest = blockIdx.x / a.splits;
+  const int r0 = (int)(rest % blocks) * R;
+  rest /= blocks;
+  const int y = rest % kvs;
+  const int64_t n = rest / kvs;
+  const Seq q(a, n);
+  float fq[R][PER], far[R];
+  int p[R], most = -1, least = 0x7fffffff;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = r0 + r, h = y * a.group + row / a.Tq, i = row % a.Tq;
+    const bool live = row < rows && i >= q.lo && i < q.hi;
+    p[r] = live ? (int)(q.at + i) : -1;
+    if (live) most = max(most, p[r]), least = min(least, p[r]);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (live && c < a.d) w = *reinterpret_cast<const uint4*>(static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d + c);
+    ops::Elem<E>::unpack(w, fq[r]);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) fq[r][e] *= a.scale;
+    far[r] = a.bias && live ? bias_at(a, h, a.reach) : 0.f;
+  }
+  const int kend = most < 0 ? 0 : a.causal ? min(q.len, most + 1) : q.len;
+  const int share = ((kend + a.splits - 1) / a.splits + STEP - 1) / STEP * STEP;
+  const int k0 = (int)min((int64_t)part * share, (int64_t)kend), k1 = min(k0 + share, kend);
+  const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d + c;
+  const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d + c;
+  float o[R][PER], m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -__builtin_inff();
+    l[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[r][e] = 0.f;
+  }
+  for (int j0 = k0 + wave * KW * U; j0 < k1; j0 += STEP) {
+    uint4 wk[U], wv[U];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * KW + g;
+      in[u] = j < k1 && (!a.keep || a.keep[(int64_t)j * a.N + n]);
+      const bool ok = in[u] && c < a.d;
+      wk[u] = ok ? *reinterpret_cast<const uint4*>(kbase + (int64_t)j * a.k.st) : make_uint4(0, 0, 0, 0);
+      wv[u] = ok ? *reinterpret_cast<const uint4*>(vbase + (int64_t)j * a.v.st) : make_uint4(0, 0, 0, 0);
+    }
+    const bool near = a.bias && least - (j0 + KW * U - 1) < a.reach;
+    const bool edge = a.causal && j0 + KW * U - 1 > least;       // not every row sees every key
+    float x[R][U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float k[PER];
+      ops::Elem<E>::unpack(wk[u], k);
+      const int j = j0 + u * KW + g;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float s = fq[r][0] * k[0];
+#pragma unroll
+        for (int e = 1; e < PER; ++e) s = fmaf(fq[r][e], k[e], s);
+        s = lanes_sum<LPK>(s);
+        if (near) s += bias_at(a, y * a.group + min(r0 + r, rows - 1) / a.Tq, (int64_t)p[r] - j);
+        else s += far[r];
+        x[r][u] = in[u] && p[r] >= 0 && (!edge || j <= p[r]) ? s : -__builtin_inff();
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float top = m[r];
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = fmaxf(top, x[r][u]);
+      const float keepf = weight_of(m[r], top);
+      m[r] = top;
+      l[r] *= keepf;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[r][e] *= keepf;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool out = edge && x[r][u] == -__builtin_inff();     // unseen: its values do not count, whatever they are
+        x[r][u] = weight_of(x[r][u], top);
+        l[r] += x[r][u];
+        float v[PER];
+        ops::Elem<E>::unpack(out ? make_uint4(0, 0, 0, 0) : wv[u], v);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[r][e] = fmaf(x[r][u], v[e], o[r][e]);
+      }
+    }
+  }
+  // The groups of a wave, then the waves.
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float top = m[r];
+    for (int s = LPK; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
+    const float f = weight_of(m[r], top);
+    m[r] = top;
+    l[r] *= f;
+    for (int s = LPK; s < 64; s *= 2) l[r] += __shfl_xor(l[r], s);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      o[r][e] *= f;
+      for (int s = LPK; s < 64; s *= 2) o[r][e] += __shfl_xor(o[r][e], s);
+    }
+    if (g == 0) {
+      float* to = joined[wave] + r * (LPK * PER + 2);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) to[c + e] = o[r][e];
+      if (c == 0) to[LPK * PER] = m[r], to[LPK * PER + 1] = l[r];
+    }
+  }
+  __syncthreads();
+  for (int r = wave; r < R; r += 4) {
+    const int row = r0 + r;
+    if (row >= rows) continue;
+    const int h = y * a.group + row / a.Tq, i = row % a.Tq;
+    if (i < q.lo || i >= q.hi) continue;
+    float top = -__builtin_inff(), f[4], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, joined[w][r * (LPK * PER + 2) + LPK * PER]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = weight_of(joined[w][r * (LPK * PER + 2) + LPK * PER], top);
+      sum = fmaf(joined[w][r * (LPK * PER + 2) + LPK * PER + 1], f[w], sum);
+    }
+    const int64_t at = (n * a.heads + h) * a.Tq + i;
+    const float by = a.splits > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    for (int e = lane; e < a.d; e += 64) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) v = fmaf(joined[w][r * (LPK * PER + 2) + e], f[w], v);
+      v *= by;
+      if (a.splits > 1) a.joint[(at * a.splits + part) * (a.d + 2) + e] = v;
+      else static_cast<E*>(const_cast<void*>(a.o.p))[(int64_t)i * a.o.st + n * a.o.sn + h * a.d + e] = ops::Elem<E>::one(v);
+    }
+    if (lane == 0) {
+      if (a.splits > 1) {
+        a.joint[(at * a.splits + part) * (a.d + 2) + a.d] = top;
+        a.joint[(at * a.splits + part) * (a.d + 2) + a.d + 1] = sum;
+      } else if (a.lse) {
+        a.lse[at] = log_sum(top, sum);
+      }
+    }
+  }
+}
+
+// The parts of split keys: a wave a row.
+template <class E>
+__global__ __launch_bounds__(256) void k_attn_join(Args a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= a.N * a.heads * a.Tq) return;
+  const int i = (int)(at % a.Tq), h = (int)(at / a.Tq % a.heads);
+  const int64_t n = at / a.Tq / a.heads;
+  const Seq q(a, n);
+  if (i < q.lo || i >= q.hi) return;
+  const float* from = a.joint + at * a.splits * (a.d + 2);
+  float top = -__builtin_inff();
+  for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, from[s * (a.d + 2) + a.d]);
+  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+  float sum = 0.f;
+  for (int s = lane; s < a.splits; s += 64) sum = fmaf(from[s * (a.d + 2) + a.d + 1], weight_of(from[s * (a.d + 2) + a.d], top), sum);
+  sum = wave_sum(sum);
+  for (int e = lane; e < a.d; e += 64) {
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v = fmaf(from[s * (a.d + 2) + e], weight_of(from[s * (a.d + 2) + a.d], top), v);
+    v = sum == 0.f ? 0.f : v / sum;
+    static_cast<E*>(const_cast<void*>(a.o.p))[(int64_t)i * a.o.st + n * a.o.sn + h * a.d + e] = ops::Elem<E>::one(v);
+  }
+  if (a.lse && lane == 0) a.lse[at] = log_sum(top, sum);
+}
+
+// ---------------------------------------------------------------------------------------------------- choice and launch
+
+template <class Tl, int NT>
+void window(Args a, hipStream_t st) {
+  const int64_t waves = 256 * 32;      // as many as the card holds at a time
+  a.slots = (int)std::min<int64_t>(a.N, (waves + a.heads - 1) / a.heads);
+  const unsigned grid = (unsigned)(((int64_t)a.slots * a.heads + 3) / 4);
+  if (a.d <= 16) hipLaunchKernelGGL((k_attn_window<Tl, NT, 1>), grid, 256, 0, st, a);
+  else if (a.d <= 32) hipLaunchKernelGGL((k_attn_window<Tl, NT, 2>), grid, 256, 0, st, a);
+  else if (a.d <= 64) hipLaunchKernelGGL((k_attn_window<Tl, NT, 4>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_attn_window<Tl, NT, 8>), grid, 256, 0, st, a);
+}
+
+template <class E, int LPK>
+void few_rows(const Args& a, int R, unsigned grid, hipStream_t st) {
+  if (R == 1) hipLaunchKernelGGL((k_attn_few<E, LPK, 1>), grid, 256, 0, st, a);
+  else if (R == 2) hipLaunchKernelGGL((k_attn_few<E, LPK, 2>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_attn_few<E, LPK, 4>), grid, 256, 0, st, a);
+}
+template <class E>
+void few(const Args& a, hipStream_t st) {
+  constexpr int PER = ops::Elem<E>::kPer;
+  const int rows = a.group * a.Tq, R = rows == 1 ? 1 : rows == 2 ? 2 : 4;
+  const unsigned grid = (unsigned)(a.N * (a.heads / a.group) * ((rows + R - 1) / R) * a.splits);
+  if (a.d <= 16) few_rows<E, 16 / PER>(a, R, grid, st);
+  else if (a.d <= 32) few_rows<E, 32 / PER>(a, R, grid, st);
+  else if (a.d <= 64) few_rows<E, 64 / PER>(a, R, grid, st);
+  else few_rows<E, 128 / PER>(a, R, grid, st);
+  if (a.splits > 1) hipLaunchKernelGGL(k_attn_join<E>, (unsigned)((a.N * a.heads * a.Tq + 3) / 4), 256, 0, st, a);
+}
+template <class Tl>
+void large(const Args& a, hipStream_t st) {
+  const unsigned grid = (unsigned)(a.N * a.heads * ((a.Tq + 4 * Tl::M - 1) / (4 * Tl::M)));
+  const unsigned lds = a.bias ? 4 * (a.causal ? a.reach + 1 : 2 * a.reach + 1) : 0;
+  if (a.d <= 16) hipLaunchKernelGGL((k_attn_forward<Tl, 1>), grid, 256, lds, st, a);
+  else if (a.d <= 32) hipLaunchKernelGGL((k_attn_forward<Tl, 2>), grid, 256, lds, st, a);
+  else if (a.d <= 64) hipLaunchKernelGGL((k_attn_forward<Tl, 4>), grid, 256, lds, st, a);
+  else hipLaunchKernelGGL((k_attn_forward<Tl, 8>), grid, 256, lds, st, a);
+}
+
+template <class Tl16, class TlLong>
+void forward(const Args& a, hipStream_t st) {
+  switch (form_of(a.Tq, a.Tk)) {
+    case kWindow:
+      if (a.Tk <= 16) window<Tl16, 1>(a, st);
+      else if (a.Tk <= 32) window<Tl16, 2>(a, st);
+      else window<Tl16, 4>(a, st);
+      break;
+    case kFew: few<typename Tl16::E>(a, st); break;
+    default: large<TlLong>(a, st);
+  }
+}
+
+}  // namespace
+
+void attn_forward_f32(const Args& a, hipStream_t st) { forward<Full, Full>(a, st); }
+void attn_forward_bf16(const Args& a, hipStream_t st) { forward<Small, Wide>(a, st); }
+
+}  // namespace attn
+}  // namespace dgc
