@@ -571,6 +571,38 @@ dgc_status_t dgc_attn_backward(const void* q, int64_t q_stride_t, int64_t q_stri
                                int64_t dk_stride_t, int64_t dk_stride_n, void* dval, int64_t dv_stride_t, int64_t dv_stride_n, float* dbias,
                                void* workspace, int64_t workspace_bytes, void* stream);
 
+/* AdamW over many tensors at once.  For every parameter of every tensor, in step number t (from 1):
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p).
+ *  A tensor is R rows of F at a pitch (ldp, ldg, ldmaster; not read where R is 1), p and g of the element type `dtype`.  master (fp32, bf16 parameters
+ *   only, NULL = none): the parameter that is stepped; p receives it rounded.  Without one a bf16 parameter is stepped as it stands.
+ *  States lie in rows at a pitch of F rounded up to a multiple of 16, columns from F on zero.  bits = 32: m and v fp32.  bits = 8: m and
+ *   r = sqrt(v) as e4m3 numbers (OCP, no infinities) times a scale for each 256 consecutive places, m_scale and v_scale fp32 [ceil(R pitch / 256)]: the least power of two with which
+ *   the largest in size is at most 448 (at least 2^-126; 1 where all are zero).  Numbers are rounded to the nearest e4m3 number, ties to even; an r that is not zero and below
+ *   the least one is raised to it; one that is not finite is held as NaN.  The step itself is taken with the states before they are rounded.
+ *   A new optimizer's states are all zero bytes, with scales of 1 or 0.
+ *  create keeps the addresses: parameters, gradients, masters and states stay where they are until destroy (what is written lies apart from all else).  It allocates a table of 16 bytes
+ *   for each 4096 parameters and some for each tensor, synchronises, and belongs to the current device.  step only enqueues; a handle runs one call at a time, and destroy
+ *   waits for it.  t: the step's number, or `steps` (device int64): the number of steps done, which the call raises by one, so a step that is captured into
+ *   a graph counts when it is replayed; then lr_at (device fp32), if not NULL, is read for lr, too. */
+typedef struct {
+  void* p;
+  const void* g;
+  float* master;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t R, ldp, ldg, ldmaster;
+  int32_t F, dtype;
+  float weight_decay;
+} dgc_adamw_tensor_t;
+typedef struct dgc_adamw dgc_adamw_t;
+dgc_status_t dgc_adamw_create(const dgc_adamw_tensor_t* tensors, int32_t n, int32_t bits, dgc_adamw_t** out);
+void dgc_adamw_destroy(dgc_adamw_t* handle);
+dgc_status_t dgc_adamw_step(dgc_adamw_t* handle, double lr, double beta1, double beta2, double eps, int64_t t, int64_t* steps,
+                            const float* lr_at, void* stream);
+
 /* Text of the last error on this layer, or (layer = NULL) of the last failed create or layer-less
  * call on the calling thread.  Never NULL; valid until the next call on the same layer / thread. */
 const char* dgc_last_error(const dgc_layer_t* layer);

@@ -37,7 +37,8 @@ EXPORTS = ["dgc_layer_create", "dgc_layer_destroy", "dgc_layer_set_param", "dgc_
            "dgc_norm_workspace_bytes", "dgc_norm_forward", "dgc_norm_backward",
            "dgc_linear_workspace_bytes", "dgc_linear_forward", "dgc_linear_backward",
            "dgc_decay_attn_workspace_bytes", "dgc_decay_attn_forward", "dgc_decay_attn_backward",
-           "dgc_attn_buckets", "dgc_attn_workspace_bytes", "dgc_attn_forward", "dgc_attn_backward"]
+           "dgc_attn_buckets", "dgc_attn_workspace_bytes", "dgc_attn_forward", "dgc_attn_backward",
+           "dgc_adamw_create", "dgc_adamw_destroy", "dgc_adamw_step"]
 THETA_VARIANT = {"printed": 0, "sigmoid": 1}
 N_STAGES = 13
 
@@ -50,6 +51,11 @@ class DgcError(RuntimeError):
 
 class ChunkT(ct.Structure):
     _fields_ = [("v_lo", ct.c_int64), ("v_hi", ct.c_int64), ("t_lo", ct.c_int32), ("t_hi", ct.c_int32)]
+
+
+class AdamwTensorT(ct.Structure):
+    _fields_ = [(n, ct.c_void_p) for n in ("p", "g", "master", "m", "v", "m_scale", "v_scale")] + \
+        [(n, ct.c_int64) for n in ("R", "ldp", "ldg", "ldmaster")] + [("F", ct.c_int32), ("dtype", ct.c_int32), ("weight_decay", ct.c_float)]
 
 
 class GraphT(ct.Structure):
@@ -107,7 +113,7 @@ def load() -> ct.CDLL:
                                             i64, vp, vp]
     lib.dgc_stale_static_max_candidates.argtypes = []
     lib.dgc_stale_static_max_candidates.restype = i64
-    f32 = ct.c_float
+    f32, f64 = ct.c_float, ct.c_double
     lib.dgc_norm_forward.argtypes = [vp, i64, i64, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]
     lib.dgc_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
     lib.dgc_norm_workspace_bytes.argtypes = [i64, i32]
@@ -124,11 +130,14 @@ def load() -> ct.CDLL:
     dims = [i64] * 3 + [i32] * 5 + [f32] + [vp] * 5 + [i32] * 2
     lib.dgc_attn_forward.argtypes = seq * 3 + dims + seq + [vp, vp, i64, vp]
     lib.dgc_attn_backward.argtypes = seq * 4 + [vp] + seq + dims + seq * 3 + [vp, vp, i64, vp]
+    lib.dgc_adamw_create.argtypes = [vp, i32, i32, ct.POINTER(vp)]
+    lib.dgc_adamw_destroy.argtypes = [vp]
+    lib.dgc_adamw_step.argtypes = [vp, f64, f64, f64, f64, i64, vp, vp, vp]
     sizes = ("dgc_norm_workspace_bytes", "dgc_linear_workspace_bytes", "dgc_decay_attn_workspace_bytes", "dgc_attn_workspace_bytes")
     for name in sizes:
         getattr(lib, name).restype = i64
     for name in EXPORTS:
-        if name not in ("dgc_last_error", "dgc_version", "dgc_stale_theta_factor", "dgc_stale_workspace_bytes",
+        if name not in ("dgc_last_error", "dgc_adamw_destroy", "dgc_version", "dgc_stale_theta_factor", "dgc_stale_workspace_bytes",
                         "dgc_stale_static_max_candidates") + sizes:
             getattr(lib, name).restype = ct.c_int
     _lib = lib
@@ -732,3 +741,43 @@ def attn_backward(q, k, v, o, lse, do, dq, dk, dv, *, heads: int, kv_heads: Opti
              *_op_seq(o, "o", dt, dev, Tq, N, fq), _op_shape(lse, "lse", (N, heads, Tq), dev), *_op_seq(do, "do", dt, dev, Tq, N, fq), *args,
              *_op_seq(dq, "dq", dt, dev, Tq, N, fq), *_op_seq(dk, "dk", dt, dev, Tk, N, fk), *_op_seq(dv, "dv", dt, dev, Tk, N, fk),
              _op_shape(dbias, "dbias", (heads, args[-2]), dev), ws, ws_bytes)
+
+
+def adamw_create(items, bits: int, dev: int):
+    """dgc_adamw_create on device `dev` for a list of dicts: p, g, and where there are some master, m_scale, v_scale (tensors of rows [..., F]), m, v,
+    weight_decay.  Returns the handle."""
+    lib = _lib if _torch is not None and _lib is not None else _op_init()
+    table = (AdamwTensorT * max(1, len(items)))()
+    for to, x in zip(table, items):
+        p = x["p"]
+        _, code, _ = _op_first(p, "a parameter")
+        p = p if p.dim() > 1 else p[None]
+        rows = lambda t, name, dtype: _op_rows(t if t is None or t.dim() > 1 else t[None], name, dtype, dev, (_op_count(p), p.shape[-1]))  # noqa: E731
+        R, F = _op_count(p), p.shape[-1]
+        (to.p, to.ldp), (to.g, to.ldg) = rows(p, "a parameter", p.dtype), rows(x["g"], "a gradient", p.dtype)
+        to.master, to.ldmaster = rows(x.get("master"), "a master", _torch.float32)
+        held = R * adamw_pitch(F)
+        state = _torch.float32 if bits == 32 else _torch.float8_e4m3fn
+        to.m, to.v = _op_flat(x["m"], "m", held, dev, state), _op_flat(x["v"], "v", held, dev, state)
+        to.m_scale, to.v_scale = (_op_flat(x.get(n), n, -(-held // 256), dev) for n in ("m_scale", "v_scale"))
+        to.R, to.F, to.dtype, to.weight_decay = R, F, code, x["weight_decay"]
+    out = ct.c_void_p()
+    with _torch.cuda.device(dev):
+        rc = lib.dgc_adamw_create(table, len(items), int(bits), ct.byref(out))
+    if rc:
+        raise DgcError(rc, lib.dgc_last_error(None).decode())
+    return out
+
+
+def adamw_pitch(F: int) -> int:
+    """Places that a row of F parameters has in a state."""
+    return -(-F // 16) * 16
+
+
+def adamw_destroy(handle):
+    load().dgc_adamw_destroy(handle)
+
+
+def adamw_step(handle, dev: int, t: int, *, lr: float, beta1: float, beta2: float, eps: float, steps=None, lr_at=None, stream=None):
+    """dgc_adamw_step: step number t, or with `steps` (int64 [1] on the device, raised by one) the next one; lr_at fp32 [1] on the device, read for lr."""
+    _op_call(_lib.dgc_adamw_step, dev, stream, handle, lr, beta1, beta2, eps, t, _op_flat(steps, "steps", 1, dev, _torch.int64), _op_flat(lr_at, "lr", 1, dev))
