@@ -10,6 +10,7 @@
 // Kernels: k_attn_window (up to 64 keys: a wave a sequence and head), k_attn_few (up to 16 queries: the keys are split among lanes, waves and
 // workgroups, and joined), k_attn_forward (the rest).
 #include <algorithm>
+#include <type_traits>
 
 #include "dgc_attn_dev.h"
 
@@ -17,20 +18,19 @@ namespace dgc {
 namespace attn {
 namespace {
 
-constexpr int kKeys = kTile;
 
 // ---------------------------------------------------------------------------------------------------- long sequences
 //
 // A workgroup takes 4 M queries of one sequence and head, a wave M of them, and walks over the keys in tiles of 64 that lie in LDS once for
 // all four; the next tile's rows are on their way in registers meanwhile.
 template <class Tl, int KS>
-__global__ __launch_bounds__(256) void k_attn_forward(Args a) {
+__global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
   typedef typename Tl::E E;
-  constexpr int M = Tl::M, NT = kKeys / M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
-  __shared__ __attribute__((aligned(16))) E sk[kKeys * P], sv[kKeys * P];
-  __shared__ float seen[kKeys];          // 0 where a key is masked
-  extern __shared__ float table[];       // bias by distance, from 0 or -reach to reach
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = Tl::col(lane), sub = Tl::sub(lane);
+  constexpr int kKeys = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  __shared__ __attribute__((aligned(16))) E room[2][2 * kKeys * P];
+  __shared__ float seens[2][kKeys];      // 0 where a key is masked
+  extern __shared__ float table[];       // bias by distance
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = Tl::col(lane), sub = Tl::sub(lane);
   const uint32_t pairs = (uint32_t)(a.N * a.heads), blocks = (uint32_t)((a.Tq + 4 * M - 1) / (4 * M));
   // The workgroups of a sequence and head lie `pairs` apart: on one chiplet's L2 where pairs are a multiple of 8.  The longest walks first.
   const uint32_t pair = blockIdx.x % pairs;
@@ -47,10 +47,9 @@ __global__ __launch_bounds__(256) void k_attn_forward(Args a) {
   const bool some = max(mine, q.lo) < min(mine + M, q.hi);
   const int p0 = some ? (int)(q.at + max(mine, q.lo)) : -1, p1 = some ? (int)(q.at + min(mine + M, q.hi) - 1) : -1, p = live ? (int)(q.at + i) : -1;
 
-  const int from = a.causal ? 0 : -a.reach;
-  if (a.bias) {
-    for (int x = threadIdx.x; x <= a.reach - from; x += 256) table[x] = bias_at(a, h, from + x);
-  }
+  const BiasTable bt(a);
+  if (a.bias) bt.fill(a, table, h, true);
+  const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place
   typename Tl::Frag fq[KS];
   {
     const E* row = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
@@ -63,27 +62,49 @@ __global__ __launch_bounds__(256) void k_attn_forward(Args a) {
   const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d;
   const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d;
   auto there = [&](int j) { return j < kend && (!a.keep || a.keep[(int64_t)j * a.N + n]); };
+  // Where tiles change their kind, so that one comparison tells it.  No key of a tile that ends by `whole` is masked; every query of the workgroup
+  // sees those up to `inside`; `plain_to`, `plain_from`: this wave's queries see the whole tile, with one bias, ahead or behind the reach.
+  const int whole = a.keep ? 0 : kend, inside = a.causal ? (int)(q.at + least) + 1 : kend + kKeys;
+  int plain_to = Tl::kExact || !(a.scale > 0.f) ? 0 : min(whole, min(a.causal ? p0 + 1 : kend, a.bias ? p0 - a.reach + 1 : kend));
+  int plain_from = Tl::kExact || !(a.scale > 0.f) || a.causal ? 0x7fffffff : p1 + a.reach;
+  auto holes = [&](int j0) { return j0 + kKeys > whole; };
   Stage<E, kKeys, KS> nk, nv;
-  nk.fetch(kbase, a.k.st, 0, a.d, there);
-  nv.fetch(vbase, a.v.st, 0, a.d, there);
+  nk.init(a.k.st, a.d);
+  nv.init(a.v.st, a.d);
+  const bool near = nk.near && nv.near;
+  const E *knext = kbase, *vnext = vbase;
+  const int64_t kstep = kKeys * a.k.st, vstep = kKeys * a.v.st;
+  auto fetch = [&](int j0) {
+    if (!holes(j0) && near) {
+      nk.fetch_all(knext);
+      nv.fetch_all(vnext);
+      knext += kstep;
+      vnext += vstep;
+    } else {
+      nk.fetch(kbase, a.k.st, j0, there);
+      nv.fetch(vbase, a.v.st, j0, there);
+    }
+  };
+  // Lays out a tile; whether a zero weight would meet a value of it that is not finite.
+  auto put = [&](int j0, int b) -> bool {
+    nk.put(room[b], P);
+    nv.put(room[b] + kKeys * P, P);
+    if (holes(j0) && threadIdx.x < kKeys) seens[b][threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
+    if (j0 + kKeys > inside) return __syncthreads_or(nv.template odd<Tl>());
+    __syncthreads();
+    return false;
+  };
   typename Tl::Acc o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = (typename Tl::Acc)(0.f);
   float m = -__builtin_inff(), l = 0.f;
-
-  for (int j0 = 0; j0 < kend; j0 += kKeys) {
-    __syncthreads();      // the tile before has been read
-    nk.put(sk, P);
-    nv.put(sv, P);
-    const bool edge = a.causal && j0 + kKeys - 1 > q.at + least;          // some query does not see some key of it
-    const bool masked = a.keep || j0 + kKeys > kend;
-    if (masked && threadIdx.x < kKeys) seen[threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
-    const bool slow = edge ? __syncthreads_or(nv.template odd<Tl>()) : (__syncthreads(), false);
-    if (j0 + kKeys < kend) {
-      nk.fetch(kbase, a.k.st, j0 + kKeys, a.d, there);
-      nv.fetch(vbase, a.v.st, j0 + kKeys, a.d, there);
-    }
-    if (!some || (a.causal && j0 > p1)) continue;      // nothing that this wave's queries see
+  // One tile.  PLAIN: every query sees all of it, with one bias, and scale > 0: scores stay as the product left them, a score's weight is one
+  // multiply-add and one power of two, and nothing branches, so products and weights of the tile's halves run side by side.
+  // SEEN: values that are not finite reach only those that see them.
+  float bias_behind = 0.f, bias_ahead = 0.f;       // beyond the reach
+  auto tile = [&](auto plain, auto seen_only, int j0, int buf) {
+    constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
+    const E *sk = room[buf], *sv = sk + kKeys * P;
     typename Tl::Acc x[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -91,35 +112,40 @@ __global__ __launch_bounds__(256) void k_attn_forward(Args a) {
 #pragma unroll
       for (int s = 0; s < KS; ++s) x[t] = Tl::mma(Tl::rows(sk + t * M * P, P, s, lane), fq[s], x[t]);
     }
-    if (!a.bias) {
+    const bool behind = p0 - (j0 + kKeys - 1) >= a.reach, ahead = p1 - j0 <= -a.reach;      // all of it as far as the reach
+    const float one = behind ? bias_behind : bias_ahead;
+    float mult = 1.f, add = 0.f;       // scores are x mult + add
+    if (PLAIN) {
+      mult = a.scale;
+      add = one;
+    } else if (!a.bias || behind || ahead) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) x[t] *= a.scale;
-    } else if (p0 - (j0 + kKeys - 1) >= a.reach) {      // all far behind
-      const float b = table[a.reach - from];
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) x[t] = x[t] * a.scale + b;
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = fmaf(x[t][r], a.scale, one);
+      }
     } else {
+      const float* const at = mytable + j0;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int r = 0; r < Tl::NR; ++r) {
-          const int away = min(max(p - (j0 + t * M + Tl::row(r, lane)), from), a.reach);
-          x[t][r] = fmaf(x[t][r], a.scale, table[away - from]);
-        }
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = fmaf(x[t][r], a.scale, at[t * M + Tl::row(r)]);
       }
     }
-    if (masked) {
+    if (!PLAIN && holes(j0)) {
+      const float* seen = seens[buf] + 4 * sub;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int r = 0; r < Tl::NR; ++r) x[t][r] = seen[t * M + Tl::row(r, lane)] == 0.f ? -__builtin_inff() : x[t][r];
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = seen[t * M + Tl::row(r)] == 0.f ? -__builtin_inff() : x[t][r];
       }
     }
-    if (a.causal && j0 + kKeys - 1 > p0) {
+    if (!PLAIN && a.causal && j0 + kKeys - 1 > p0) {
+      const int upto = p - j0 - 4 * sub;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int r = 0; r < Tl::NR; ++r) x[t][r] = j0 + t * M + Tl::row(r, lane) > p ? -__builtin_inff() : x[t][r];
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = t * M + Tl::row(r) > upto ? -__builtin_inff() : x[t][r];
       }
     }
     float top = x[0][0];
@@ -128,29 +154,65 @@ __global__ __launch_bounds__(256) void k_attn_forward(Args a) {
 #pragma unroll
       for (int r = 0; r < Tl::NR; ++r) top = fmaxf(top, x[t][r]);
     }
-    top = fmaxf(m, column_max<Tl::SUBS>(top));
-    const float off = top == -__builtin_inff() ? 0.f : top, off2 = off * kLog2e;        // no key seen so far: all terms are zero
-    const float keepf = exp2_((m - off) * kLog2e);
-    const bool exact = Tl::kExact || __any(far_off(off));
+    top = fmaxf(m, fmaf(column_max<Tl::SUBS>(top), mult, add));
+    const float off = top == -__builtin_inff() ? 0.f : top;        // no key seen so far: all terms are zero
+    const float f = exp2_((m - off) * kLog2e);
     m = top;
+    if (PLAIN) {
+      mult *= kLog2e;
+      add = (add - off) * kLog2e;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = exp2_(fmaf(x[t][r], mult, add));
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = exp2_((x[t][r] - off) * kLog2e);
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int r = 0; r < Tl::NR; ++r) {
-        x[t][r] = weight(x[t][r], off, off2, exact);
-        sum += x[t][r];
-      }
+      for (int r = 0; r < Tl::NR; ++r) sum += x[t][r];
     }
-    l = fmaf(l, keepf, sum);
-    if (__any(keepf != 1.f)) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] *= keepf;
-    }
+    l = fmaf(l, f, sum);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int first = j0 + t * M;
-      gather<Tl, DT>(o, sv + t * M * P, P, Packed<Tl>(x[t]), lane, slow, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
+      if (SEEN) gather_seen<Tl, DT>(o, sv + t * M * P, P, Packed<Tl>(x[t]), lane, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - j0 - t * M; });
+      else gather<Tl, DT>(o, sv + t * M * P, P, Packed<Tl>(x[t]), lane);
+    }
+  };
+  const int last = !some ? -1 : a.causal ? p1 : kend;
+  fetch(0);
+  bool odd = put(0, 0), odds = odd;
+  if (a.bias) {
+    bias_behind = table[0];
+    bias_ahead = table[bt.size - 1];
+    if (far_off(bias_behind)) plain_to = 0;
+    if (far_off(bias_ahead)) plain_from = 0x7fffffff;
+  }
+  for (int j0 = 0, buf = 0; j0 < kend; j0 += kKeys, buf ^= 1) {
+    const bool next = j0 + kKeys < kend;
+    if (next) fetch(j0 + kKeys);
+    if (j0 <= last && !odd) {      // this wave's queries see something of it
+      if (j0 + kKeys <= plain_to || (j0 >= plain_from && j0 + kKeys <= whole)) tile(std::true_type(), std::false_type(), j0, buf);
+      else tile(std::false_type(), std::false_type(), j0, buf);
+    }
+    if (next) odd = put(j0 + kKeys, buf ^ 1), odds |= odd;
+  }
+  if (odds) {      // what was left out
+    for (int j0 = 0; j0 < kend; j0 += kKeys) {
+      if (j0 + kKeys <= inside) continue;
+      nk.fetch(kbase, a.k.st, j0, there);
+      nv.fetch(vbase, a.v.st, j0, there);
+      __syncthreads();
+      if (put(j0, 0) && j0 <= last) tile(std::false_type(), std::true_type(), j0, 0);
     }
   }
   l = column_sum<Tl::SUBS>(l);
@@ -171,7 +233,7 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
   constexpr int DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P, W = 16 * NT;
   __shared__ __attribute__((aligned(16))) E values[4][W * P];
   __shared__ float tables[4][2 * W];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, sub = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, sub = lane >> 4;
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
   const int h = (int)(id % a.heads), y = h / a.group;
   int64_t n = id / a.heads;
@@ -253,7 +315,8 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
           x[t][r] = weight_of(x[t][r], top);
           l += x[t][r];
         }
-        gather<Tl, DT>(o, sv + 16 * t * P, P, Packed<Tl>(x[t]), lane, slow, [](int) { return 0; }, [&](int c) { return (int)(q.at + i0 + c) - 16 * t; });
+        if (!slow) gather<Tl, DT>(o, sv + 16 * t * P, P, Packed<Tl>(x[t]), lane);
+        else gather_seen<Tl, DT>(o, sv + 16 * t * P, P, Packed<Tl>(x[t]), lane, [](int) { return 0; }, [&](int c) { return (int)(q.at + i0 + c) - 16 * t; });
       }
       l = column_sum<4>(l);
       if (!live) continue;
@@ -289,7 +352,7 @@ __global__ __launch_bounds__(256) void k_attn_few(Args a) {
   constexpr int PER = ops::Elem<E>::kPer, KW = 64 / LPK, U = 4, STEP = 4 * KW * U;      // keys of a workgroup's step
   constexpr int ROOM = R * (LPK * PER + 2);
   __shared__ float joined[4][ROOM];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (lane % LPK) * PER, g = lane / LPK;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = (lane % LPK) * PER, g = lane / LPK;
   const int rows = a.group * a.Tq, blocks = (rows + R - 1) / R, kvs = a.heads / a.group;
   const uint32_t part = blockIdx.x % a.splits;
   uint32_t rest = blockIdx.x / a.splits;
@@ -438,7 +501,7 @@ __global__ __launch_bounds__(256) void k_attn_few(Args a) {
 template <class E>
 __global__ __launch_bounds__(256) void k_attn_join(Args a) {
   const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t at = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
   if (at >= a.N * a.heads * a.Tq) return;
   const int i = (int)(at % a.Tq), h = (int)(at / a.Tq % a.heads);
   const int64_t n = at / a.Tq / a.heads;
@@ -493,7 +556,7 @@ void few(const Args& a, hipStream_t st) {
 template <class Tl>
 void large(const Args& a, hipStream_t st) {
   const unsigned grid = (unsigned)(a.N * a.heads * ((a.Tq + 4 * Tl::M - 1) / (4 * Tl::M)));
-  const unsigned lds = a.bias ? 4 * (a.causal ? a.reach + 1 : 2 * a.reach + 1) : 0;
+  const unsigned lds = bias_bytes(a);
   if (a.d <= 16) hipLaunchKernelGGL((k_attn_forward<Tl, 1>), grid, 256, lds, st, a);
   else if (a.d <= 32) hipLaunchKernelGGL((k_attn_forward<Tl, 2>), grid, 256, lds, st, a);
   else if (a.d <= 64) hipLaunchKernelGGL((k_attn_forward<Tl, 4>), grid, 256, lds, st, a);

@@ -34,12 +34,14 @@ int32_t splits_of(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_h
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>((2048 + items - 1) / std::max<int64_t>(items, 1), Tk / 256));
 }
 struct Room {
-  int64_t delta, part;      // bytes
+  int64_t delta, part, joint;      // bytes
 };
-Room back_room(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t causal, int32_t buckets, int32_t reach) {
+Room back_room(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal, int32_t buckets, int32_t reach) {
   // `first`, which decides between the two forms, is not known here.
   const bool window = takes_window_back(Tk, d, heads / kv_heads, false);
-  Room r{round16(4 * N * heads * Tq), 0};
+  Room r{round16(4 * N * heads * Tq), 0, 0};
+  const Parts p = key_parts(Tq, Tk, N, heads, kv_heads, dtype == DGC_DTYPE_F32);
+  if (p.heads * p.rows > 1) r.joint = 8 * N * kv_heads * Tk * d * p.heads * p.rows;
   if (buckets) {
     // The larger of both row tiles' numbers of blocks.
     r.part = 4 * (int64_t)heads * back_slots(false, N, heads, 0, (Tq + 63) / 64) * table_size(reach, causal);
@@ -124,8 +126,8 @@ int64_t dgc_attn_workspace_bytes(int64_t Tq, int64_t Tk, int64_t N, int32_t head
   if (check(Tq, Tk, N, heads, kv_heads, d, dtype, buckets, reach) || too_many(Tq, Tk, N, heads)) return -1;
   if (N == 0 || Tq == 0) return 0;
   if (backward) {
-    const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, causal, buckets, reach);
-    return r.delta + r.part;
+    const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, dtype, causal, buckets, reach);
+    return r.delta + r.part + r.joint;
   }
   if (form_of(Tq, Tk) != kFew) return 0;
   const int64_t splits = splits_of(Tq, Tk, N, heads, kv_heads);
@@ -209,7 +211,8 @@ dgc_status_t dgc_attn_backward(const void* q, int64_t qt, int64_t qn, const void
     if (meet(in[x], in[11])) return ops::refuse(DGC_ERR_INVALID_ARG, kMeet);
   }
   a.lse = const_cast<float*>(lse);
-  const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, causal, buckets, reach);
+  const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, dtype, causal, buckets, reach);
+  a.joint = reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta + r.part);
   a.delta = static_cast<float*>(workspace);
   a.part = dbias && N > 0 && Tq > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta) : nullptr;
   (dtype == DGC_DTYPE_F32 ? attn_backward_f32 : attn_backward_bf16)(a, dbias, static_cast<hipStream_t>(stream));

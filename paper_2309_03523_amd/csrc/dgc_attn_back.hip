@@ -9,10 +9,12 @@
 // Rounding: bf16 tensors enter products as they are, scores, P, dP, D and dS are fp32; P and dS are rounded to bf16 (2^-9 of themselves)
 // for the products of dv, dq and dk, which are summed in fp32; the bias' gradient sums dS as it is, in fp32 and at the end in double.
 //
-// The bias' gradient: every wave adds dS by distance into tables of its own in LDS.  Lanes of one row of lanes hold one key (or query) and neighbouring
-// queries (keys), so their distances differ; each row of lanes has a table, so an instruction never adds twice to one place, and a
-// wave's instructions are taken in order: the sums have one order.  k_attn_bias joins the tables.
+// The bias' gradient: every wave sums dS by distance into a table of its own in LDS.  In k_attn_dq it lays a tile's dS out slanted, so that a distance is
+// a column, and each lane sums one (adding with LDS atomics took 126 cycles an instruction, five times as much).  In
+// k_attn_window_back tiles are few and atomics do: each of the four rows of lanes holds one key and neighbouring queries, whose distances differ, and
+// has a table, so an instruction never adds twice to one place.  All sums have one order; k_attn_bias joins the tables.
 #include <algorithm>
+#include <type_traits>
 
 #include "dgc_attn_dev.h"
 
@@ -30,7 +32,7 @@ __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
   constexpr int DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P, W = 16 * NT, PT = 16 + 16 / (int)sizeof(E);
   __shared__ __attribute__((aligned(16))) E room[4][(W + 32) * P + 2 * 16 * PT];
   extern __shared__ float tables[];       // with a bias: [4 waves][group][1 + 4][2 W], the bias by distance and four tables of sums
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, sub = lane >> 4, kvs = a.heads / a.group;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, sub = lane >> 4, kvs = a.heads / a.group;
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
   const int y = (int)(id % kvs), slot = (int)(id / kvs);
   if (slot >= a.slots) return;
@@ -134,9 +136,18 @@ __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
           Tl::store(ss + col * PT + 4 * sub, ds);
           wave_fence();
           const int apart = 16 * t - at - i0;       // key c is seen from query apart + c of the tile on
-          gather<Tl, DT>(dq, sk + 16 * t * P, P, Packed<Tl>(ds), lane, odd_k, [](int) { return 0; }, [&](int c) { return c - apart; });
-          gather<Tl, DT>(dv[t], sg, P, Packed<Tl>(Tl::across(sp, PT, 0, 0, lane)), lane, odd_qg, [&](int c) { return apart + c; }, [](int) { return 15; });
-          gather<Tl, DT>(dk[t], sq, P, Packed<Tl>(Tl::across(ss, PT, 0, 0, lane)), lane, odd_qg, [&](int c) { return apart + c; }, [](int) { return 15; });
+          const Packed<Tl> p_t(Tl::across(sp, PT, 0, 0, lane)), ds_t(Tl::across(ss, PT, 0, 0, lane));
+          if (!odd_k) gather<Tl, DT>(dq, sk + 16 * t * P, P, Packed<Tl>(ds), lane);
+          else gather_seen<Tl, DT>(dq, sk + 16 * t * P, P, Packed<Tl>(ds), lane, [](int) { return 0; }, [&](int c) { return c - apart; });
+          if (!odd_qg) {
+            gather<Tl, DT>(dv[t], sg, P, p_t, lane);
+            gather<Tl, DT>(dk[t], sq, P, ds_t, lane);
+          } else {
+            auto lo = [&](int c) { return apart + c; };
+            auto hi = [](int) { return 15; };
+            gather_seen<Tl, DT>(dv[t], sg, P, p_t, lane, lo, hi);
+            gather_seen<Tl, DT>(dk[t], sq, P, ds_t, lane, lo, hi);
+          }
         }
         if (i < hi && a.dq.p) {
           if (!live) {
@@ -198,28 +209,36 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 
 // ---------------------------------------------------------------------------------------------------- dq, and the bias' gradient
 //
-// As the forward pass: 4 M queries a workgroup, keys in tiles of 64 through LDS.
+// As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it leaves dP - D.
 template <class Tl, int KS>
-__global__ __launch_bounds__(256) void k_attn_dq(Args a) {
+__global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args a) {
   typedef typename Tl::E E;
-  constexpr int M = Tl::M, NT = kTile / M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
-  constexpr int SETS = M == 32 ? 2 : 1;     // tables of a wave: 16-column tiles add one row of lanes after the other to one
-  __shared__ __attribute__((aligned(16))) E sk[kTile * P], sv[kTile * P];
-  __shared__ float seen[kTile];
-  extern __shared__ float table[];          // the bias by distance, then the waves' tables of sums
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = Tl::col(lane), sub = Tl::sub(lane);
+  constexpr int kKeys = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  __shared__ __attribute__((aligned(16))) E room[2][2 * kKeys * P];
+  __shared__ float seens[2][kKeys];
+  extern __shared__ float table[];          // the bias by distance, then the waves' tables of sums and their slanted tiles
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = Tl::col(lane), sub = Tl::sub(lane);
   const int blocks = (a.Tq + 4 * M - 1) / (4 * M), h = blockIdx.x % a.heads, slot = blockIdx.x / a.heads, y = h / a.group;
-  const int from = a.causal ? 0 : -a.reach, tfrom = table_from(a.reach, a.causal), tsize = table_size(a.reach, a.causal);
-  float* const sums = table + a.reach - from + 1;
+  const BiasTable bt(a);
+  const int tfrom = table_from(a.reach, a.causal), tsize = table_size(a.reach, a.causal);
+  float* const sums = table + bt.size;
   if (a.bias) {
-    for (int x = threadIdx.x; x <= a.reach - from; x += 256) table[x] = bias_at(a, h, from + x);
+    bt.fill(a, table, h, true);
     if (a.part) {
-      for (int x = threadIdx.x; x < 4 * SETS * tsize; x += 256) sums[x] = 0.f;
+      for (int x = threadIdx.x; x < 4 * tsize; x += 256) sums[x] = 0.f;
     }
   }
-  float* const mysums = sums + (wave * SETS + (SETS == 2 ? sub : 0)) * tsize;
-  float behind = 0.f, ahead = 0.f;          // sums of tiles that are far off as a whole
-  for (int64_t item = slot; item < a.N * blocks; item += a.slots) {
+  float* const mysums = sums + wave * tsize;
+  float* const slant = sums + 4 * tsize + wave * (2 * M * M);      // row q: dS of query q at column M - 1 + q - key
+  float farsum = 0.f, aheadsum = 0.f;       // sums of tiles that are far off as a whole
+  Stage<E, kKeys, KS> nk, nv;
+  nk.init(a.k.st, a.d);
+  nv.init(a.v.st, a.d);
+  const int64_t items = a.N * blocks;
+  for (int64_t round = 0; round * a.slots < items; ++round) {
+    // The longest walks first, every second round backwards: with several items a workgroup, long ones go with short ones.
+    const int64_t item = round * a.slots + (round & 1 ? a.slots - 1 - slot : slot);
+    if (item >= items) continue;
     const int64_t n = item % a.N;
     const int i0 = (int)(blocks - 1 - item / a.N) * 4 * M;
     const Seq q(a, n);
@@ -229,12 +248,15 @@ __global__ __launch_bounds__(256) void k_attn_dq(Args a) {
     const int mine = i0 + wave * M, i = mine + col;
     const bool row = i >= q.lo && i < q.hi;
     const int64_t stat = (n * a.heads + h) * a.Tq + i;
-    const float lse = row ? a.lse[stat] : -__builtin_inff(), D = row ? a.delta[stat] : 0.f, lse2 = lse * kLog2e;
-    const bool live = lse != -__builtin_inff();
-    const bool exact = Tl::kExact || __any(live && far_off(lse));
+    const float given = row ? a.lse[stat] : -__builtin_inff();
+    const bool live = given != -__builtin_inff();
+    const float lse = live ? given : __builtin_inff();       // of a query without gradients: all weights are zero
+    const bool clean = !Tl::kExact && !__any(row && !live);
     const bool some = max(mine, q.lo) < min(mine + M, q.hi);
     const int p0 = some ? (int)(q.at + max(mine, q.lo)) : -1, p1 = some ? (int)(q.at + min(mine + M, q.hi) - 1) : -1, p = live ? (int)(q.at + i) : -1;
+    const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place
     typename Tl::Frag fq[KS], fg[KS];
+    typename Tl::Acc minus_D = (typename Tl::Acc)(live ? -a.delta[stat] : 0.f);
     {
       const E* qrow = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
       const E* grow = static_cast<const E*>(a.go.p) + (int64_t)i * a.go.st + n * a.go.sn + h * a.d;
@@ -249,79 +271,126 @@ __global__ __launch_bounds__(256) void k_attn_dq(Args a) {
     const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d;
     const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d;
     auto there = [&](int j) { return j < kend && (!a.keep || a.keep[(int64_t)j * a.N + n]); };
-    Stage<E, kTile, KS> nk, nv;
-    nk.fetch(kbase, a.k.st, 0, a.d, there);
-    nv.fetch(vbase, a.v.st, 0, a.d, there);
+    // As in the forward pass: where tiles change their kind.
+    const int whole = a.keep ? 0 : kend, inside = a.causal ? (int)(q.at + least) + 1 : kend + kKeys;
+    int plain_to = !clean ? 0 : min(whole, min(a.causal ? p0 + 1 : kend, a.bias ? p0 - a.reach + 1 : kend));
+    int plain_from = !clean || a.causal ? 0x7fffffff : p1 + a.reach;
+    const int last = !some ? -1 : a.causal ? p1 : kend;
+    auto holes = [&](int j0) { return j0 + kKeys > whole; };
+    const bool near = nk.near && nv.near;
+    const E *knext = kbase, *vnext = vbase;
+    auto fetch = [&](int j0) {
+      if (!holes(j0) && near) {
+        nk.fetch_all(knext);
+        nv.fetch_all(vnext);
+        knext += kKeys * a.k.st;
+        vnext += kKeys * a.v.st;
+      } else {
+        nk.fetch(kbase, a.k.st, j0, there);
+        nv.fetch(vbase, a.v.st, j0, there);
+      }
+    };
+    // Lays out a tile; whether a zero gradient would meet a key of it that is not finite.
+    auto put = [&](int j0, int b) -> bool {
+      nk.put(room[b], P);
+      nv.put(room[b] + kKeys * P, P);
+      if (holes(j0) && threadIdx.x < kKeys) seens[b][threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
+      if (j0 + kKeys > inside) return __syncthreads_or(nk.template odd<Tl>());
+      __syncthreads();
+      return false;
+    };
     typename Tl::Acc dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt] = (typename Tl::Acc)(0.f);
 
-    for (int j0 = 0; j0 < kend; j0 += kTile) {
-      __syncthreads();
-      nk.put(sk, P);
-      nv.put(sv, P);
-      const bool edge = a.causal && j0 + kTile - 1 > q.at + least;
-      const bool masked = a.keep || j0 + kTile > kend;
-      if (masked && threadIdx.x < kTile) seen[threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
-      const bool slow = edge ? __syncthreads_or(nk.template odd<Tl>()) : (__syncthreads(), false);
-      if (j0 + kTile < kend) {
-        nk.fetch(kbase, a.k.st, j0 + kTile, a.d, there);
-        nv.fetch(vbase, a.v.st, j0 + kTile, a.d, there);
-      }
-      if (!some || (a.causal && j0 > p1)) continue;
-      const bool far = a.bias && p0 - (j0 + kTile - 1) >= a.reach, before = a.bias && p1 - j0 <= -a.reach;
-#pragma unroll
+    // One tile.  PLAIN: every query sees all of it, with one bias.  SEEN: keys that are not finite reach only those that see them.
+    float bias_behind = 0.f, bias_ahead = 0.f;
+    auto tile = [&](auto plain, auto seen_only, int j0, int buf) {
+      constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
+      const E *sk = room[buf], *sv = sk + kKeys * P;
+      const bool behind = p0 - (j0 + kKeys - 1) >= a.reach, ahead = p1 - j0 <= -a.reach;
+      const float one = behind ? bias_behind : bias_ahead;
+      const float mult = a.scale * kLog2e, add = (one - lse) * kLog2e;
+#pragma unroll KS >= 4 ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int first = j0 + t * M;
-        if (a.causal && first > p1) break;
-        typename Tl::Acc x = (typename Tl::Acc)(0.f), z = x;
+        if (!PLAIN && (first >= kend || (a.causal && first > p1))) break;
+        typename Tl::Acc x = (typename Tl::Acc)(0.f), z = minus_D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           x = Tl::mma(Tl::rows(sk + t * M * P, P, s, lane), fq[s], x);
           z = Tl::mma(Tl::rows(sv + t * M * P, P, s, lane), fg[s], z);
         }
-        if (!a.bias || far || before) {
-          const float b = !a.bias ? 0.f : table[far ? a.reach - from : 0];
+        if (PLAIN) {
 #pragma unroll
-          for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, b);
+          for (int r = 0; r < Tl::NR; ++r) z[r] *= exp2_(fmaf(x[r], mult, add));
         } else {
+          if (!a.bias || behind || ahead) {
 #pragma unroll
-          for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, table[min(max(p - (first + Tl::row(r, lane)), from), a.reach) - from]);
-        }
-        const bool holes = masked || (a.causal && first + M - 1 > p0) || !__all(live);
-        if (holes) {
+            for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, one);
+          } else {
+#pragma unroll
+            for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, mytable[first + Tl::row(r)]);
+          }
+          const bool masked = holes(j0);
+          const float* seen = seens[buf] + t * M + 4 * sub;
+          const int upto = !live ? -1 : a.causal ? p - first - 4 * sub : M;
 #pragma unroll
           for (int r = 0; r < Tl::NR; ++r) {
-            const int j = first + Tl::row(r, lane);
-            const bool out = !live || (a.causal && j > p) || (masked && seen[j - j0] == 0.f);
-            x[r] = out ? 0.f : weight(x[r], lse, lse2, exact);
-            z[r] = out ? 0.f : x[r] * (z[r] - D);
+            const bool out = Tl::row(r) > upto || (masked && seen[Tl::row(r)] == 0.f);
+            z[r] = out ? 0.f : z[r] * exp2_((x[r] - lse) * kLog2e);
           }
-        } else {
-#pragma unroll
-          for (int r = 0; r < Tl::NR; ++r) z[r] = weight(x[r], lse, lse2, exact) * (z[r] - D);
         }
         if (a.part) {
-          if (far || before) {
+          if (behind || ahead) {
             float s = 0.f;
 #pragma unroll
             for (int r = 0; r < Tl::NR; ++r) s += z[r];
-            (far ? behind : ahead) += s;
+            if (behind) farsum += s;
+            else aheadsum += s;
           } else {
+            float* const at = slant + col * (2 * M + 1) + M - 1 - 4 * sub;
+            wave_fence();
 #pragma unroll
-            for (int r = 0; r < Tl::NR; ++r) {
-              const int away = p - (first + Tl::row(r, lane)) - tfrom;
-              if constexpr (SETS == 2) {
-                if (z[r] != 0.f) add_lds(mysums + away, z[r]);
-              } else {
-                for (int s = 0; s < Tl::SUBS; ++s) {
-                  if (s == sub && z[r] != 0.f) add_lds(mysums + away, z[r]);
-                }
-              }
+            for (int r = 0; r < Tl::NR; ++r) at[-Tl::row(r)] = z[r];
+            wave_fence();
+            if (lane < 2 * M) {
+              float s = 0.f;
+#pragma unroll 8
+              for (int x = 0; x < M; ++x) s += (unsigned)(lane - x) < (unsigned)M ? slant[x * 2 * M + lane] : 0.f;
+              const int64_t place = q.at + mine - first + lane - (M - 1) - tfrom;
+              if (s != 0.f && place >= 0 && place < tsize) mysums[place] += s;
             }
           }
         }
-        gather<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane, slow, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
+        if (SEEN) gather_seen<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
+        else gather<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane);
+      }
+    };
+    fetch(0);
+    bool odd = put(0, 0), odds = odd;
+    if (a.bias) {
+      bias_behind = table[0];
+      bias_ahead = table[bt.size - 1];
+      if (far_off(bias_behind)) plain_to = 0;
+      if (far_off(bias_ahead)) plain_from = 0x7fffffff;
+    }
+    for (int j0 = 0, buf = 0; j0 < kend; j0 += kKeys, buf ^= 1) {
+      const bool next = j0 + kKeys < kend;
+      if (next) fetch(j0 + kKeys);
+      if (j0 <= last && !odd) {
+        if (j0 + kKeys <= plain_to || (j0 >= plain_from && j0 + kKeys <= whole)) tile(std::true_type(), std::false_type(), j0, buf);
+        else tile(std::false_type(), std::false_type(), j0, buf);
+      }
+      if (next) odd = put(j0 + kKeys, buf ^ 1), odds |= odd;
+    }
+    if (odds) {      // what was left out
+      for (int j0 = 0; j0 < kend; j0 += kKeys) {
+        if (j0 + kKeys <= inside) continue;
+        nk.fetch(kbase, a.k.st, j0, there);
+        nv.fetch(vbase, a.v.st, j0, there);
+        __syncthreads();
+        if (put(j0, 0) && j0 <= last) tile(std::false_type(), std::true_type(), j0, 0);
       }
     }
     if (row && a.dq.p) {
@@ -335,16 +404,16 @@ __global__ __launch_bounds__(256) void k_attn_dq(Args a) {
   }
   if (a.part) {
     __syncthreads();
-    behind = wave_sum(behind);
-    ahead = wave_sum(ahead);
+    farsum = wave_sum(farsum);
+    aheadsum = wave_sum(aheadsum);
     if (lane == 0) {
-      sums[wave * SETS * tsize + a.reach - tfrom] += behind;
-      if (!a.causal) sums[wave * SETS * tsize - a.reach - tfrom] += ahead;
+      mysums[a.reach - tfrom] += farsum;
+      if (!a.causal) mysums[-a.reach - tfrom] += aheadsum;
     }
     __syncthreads();
     for (int x = threadIdx.x; x < tsize; x += 256) {
       float s = 0.f;
-      for (int w = 0; w < 4 * SETS; ++w) s += sums[w * tsize + x];
+      for (int w = 0; w < 4; ++w) s += sums[w * tsize + x];
       a.part[((int64_t)h * a.slots + slot) * tsize + x] = s;
     }
   }
@@ -353,23 +422,25 @@ __global__ __launch_bounds__(256) void k_attn_dq(Args a) {
 // ---------------------------------------------------------------------------------------------------- dk, dv
 //
 // A workgroup takes 4 M keys of one sequence and key head, a wave M of them in registers, and walks over the queries that see them in tiles of
-// 64 that lie in LDS, for one head that shares the keys after the other.
+// 2 M that lie in LDS, for one head that shares the keys after the other.  The products that form scores and dP start from -lse / scale and -D of
+// their rows, which come from LDS as four numbers at a time: they leave (s - lse) / scale and dP - D.
 template <class Tl, int KS>
-__global__ __launch_bounds__(256) void k_attn_dkv(Args a) {
+__global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args a) {
   typedef typename Tl::E E;
-  constexpr int M = Tl::M, NT = kTile / M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
-  __shared__ __attribute__((aligned(16))) E sq[kTile * P], sg[kTile * P];
-  __shared__ __attribute__((aligned(16))) float slse[kTile], sD[kTile];
+  constexpr int kRows = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  __shared__ __attribute__((aligned(16))) E room[2][2 * kRows * P];
+  __shared__ __attribute__((aligned(16))) float stats[2][3][kRows];      // lse, -lse / scale, -D
   extern __shared__ float table[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = Tl::col(lane), sub = Tl::sub(lane), kvs = a.heads / a.group;
-  const uint32_t pairs = (uint32_t)(a.N * kvs), pair = blockIdx.x % pairs;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = Tl::col(lane), sub = Tl::sub(lane), kvs = a.heads / a.group;
+  const uint32_t pairs = (uint32_t)(a.N * kvs), pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, parts = a.head_parts * a.row_parts;
   const int64_t n = pair / kvs;
-  const int y = pair % kvs, k0 = (int)(blockIdx.x / pairs) * 4 * M;
+  const int y = pair % kvs, k0 = (int)(rest / parts) * 4 * M, part = rest % parts, head_part = part / a.row_parts, row_part = part % a.row_parts;
   const Seq q(a, n);
   if (k0 >= q.len) return;
   const int mine = k0 + wave * M, j = mine + col;
   const bool there = j < q.len && (!a.keep || a.keep[(int64_t)j * a.N + n]);
-  const int from = a.causal ? 0 : -a.reach;
+  const BiasTable bt(a);
+  const float* const mytable = table - j - bt.from + 4 * sub;      // plus a query's position
   typename Tl::Frag fk[KS], fv[KS];
   {
     const E* krow = static_cast<const E*>(a.k.p) + (int64_t)j * a.k.st + n * a.k.sn + y * a.d;
@@ -385,87 +456,167 @@ __global__ __launch_bounds__(256) void k_attn_dkv(Args a) {
   typename Tl::Acc dk[DT], dv[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = (typename Tl::Acc)(0.f);
-  const int begin = a.causal ? (int)min((int64_t)q.hi, max((int64_t)q.lo, k0 - q.at)) : q.lo;      // the first query that sees one of these keys
-  for (int g = 0; g < a.group; ++g) {
+  const int begin_all = a.causal ? (int)min((int64_t)q.hi, max((int64_t)q.lo, k0 - q.at)) : q.lo;      // the first query that sees one of these keys
+  Stage<E, kRows, KS> nq, ng;
+  nq.init(a.q.st, a.d);
+  ng.init(a.go.st, a.d);
+  const bool near = nq.near && ng.near;
+  constexpr int NS = Stage<E, kRows, KS>::N;
+  const bool started = !Tl::kExact && a.scale > 1e-6f;      // products may start from -lse / scale
+  // This workgroup's part of the heads that share the keys, and of their queries.
+  const int heads_each = a.group / a.head_parts, rows_each = ((q.hi - begin_all + a.row_parts - 1) / a.row_parts + kRows - 1) / kRows * kRows;
+  const int begin = min(begin_all + row_part * rows_each, q.hi), end = min(begin + rows_each, q.hi);
+  for (int g = head_part * heads_each; g < (head_part + 1) * heads_each; ++g) {
     const int h = y * a.group + g;
     __syncthreads();
-    if (a.bias) {
-      for (int x = threadIdx.x; x <= a.reach - from; x += 256) table[x] = bias_at(a, h, from + x);
-    }
+    if (a.bias) bt.fill(a, table, h, false);
     const E* qbase = static_cast<const E*>(a.q.p) + n * a.q.sn + h * a.d;
     const E* gbase = static_cast<const E*>(a.go.p) + n * a.go.sn + h * a.d;
     const float* lses = a.lse + (n * a.heads + h) * a.Tq;
     const float* Ds = a.delta + (n * a.heads + h) * a.Tq;
-    // A query that sees nothing gives no gradient: its rows are zero, whatever they hold.
-    auto live = [&](int i) { return i >= q.lo && i < q.hi && lses[i] != -__builtin_inff(); };
-    Stage<E, kTile, KS> nq, ng;
-    float nlse = 0.f, nD = 0.f;
+    float nlse = 0.f, nD = 0.f, rowlse[NS];
+    auto token = [&](int i) { return i >= q.lo && i < end; };
     auto fetch = [&](int i0) {
-      nq.fetch(qbase, a.q.st, i0, a.d, live);
-      ng.fetch(gbase, a.go.st, i0, a.d, live);
-      if (threadIdx.x < kTile) {
+      if (i0 + kRows <= end && near) {
+        nq.fetch_all(qbase + i0 * a.q.st);
+        ng.fetch_all(gbase + i0 * a.go.st);
+#pragma unroll
+        for (int x = 0; x < NS; ++x) rowlse[x] = nq.has[x] ? lses[i0 + nq.row(x)] : 0.f;
+      } else {
+        nq.fetch(qbase, a.q.st, i0, token);
+        ng.fetch(gbase, a.go.st, i0, token);
+#pragma unroll
+        for (int x = 0; x < NS; ++x) rowlse[x] = nq.has[x] && token(i0 + nq.row(x)) ? lses[i0 + nq.row(x)] : 0.f;
+      }
+      if (threadIdx.x < kRows) {
         const int i = i0 + threadIdx.x;
-        const bool ok = live(i);
-        nlse = ok ? lses[i] : __builtin_inff();      // its weights are zero
+        const float given = token(i) ? lses[i] : -__builtin_inff();
+        const bool ok = given != -__builtin_inff();
+        nlse = ok ? given : __builtin_inff();      // its weights are zero
         nD = ok ? Ds[i] : 0.f;
       }
     };
-    if (begin < q.hi) fetch(begin);
-    for (int i0 = begin; i0 < q.hi; i0 += kTile) {
-      __syncthreads();
-      nq.put(sq, P);
-      ng.put(sg, P);
-      if (threadIdx.x < kTile) slse[threadIdx.x] = nlse, sD[threadIdx.x] = nD;
-      const bool edge = a.causal && q.at + i0 < k0 + 4 * M - 1;
-      const bool slow = edge ? __syncthreads_or(nq.template odd<Tl>() || ng.template odd<Tl>()) : (__syncthreads(), false);
-      if (i0 + kTile < q.hi) fetch(i0 + kTile);
-      const int first_p = (int)(q.at + i0);
-      if (mine >= q.len || (a.causal && first_p + kTile - 1 < mine)) continue;
-      const float mylse = slse[lane];
-      const bool exact = Tl::kExact || __any(mylse < __builtin_inff() && far_off(mylse));
-      const bool far = a.bias && first_p - (mine + M - 1) >= a.reach, before = a.bias && first_p + kTile - 1 - mine <= -a.reach;
+    auto put = [&](int i0, int b) -> bool {
+      // A query that sees nothing gives no gradient: its rows are zero, whatever they hold.
 #pragma unroll
+      for (int x = 0; x < NS; ++x) {
+        if (__any(rowlse[x] == -__builtin_inff())) {
+          if (rowlse[x] == -__builtin_inff()) nq.w[x] = ng.w[x] = make_uint4(0, 0, 0, 0);
+        }
+      }
+      nq.put(room[b], P);
+      ng.put(room[b] + kRows * P, P);
+      if (threadIdx.x < kRows) {
+        stats[b][0][threadIdx.x] = nlse;
+        stats[b][1][threadIdx.x] = started ? -nlse / a.scale : 0.f;
+        stats[b][2][threadIdx.x] = -nD;
+      }
+      if (a.causal && q.at + i0 < k0 + 4 * M - 1) return __syncthreads_or(nq.template odd<Tl>() || ng.template odd<Tl>());
+      __syncthreads();
+      return false;
+    };
+    // One tile.  PLAIN: all its queries see all of the wave's keys, with one bias.  SEEN: queries that are not finite reach only the keys that they see.
+    float bias_behind = 0.f, bias_ahead = 0.f;
+    auto tile = [&](auto plain, auto seen_only, int i0, int buf, bool exact) {
+      constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
+      const E *sq = room[buf], *sg = sq + kRows * P;
+      const int first_p = (int)(q.at + i0);
+      const bool behind = first_p - (mine + M - 1) >= a.reach, ahead = first_p + kRows - 1 - mine <= -a.reach;
+      const float one = behind ? bias_behind : bias_ahead, mult = a.scale * kLog2e, add = one * kLog2e;
+#pragma unroll KS >= 4 ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int pt = first_p + t * M;
-        if (a.causal && pt + M - 1 < mine) continue;
-        typename Tl::Acc x = (typename Tl::Acc)(0.f), z = x;
+        if (!PLAIN && ((a.causal && pt + M - 1 < mine) || i0 + t * M >= end)) continue;
+        typename Tl::Acc x, z;
+#pragma unroll
+        for (int r = 0; r < Tl::NR; r += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(stats[buf][2] + t * M + 4 * sub + Tl::row(r));
+          z[r] = u.x; z[r + 1] = u.y; z[r + 2] = u.z; z[r + 3] = u.w;
+        }
+        if (PLAIN || !exact) {
+#pragma unroll
+          for (int r = 0; r < Tl::NR; r += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(stats[buf][1] + t * M + 4 * sub + Tl::row(r));
+            x[r] = u.x; x[r + 1] = u.y; x[r + 2] = u.z; x[r + 3] = u.w;
+          }
+        } else {
+          x = (typename Tl::Acc)(0.f);
+        }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           x = Tl::mma(Tl::rows(sq + t * M * P, P, s, lane), fk[s], x);
           z = Tl::mma(Tl::rows(sg + t * M * P, P, s, lane), fv[s], z);
         }
-        if (!a.bias || far || before) {
-          const float b = !a.bias ? 0.f : table[far ? a.reach - from : 0];
-#pragma unroll
-          for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, b);
-        } else {
-#pragma unroll
-          for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, table[min(max(pt + Tl::row(r, lane) - j, from), a.reach) - from]);
-        }
-        const bool holes = a.causal && pt < mine + M - 1;
-#pragma unroll
-        for (int r = 0; r < Tl::NR; r += 4) {
-          const float4 l4 = *reinterpret_cast<const float4*>(slse + t * M + Tl::row(r, lane));
-          const float4 d4 = *reinterpret_cast<const float4*>(sD + t * M + Tl::row(r, lane));
-          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[r + e] = weight(x[r + e], ls[e], ls[e] * kLog2e, exact);
-            z[r + e] = x[r + e] * (z[r + e] - ds[e]);
-          }
-        }
-        if (holes) {
+        if (PLAIN) {
 #pragma unroll
           for (int r = 0; r < Tl::NR; ++r) {
-            const bool out = pt + Tl::row(r, lane) < j;
-            x[r] = out ? 0.f : x[r];
-            z[r] = out ? 0.f : z[r];
+            x[r] = exp2_(fmaf(x[r], mult, add));
+            z[r] *= x[r];
+          }
+        } else {
+          if (!a.bias || behind || ahead) {
+#pragma unroll
+            for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, one);
+          } else {
+#pragma unroll
+            for (int r = 0; r < Tl::NR; ++r) x[r] = fmaf(x[r], a.scale, mytable[pt + Tl::row(r)]);
+          }
+          if (exact) {
+#pragma unroll
+            for (int r = 0; r < Tl::NR; r += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(stats[buf][0] + t * M + 4 * sub + Tl::row(r));
+              x[r] -= u.x; x[r + 1] -= u.y; x[r + 2] -= u.z; x[r + 3] -= u.w;
+            }
+          }
+          const int least = a.causal ? j - pt - 4 * sub : -1;
+#pragma unroll
+          for (int r = 0; r < Tl::NR; ++r) {
+            const bool out = Tl::row(r) < least;
+            x[r] = out ? 0.f : exp2_(x[r] * kLog2e);
+            z[r] = out ? 0.f : z[r] * x[r];
           }
         }
-        auto lo = [&](int c) { return mine + c - pt; };
-        auto hi = [](int) { return M - 1; };
-        gather<Tl, DT>(dv, sg + t * M * P, P, Packed<Tl>(x), lane, slow, lo, hi);
-        gather<Tl, DT>(dk, sq + t * M * P, P, Packed<Tl>(z), lane, slow, lo, hi);
+        if (SEEN) {
+          auto lo = [&](int c) { return mine + c - pt; };
+          auto hi = [](int) { return M - 1; };
+          gather_seen<Tl, DT>(dv, sg + t * M * P, P, Packed<Tl>(x), lane, lo, hi);
+          gather_seen<Tl, DT>(dk, sq + t * M * P, P, Packed<Tl>(z), lane, lo, hi);
+        } else {
+          gather<Tl, DT>(dv, sg + t * M * P, P, Packed<Tl>(x), lane);
+          gather<Tl, DT>(dk, sq + t * M * P, P, Packed<Tl>(z), lane);
+        }
+      }
+    };
+    if (begin >= end) continue;
+    // This wave: its keys are seen from query `from_i` on, and by all of a tile from `full_i` on; `plain_from`, `plain_to`: with one bias, behind or ahead.
+    const int from_i = mine >= q.len ? 0x7fffffff : a.causal ? (int)(mine - q.at) - (kRows - 1) : begin;
+    int plain_from = !started ? 0x7fffffff : (int)min(max(a.causal ? mine + M - 1 - q.at : (int64_t)begin, a.bias ? mine + M - 1 + a.reach - q.at : (int64_t)begin), (int64_t)0x7fffffff);
+    int plain_to = !started || a.causal || !a.bias ? -1 : (int)max(mine - a.reach - (kRows - 1) - q.at, (int64_t)-1);
+    auto take = [&](auto seen_only, int i0, int buf) {
+      const float mylse = stats[buf][0][lane % kRows];
+      const bool exact = !started || __any(mylse < __builtin_inff() && far_off(mylse));
+      if (!decltype(seen_only)::value && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), std::false_type(), i0, buf, false);
+      else tile(std::false_type(), seen_only, i0, buf, exact);
+    };
+    fetch(begin);
+    bool odd = put(begin, 0), odds = odd;
+    if (a.bias) {
+      bias_behind = table[bt.size - 1];
+      bias_ahead = table[0];
+      if (far_off(bias_behind)) plain_from = 0x7fffffff;
+      if (far_off(bias_ahead)) plain_to = -1;
+    }
+    for (int i0 = begin, buf = 0; i0 < end; i0 += kRows, buf ^= 1) {
+      const bool next = i0 + kRows < end;
+      if (next) fetch(i0 + kRows);
+      if (i0 >= from_i && !odd) take(std::false_type(), i0, buf);
+      if (next) odd = put(i0 + kRows, buf ^ 1), odds |= odd;
+    }
+    if (odds) {      // what was left out
+      for (int i0 = begin; i0 < end && q.at + i0 < k0 + 4 * M - 1; i0 += kRows) {
+        fetch(i0);
+        __syncthreads();
+        if (put(i0, 0) && i0 >= from_i) take(std::true_type(), i0, 0);
       }
     }
   }
@@ -474,21 +625,59 @@ __global__ __launch_bounds__(256) void k_attn_dkv(Args a) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = (typename Tl::Acc)(0.f);
   }
+  if (parts > 1) {
+    float* to = a.joint + (((int64_t)part * pairs + pair) * a.Tk + j) * 2 * a.d;
+    store_sums<Tl, DT>(to, dk, a.scale, a.d, lane);
+    store_sums<Tl, DT>(to + a.d, dv, 1.f, a.d, lane);
+    return;
+  }
   if (a.dk.p) store_column<Tl, DT>(static_cast<E*>(const_cast<void*>(a.dk.p)) + (int64_t)j * a.dk.st + n * a.dk.sn + y * a.d, dk, a.scale, a.d, lane);
   if (a.dv.p) store_column<Tl, DT>(static_cast<E*>(const_cast<void*>(a.dv.p)) + (int64_t)j * a.dv.st + n * a.dv.sn + y * a.d, dv, 1.f, a.d, lane);
 }
 
+// The sum of the parts: four numbers a thread, dk and dv of a key side by side.
+template <class E>
+__global__ __launch_bounds__(256) void k_attn_dkv_join(Args a) {
+  const int kvs = a.heads / a.group, parts = a.head_parts * a.row_parts, per = a.d / 2;      // 2 d / 4
+  const int64_t keys = a.N * kvs * a.Tk, all = keys * per;
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < all; x += (int64_t)gridDim.x * 256) {
+    const int64_t key = x / per;
+    int c = (int)(x % per) * 4;
+    const int j = (int)(key % a.Tk), y = (int)(key / a.Tk % kvs);
+    const int64_t n = key / a.Tk / kvs;
+    const int len = a.lengths ? min(max(a.lengths[n], 0), a.Tk) : a.Tk;
+    if (j >= len) continue;
+    float4 s = *reinterpret_cast<const float4*>(a.joint + key * 2 * a.d + c);
+    for (int k = 1; k < parts; ++k) {
+      const float4 u = *reinterpret_cast<const float4*>(a.joint + (k * keys + key) * 2 * a.d + c);
+      s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
+    }
+    const Rows& to = c < a.d ? a.dk : a.dv;
+    if (c >= a.d) c -= a.d;
+    if (!to.p) continue;
+    E* at = static_cast<E*>(const_cast<void*>(to.p)) + (int64_t)j * to.st + n * to.sn + y * a.d + c;
+    if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(at) = make_uint2(pack2(s.x, s.y), pack2(s.z, s.w));
+    else *reinterpret_cast<float4*>(at) = s;
+  }
+}
+
+
 // ---------------------------------------------------------------------------------------------------- the bias' gradient
 //
-// part[h][slot][x] holds sums of distance from + x: one workgroup a head and bucket sums those of the bucket, in one order, in double.
+// part[h][slot][x] holds sums of distance from + x: one workgroup a head and bucket sums those of the bucket, in one order, in double: 16 distances at a
+// time, 16 slots.
 __global__ __launch_bounds__(256) void k_attn_bias(Args a, int size, int64_t from, float* dbias) {
   __shared__ double partial[256];
+  __shared__ uint8_t map[2 * kMaxReach + 1];
   const int b = blockIdx.x % a.buckets, h = blockIdx.x / a.buckets;
+  for (int x = threadIdx.x; x <= 2 * a.reach; x += 256) map[x] = a.map[x];
+  __syncthreads();
   double s = 0.;
-  for (int x = 0; x < size; ++x) {
+  for (int x = threadIdx.x & 15; x < size; x += 16) {
     const int c = (int)min(max(from + x, -(int64_t)a.reach), (int64_t)a.reach) + a.reach;
-    if (min((int)a.map[c], a.buckets - 1) != b) continue;
-    for (int slot = threadIdx.x; slot < a.slots; slot += 256) s += (double)a.part[((int64_t)h * a.slots + slot) * size + x];
+    if (min((int)map[c], a.buckets - 1) != b) continue;
+#pragma unroll 4
+    for (int slot = threadIdx.x >> 4; slot < a.slots; slot += 16) s += (double)a.part[((int64_t)h * a.slots + slot) * size + x];
   }
   partial[threadIdx.x] = s;
   __syncthreads();
@@ -516,16 +705,23 @@ void long_back(Args& a, hipStream_t st) {
   constexpr int M = Tl::M, LPR = KS * 16 / ops::Elem<E>::kPer;
   const int64_t rows = (int64_t)a.Tq * a.N * a.heads;
   if (rows > 0) hipLaunchKernelGGL((k_attn_delta<E, LPR>), (unsigned)std::min<int64_t>((rows * LPR + 255) / 256, 256 * 32), 256, 0, st, a);
-  const unsigned lds = a.bias ? 4 * (a.causal ? a.reach + 1 : 2 * a.reach + 1) : 0;
+  const unsigned lds = bias_bytes(a);
   if (rows > 0 && (a.dq.p || a.part)) {
     const int64_t blocks = (a.Tq + 4 * M - 1) / (4 * M);
     a.slots = a.part ? back_slots(false, a.N, a.heads, 0, blocks) : (int)(a.N * blocks);
-    const unsigned more = a.part ? 4 * 4 * (M == 32 ? 2 : 1) * table_size(a.reach, a.causal) : 0;
+    const unsigned more = a.part ? 4 * 4 * (table_size(a.reach, a.causal) + 2 * M * M) : 0;
     hipLaunchKernelGGL((k_attn_dq<Tl, KS>), (unsigned)(a.slots * a.heads), 256, lds + more, st, a);
   }
   if (a.dk.p || a.dv.p) {
     const int64_t blocks = (a.Tk + 4 * M - 1) / (4 * M);
-    hipLaunchKernelGGL((k_attn_dkv<Tl, KS>), (unsigned)(a.N * (a.heads / a.group) * blocks), 256, lds, st, a);
+    const Parts p = key_parts(a.Tq, a.Tk, a.N, a.heads, a.heads / a.group, sizeof(E) == 4);
+    a.head_parts = p.heads;
+    a.row_parts = p.rows;
+    hipLaunchKernelGGL((k_attn_dkv<Tl, KS>), (unsigned)(a.N * (a.heads / a.group) * blocks * p.heads * p.rows), 256, lds, st, a);
+    if (p.heads * p.rows > 1) {
+      const int64_t threads = a.N * (a.heads / a.group) * a.Tk * (a.d / 2);
+      hipLaunchKernelGGL(k_attn_dkv_join<E>, (unsigned)std::min<int64_t>((threads + 255) / 256, 256 * 32), 256, 0, st, a);
+    }
   }
 }
 

@@ -45,17 +45,14 @@ struct Args {
   float* part;         // partial sums of the bias' gradient: [heads][slots][kind of table]
   int32_t slots;       // workgroups (windows: waves) of a head
   int32_t splits;      // few queries: parts of the keys
-  float* joint;        // their outputs, not divided, and statistics
+  int32_t head_parts, row_parts;       // parts of the heads and queries that a key's gradients are summed over
+  float* joint;        // few queries: the parts' outputs, not divided, and statistics; keys: the parts' gradients
 };
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, 0 for -inf
-// e^(x - off).  As one fused multiply-add and a power of two where off2 = off log2(e) is rounded to 2^-24 of itself, which a row's
-// weights and their sum have in common; from |off| = 2^20 on, as with biases of the type's lowest value, that would be more than they are.
-__device__ __forceinline__ float weight(float x, float off, float off2, bool exact) {
-  return exp2_(exact ? (x - off) * kLog2e : fmaf(x, kLog2e, -off2));
-}
+// Biases, and statistics, of the type's lowest value or near it: scores have no bits left beside them, and are to lose them everywhere.
 __device__ __forceinline__ bool far_off(float off) { return fabsf(off) > 1048576.f; }
-// e^(x - off) where time does not count; off is a maximum, -inf if there is nothing.
+// e^(x - off); off is a maximum, -inf if there is nothing.
 __device__ __forceinline__ float weight_of(float x, float off) { return exp2_((x - (off == -__builtin_inff() ? 0.f : off)) * kLog2e); }
 __device__ __forceinline__ float log_sum(float top, float sum) { return sum == 0.f ? -__builtin_inff() : top + logf(sum); }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -75,7 +72,7 @@ struct Wide {
   static constexpr bool kExact = false;
   static __device__ __forceinline__ int col(int lane) { return lane & 31; }
   static __device__ __forceinline__ int sub(int lane) { return lane >> 5; }
-  static __device__ __forceinline__ int row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+  static constexpr __device__ __forceinline__ int row(int r) { return 8 * (r >> 2) + (r & 3); }      // of lane 0; 4 sub more of another
   // The row that element e of a fragment packed from rows, step s, stands for.
   static __device__ __forceinline__ int index(int s, int e, int lane) { return 16 * s + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
   static __device__ __forceinline__ Acc mma(Frag a, Frag b, Acc c) {
@@ -115,7 +112,7 @@ struct Small {
   static constexpr bool kExact = false;
   static __device__ __forceinline__ int col(int lane) { return lane & 15; }
   static __device__ __forceinline__ int sub(int lane) { return lane >> 4; }
-  static __device__ __forceinline__ int row(int r, int lane) { return 4 * (lane >> 4) + r; }
+  static constexpr __device__ __forceinline__ int row(int r) { return r; }
   static __device__ __forceinline__ int index(int s, int e, int lane) { return 16 * s + 4 * (lane >> 4) + e; }
   static __device__ __forceinline__ Acc mma(Frag a, Frag b, Acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, a), __builtin_bit_cast(shortx4, b), c, 0, 0, 0);
@@ -160,7 +157,7 @@ struct Full {
   static constexpr bool kExact = true;        // the difference of exponents is taken before it is multiplied
   static __device__ __forceinline__ int col(int lane) { return lane & 15; }
   static __device__ __forceinline__ int sub(int lane) { return lane >> 4; }
-  static __device__ __forceinline__ int row(int r, int lane) { return 4 * (lane >> 4) + r; }
+  static constexpr __device__ __forceinline__ int row(int r) { return r; }
   static __device__ __forceinline__ int index(int s, int e, int lane) { return 16 * s + 4 * (lane >> 4) + e; }
   static __device__ __forceinline__ Acc mma(Frag a, Frag b, Acc c) {
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
@@ -196,6 +193,9 @@ struct Full {
     return fmaf(__uint_as_float(a.w), __uint_as_float(b.w), s);
   }
 };
+
+// What all lanes of a wave agree on, as the compiler cannot know.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Sums and maxima over the lanes that hold rows of one column.
 template <int SUBS>
@@ -255,17 +255,22 @@ struct Packed {
   __device__ __forceinline__ explicit Packed(typename Tl::Frag x) { f[0] = x; }
 };
 
-// acc += left^T right for M rows of left, which lie in LDS.  `slow`: a zero of `right` may meet something in left that is not finite; then
-// column c takes only the rows [lo(c), hi(c)] that it sees, one column after the other.
-template <class Tl, int DT, class Lo, class Hi>
-__device__ __forceinline__ void gather(typename Tl::Acc (&acc)[DT], const typename Tl::E* left, int pitch, const Packed<Tl>& right, int lane, bool slow, Lo lo, Hi hi) {
+// acc += left^T right for M rows of left, which lie in LDS.
+template <class Tl, int DT>
+__device__ __forceinline__ void gather(typename Tl::Acc (&acc)[DT], const typename Tl::E* left, int pitch, const Packed<Tl>& right, int lane) {
 #pragma unroll
   for (int s = 0; s < Tl::KSM; ++s) {
-    if (!slow) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[dt] = Tl::mma(Tl::across(left, pitch, s, dt, lane), right.f[s], acc[dt]);
-      continue;
-    }
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = Tl::mma(Tl::across(left, pitch, s, dt, lane), right.f[s], acc[dt]);
+  }
+}
+// The same where a zero of `right` may meet something in left that is not finite: column c takes only the rows [lo(c), hi(c)] that it sees, one
+// column after the other.
+template <class Tl, int DT, class Lo, class Hi>
+__device__ __forceinline__ void gather_seen(typename Tl::Acc (&acc)[DT], const typename Tl::E* left, int pitch, const Packed<Tl>& right, int lane, Lo lo, Hi hi) {
+  asm volatile("" : "+v"(lane));      // this is rare: nothing of it is to be held in registers meanwhile
+#pragma unroll
+  for (int s = 0; s < Tl::KSM; ++s) {
     for (int c = 0; c < Tl::M; ++c) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -285,11 +290,24 @@ __device__ __forceinline__ void store_column(typename Tl::E* row, const typename
   for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
     for (int r = 0; r < Tl::NR; r += 4) {
-      const int c = dt * Tl::M + Tl::row(r, lane);
+      const int c = dt * Tl::M + Tl::row(r) + 4 * Tl::sub(lane);
       if (c >= d) continue;
       const float x[4] = {acc[dt][r] * by, acc[dt][r + 1] * by, acc[dt][r + 2] * by, acc[dt][r + 3] * by};
       if constexpr (sizeof(typename Tl::E) == 2) *reinterpret_cast<uint2*>(row + c) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
       else *reinterpret_cast<float4*>(row + c) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+  }
+}
+
+// The same in fp32, into a row of its own.
+template <class Tl, int DT>
+__device__ __forceinline__ void store_sums(float* row, const typename Tl::Acc (&acc)[DT], float by, int d, int lane) {
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+    for (int r = 0; r < Tl::NR; r += 4) {
+      const int c = dt * Tl::M + Tl::row(r) + 4 * Tl::sub(lane);
+      if (c < d) *reinterpret_cast<float4*>(row + c) = make_float4(acc[dt][r] * by, acc[dt][r + 1] * by, acc[dt][r + 2] * by, acc[dt][r + 3] * by);
     }
   }
 }
@@ -299,20 +317,46 @@ template <class E, int ROWS, int KS>
 struct Stage {
   static constexpr int PER = 16 / sizeof(E), CPR = KS * 16 / PER, N = (ROWS * CPR + 255) / 256;
   uint4 w[N];
-  template <class In>
-  __device__ __forceinline__ void fetch(const E* base, int64_t st, int row0, int d, In in) {
+  uint32_t off[N];      // bytes from the tile's first row
+  bool near, has[N];    // the tile spans less than 2^31 bytes; this chunk is one of the rows'
+  static __device__ __forceinline__ int row(int i) { return (int)(threadIdx.x + 256 * i) / CPR; }
+  __device__ __forceinline__ void init(int64_t st, int d) {
+    near = st < (int64_t)(((uint64_t)1 << 31) / (ROWS * sizeof(E)));
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + 256 * i, r = c / CPR, x = (c % CPR) * PER;
-      const bool ok = (ROWS * CPR % 256 == 0 || r < ROWS) && x < d && in(row0 + r);
-      w[i] = ok ? *reinterpret_cast<const uint4*>(base + (int64_t)(row0 + r) * st + x) : make_uint4(0, 0, 0, 0);
+      const int x = (int)((threadIdx.x + 256 * i) % CPR) * PER;
+      off[i] = (uint32_t)((row(i) * (uint64_t)st + x) * sizeof(E));
+      has[i] = (ROWS * CPR % 256 == 0 || row(i) < ROWS) && x < d;
+      w[i] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  // A whole tile from its first row on: an address that the workgroup has in common, and a thread's own 32 bits.
+  __device__ __forceinline__ void fetch_all(const E* tile) {
+    if constexpr (256 % CPR == 0 && ROWS * CPR % 256 == 0) {      // a thread's chunks have their columns in common
+      if (has[0]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(tile) + off[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (has[i]) w[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(tile) + off[i]);
+      }
+    }
+  }
+  template <class In>
+  __device__ __forceinline__ void fetch(const E* base, int64_t st, int row0, In in) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int x = (int)((threadIdx.x + 256 * i) % CPR) * PER;
+      w[i] = has[i] && in(row0 + row(i)) ? *reinterpret_cast<const uint4*>(base + (int64_t)(row0 + row(i)) * st + x) : make_uint4(0, 0, 0, 0);
     }
   }
   __device__ __forceinline__ void put(E* lds, int pitch) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + 256 * i, r = c / CPR, x = (c % CPR) * PER;
-      if (ROWS * CPR % 256 == 0 || r < ROWS) *reinterpret_cast<uint4*>(lds + r * pitch + x) = w[i];
+      const int x = (int)((threadIdx.x + 256 * i) % CPR) * PER;
+      if (ROWS * CPR % 256 == 0 || row(i) < ROWS) *reinterpret_cast<uint4*>(lds + row(i) * pitch + x) = w[i];
     }
   }
   template <class Tl>
@@ -324,6 +368,17 @@ struct Stage {
       else f = f || odd_f32(w[i].x) || odd_f32(w[i].y) || odd_f32(w[i].z) || odd_f32(w[i].w);
     }
     return f;
+  }
+};
+
+// The bias by distance in LDS, past its reach by as much as a tile that is not far off as a whole can be, so that the tiles' places need no limits.
+constexpr int kPast = 96;
+struct BiasTable {
+  int from, size;
+  __device__ __forceinline__ explicit BiasTable(const Args& a) : from((a.causal ? 0 : -a.reach) - kPast), size(a.reach + kPast + 1 - from) {}
+  // By distance, or (turned) from the farthest to the nearest: a lane's entries then ascend with its keys.
+  __device__ __forceinline__ void fill(const Args& a, float* table, int h, bool turned) const {
+    for (int x = threadIdx.x; x < size; x += 256) table[turned ? size - 1 - x : x] = bias_at(a, h, from + x);
   }
 };
 
@@ -349,6 +404,26 @@ inline int back_slots(bool window, int64_t N, int64_t heads, int64_t kvs, int64_
   const int64_t most = window ? (256 * 16 + kvs - 1) / kvs : (512 + heads - 1) / heads, all = window ? N : N * blocks;
   return (int)(all < most ? all : most);
 }
+// Where keys have too few workgroups to fill the card, their gradients are summed in parts: of the heads that share them first, then of the queries,
+// 256 at least.
+struct Parts {
+  int32_t heads, rows;
+};
+inline Parts key_parts(int64_t Tq, int64_t Tk, int64_t N, int64_t heads, int64_t kvs, bool f32) {
+  const int64_t all = N * kvs * ((Tk + (f32 ? 63 : 127)) / (f32 ? 64 : 128)), group = heads / kvs;
+  int64_t want = all ? (1024 + all - 1) / all : 1;
+  if (all >= 512) want = 1;
+  Parts p{1, 1};
+  for (int64_t g = 2; g <= group && g <= 2 * want; ++g) {
+    if (group % g == 0) p.heads = (int32_t)g;
+  }
+  want = (want + p.heads - 1) / p.heads;
+  if (all >= 512) p.heads = 1;
+  p.rows = (int32_t)(want < Tq / 256 ? want : Tq / 256);
+  if (p.rows < 1) p.rows = 1;
+  return p;
+}
+inline unsigned bias_bytes(const Args& a) { return a.bias ? 4 * (unsigned)((a.causal ? a.reach : 2 * a.reach) + 2 * kPast + 1) : 0; }
 void attn_forward_f32(const Args& a, hipStream_t st);
 void attn_forward_bf16(const Args& a, hipStream_t st);
 void attn_backward_f32(const Args& a, float* dbias, hipStream_t st);

@@ -310,7 +310,9 @@ def test_a_token_that_is_not_finite_reaches_what_sees_it(T, value, dtype):
     x = dict(c, v=c["v"].clone())
     x["v"][J, 0, 3] = value      # head 0's column 3
     o, lse = _forward(x)
-    assert torch.equal(lse, clean_lse) and torch.equal(o[:, 1], clean_o[:, 1]) and torch.equal(o[:, 0, 16:], clean_o[:, 0, 16:])
+    # lse does not depend on v, but the order of its sum may: it is held to its formula.  What is of another sequence or head keeps its bits.
+    _near(lse, *_reference(c)[1], "lse")
+    assert torch.equal(o[:, 1], clean_o[:, 1]) and torch.equal(o[:, 0, 16:], clean_o[:, 0, 16:])
     assert not torch.isfinite(o[J:, 0, 3]).any() and torch.isfinite(o[:J]).all()
     _check_forward(dict(c, v=torch.where(torch.isfinite(x["v"]), x["v"], 0)), torch.where((torch.arange(T, device="cuda") >= J)[:, None, None] & (torch.arange(32, device="cuda") == 3), _zeroed(c, J)[0], o), lse)
     # A key: scores of the queries from J on; gradients of earlier queries stay as they were.
