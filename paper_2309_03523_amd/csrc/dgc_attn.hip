@@ -26,7 +26,7 @@ namespace {
 template <class Tl, int KS>
 __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
   typedef typename Tl::E E;
-  constexpr int kKeys = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  constexpr int M = Tl::M, NT = Geometry<Tl, KS>::NT, kKeys = NT * M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
   __shared__ __attribute__((aligned(16))) E room[2][2 * kKeys * P];
   __shared__ float seens[2][kKeys];      // 0 where a key is masked
   extern __shared__ float table[];       // bias by distance
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
 
 // ---------------------------------------------------------------------------------------------------- few queries
 //
-// Up to 16 queries (one: a new snapshot) against many keys.  The rows of a key head, its heads' queries, are taken R at a time; a key's row is
+// Up to 16 queries (one: a new snapshot) against many keys.  Up to R = 2 rows, of heads that share a key head or of queries, on the vector unit: a key's row is
 // read by LPK lanes, 16 bytes each, by each of the wave's 64 / LPK groups another key, four keys of a group at a time.  Every group has a
 // softmax of its own, over its own keys; they are joined at the end, in the wave, in the workgroup, and by k_attn_join where the keys
 // are split among workgroups.
@@ -497,30 +497,257 @@ __global__ __launch_bounds__(256) void k_attn_few(Args a) {
   }
 }
 
-// The parts of split keys: a wave a row.
+// More rows than two, of heads that share a key head or of several queries: 16 of them are the columns of a matrix product, so a key is read once for
+// all.  A wave takes 32 keys at a time (16 of wide fp32 rows): their rows go from memory into operands, values through LDS (each wave's own part), four waves a workgroup.
+template <class E> struct Slab;
+template <> struct Slab<uint16_t> {
+  static constexpr int PER = 8, STEP = 32;      // elements of a lane, contraction of a product
+  static __device__ __forceinline__ floatx4 mma(uint4 a, uint4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  // o += values^T weights for 32 keys: element e of a lane stands for key 4 sub + e of the first 16, then of the second.
+  template <int DT, int NT>
+  static __device__ __forceinline__ void add(floatx4 (&o)[DT], const uint16_t* sv, int pitch, const floatx4 (&x)[NT], int lane) {
+    const uint4 b = make_uint4(pack2(x[0][0], x[0][1]), pack2(x[0][2], x[0][3]), pack2(x[1][0], x[1][1]), pack2(x[1][2], x[1][3]));
+    const uint16_t* at = sv + (4 * (lane >> 4) + ((lane & 15) >> 2)) * pitch + 4 * (lane & 3);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(at + 16 * dt)));
+      const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(at + 16 * pitch + 16 * dt)));
+      o[dt] = mma(make_uint4(u.x, u.y, w.x, w.y), b, o[dt]);
+    }
+  }
+  static __device__ __forceinline__ bool odd(uint4 w) { return Wide::odd(w); }
+  static __device__ __forceinline__ float get(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+};
+template <> struct Slab<float> {
+  static constexpr int PER = 4, STEP = 16;
+  static __device__ __forceinline__ floatx4 mma(uint4 a, uint4 b, floatx4 c) { return Full::mma(a, b, c); }
+  template <int DT, int NT>
+  static __device__ __forceinline__ void add(floatx4 (&o)[DT], const float* sv, int pitch, const floatx4 (&x)[NT], int lane) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) gather<Full, DT>(o, sv + 16 * t * pitch, pitch, Packed<Full>(x[t]), lane);
+  }
+  static __device__ __forceinline__ bool odd(uint4 w) { return Full::odd(w); }
+  static __device__ __forceinline__ float get(const float* p) { return *p; }
+};
+
+template <class E, int D>
+__global__ __launch_bounds__(256, 2) void k_attn_rows(Args a) {
+  typedef Slab<E> S;
+  constexpr int NT = sizeof(E) * D > 256 ? 1 : 2, KEYS = 16 * NT;      // of a step, as registers allow
+  constexpr int KS = D / S::STEP, DT = D / 16, P = D + 16 / (int)sizeof(E), ROW = D + 2;
+  constexpr int VALUES = 4 * KEYS * P * (int)sizeof(E), JOINED = 4 * 16 * ROW * 4;
+  __shared__ __attribute__((aligned(16))) char room[VALUES > JOINED ? VALUES : JOINED];
+  __shared__ float weights[4][KEYS][17];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, sub = lane >> 4;
+  const int rows = a.group * a.Tq, blocks = (rows + 15) / 16, kvs = a.heads / a.group;
+  const uint32_t part = blockIdx.x % a.splits;
+  uint32_t rest = blockIdx.x / a.splits;
+  const int r0 = (int)(rest % blocks) * 16;
+  rest /= blocks;
+  const int y = rest % kvs;
+  const int64_t n = rest / kvs;
+  const Seq q(a, n);
+  E* const sv = reinterpret_cast<E*>(room) + wave * KEYS * P;
+  const int row = r0 + col, h = y * a.group + min(row, rows - 1) / a.Tq, i = row % a.Tq;
+  const bool live = row < rows && i >= q.lo && i < q.hi;
+  const int p = live ? (int)(q.at + i) : -1;
+  int most = p, least = live ? p : 0x7fffffff;
+#pragma unroll
+  for (int m = 1; m < 16; m *= 2) most = max(most, __shfl_xor(most, m)), least = min(least, __shfl_xor(least, m));
+  most = uniform(most);
+  least = uniform(least);
+  uint4 fq[KS];
+  const E* qrow = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int c = S::STEP * s + S::PER * sub;
+    fq[s] = live && c < a.d ? *reinterpret_cast<const uint4*>(qrow + c) : make_uint4(0, 0, 0, 0);
+  }
+  const float far = a.bias ? bias_at(a, h, a.reach) : 0.f;
+  const int kend = most < 0 ? 0 : a.causal ? min(q.len, most + 1) : q.len;
+  const int share = ((kend + a.splits - 1) / a.splits + 127) / 128 * 128;
+  const int k0 = (int)min((int64_t)part * share, (int64_t)kend), k1 = min(k0 + share, kend);
+  const E* kbase = static_cast<const E*>(a.k.p) + n * a.k.sn + y * a.d + S::PER * sub;
+  const E* vbase = static_cast<const E*>(a.v.p) + n * a.v.sn + y * a.d + S::PER * sub;
+  floatx4 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = (floatx4)(0.f);
+  float m = -__builtin_inff(), l = 0.f;
+  uint4 wk[NT][KS], wv[NT][KS];
+  uint32_t bits = 0;         // which of the step's keys are there
+  auto fetch = [&](int j0) {
+    const int mine = j0 + (lane & (KEYS - 1));
+    bits = (uint32_t)__ballot(mine < k1 && (!a.keep || a.keep[(int64_t)mine * a.N + n]));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int j = j0 + 16 * t + col;
+      const bool in = bits >> (16 * t + col) & 1;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const bool ok = in && S::STEP * s + S::PER * sub < a.d;
+        wk[t][s] = ok ? *reinterpret_cast<const uint4*>(kbase + (int64_t)j * a.k.st + S::STEP * s) : make_uint4(0, 0, 0, 0);
+        wv[t][s] = ok ? *reinterpret_cast<const uint4*>(vbase + (int64_t)j * a.v.st + S::STEP * s) : make_uint4(0, 0, 0, 0);
+      }
+    }
+  };
+  int j0 = k0 + wave * KEYS;
+  if (j0 < k1) fetch(j0);
+  for (; j0 < k1; j0 += 4 * KEYS) {
+    wave_fence();
+    bool bad = false;
+    floatx4 x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      x[t] = (floatx4)(0.f);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        x[t] = S::mma(wk[t][s], fq[s], x[t]);
+        bad = bad || S::odd(wv[t][s]);
+        *reinterpret_cast<uint4*>(sv + (16 * t + col) * P + S::STEP * s + S::PER * sub) = wv[t][s];
+      }
+    }
+    const uint32_t there = bits;
+    if (j0 + 4 * KEYS < k1) fetch(j0 + 4 * KEYS);
+    const bool near = a.bias && least - (j0 + KEYS - 1) < a.reach, edge = a.causal && j0 + KEYS - 1 > least;
+    float top = m;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int at = 16 * t + 4 * sub + r;
+        const float b = near ? bias_at(a, h, (int64_t)p - (j0 + at)) : far;
+        x[t][r] = live && (there >> at & 1) && (!edge || j0 + at <= p) ? fmaf(x[t][r], a.scale, b) : -__builtin_inff();
+        top = fmaxf(top, x[t][r]);
+      }
+    }
+    top = column_max<4>(top);
+    const float f = weight_of(m, top);
+    m = top;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = weight_of(x[t][r], top);
+        sum += x[t][r];
+      }
+    }
+    l = fmaf(l, f, sum);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+    wave_fence();
+    if (!edge || !__any(bad)) {
+      S::add(o, sv, P, x, lane);
+    } else {      // a zero weight would meet a value that is not finite: key by key, only where it is seen
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) weights[wave][16 * t + 4 * sub + r][col] = x[t][r];
+      }
+      wave_fence();
+#pragma unroll 1
+      for (int at = 0; at < KEYS; ++at) {
+        const bool seen = j0 + at <= p;
+        const float w = weights[wave][at][col];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float v = seen ? S::get(sv + at * P + 16 * dt + 4 * sub + r) : 0.f;
+            o[dt][r] = fmaf(w, v, o[dt][r]);
+          }
+        }
+      }
+    }
+  }
+  l = column_sum<4>(l);
+  // The waves' parts: a row's D sums, its maximum and its sum.
+  __syncthreads();
+  float* const joined = reinterpret_cast<float*>(room);
+  float* to = joined + (wave * 16 + col) * ROW;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) to[16 * dt + 4 * sub + r] = o[dt][r];
+  }
+  if (sub == 0) to[D] = m, to[D + 1] = l;
+  __syncthreads();
+  const int mine = threadIdx.x >> 4, r = r0 + mine, hm = y * a.group + min(r, rows - 1) / a.Tq, im = r % a.Tq;
+  if (r >= rows || im < q.lo || im >= q.hi) return;
+  float top = -__builtin_inff(), f[4], sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, joined[(w * 16 + mine) * ROW + D]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = weight_of(joined[(w * 16 + mine) * ROW + D], top);
+    sum = fmaf(joined[(w * 16 + mine) * ROW + D + 1], f[w], sum);
+  }
+  const int64_t at = (n * a.heads + hm) * a.Tq + im;
+  const float by = a.splits > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  for (int e = threadIdx.x & 15; e < a.d; e += 16) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v = fmaf(joined[(w * 16 + mine) * ROW + e], f[w], v);
+    v *= by;
+    if (a.splits > 1) a.joint[(at * a.splits + part) * (a.d + 2) + e] = v;
+    else static_cast<E*>(const_cast<void*>(a.o.p))[(int64_t)im * a.o.st + n * a.o.sn + hm * a.d + e] = ops::Elem<E>::one(v);
+  }
+  if ((threadIdx.x & 15) == 0) {
+    if (a.splits > 1) {
+      a.joint[(at * a.splits + part) * (a.d + 2) + a.d] = top;
+      a.joint[(at * a.splits + part) * (a.d + 2) + a.d + 1] = sum;
+    } else if (a.lse) {
+      a.lse[at] = log_sum(top, sum);
+    }
+  }
+}
+
+// The parts of split keys: a workgroup a row, two elements a lane, a quarter of the parts a wave.
 template <class E>
 __global__ __launch_bounds__(256) void k_attn_join(Args a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
-  if (at >= a.N * a.heads * a.Tq) return;
+  __shared__ float factor[kMaxSplits], tops[4], sums[4], joined[4][kMaxDim];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int64_t at = blockIdx.x;
   const int i = (int)(at % a.Tq), h = (int)(at / a.Tq % a.heads);
   const int64_t n = at / a.Tq / a.heads;
   const Seq q(a, n);
   if (i < q.lo || i >= q.hi) return;
   const float* from = a.joint + at * a.splits * (a.d + 2);
   float top = -__builtin_inff();
-  for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, from[s * (a.d + 2) + a.d]);
+  for (int s = threadIdx.x; s < a.splits; s += 256) top = fmaxf(top, from[s * (a.d + 2) + a.d]);
   for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   float sum = 0.f;
-  for (int s = lane; s < a.splits; s += 64) sum = fmaf(from[s * (a.d + 2) + a.d + 1], weight_of(from[s * (a.d + 2) + a.d], top), sum);
-  sum = wave_sum(sum);
-  for (int e = lane; e < a.d; e += 64) {
-    float v = 0.f;
-    for (int s = 0; s < a.splits; ++s) v = fmaf(from[s * (a.d + 2) + e], weight_of(from[s * (a.d + 2) + a.d], top), v);
-    v = sum == 0.f ? 0.f : v / sum;
-    static_cast<E*>(const_cast<void*>(a.o.p))[(int64_t)i * a.o.st + n * a.o.sn + h * a.d + e] = ops::Elem<E>::one(v);
+  for (int s = threadIdx.x; s < a.splits; s += 256) {
+    factor[s] = weight_of(from[s * (a.d + 2) + a.d], top);
+    sum = fmaf(from[s * (a.d + 2) + a.d + 1], factor[s], sum);
   }
-  if (a.lse && lane == 0) a.lse[at] = log_sum(top, sum);
+  sum = wave_sum(sum);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  float v[2] = {0.f, 0.f};
+  const int e = 2 * lane;
+  if (e < a.d) {
+#pragma unroll 8
+    for (int s = wave; s < a.splits; s += 4) {
+      const float2 u = *reinterpret_cast<const float2*>(from + s * (a.d + 2) + e);
+      v[0] = fmaf(u.x, factor[s], v[0]);
+      v[1] = fmaf(u.y, factor[s], v[1]);
+    }
+    joined[wave][e] = v[0];
+    joined[wave][e + 1] = v[1];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < a.d) {
+    const float x = (joined[0][threadIdx.x] + joined[1][threadIdx.x]) + (joined[2][threadIdx.x] + joined[3][threadIdx.x]);
+    static_cast<E*>(const_cast<void*>(a.o.p))[(int64_t)i * a.o.st + n * a.o.sn + h * a.d + threadIdx.x] = ops::Elem<E>::one(sum == 0.f ? 0.f : x / sum);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[at] = log_sum(top, sum);
 }
 
 // ---------------------------------------------------------------------------------------------------- choice and launch
@@ -536,22 +763,23 @@ void window(Args a, hipStream_t st) {
   else hipLaunchKernelGGL((k_attn_window<Tl, NT, 8>), grid, 256, 0, st, a);
 }
 
-template <class E, int LPK>
-void few_rows(const Args& a, int R, unsigned grid, hipStream_t st) {
-  if (R == 1) hipLaunchKernelGGL((k_attn_few<E, LPK, 1>), grid, 256, 0, st, a);
-  else if (R == 2) hipLaunchKernelGGL((k_attn_few<E, LPK, 2>), grid, 256, 0, st, a);
-  else hipLaunchKernelGGL((k_attn_few<E, LPK, 4>), grid, 256, 0, st, a);
+template <class E, int D>
+void few_rows(const Args& a, unsigned grid, hipStream_t st) {
+  constexpr int LPK = D / ops::Elem<E>::kPer;
+  const int rows = a.group * a.Tq;
+  if (rows == 1) hipLaunchKernelGGL((k_attn_few<E, LPK, 1>), grid, 256, 0, st, a);
+  else if (rows == 2) hipLaunchKernelGGL((k_attn_few<E, LPK, 2>), grid, 256, 0, st, a);
+  else hipLaunchKernelGGL((k_attn_rows<E, (D > 16 || sizeof(E) == 4 ? D : 32)>), grid, 256, 0, st, a);
 }
 template <class E>
 void few(const Args& a, hipStream_t st) {
-  constexpr int PER = ops::Elem<E>::kPer;
-  const int rows = a.group * a.Tq, R = rows == 1 ? 1 : rows == 2 ? 2 : 4;
-  const unsigned grid = (unsigned)(a.N * (a.heads / a.group) * ((rows + R - 1) / R) * a.splits);
-  if (a.d <= 16) few_rows<E, 16 / PER>(a, R, grid, st);
-  else if (a.d <= 32) few_rows<E, 32 / PER>(a, R, grid, st);
-  else if (a.d <= 64) few_rows<E, 64 / PER>(a, R, grid, st);
-  else few_rows<E, 128 / PER>(a, R, grid, st);
-  if (a.splits > 1) hipLaunchKernelGGL(k_attn_join<E>, (unsigned)((a.N * a.heads * a.Tq + 3) / 4), 256, 0, st, a);
+  const int64_t rows = (int64_t)a.group * a.Tq;
+  const unsigned grid = (unsigned)(a.N * (a.heads / a.group) * ((rows + 15) / 16) * a.splits);
+  if (a.d <= 16) few_rows<E, 16>(a, grid, st);
+  else if (a.d <= 32) few_rows<E, 32>(a, grid, st);
+  else if (a.d <= 64) few_rows<E, 64>(a, grid, st);
+  else few_rows<E, 128>(a, grid, st);
+  if (a.splits > 1) hipLaunchKernelGGL(k_attn_join<E>, (unsigned)(a.N * a.heads * a.Tq), 256, 0, st, a);
 }
 template <class Tl>
 void large(const Args& a, hipStream_t st) {

@@ -28,19 +28,21 @@ bool too_many(int64_t Tq, int64_t Tk, int64_t N, int32_t heads) {      // workgr
 
 int64_t round16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
-// Parts of the keys of a few queries: enough workgroups to fill the card twice, of 256 keys at least.
+// Parts of the keys of a few queries: enough workgroups to fill the card, of 256 keys at least.
 int32_t splits_of(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads) {
-  const int64_t rows = heads / kv_heads * Tq, items = N * kv_heads * ((rows + 3) / 4);
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>((2048 + items - 1) / std::max<int64_t>(items, 1), Tk / 256));
+  const int64_t rows = heads / kv_heads * Tq, items = std::max<int64_t>(1, N * kv_heads * ((rows + 15) / 16));
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(1024 + items - 1) / items, Tk / 256, kMaxSplits}));
 }
 struct Room {
-  int64_t delta, part, joint;      // bytes
+  int64_t delta, odd, part, joint;      // bytes
 };
 Room back_room(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal, int32_t buckets, int32_t reach) {
   // `first`, which decides between the two forms, is not known here.
   const bool window = takes_window_back(Tk, d, heads / kv_heads, false);
-  Room r{round16(4 * N * heads * Tq), 0, 0};
+  // A flag for each workgroup of the kernels that have one, 64 queries or keys each.
+  Room r{round16(4 * N * heads * Tq), 0, 0, 0};
   const Parts p = key_parts(Tq, Tk, N, heads, kv_heads, dtype == DGC_DTYPE_F32);
+  r.odd = round16(4 * N * std::max<int64_t>(heads * ((Tq + 63) / 64), kv_heads * ((Tk + 63) / 64) * p.heads * p.rows));
   if (p.heads * p.rows > 1) r.joint = 8 * N * kv_heads * Tk * d * p.heads * p.rows;
   if (buckets) {
     // The larger of both row tiles' numbers of blocks.
@@ -124,12 +126,12 @@ dgc_status_t dgc_attn_buckets(int32_t buckets, int32_t reach, int32_t causal, ui
 int64_t dgc_attn_workspace_bytes(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_heads, int32_t d, int32_t dtype, int32_t causal,
                                  int32_t buckets, int32_t reach, int32_t backward) {
   if (check(Tq, Tk, N, heads, kv_heads, d, dtype, buckets, reach) || too_many(Tq, Tk, N, heads)) return -1;
-  if (N == 0 || Tq == 0) return 0;
-  if (backward) {
+  if (N == 0 || Tk == 0) return 0;
+  if (backward) {      // without queries, too: keys have gradients of zero
     const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, dtype, causal, buckets, reach);
-    return r.delta + r.part + r.joint;
+    return r.delta + r.odd + r.part + r.joint;
   }
-  if (form_of(Tq, Tk) != kFew) return 0;
+  if (Tq == 0 || form_of(Tq, Tk) != kFew) return 0;
   const int64_t splits = splits_of(Tq, Tk, N, heads, kv_heads);
   return splits > 1 ? round16(4 * N * heads * Tq * splits * (d + 2)) : 0;
 }
@@ -212,9 +214,10 @@ dgc_status_t dgc_attn_backward(const void* q, int64_t qt, int64_t qn, const void
   }
   a.lse = const_cast<float*>(lse);
   const Room r = back_room(Tq, Tk, N, heads, kv_heads, d, dtype, causal, buckets, reach);
-  a.joint = reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta + r.part);
+  a.joint = reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta + r.odd + r.part);
+  a.odd = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + r.delta);
   a.delta = static_cast<float*>(workspace);
-  a.part = dbias && N > 0 && Tq > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta) : nullptr;
+  a.part = dbias && N > 0 && Tq > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + r.delta + r.odd) : nullptr;
   (dtype == DGC_DTYPE_F32 ? attn_backward_f32 : attn_backward_bf16)(a, dbias, static_cast<hipStream_t>(stream));
   return ops::launched("attention");
 }

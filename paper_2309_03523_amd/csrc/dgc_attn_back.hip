@@ -210,21 +210,32 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 // ---------------------------------------------------------------------------------------------------- dq, and the bias' gradient
 //
 // As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it leaves dP - D.
-template <class Tl, int KS>
-__global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args a) {
+// Where a zero gradient would meet a key that is not finite, this kernel leaves dq to the same one with SEEN, which is launched behind it and takes
+// such items alone: with both in one kernel the registers do not do.
+template <class Tl, int KS, bool SEEN>
+__global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
   typedef typename Tl::E E;
-  constexpr int kKeys = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  constexpr int M = Tl::M, NT = Geometry<Tl, KS>::NT, kKeys = NT * M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
   __shared__ __attribute__((aligned(16))) E room[2][2 * kKeys * P];
   __shared__ float seens[2][kKeys];
   extern __shared__ float table[];          // the bias by distance, then the waves' tables of sums and their slanted tiles
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = Tl::col(lane), sub = Tl::sub(lane);
   const int blocks = (a.Tq + 4 * M - 1) / (4 * M), h = blockIdx.x % a.heads, slot = blockIdx.x / a.heads, y = h / a.group;
+  const int64_t items = a.N * blocks;
+  if (SEEN) {
+    bool any = false;
+    for (int64_t x = slot; x < (items + a.slots - 1) / a.slots * a.slots; x += a.slots) {
+      const int64_t item = x / a.slots & 1 ? x / a.slots * a.slots + a.slots - 1 - slot : x;
+      any = any || (item < items && a.odd[item * a.heads + h]);
+    }
+    if (!any) return;
+  }
   const BiasTable bt(a);
   const int tfrom = table_from(a.reach, a.causal), tsize = table_size(a.reach, a.causal);
   float* const sums = table + bt.size;
   if (a.bias) {
     bt.fill(a, table, h, true);
-    if (a.part) {
+    if (!SEEN && a.part) {
       for (int x = threadIdx.x; x < 4 * tsize; x += 256) sums[x] = 0.f;
     }
   }
@@ -234,7 +245,6 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
   Stage<E, kKeys, KS> nk, nv;
   nk.init(a.k.st, a.d);
   nv.init(a.v.st, a.d);
-  const int64_t items = a.N * blocks;
   for (int64_t round = 0; round * a.slots < items; ++round) {
     // The longest walks first, every second round backwards: with several items a workgroup, long ones go with short ones.
     const int64_t item = round * a.slots + (round & 1 ? a.slots - 1 - slot : slot);
@@ -242,7 +252,10 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
     const int64_t n = item % a.N;
     const int i0 = (int)(blocks - 1 - item / a.N) * 4 * M;
     const Seq q(a, n);
-    if (i0 >= q.hi || i0 + 4 * M <= q.lo) continue;
+    if (SEEN ? !a.odd[item * a.heads + h] : i0 >= q.hi || i0 + 4 * M <= q.lo) {
+      if (!SEEN && threadIdx.x == 0 && a.causal) a.odd[item * a.heads + h] = 0;
+      continue;
+    }
     const int least = max(i0, q.lo), most = min(i0 + 4 * M, q.hi) - 1;
     const int kend = a.causal ? (int)min((int64_t)q.len, q.at + most + 1) : q.len;
     const int mine = i0 + wave * M, i = mine + col;
@@ -251,7 +264,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
     const float given = row ? a.lse[stat] : -__builtin_inff();
     const bool live = given != -__builtin_inff();
     const float lse = live ? given : __builtin_inff();       // of a query without gradients: all weights are zero
-    const bool clean = !Tl::kExact && !__any(row && !live);
+    const bool clean = !SEEN && !Tl::kExact && !__any(row && !live);
     const bool some = max(mine, q.lo) < min(mine + M, q.hi);
     const int p0 = some ? (int)(q.at + max(mine, q.lo)) : -1, p1 = some ? (int)(q.at + min(mine + M, q.hi) - 1) : -1, p = live ? (int)(q.at + i) : -1;
     const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place
@@ -303,15 +316,15 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt] = (typename Tl::Acc)(0.f);
 
-    // One tile.  PLAIN: every query sees all of it, with one bias.  SEEN: keys that are not finite reach only those that see them.
+    // One tile.  PLAIN: every query sees all of it, with one bias.  odd: dq is left out, or (SEEN) keys that are not finite reach only those that see them.
     float bias_behind = 0.f, bias_ahead = 0.f;
-    auto tile = [&](auto plain, auto seen_only, int j0, int buf) {
-      constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
+    auto tile = [&](auto plain, int j0, int buf, bool odd) {
+      constexpr bool PLAIN = decltype(plain)::value;
       const E *sk = room[buf], *sv = sk + kKeys * P;
       const bool behind = p0 - (j0 + kKeys - 1) >= a.reach, ahead = p1 - j0 <= -a.reach;
       const float one = behind ? bias_behind : bias_ahead;
       const float mult = a.scale * kLog2e, add = (one - lse) * kLog2e;
-#pragma unroll KS >= 4 ? 1 : 2
+#pragma unroll KS >= 4 || SEEN ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int first = j0 + t * M;
         if (!PLAIN && (first >= kend || (a.causal && first > p1))) break;
@@ -341,7 +354,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
             z[r] = out ? 0.f : z[r] * exp2_((x[r] - lse) * kLog2e);
           }
         }
-        if (a.part) {
+        if (!SEEN && a.part) {
           if (behind || ahead) {
             float s = 0.f;
 #pragma unroll
@@ -363,7 +376,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
             }
           }
         }
-        if (SEEN) gather_seen<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
+        if (SEEN && odd) gather_seen<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane, [](int) { return 0; }, [&](int c) { return (int)(q.at + mine + c) - first; });
         else gather<Tl, DT>(dq, sk + t * M * P, P, Packed<Tl>(z), lane);
       }
     };
@@ -378,22 +391,14 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
     for (int j0 = 0, buf = 0; j0 < kend; j0 += kKeys, buf ^= 1) {
       const bool next = j0 + kKeys < kend;
       if (next) fetch(j0 + kKeys);
-      if (j0 <= last && !odd) {
-        if (j0 + kKeys <= plain_to || (j0 >= plain_from && j0 + kKeys <= whole)) tile(std::true_type(), std::false_type(), j0, buf);
-        else tile(std::false_type(), std::false_type(), j0, buf);
+      if (j0 <= last) {
+        if (!SEEN && (j0 + kKeys <= plain_to || (j0 >= plain_from && j0 + kKeys <= whole))) tile(std::true_type(), j0, buf, false);
+        else tile(std::false_type(), j0, buf, odd);
       }
       if (next) odd = put(j0 + kKeys, buf ^ 1), odds |= odd;
     }
-    if (odds) {      // what was left out
-      for (int j0 = 0; j0 < kend; j0 += kKeys) {
-        if (j0 + kKeys <= inside) continue;
-        nk.fetch(kbase, a.k.st, j0, there);
-        nv.fetch(vbase, a.v.st, j0, there);
-        __syncthreads();
-        if (put(j0, 0) && j0 <= last) tile(std::false_type(), std::true_type(), j0, 0);
-      }
-    }
-    if (row && a.dq.p) {
+    if (!SEEN && threadIdx.x == 0 && a.causal) a.odd[item * a.heads + h] = odds;
+    if (row && a.dq.p && (SEEN || !odds)) {
       if (!live) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) dq[dt] = (typename Tl::Acc)(0.f);
@@ -402,7 +407,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
     }
     __syncthreads();      // before the next item's keys
   }
-  if (a.part) {
+  if (!SEEN && a.part) {
     __syncthreads();
     farsum = wave_sum(farsum);
     aheadsum = wave_sum(aheadsum);
@@ -424,10 +429,11 @@ __global__ __launch_bounds__(256, KS * Tl::M > 256 ? 1 : 2) void k_attn_dq(Args 
 // A workgroup takes 4 M keys of one sequence and key head, a wave M of them in registers, and walks over the queries that see them in tiles of
 // 2 M that lie in LDS, for one head that shares the keys after the other.  The products that form scores and dP start from -lse / scale and -D of
 // their rows, which come from LDS as four numbers at a time: they leave (s - lse) / scale and dP - D.
-template <class Tl, int KS>
+// Queries that are not finite: as in k_attn_dq.
+template <class Tl, int KS, bool SEEN>
 __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args a) {
   typedef typename Tl::E E;
-  constexpr int kRows = 2 * Tl::M, M = Tl::M, NT = 2, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
+  constexpr int M = Tl::M, NT = M == 32 && KS >= 4 ? 1 : 2, kRows = NT * M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
   __shared__ __attribute__((aligned(16))) E room[2][2 * kRows * P];
   __shared__ __attribute__((aligned(16))) float stats[2][3][kRows];      // lse, -lse / scale, -D
   extern __shared__ float table[];
@@ -436,7 +442,10 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
   const int64_t n = pair / kvs;
   const int y = pair % kvs, k0 = (int)(rest / parts) * 4 * M, part = rest % parts, head_part = part / a.row_parts, row_part = part % a.row_parts;
   const Seq q(a, n);
-  if (k0 >= q.len) return;
+  if (SEEN ? !a.odd[blockIdx.x] : k0 >= q.len) {
+    if (!SEEN && threadIdx.x == 0 && a.causal) a.odd[blockIdx.x] = 0;
+    return;
+  }
   const int mine = k0 + wave * M, j = mine + col;
   const bool there = j < q.len && (!a.keep || a.keep[(int64_t)j * a.N + n]);
   const BiasTable bt(a);
@@ -462,10 +471,11 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
   ng.init(a.go.st, a.d);
   const bool near = nq.near && ng.near;
   constexpr int NS = Stage<E, kRows, KS>::N;
-  const bool started = !Tl::kExact && a.scale > 1e-6f;      // products may start from -lse / scale
+  const bool started = !SEEN && !Tl::kExact && a.scale > 1e-6f;      // products may start from -lse / scale
   // This workgroup's part of the heads that share the keys, and of their queries.
   const int heads_each = a.group / a.head_parts, rows_each = ((q.hi - begin_all + a.row_parts - 1) / a.row_parts + kRows - 1) / kRows * kRows;
   const int begin = min(begin_all + row_part * rows_each, q.hi), end = min(begin + rows_each, q.hi);
+  bool odds = false;
   for (int g = head_part * heads_each; g < (head_part + 1) * heads_each; ++g) {
     const int h = y * a.group + g;
     __syncthreads();
@@ -515,15 +525,15 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       __syncthreads();
       return false;
     };
-    // One tile.  PLAIN: all its queries see all of the wave's keys, with one bias.  SEEN: queries that are not finite reach only the keys that they see.
+    // One tile.  PLAIN: all its queries see all of the wave's keys, with one bias.
     float bias_behind = 0.f, bias_ahead = 0.f;
-    auto tile = [&](auto plain, auto seen_only, int i0, int buf, bool exact) {
-      constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
+    auto tile = [&](auto plain, int i0, int buf, bool exact, bool odd) {
+      constexpr bool PLAIN = decltype(plain)::value;
       const E *sq = room[buf], *sg = sq + kRows * P;
       const int first_p = (int)(q.at + i0);
       const bool behind = first_p - (mine + M - 1) >= a.reach, ahead = first_p + kRows - 1 - mine <= -a.reach;
       const float one = behind ? bias_behind : bias_ahead, mult = a.scale * kLog2e, add = one * kLog2e;
-#pragma unroll KS >= 4 ? 1 : 2
+#pragma unroll KS >= 4 || SEEN ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int pt = first_p + t * M;
         if (!PLAIN && ((a.causal && pt + M - 1 < mine) || i0 + t * M >= end)) continue;
@@ -576,7 +586,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
             z[r] = out ? 0.f : z[r] * x[r];
           }
         }
-        if (SEEN) {
+        if (SEEN && odd) {
           auto lo = [&](int c) { return mine + c - pt; };
           auto hi = [](int) { return M - 1; };
           gather_seen<Tl, DT>(dv, sg + t * M * P, P, Packed<Tl>(x), lane, lo, hi);
@@ -592,14 +602,9 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     const int from_i = mine >= q.len ? 0x7fffffff : a.causal ? (int)(mine - q.at) - (kRows - 1) : begin;
     int plain_from = !started ? 0x7fffffff : (int)min(max(a.causal ? mine + M - 1 - q.at : (int64_t)begin, a.bias ? mine + M - 1 + a.reach - q.at : (int64_t)begin), (int64_t)0x7fffffff);
     int plain_to = !started || a.causal || !a.bias ? -1 : (int)max(mine - a.reach - (kRows - 1) - q.at, (int64_t)-1);
-    auto take = [&](auto seen_only, int i0, int buf) {
-      const float mylse = stats[buf][0][lane % kRows];
-      const bool exact = !started || __any(mylse < __builtin_inff() && far_off(mylse));
-      if (!decltype(seen_only)::value && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), std::false_type(), i0, buf, false);
-      else tile(std::false_type(), seen_only, i0, buf, exact);
-    };
     fetch(begin);
-    bool odd = put(begin, 0), odds = odd;
+    bool odd = put(begin, 0);
+    odds |= odd;
     if (a.bias) {
       bias_behind = table[bt.size - 1];
       bias_ahead = table[0];
@@ -609,17 +614,17 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     for (int i0 = begin, buf = 0; i0 < end; i0 += kRows, buf ^= 1) {
       const bool next = i0 + kRows < end;
       if (next) fetch(i0 + kRows);
-      if (i0 >= from_i && !odd) take(std::false_type(), i0, buf);
+      if (i0 >= from_i) {
+        const float mylse = stats[buf][0][lane % kRows];
+        const bool exact = !started || __any(mylse < __builtin_inff() && far_off(mylse));
+        if (!SEEN && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), i0, buf, false, false);
+        else tile(std::false_type(), i0, buf, exact, odd);
+      }
       if (next) odd = put(i0 + kRows, buf ^ 1), odds |= odd;
     }
-    if (odds) {      // what was left out
-      for (int i0 = begin; i0 < end && q.at + i0 < k0 + 4 * M - 1; i0 += kRows) {
-        fetch(i0);
-        __syncthreads();
-        if (put(i0, 0) && i0 >= from_i) take(std::true_type(), i0, 0);
-      }
-    }
   }
+  if (!SEEN && threadIdx.x == 0 && a.causal) a.odd[blockIdx.x] = odds;
+  if (!SEEN && odds) return;
   if (j >= q.len) return;
   if (!there) {
 #pragma unroll
@@ -710,14 +715,17 @@ void long_back(Args& a, hipStream_t st) {
     const int64_t blocks = (a.Tq + 4 * M - 1) / (4 * M);
     a.slots = a.part ? back_slots(false, a.N, a.heads, 0, blocks) : (int)(a.N * blocks);
     const unsigned more = a.part ? 4 * 4 * (table_size(a.reach, a.causal) + 2 * M * M) : 0;
-    hipLaunchKernelGGL((k_attn_dq<Tl, KS>), (unsigned)(a.slots * a.heads), 256, lds + more, st, a);
+    hipLaunchKernelGGL((k_attn_dq<Tl, KS, false>), (unsigned)(a.slots * a.heads), 256, lds + more, st, a);
+    if (a.causal && a.dq.p) hipLaunchKernelGGL((k_attn_dq<Tl, KS, true>), (unsigned)(a.slots * a.heads), 256, lds, st, a);
   }
   if (a.dk.p || a.dv.p) {
     const int64_t blocks = (a.Tk + 4 * M - 1) / (4 * M);
     const Parts p = key_parts(a.Tq, a.Tk, a.N, a.heads, a.heads / a.group, sizeof(E) == 4);
     a.head_parts = p.heads;
     a.row_parts = p.rows;
-    hipLaunchKernelGGL((k_attn_dkv<Tl, KS>), (unsigned)(a.N * (a.heads / a.group) * blocks * p.heads * p.rows), 256, lds, st, a);
+    const unsigned grid = (unsigned)(a.N * (a.heads / a.group) * blocks * p.heads * p.rows);
+    hipLaunchKernelGGL((k_attn_dkv<Tl, KS, false>), grid, 256, lds, st, a);
+    if (a.causal) hipLaunchKernelGGL((k_attn_dkv<Tl, KS, true>), grid, 256, lds, st, a);
     if (p.heads * p.rows > 1) {
       const int64_t threads = a.N * (a.heads / a.group) * a.Tk * (a.d / 2);
       hipLaunchKernelGGL(k_attn_dkv_join<E>, (unsigned)std::min<int64_t>((threads + 255) / 256, 256 * 32), 256, 0, st, a);

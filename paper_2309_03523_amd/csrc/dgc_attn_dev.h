@@ -23,7 +23,7 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kMaxHeads = 1024, kMaxDim = 128, kMaxReach = 1024, kMaxBuckets = 256;
+constexpr int kMaxHeads = 1024, kMaxDim = 128, kMaxReach = 1024, kMaxBuckets = 256, kMaxSplits = 1024;
 
 struct Rows {          // row (t, i) at p + t st + i sn, in elements
   const void* p;
@@ -42,6 +42,7 @@ struct Args {
   const float* bias;
   float* lse;          // [N][heads][Tq]
   float* delta;        // the same
+  int32_t* odd;        // whether a workgroup's work is to be done again by the kernel that keeps what is not finite apart
   float* part;         // partial sums of the bias' gradient: [heads][slots][kind of table]
   int32_t slots;       // workgroups (windows: waves) of a head
   int32_t splits;      // few queries: parts of the keys
@@ -386,6 +387,7 @@ template <class Tl, int KS>
 struct Geometry {
   static constexpr int DT = (KS * 16 + Tl::M - 1) / Tl::M;                    // row tiles of a head
   static constexpr int P = DT * Tl::M + 16 / (int)sizeof(typename Tl::E);     // pitch of rows in LDS: 16 bytes more, so that rows begin in other banks
+  static constexpr int NT = Tl::M == 32 && KS >= 8 ? 1 : 2;                   // tiles of M rows on their way at a time, as registers allow
 };
 
 // Host side.  The form of a forward pass goes by its lengths alone.
