@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
   const bool near = nk.near && nv.near;
   const E *knext = kbase, *vnext = vbase;
   const int64_t kstep = kKeys * a.k.st, vstep = kKeys * a.v.st;
-  auto fetch = [&](int j0) {
+  auto fetch = [&](int j0) __attribute__((always_inline)) {
     if (!holes(j0) && near) {
       nk.fetch_all(knext);
       nv.fetch_all(vnext);
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
     }
   };
   // Lays out a tile; whether a zero weight would meet a value of it that is not finite.
-  auto put = [&](int j0, int b) -> bool {
+  auto put = [&](int j0, int b) __attribute__((always_inline)) -> bool {
     nk.put(room[b], P);
     nv.put(room[b] + kKeys * P, P);
     if (holes(j0) && threadIdx.x < kKeys) seens[b][threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
   // multiply-add and one power of two, and nothing branches, so products and weights of the tile's halves run side by side.
   // SEEN: values that are not finite reach only those that see them.
   float bias_behind = 0.f, bias_ahead = 0.f;       // beyond the reach
-  auto tile = [&](auto plain, auto seen_only, int j0, int buf) {
+  auto tile = [&](auto plain, auto seen_only, int j0, int buf) __attribute__((always_inline)) {
     constexpr bool PLAIN = decltype(plain)::value, SEEN = decltype(seen_only)::value;
     const E *sk = room[buf], *sv = sk + kKeys * P;
     typename Tl::Acc x[NT];
@@ -326,6 +326,197 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
     }
     wave_fence();
   }
+}
+
+// The same for up to 32 keys where all sequences' queries stand at one position, as a batch of windows has it.  What bounds it is how many pieces of
+// memory a load touches: operands straight from memory are 32 bytes of each of 16 rows, and ran at 2.4 TB/s.  So a workgroup takes the rows of `together`
+// neighbouring heads, up to 256 bytes, of one or two sequences as they lie, through LDS, and its waves a sequence and head each from there; the outputs go back
+// the same way.  The next rows are on their way meanwhile; outputs leave after they have come and before more are asked for: memory answers in
+// order, so rows asked for before a store would come after it.
+struct WindowArgs {
+  Args a;
+  int32_t together, seqs, groups;      // heads, sequences of a workgroup at a time; groups of heads
+  int32_t pitch;                       // of a row in LDS
+};
+template <class Tl, int NT, int KS, int NC>      // NC: pieces of 16 bytes of a tensor that a thread takes
+__global__ __launch_bounds__(256, NT == 1 && KS < 8 ? 4 : 2) void k_attn_windows(WindowArgs w) {
+  typedef typename Tl::E E;
+  typedef typename Tl::Frag Frag;
+  const Args& a = w.a;
+  constexpr int DT = Geometry<Tl, KS>::DT, W = 16 * NT, PER = 16 / (int)sizeof(E);
+  extern __shared__ __attribute__((aligned(16))) char window_room[];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, sub = lane >> 4;
+  const int group = blockIdx.x % w.groups, slot = blockIdx.x / w.groups, h0 = group * w.together, heads = min(w.together, a.heads - h0), at = a.Tk - a.Tq;
+  const int y0 = h0 / a.group, kvs = (h0 + heads - 1) / a.group - y0 + 1;
+  const int P = w.pitch, rows = w.seqs * W;
+  E *sk = reinterpret_cast<E*>(window_room), *sv = sk + rows * P, *sq = sv + rows * P, *so = sq + rows * P;
+  float* add = reinterpret_cast<float*>(so + rows * P);       // [together][2 W]: the bias by distance, -inf where the position masks
+  int* there = reinterpret_cast<int*>(add + w.together * 2 * W);      // [seqs][W]: whether a key is there
+  int* lens = there + rows;
+  for (int x = threadIdx.x; x < rows * P; x += 256) sv[x] = 0;       // rows behind Tk meet weights of zero
+  __syncthreads();
+  for (int x = threadIdx.x; x < heads * 2 * W; x += 256) {
+    const int away = at + x % (2 * W) - W + 1;
+    add[x] = a.causal && away < 0 ? -__builtin_inff() : a.bias ? bias_at(a, h0 + x / (2 * W), away) : 0.f;
+  }
+  // A thread's pieces of 16 bytes: where in LDS, how far from the first sequence's first row, which sequence and row.
+  const int kcpr = kvs * a.d / PER, qcpr = heads * a.d / PER, kpieces = w.seqs * a.Tk * kcpr, qpieces = w.seqs * a.Tq * qcpr;
+  uint32_t koff[NC], voff[NC], qoff[NC], ooff[NC];
+  int kat[NC], qat[NC], kseq[NC], krow[NC], qseq[NC], qrow[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int c = threadIdx.x + 256 * i;
+    const int kr = c / kcpr, kx = (c % kcpr) * PER, qr = c / qcpr, qx = (c % qcpr) * PER;
+    kseq[i] = c < kpieces ? kr / a.Tk : w.seqs;
+    krow[i] = kr % a.Tk;
+    kat[i] = (kseq[i] * W + krow[i]) * P + kx;
+    koff[i] = (uint32_t)((kseq[i] * a.k.sn + krow[i] * a.k.st + kx) * sizeof(E));
+    voff[i] = (uint32_t)((kseq[i] * a.v.sn + krow[i] * a.v.st + kx) * sizeof(E));
+    qseq[i] = c < qpieces ? qr / max(a.Tq, 1) : w.seqs;
+    qrow[i] = qr % max(a.Tq, 1);
+    qat[i] = (qseq[i] * W + qrow[i]) * P + qx;
+    qoff[i] = (uint32_t)((qseq[i] * a.q.sn + qrow[i] * a.q.st + qx) * sizeof(E));
+    ooff[i] = (uint32_t)((qseq[i] * a.o.sn + qrow[i] * a.o.st + qx) * sizeof(E));
+  }
+  const bool whole = a.Tk == W && a.d == 16 * KS;
+  uint4 nk[NC], nv[NC], nq[NC];
+  uint32_t nkeep = 0;
+  int nlen = 0;
+  auto fetch = [&](int64_t n0) __attribute__((always_inline)) {
+    const int here = (int)min((int64_t)w.seqs, a.N - n0);
+    const char* kb = reinterpret_cast<const char*>(static_cast<const E*>(a.k.p) + n0 * a.k.sn + y0 * a.d);
+    const char* vb = reinterpret_cast<const char*>(static_cast<const E*>(a.v.p) + n0 * a.v.sn + y0 * a.d);
+    const char* qb = reinterpret_cast<const char*>(static_cast<const E*>(a.q.p) + n0 * a.q.sn + h0 * a.d);
+    nkeep = 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      bool in = kseq[i] < here;
+      if (a.lengths) in = in && krow[i] < a.lengths[n0 + min(kseq[i], here - 1)];
+      if (a.keep) in = in && a.keep[krow[i] * a.N + n0 + min(kseq[i], here - 1)];
+      nkeep |= in ? 1u << i : 0;
+      nk[i] = in ? *reinterpret_cast<const uint4*>(kb + koff[i]) : make_uint4(0, 0, 0, 0);
+      nv[i] = in ? *reinterpret_cast<const uint4*>(vb + voff[i]) : make_uint4(0, 0, 0, 0);
+      nq[i] = qseq[i] < here ? *reinterpret_cast<const uint4*>(qb + qoff[i]) : make_uint4(0, 0, 0, 0);
+    }
+    if ((int)threadIdx.x < w.seqs) nlen = (int)threadIdx.x >= here ? 0 : a.lengths ? min(max(a.lengths[n0 + threadIdx.x], 0), a.Tk) : a.Tk;
+  };
+  auto leave = [&](int64_t n0) __attribute__((always_inline)) {      // the outputs, as they lie in LDS, of queries that are tokens
+    char* ob = reinterpret_cast<char*>(static_cast<E*>(const_cast<void*>(a.o.p)) + n0 * a.o.sn + h0 * a.d);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      if (qseq[i] < w.seqs && at + qrow[i] < lens[qseq[i]]) *reinterpret_cast<uint4*>(ob + ooff[i]) = *reinterpret_cast<const uint4*>(so + qat[i]);
+    }
+  };
+  const int64_t step = (int64_t)a.slots * w.seqs;
+  int64_t n0 = (int64_t)slot * w.seqs;
+  fetch(n0);
+  bool begun = false;
+  for (; n0 < a.N; n0 += step) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      if (kseq[i] < w.seqs) {
+        *reinterpret_cast<uint4*>(sk + kat[i]) = nk[i];
+        *reinterpret_cast<uint4*>(sv + kat[i]) = nv[i];
+        if (kat[i] % P == 0) there[kseq[i] * W + krow[i]] = nkeep >> i & 1;
+        if constexpr (sizeof(E) == 2) odd = odd || Wide::odd(nk[i]) || Wide::odd(nv[i]);
+        else odd = odd || Full::odd(nk[i]) || Full::odd(nv[i]);
+      }
+      if (qseq[i] < w.seqs) *reinterpret_cast<uint4*>(sq + qat[i]) = nq[i];
+    }
+    if (begun) leave(n0 - step);
+    begun = true;
+    bool some_odd = false;
+    if (a.causal) some_odd = __syncthreads_or(odd);
+    else __syncthreads();
+    if ((int)threadIdx.x < w.seqs) lens[threadIdx.x] = nlen;      // for the outputs, after the last ones have gone
+    if (n0 + step < a.N) fetch(n0 + step);
+    for (int seq = 0, g = wave; ; g += 4) {
+      while (g >= heads && seq < w.seqs) g -= heads, ++seq;
+      const int64_t n = n0 + seq;
+      if (seq >= w.seqs || n >= a.N) break;
+      const int h = h0 + g, kc = (a.group == 1 ? g : h / a.group - y0) * a.d;
+      const uint32_t keys = (uint32_t)__ballot(lane < a.Tk && there[seq * W + (lane & (W - 1))]);
+      const bool all = keys == (uint32_t)((1ull << W) - 1);
+      const E *uk = sk + seq * W * P + kc, *uv = sv + seq * W * P + kc, *uq = sq + seq * W * P + g * a.d;
+      E* uo = so + seq * W * P + g * a.d;
+      const float* table = add + g * 2 * W + W - 1 + col - 4 * sub;      // less a key's place
+      Frag fk[NT][KS];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          fk[t][s] = Tl::rows(uk + t * 16 * P, P, s, lane);
+          if (!whole && (16 * s + 4 * sub >= a.d || 16 * t + col >= a.Tk)) fk[t][s] = Tl::zero();
+        }
+      }
+      bool slow = false;       // of this sequence and head: others keep their bits
+      if (some_odd) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int s = 0; s < KS; ++s) slow = slow || (16 * s + 4 * sub < a.d && (Tl::odd(fk[t][s]) || Tl::odd(Tl::rows(uv + t * 16 * P, P, s, lane))));
+        }
+        slow = __any(slow);
+      }
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        if (16 * u >= a.Tq) break;
+        const int last = a.causal ? at + 16 * u + 15 : a.Tk - 1;        // no query of this tile sees a later key
+        Frag fq[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          fq[s] = Tl::rows(uq + u * 16 * P, P, s, lane);
+          if (!whole && 16 * s + 4 * sub >= a.d) fq[s] = Tl::zero();
+        }
+        floatx4 x[NT];
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (16 * t > last) break;
+          floatx4 b;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) b[r] = table[16 * (u - t) - r];
+          x[t] = (floatx4)(0.f);
+#pragma unroll
+          for (int s = 0; s < KS; ++s) x[t] = Tl::mma(fk[t][s], fq[s], x[t]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[t][r] = fmaf(x[t][r], a.scale, b[r]);
+          if (slow || !all) {
+            const uint32_t bits = keys >> (16 * t + 4 * sub);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = (bits >> r & 1) && b[r] != -__builtin_inff() ? x[t][r] : -__builtin_inff();
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, x[t][r]);
+        }
+        top = column_max<4>(top);
+        float l = 0.f;
+        floatx4 o[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = (floatx4)(0.f);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (16 * t > last) break;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[t][r] = weight_of(x[t][r], top);
+            l += x[t][r];
+          }
+          if (!slow) gather<Tl, DT>(o, uv + 16 * t * P, P, Packed<Tl>(x[t]), lane);
+          else gather_seen<Tl, DT>(o, uv + 16 * t * P, P, Packed<Tl>(x[t]), lane, [](int) { return 0; }, [&](int c) { return at + 16 * u + c - 16 * t; });
+        }
+        l = column_sum<4>(l);
+        const int i = 16 * u + col;
+        if (i < a.Tq) {
+          store_column<Tl, DT>(uo + i * P, o, l == 0.f ? 0.f : sizeof(E) == 2 ? __builtin_amdgcn_rcpf(l) : 1.f / l, a.d, lane);
+          if (a.lse && sub == 0 && (!a.lengths || at + i < a.lengths[n])) a.lse[(n * a.heads + h) * a.Tq + i] = log_sum(top, l);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (begun) leave(n0 - step);
 }
 
 // ---------------------------------------------------------------------------------------------------- few queries
@@ -577,7 +768,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_rows(Args a) {
   float m = -__builtin_inff(), l = 0.f;
   uint4 wk[NT][KS], wv[NT][KS];
   uint32_t bits = 0;         // which of the step's keys are there
-  auto fetch = [&](int j0) {
+  auto fetch = [&](int j0) __attribute__((always_inline)) {
     const int mine = j0 + (lane & (KEYS - 1));
     bits = (uint32_t)__ballot(mine < k1 && (!a.keep || a.keep[(int64_t)mine * a.N + n]));
 #pragma unroll
@@ -757,6 +948,37 @@ void window(Args a, hipStream_t st) {
   const int64_t waves = 256 * 32;      // as many as the card holds at a time
   a.slots = (int)std::min<int64_t>(a.N, (waves + a.heads - 1) / a.heads);
   const unsigned grid = (unsigned)(((int64_t)a.slots * a.heads + 3) / 4);
+  if constexpr (NT <= 2) {
+    const int e = sizeof(typename Tl::E), W = 16 * NT;
+    auto far = [&](const Rows& x) { return (x.st > x.sn ? x.st : x.sn) >= ((int64_t)1 << 31) / e / (W + 2); };      // beyond 32-bit offsets
+    if (!a.first && !far(a.k) && !far(a.v) && !far(a.q) && !far(a.o)) {
+      WindowArgs w{a};
+      w.together = std::min(a.heads, std::max(1, 256 / (a.d * e)));
+      w.seqs = w.together >= 4 || a.d * e > 256 ? 1 : 2;
+      w.groups = (a.heads + w.together - 1) / w.together;
+      w.pitch = w.together * a.d + 16 / e;
+      const int64_t blocks = (a.N + w.seqs - 1) / w.seqs, most = 256 * 8;
+      w.a.slots = (int)std::min<int64_t>(blocks, (most + w.groups - 1) / w.groups);
+      const unsigned lds = 4 * w.seqs * W * w.pitch * e + 64 * e + 4 * (w.together * 2 * W + w.seqs * W + w.seqs), wgs = (unsigned)(w.a.slots * w.groups);
+      const bool more = w.seqs * W * std::max(1, w.together * a.d * e / 16) > 256 * NT;
+#define DGC_WINDOWS(KS)                                                                                  \
+  if (more) hipLaunchKernelGGL((k_attn_windows<Tl, NT, KS, 2 * NT>), wgs, 256, lds, st, w);    \
+  else hipLaunchKernelGGL((k_attn_windows<Tl, NT, KS, NT>), wgs, 256, lds, st, w)
+      if (lds > 65536) {
+        // rows of more than 256 bytes: below
+      } else if (a.d <= 16) {
+        DGC_WINDOWS(1);
+      } else if (a.d <= 32) {
+        DGC_WINDOWS(2);
+      } else if (a.d <= 64) {
+        DGC_WINDOWS(4);
+      } else {
+        DGC_WINDOWS(8);
+      }
+#undef DGC_WINDOWS
+      if (lds <= 65536) return;
+    }
+  }
   if (a.d <= 16) hipLaunchKernelGGL((k_attn_window<Tl, NT, 1>), grid, 256, 0, st, a);
   else if (a.d <= 32) hipLaunchKernelGGL((k_attn_window<Tl, NT, 2>), grid, 256, 0, st, a);
   else if (a.d <= 64) hipLaunchKernelGGL((k_attn_window<Tl, NT, 4>), grid, 256, 0, st, a);

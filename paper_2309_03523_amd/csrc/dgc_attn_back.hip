@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
     auto holes = [&](int j0) { return j0 + kKeys > whole; };
     const bool near = nk.near && nv.near;
     const E *knext = kbase, *vnext = vbase;
-    auto fetch = [&](int j0) {
+    auto fetch = [&](int j0) __attribute__((always_inline)) {
       if (!holes(j0) && near) {
         nk.fetch_all(knext);
         nv.fetch_all(vnext);
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
       }
     };
     // Lays out a tile; whether a zero gradient would meet a key of it that is not finite.
-    auto put = [&](int j0, int b) -> bool {
+    auto put = [&](int j0, int b) __attribute__((always_inline)) -> bool {
       nk.put(room[b], P);
       nv.put(room[b] + kKeys * P, P);
       if (holes(j0) && threadIdx.x < kKeys) seens[b][threadIdx.x] = there(j0 + (int)threadIdx.x) ? 1.f : 0.f;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
 
     // One tile.  PLAIN: every query sees all of it, with one bias.  odd: dq is left out, or (SEEN) keys that are not finite reach only those that see them.
     float bias_behind = 0.f, bias_ahead = 0.f;
-    auto tile = [&](auto plain, int j0, int buf, bool odd) {
+    auto tile = [&](auto plain, int j0, int buf, bool odd) __attribute__((always_inline)) {
       constexpr bool PLAIN = decltype(plain)::value;
       const E *sk = room[buf], *sv = sk + kKeys * P;
       const bool behind = p0 - (j0 + kKeys - 1) >= a.reach, ahead = p1 - j0 <= -a.reach;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     const float* Ds = a.delta + (n * a.heads + h) * a.Tq;
     float nlse = 0.f, nD = 0.f, rowlse[NS];
     auto token = [&](int i) { return i >= q.lo && i < end; };
-    auto fetch = [&](int i0) {
+    auto fetch = [&](int i0) __attribute__((always_inline)) {
       if (i0 + kRows <= end && near) {
         nq.fetch_all(qbase + i0 * a.q.st);
         ng.fetch_all(gbase + i0 * a.go.st);
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
         nD = ok ? Ds[i] : 0.f;
       }
     };
-    auto put = [&](int i0, int b) -> bool {
+    auto put = [&](int i0, int b) __attribute__((always_inline)) -> bool {
       // A query that sees nothing gives no gradient: its rows are zero, whatever they hold.
 #pragma unroll
       for (int x = 0; x < NS; ++x) {
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     };
     // One tile.  PLAIN: all its queries see all of the wave's keys, with one bias.
     float bias_behind = 0.f, bias_ahead = 0.f;
-    auto tile = [&](auto plain, int i0, int buf, bool exact, bool odd) {
+    auto tile = [&](auto plain, int i0, int buf, bool exact, bool odd) __attribute__((always_inline)) {
       constexpr bool PLAIN = decltype(plain)::value;
       const E *sq = room[buf], *sg = sq + kRows * P;
       const int first_p = (int)(q.at + i0);

@@ -55,7 +55,7 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ bool far_off(float off) { return fabsf(off) > 1048576.f; }
 // e^(x - off); off is a maximum, -inf if there is nothing.
 __device__ __forceinline__ float weight_of(float x, float off) { return exp2_((x - (off == -__builtin_inff() ? 0.f : off)) * kLog2e); }
-__device__ __forceinline__ float log_sum(float top, float sum) { return sum == 0.f ? -__builtin_inff() : top + logf(sum); }
+__device__ __forceinline__ float log_sum(float top, float sum) { return sum == 0.f ? -__builtin_inff() : fmaf(__builtin_amdgcn_logf(sum), kLn2, top); }      // the sum has a term of 1: its logarithm is off by 2^-23
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const bf16x2 v = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, v);
