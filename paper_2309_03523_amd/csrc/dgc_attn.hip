@@ -437,6 +437,7 @@ __global__ __launch_bounds__(256, NT == 1 && KS < 8 ? 4 : 2) void k_attn_windows
       if (seq >= w.seqs || n >= a.N) break;
       const int h = h0 + g, kc = (a.group == 1 ? g : h / a.group - y0) * a.d;
       const uint32_t keys = (uint32_t)__ballot(lane < a.Tk && there[seq * W + (lane & (W - 1))]);
+      const int len = a.lengths ? min(max(uniform(a.lengths[n]), 0), a.Tk) : a.Tk;
       const bool all = keys == (uint32_t)((1ull << W) - 1);
       const E *uk = sk + seq * W * P + kc, *uv = sv + seq * W * P + kc, *uq = sq + seq * W * P + g * a.d;
       E* uo = so + seq * W * P + g * a.d;
@@ -461,8 +462,8 @@ __global__ __launch_bounds__(256, NT == 1 && KS < 8 ? 4 : 2) void k_attn_windows
       }
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        if (16 * u >= a.Tq) break;
-        const int last = a.causal ? at + 16 * u + 15 : a.Tk - 1;        // no query of this tile sees a later key
+        if (16 * u >= a.Tq || at + 16 * u >= len) break;
+        const int last = a.causal ? min(at + 16 * u + 15, len - 1) : len - 1;        // no query of this tile sees a later key
         Frag fq[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -510,7 +511,7 @@ __global__ __launch_bounds__(256, NT == 1 && KS < 8 ? 4 : 2) void k_attn_windows
         const int i = 16 * u + col;
         if (i < a.Tq) {
           store_column<Tl, DT>(uo + i * P, o, l == 0.f ? 0.f : sizeof(E) == 2 ? __builtin_amdgcn_rcpf(l) : 1.f / l, a.d, lane);
-          if (a.lse && sub == 0 && (!a.lengths || at + i < a.lengths[n])) a.lse[(n * a.heads + h) * a.Tq + i] = log_sum(top, l);
+          if (a.lse && sub == 0 && at + i < len) a.lse[(n * a.heads + h) * a.Tq + i] = log_sum(top, l);
         }
       }
     }

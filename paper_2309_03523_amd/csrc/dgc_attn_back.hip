@@ -181,6 +181,287 @@ __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
   }
 }
 
+// The same where every head has a key head of its own, and rows go through LDS as they lie (as in the forward pass' k_attn_windows; straight from memory
+// it took 2.6 times as long): all gradients take the place of what they are gradients of, and leave from there.  A wave keeps to one head, or two, so
+// the bias' gradient is summed in registers, element by element, until the end.
+struct WindowBack {
+  Args a;
+  int32_t together, seqs, groups, pitch, tables;
+};
+template <class Tl, int NT, int KS, int NC, int HW>      // NC: pieces of 16 bytes of a tensor that a thread takes; HW: heads of a wave
+__global__ __launch_bounds__(256, 2) void k_attn_windows_back(WindowBack w) {
+  typedef typename Tl::E E;
+  typedef typename Tl::Frag Frag;
+  const Args& a = w.a;
+  constexpr int DT = Geometry<Tl, KS>::DT, W = 16 * NT, PER = 16 / (int)sizeof(E), PT = 16 + PER;
+  extern __shared__ __attribute__((aligned(16))) char window_room[];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, sub = lane >> 4;
+  const int group = blockIdx.x % w.groups, slot = blockIdx.x / w.groups, h0 = group * w.together, heads = min(w.together, a.heads - h0), at = a.Tk - a.Tq;
+  const int P = w.pitch, rows = w.seqs * W, cpr = heads * a.d / PER;
+  E *sk = reinterpret_cast<E*>(window_room), *sv = sk + rows * P, *sq = sv + rows * P, *sg = sq + rows * P, *sp = sg + rows * P + wave * 2 * 16 * PT, *ss = sp + 16 * PT;
+  float* add = reinterpret_cast<float*>(sg + rows * P + 4 * 2 * 16 * PT + 64);       // [together][2 W]: the bias by distance
+  float* lses = add + w.together * 2 * W;            // [seqs][together][W]
+  float* dots = lses + rows * w.together;            // [rows][pieces of a row]: parts of D
+  int* there = reinterpret_cast<int*>(dots + rows * (w.together * a.d / PER));      // [seqs][W]: whether a key is there
+  int* lens = there + rows;
+  for (int x = threadIdx.x; x < 4 * rows * P; x += 256) sk[x] = 0;       // rows behind Tk and Tq meet weights of zero
+  for (int x = threadIdx.x; x < heads * 2 * W; x += 256) add[x] = a.bias ? bias_at(a, h0 + x / (2 * W), at + x % (2 * W) - W + 1) : 0.f;
+  for (int x = threadIdx.x; x < rows * w.together; x += 256) lses[x] = -__builtin_inff();
+  for (int x = threadIdx.x; x < rows; x += 256) there[x] = 0;
+  __syncthreads();
+  const int kpieces = w.seqs * a.Tk * cpr, qpieces = w.seqs * a.Tq * cpr;
+  // A thread's pieces: sequence and row, among the keys' and among the queries' (seqs: none), and column.  Places and distances are made of them each
+  // time: kept, they would not fit the registers.
+  int kseq[NC], krow[NC], qseq[NC], qrow[NC], px[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int c = threadIdx.x + 256 * i, r = c / cpr;
+    px[i] = (c % cpr) * PER;
+    kseq[i] = c < kpieces ? r / a.Tk : w.seqs;
+    krow[i] = r % a.Tk;
+    qseq[i] = c < qpieces ? r / max(a.Tq, 1) : w.seqs;
+    qrow[i] = r % max(a.Tq, 1);
+  }
+  auto place = [&](int seq, int row, int x) { return (seq * W + row) * P + x; };
+  auto bytes = [&](const Rows& t, int seq, int row, int x) { return ((uint32_t)seq * (uint32_t)t.sn + (uint32_t)row * (uint32_t)t.st + (uint32_t)x) * (uint32_t)sizeof(E); };
+  auto base = [&](const Rows& x, int64_t n0) { return reinterpret_cast<char*>(static_cast<E*>(const_cast<void*>(x.p)) + n0 * x.sn + h0 * a.d); };
+  uint4 nk[NC], nv[NC], nq[NC], ng[NC];
+  float nl[NC], nd[NC];
+  uint32_t nkeep = 0;
+  int nlen = 0;
+  auto fetch = [&](int64_t n0) __attribute__((always_inline)) {
+    const int here = (int)min((int64_t)w.seqs, a.N - n0);
+    nkeep = 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      bool in = kseq[i] < here;
+      if (a.lengths) in = in && krow[i] < a.lengths[n0 + min(kseq[i], here - 1)];
+      if (a.keep) in = in && a.keep[krow[i] * a.N + n0 + min(kseq[i], here - 1)];
+      nkeep |= in ? 1u << i : 0;
+      nk[i] = in ? *reinterpret_cast<const uint4*>(base(a.k, n0) + bytes(a.k, kseq[i], krow[i], px[i])) : make_uint4(0, 0, 0, 0);
+      nv[i] = in ? *reinterpret_cast<const uint4*>(base(a.v, n0) + bytes(a.v, kseq[i], krow[i], px[i])) : make_uint4(0, 0, 0, 0);
+      bool token = qseq[i] < here;
+      if (a.lengths) token = token && at + qrow[i] < a.lengths[n0 + min(qseq[i], here - 1)];
+      nq[i] = token ? *reinterpret_cast<const uint4*>(base(a.q, n0) + bytes(a.q, qseq[i], qrow[i], px[i])) : make_uint4(0, 0, 0, 0);
+      ng[i] = token ? *reinterpret_cast<const uint4*>(base(a.go, n0) + bytes(a.go, qseq[i], qrow[i], px[i])) : make_uint4(0, 0, 0, 0);
+      const uint4 o = token ? *reinterpret_cast<const uint4*>(base(a.o, n0) + bytes(a.o, qseq[i], qrow[i], px[i])) : make_uint4(0, 0, 0, 0);
+      nl[i] = token ? a.lse[((n0 + qseq[i]) * a.heads + h0 + px[i] / a.d) * a.Tq + qrow[i]] : -__builtin_inff();
+      float x[PER], y[PER];
+      ops::Elem<E>::unpack(ng[i], x);
+      ops::Elem<E>::unpack(o, y);
+      nd[i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) nd[i] = fmaf(x[e], y[e], nd[i]);
+    }
+    if ((int)threadIdx.x < w.seqs) nlen = (int)threadIdx.x >= here ? 0 : a.lengths ? min(max(a.lengths[n0 + threadIdx.x], 0), a.Tk) : a.Tk;
+  };
+  auto put = [&]() __attribute__((always_inline)) -> bool {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      // A query that sees nothing gives no gradient: its rows are zero, whatever they hold.
+      const bool live = nl[i] != -__builtin_inff();
+      const uint4 q = kept(nq[i], live), g = kept(ng[i], live);
+      if (kseq[i] < w.seqs) {
+        *reinterpret_cast<uint4*>(sk + place(kseq[i], krow[i], px[i])) = nk[i];
+        *reinterpret_cast<uint4*>(sv + place(kseq[i], krow[i], px[i])) = nv[i];
+        if (px[i] == 0) there[kseq[i] * W + krow[i]] = nkeep >> i & 1;
+      }
+      if (qseq[i] < w.seqs) {
+        *reinterpret_cast<uint4*>(sq + place(qseq[i], qrow[i], px[i])) = q;
+        *reinterpret_cast<uint4*>(sg + place(qseq[i], qrow[i], px[i])) = g;
+        dots[(qseq[i] * W + qrow[i]) * cpr + px[i] / PER] = live ? nd[i] : 0.f;
+        if (px[i] % a.d == 0) lses[(qseq[i] * w.together + px[i] / a.d) * W + qrow[i]] = nl[i];
+      }
+      if constexpr (sizeof(E) == 2) odd = odd || Wide::odd(nk[i]) || Wide::odd(q) || Wide::odd(g);
+      else odd = odd || Full::odd(nk[i]) || Full::odd(q) || Full::odd(g);
+    }
+    return odd;
+  };
+  floatx4 sums[HW][NT][NT];
+#pragma unroll
+  for (int k = 0; k < HW; ++k) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sums[k][u][t] = (floatx4)(0.f);
+    }
+  }
+  const auto acc0 = (floatx4)(0.f);
+  auto unit = [&](int seq, int g, int64_t n, bool some_odd, floatx4 (&sum)[NT][NT]) __attribute__((always_inline)) {
+    const uint32_t keys = (uint32_t)__ballot(lane < a.Tk && there[seq * W + (lane & (W - 1))]);
+    const int len = uniform(lens[seq]), hi = len - at;       // queries that are tokens
+    E *uk = sk + seq * W * P + g * a.d, *uv = sv + seq * W * P + g * a.d, *uq = sq + seq * W * P + g * a.d, *ug = sg + seq * W * P + g * a.d;
+    const float* table = add + g * 2 * W + W - 1 + col - 4 * sub;
+    bool odd_k = false, odd_qg = false;      // of this sequence and head: others keep their bits
+    if (some_odd) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const bool in = 16 * s + 4 * sub < a.d;
+          odd_k = odd_k || (in && Tl::odd(Tl::rows(uk + t * 16 * P, P, s, lane)));
+          odd_qg = odd_qg || (in && (Tl::odd(Tl::rows(uq + t * 16 * P, P, s, lane)) || Tl::odd(Tl::rows(ug + t * 16 * P, P, s, lane))));
+        }
+      }
+      odd_k = __any(odd_k);
+      odd_qg = __any(odd_qg);
+    }
+    floatx4 dk[NT][DT], dv[NT][DT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) dk[t][dt] = dv[t][dt] = acc0;
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      if (16 * u >= a.Tq || 16 * u >= hi) break;
+      const int i = 16 * u + col, p = at + i;
+      const float lse = i < a.Tq ? lses[(seq * w.together + g) * W + i] : -__builtin_inff();
+      const bool live = lse != -__builtin_inff();
+      const uint32_t sees = !live ? 0 : a.causal ? keys & ((2u << p) - 1) : keys;
+      const int last = a.causal ? min(at + 16 * u + 15, len - 1) : len - 1;
+      Frag fq[KS], fg[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        fq[s] = Tl::rows(uq + u * 16 * P, P, s, lane);
+        fg[s] = Tl::rows(ug + u * 16 * P, P, s, lane);
+        if (16 * s + 4 * sub >= a.d) fq[s] = fg[s] = Tl::zero();
+      }
+      float D = 0.f;
+      for (int x = sub; x < a.d / PER; x += 4) D += i < a.Tq ? dots[(seq * W + i) * cpr + g * (a.d / PER) + x] : 0.f;
+      D = column_sum<4>(D);
+      floatx4 dq[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) dq[dt] = acc0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (16 * t > last) break;
+        floatx4 x = acc0, z = acc0;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          Frag fk = Tl::rows(uk + t * 16 * P, P, s, lane), fv = Tl::rows(uv + t * 16 * P, P, s, lane);
+          if (16 * s + 4 * sub >= a.d) fk = fv = Tl::zero();
+          x = Tl::mma(fk, fq[s], x);
+          z = Tl::mma(fv, fg[s], z);
+        }
+        const uint32_t bits = sees >> (16 * t + 4 * sub);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool seen = bits >> r & 1;
+          x[r] = seen ? exp2_((fmaf(x[r], a.scale, table[16 * (u - t) - r]) - lse) * kLog2e) : 0.f;
+          z[r] = seen ? x[r] * (z[r] - D) : 0.f;
+        }
+        sum[u][t] += z;
+        const Frag ds = Tl::pack(z, 0);
+        wave_fence();
+        Tl::store(sp + col * PT + 4 * sub, Tl::pack(x, 0));
+        Tl::store(ss + col * PT + 4 * sub, ds);
+        wave_fence();
+        const Packed<Tl> p_t(Tl::across(sp, PT, 0, 0, lane)), ds_t(Tl::across(ss, PT, 0, 0, lane));
+        const int apart = 16 * t - at - 16 * u;       // key c is seen from query apart + c of the tile on
+        if (!odd_k) gather<Tl, DT>(dq, uk + t * 16 * P, P, Packed<Tl>(ds), lane);
+        else gather_seen<Tl, DT>(dq, uk + t * 16 * P, P, Packed<Tl>(ds), lane, [](int) { return 0; }, [&](int c) { return c - apart; });
+        if (!odd_qg) {
+          gather<Tl, DT>(dv[t], ug + u * 16 * P, P, p_t, lane);
+          gather<Tl, DT>(dk[t], uq + u * 16 * P, P, ds_t, lane);
+        } else {
+          auto lo = [&](int c) { return apart + c; };
+          auto up = [](int) { return 15; };
+          gather_seen<Tl, DT>(dv[t], ug + u * 16 * P, P, p_t, lane, lo, up);
+          gather_seen<Tl, DT>(dk[t], uq + u * 16 * P, P, ds_t, lane, lo, up);
+        }
+      }
+      wave_fence();       // this tile's queries have been read
+      if (!live) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) dq[dt] = acc0;
+      }
+      if (i < a.Tq && i < hi) store_column<Tl, DT>(uq + i * P, dq, a.scale, a.d, lane);
+    }
+    wave_fence();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int j = 16 * t + col;
+      if (j >= a.Tk) continue;
+      if (!(keys >> j & 1)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) dk[t][dt] = dv[t][dt] = acc0;
+      }
+      store_column<Tl, DT>(uk + j * P, dk[t], a.scale, a.d, lane);
+      store_column<Tl, DT>(uv + j * P, dv[t], 1.f, a.d, lane);
+    }
+  };
+  const int64_t step = (int64_t)a.slots * w.seqs;
+  int64_t n0 = (int64_t)slot * w.seqs;
+  fetch(n0);
+  for (bool begun = false; ; n0 += step, begun = true) {
+    // The gradients of the last sequences, from where those of the next ones go.
+    wordx4 out[3][NC];
+    {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        out[0][i] = *reinterpret_cast<const wordx4*>(sq + (qseq[i] < w.seqs ? place(qseq[i], qrow[i], px[i]) : 0));
+        out[1][i] = *reinterpret_cast<const wordx4*>(sk + (kseq[i] < w.seqs ? place(kseq[i], krow[i], px[i]) : 0));
+        out[2][i] = *reinterpret_cast<const wordx4*>(sv + (kseq[i] < w.seqs ? place(kseq[i], krow[i], px[i]) : 0));
+      }
+    }
+    const bool more = n0 < a.N;
+    const bool odd = more && put();
+    if (begun) {
+      const int64_t m = n0 - step;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        if (a.dq.p && qseq[i] < w.seqs && at + qrow[i] < lens[qseq[i]]) *reinterpret_cast<wordx4*>(base(a.dq, m) + bytes(a.dq, qseq[i], qrow[i], px[i])) = out[0][i];
+        if (kseq[i] < w.seqs && krow[i] < lens[kseq[i]]) {
+          if (a.dk.p) *reinterpret_cast<wordx4*>(base(a.dk, m) + bytes(a.dk, kseq[i], krow[i], px[i])) = out[1][i];
+          if (a.dv.p) *reinterpret_cast<wordx4*>(base(a.dv, m) + bytes(a.dv, kseq[i], krow[i], px[i])) = out[2][i];
+        }
+      }
+    }
+    if (!more) break;
+    bool some_odd = false;
+    if (a.causal) some_odd = __syncthreads_or(odd);
+    else __syncthreads();
+    if ((int)threadIdx.x < w.seqs) lens[threadIdx.x] = nlen;
+    if (n0 + step < a.N) fetch(n0 + step);
+    __syncthreads();       // the lengths
+#pragma unroll
+    for (int k = 0; k < HW; ++k) {
+      const int x = wave + 4 * k, seq = x / w.together, g = x % w.together;
+      if (g < heads && n0 + seq < a.N) unit(seq, g, n0 + seq, some_odd, sums[k]);
+    }
+    __syncthreads();
+  }
+  if (a.part) {
+    // By distance: a wave's sums as a slanted table in its part of the room, a column a lane.
+    float* slant = reinterpret_cast<float*>(window_room) + wave * W * 2 * W;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < HW; ++k) {
+      const int x = wave + 4 * k, g = x % w.together;
+      wave_fence();
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = 16 * u + col, j = 16 * t + 4 * sub + r;
+            slant[i * 2 * W + W - 1 + i - j] = sums[k][u][t][r];
+          }
+        }
+      }
+      wave_fence();
+      if (g < heads && lane < 2 * W) {
+        float s = 0.f;
+        for (int i = 0; i < W; ++i) s += (unsigned)(lane - i) < (unsigned)W ? slant[i * 2 * W + lane] : 0.f;
+        a.part[((int64_t)(h0 + g) * a.slots * w.tables + slot * w.tables + x / w.together % w.tables) * 2 * W + lane] = s;
+      }
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------- D = do . o, a row of LPR lanes
 template <class E, int LPR>
 __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
@@ -695,7 +976,38 @@ __global__ __launch_bounds__(256) void k_attn_bias(Args a, int size, int64_t fro
 
 // ---------------------------------------------------------------------------------------------------- launch
 template <class Tl, int NT>
+bool windows_back(Args& a, hipStream_t st) {
+  const int e = sizeof(typename Tl::E), W = 16 * NT;
+  const Rows* const all[8] = {&a.q, &a.k, &a.v, &a.o, &a.go, &a.dq, &a.dk, &a.dv};
+  for (const Rows* x : all) {
+    if (x->p && std::max(x->st, x->sn) >= ((int64_t)1 << 31) / e / (W + 4)) return false;      // beyond 32-bit offsets
+  }
+  const WindowPlan p = plan_windows(a.N, a.heads, a.d, e);
+  WindowBack w{a, p.together, p.seqs, p.groups, p.together * a.d + 16 / e, p.tables};
+  const int rows = p.seqs * W, cpr = p.together * a.d * e / 16, pieces = (rows * cpr + 255) / 256;
+  const int need = 4 * rows * w.pitch * e + (4 * 2 * 16 * (16 + 16 / e) + 64) * e + 4 * (p.together * 2 * W + rows * p.together + rows * cpr + rows + p.seqs);
+  const unsigned lds = (unsigned)std::max(need, 4 * 4 * W * 2 * W), wgs = (unsigned)(p.slots * p.groups);
+  if (lds > 65536 || pieces > 2 * NT || (pieces > NT && p.together == 8)) return false;
+  w.a.slots = p.slots;
+#define DGC_WINDOWS(KS)                                                                                                  \
+  if (p.together == 8) hipLaunchKernelGGL((k_attn_windows_back<Tl, NT, KS, NT, 2>), wgs, 256, lds, st, w);              \
+  else if (pieces > NT) hipLaunchKernelGGL((k_attn_windows_back<Tl, NT, KS, 2 * NT, 1>), wgs, 256, lds, st, w);         \
+  else hipLaunchKernelGGL((k_attn_windows_back<Tl, NT, KS, NT, 1>), wgs, 256, lds, st, w)
+  if (a.d <= 16) {
+    DGC_WINDOWS(1);
+  } else if (a.d <= 32) {
+    DGC_WINDOWS(2);
+  } else {
+    DGC_WINDOWS(4);
+  }
+#undef DGC_WINDOWS
+  a.slots = p.slots * p.tables;
+  return true;
+}
+
+template <class Tl, int NT>
 void window_back(Args& a, hipStream_t st) {
+  if (a.group == 1 && windows_back<Tl, NT>(a, st)) return;
   const int kvs = a.heads / a.group;
   a.slots = back_slots(true, a.N, a.heads, kvs, 0);
   const unsigned grid = (unsigned)(((int64_t)a.slots * kvs + 3) / 4), lds = a.bias ? 4 * 4 * a.group * 10 * 16 * NT : 0;

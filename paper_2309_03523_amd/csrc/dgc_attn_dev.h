@@ -19,6 +19,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t wordx4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
 
@@ -64,6 +65,8 @@ __device__ __forceinline__ bool odd_bf16(uint32_t w) {   // one of two bf16 numb
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 __device__ __forceinline__ bool odd_f32(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+
+__device__ __forceinline__ uint4 kept(uint4 w, bool ok) { return make_uint4(ok ? w.x : 0u, ok ? w.y : 0u, ok ? w.z : 0u, ok ? w.w : 0u); }
 
 struct Wide {
   typedef uint16_t E;
@@ -426,6 +429,21 @@ inline Parts key_parts(int64_t Tq, int64_t Tk, int64_t N, int64_t heads, int64_t
   return p;
 }
 inline unsigned bias_bytes(const Args& a) { return a.bias ? 4 * (unsigned)((a.causal ? a.reach : 2 * a.reach) + 2 * kPast + 1) : 0; }
+// Windows backward: whole rows of `together` neighbouring heads of `seqs` sequences a workgroup, four sequences and heads or eight at a time; `slots`
+// workgroups a group of heads, each of which leaves `tables` tables of the bias' gradient a head.
+struct WindowPlan {
+  int32_t together, seqs, groups, slots, tables;
+};
+inline WindowPlan plan_windows(int64_t N, int64_t heads, int64_t d, int e) {
+  WindowPlan p{1, 1, 1, 1, 1};
+  while (p.together < 8 && 2 * p.together <= heads && 2 * p.together * d * e <= 256) p.together *= 2;
+  p.seqs = p.together < 4 ? 4 / p.together : 1;
+  p.groups = (int32_t)((heads + p.together - 1) / p.together);
+  p.tables = p.together < 4 ? 4 / p.together : 1;
+  const int64_t blocks = (N + p.seqs - 1) / p.seqs, most = (1024 + p.groups - 1) / p.groups;
+  p.slots = (int32_t)(blocks < most ? blocks : most);
+  return p;
+}
 void attn_forward_f32(const Args& a, hipStream_t st);
 void attn_forward_bf16(const Args& a, hipStream_t st);
 void attn_backward_f32(const Args& a, float* dbias, hipStream_t st);
