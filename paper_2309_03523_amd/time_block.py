@@ -1,11 +1,12 @@
 """A pre-norm time block over snapshots, built of the library's operators: a trainable time encoder whose state is carried
 from window to window (as H0 / HN of the recurrent layers), to stand behind a structure encoder or another block.
 
-    n = norm1(x);  q, k, v = qkv(n);  o = linear attention with a decay per head over every vertex' sequence
+    n = norm1(x);  q, k, v = qkv(n);  o = linear attention with a decay per head over every vertex' sequence, or
+                                          softmax attention with a learned bias by buckets of distance
     m = x + out(o);  y = m + down(act(up(norm2(m))))
 
 x, y are [T, N, width], snapshots by vertices, float32 or bfloat16.  Every step runs in the HIP library
-(binding.norm_*, linear_*, decay_attn_*); PyTorch supplies device memory and the stream.
+(binding.norm_*, linear_*, decay_attn_*, attn_*); PyTorch supplies device memory and the stream.
 """
 from __future__ import annotations
 
@@ -22,16 +23,23 @@ class TimeBlock:
     [0, 1] a head, default 1 - 2^-(2 + 6 h / heads), memories of 4 to some 200 snapshots.  exact: binding.linear_backward's, for
     the gradients behind the activation.
 
+    attention="softmax": every snapshot attends to itself and those before it, with a learned bias, the parameter "attn.bias" [heads, buckets]: of
+    the distances' `buckets` (0: no bias) half hold one distance each and the rest grow up to `reach` (binding.attn_buckets).  Then no state is carried: a new
+    snapshot attends to the keys and values of those before it, which the caller keeps in a cache.
+
     Parameters are fp32, (out, in), named as in NAMES; set_param copies them in, get_param reads one or "<name>.grad": they and release()
     wait for the device, forward and backward only enqueue.  A block runs one call at a time.  Its buffers are made at the first call
     with new sizes, so a call may be captured into a HIP graph after an eager one of the same sizes.  Those of the last SIZES sizes
     and all that a captured call uses are kept until release()."""
 
+    attention, buckets = "decay", 0
     SIZES = 8      # a program trains, evaluates and steps at a few sizes; the vertices of a served graph change in number for ever
 
     def __init__(self, width: int, heads: int, hidden: int, *, dtype: str = "f32", act: str = "gelu", decay=None, eps: float = 1e-5,
-                 exact: bool = False, device="cuda:0"):
+                 exact: bool = False, attention: str = "decay", buckets: int = 16, reach: int = 32, device="cuda:0"):
         import torch
+        if attention not in ("decay", "softmax") or (attention == "softmax" and decay is not None):
+            raise ValueError("attention must be decay or softmax; only the former has decays")
         if heads < 1 or width % heads or (width // heads) % 8 or width // heads > 128:
             raise ValueError("width must be heads times a multiple of 8 that is at most 128")
         if hidden < 1 or act not in binding.LINEAR_ACT or dtype not in binding.DTYPE:
@@ -41,6 +49,9 @@ class TimeBlock:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self.attention, self.buckets = attention, int(buckets) if attention == "softmax" else 0
+        bias_map = binding.attn_buckets(self.buckets, reach) if self.buckets else None
+        self.reach = int(reach) if self.buckets else 0
         g = np.asarray(decay if decay is not None else 1.0 - 2.0 ** -(2.0 + 6.0 * np.arange(heads) / heads), np.float32).reshape(-1)
         if g.size != heads or not ((g >= 0) & (g <= 1)).all():
             raise ValueError("decay must hold one number in [0, 1] for each head")
@@ -49,6 +60,11 @@ class TimeBlock:
         self.shapes = {"norm1.weight": (W,), "norm1.bias": (W,), "qkv.weight": (3 * W, W), "qkv.bias": (3 * W,), "out.weight": (W, W),
                        "out.bias": (W,), "norm2.weight": (W,), "norm2.bias": (W,), "up.weight": (hidden, W), "up.bias": (hidden,),
                        "down.weight": (W, hidden), "down.bias": (W,)}
+        self.names = list(NAMES)
+        if self.buckets:
+            self.names.append("attn.bias")
+            self.shapes["attn.bias"] = (heads, self.buckets)
+        self._map = torch.from_numpy(bias_map).to(self.device) if self.buckets else None
         self._p = {n: self._room(s, self._kind(n)) for n, s in self.shapes.items()}
         for n in ("norm1.weight", "norm2.weight"):
             self._p[n].fill_(1.0)
@@ -59,11 +75,26 @@ class TimeBlock:
 
     def _kind(self, name: str):
         import torch
-        return self.dtype if len(self.shapes[name]) == 2 else torch.float32
+        return self.dtype if len(self.shapes[name]) == 2 and name != "attn.bias" else torch.float32
+
+    def _grads(self):
+        if not self._g:
+            self._g = {n: self._room(s, self._kind(n)) for n, s in self.shapes.items()}
+        return self._g
+
+    def trained(self):
+        """(parameters, gradients): the device tensors in the order of `names`, as an optimizer takes them (optimizer.AdamW(*block.trained())).  They
+        stay where they are; backward writes the gradients.  attn.bias is one row."""
+        g = self._grads()
+        self._settle()
+        flat = lambda t, n: t.view(1, -1) if n == "attn.bias" else t  # noqa: E731
+        return [flat(self._p[n], n) for n in self.names], [flat(g[n], n) for n in self.names]
 
     def _room(self, shape, dtype):
         """Zeroed rows at a pitch that is a multiple of 16 bytes."""
         import torch
+        if shape == self.shapes.get("attn.bias"):       # one piece, as the library takes it
+            return torch.zeros(shape, dtype=dtype, device=self.device)
         per = 16 // torch.empty(0, dtype=dtype).element_size()
         buf = torch.zeros(*shape[:-1], -(-shape[-1] // per) * per, dtype=dtype, device=self.device)
         return buf[..., :shape[-1]]
@@ -119,9 +150,9 @@ class TimeBlock:
         with torch.cuda.stream(stream):
             return torch.cuda.is_current_stream_capturing()
 
-    def _made(self, T: int, N: int, train: bool, stream):
+    def _made(self, T: int, N: int, train: bool, stream, kept: int = 0):
         import torch
-        key = (T, N, train)
+        key = (T, N, train, kept) if kept else (T, N, train)
         b = self._buffers.pop(key, None)
         if b is not None:
             self._buffers[key] = b      # the last to go
@@ -131,7 +162,11 @@ class TimeBlock:
         W, Hd, h = self.width, self.hidden, self.heads
         b = {"n": self._room((T, N, W), self.dtype), "qkv": self._room((T, N, 3 * W), self.dtype), "o": self._room((T, N, W), self.dtype),
              "m": self._room((T, N, W), self.dtype), "u": self._room((T, N, Hd), self.dtype)}
-        ws = binding.decay_attn_workspace_bytes(T, N, h, W // h, W // h, backward=train)
+        if self.attention == "softmax":
+            size = lambda Tk, back: binding.attn_workspace_bytes(T, Tk, N, h, W // h, dtype=self.dtype_name, buckets=self.buckets, reach=self.reach, backward=back)  # noqa: E731
+            ws = max([size(kept or T, False), size(T, True)] if train else [size(kept or T, False)])      # it grows with the keys
+        else:
+            ws = binding.decay_attn_workspace_bytes(T, N, h, W // h, W // h, backward=train)
         if train:
             R = T * N
             b["n2"], b["pre"] = self._room((T, N, W), self.dtype), self._room((T, N, Hd), self.dtype)
@@ -142,8 +177,8 @@ class TimeBlock:
             size = lambda k, m, act: binding.linear_workspace_bytes(R, k, m, dtype=self.dtype_name, act=act, exact=self.exact)  # noqa: E731
             ws = max(ws, binding.norm_workspace_bytes(R, W), size(W, 3 * W, "none"), size(W, W, "none"), size(W, Hd, self.act),
                      size(Hd, W, "none"))
-            if not self._g:
-                self._g = {n: self._room(s, self._kind(n)) for n, s in self.shapes.items()}
+            b["lse"] = torch.empty(N, h, T, device=self.device) if self.attention == "softmax" else None
+            self._grads()
         else:
             b["n2"] = b["n"]       # nothing is read again
         b["ws"] = torch.empty(max(ws, 16), dtype=torch.uint8, device=self.device)
@@ -213,36 +248,65 @@ class TimeBlock:
             raise ValueError(f"{name} must have the shape of X, {list(like.shape)}, not {list(t.shape)}")
 
     # -- the path
-    def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, train: bool = True, stream=None):
+    def forward(self, X, Y, *, S0=None, SN=None, lengths=None, reset=None, keep=None, cache=None, at: int = 0, train: bool = True, stream=None):
         """Y = block(X).  S0, SN fp32 [N, heads, d, d]: states entering and leaving the window (SN may be S0, of which train=True then
         keeps a copy); lengths, reset as binding.decay_attn_forward has them (rows behind a sequence take part in the row-wise steps
         alone).  train=True keeps what backward reads, X and S0 among it, so Y must lie apart from X; with train=False Y may be X.
-        T = 1 with train=False is the form for one new snapshot."""
+        T = 1 with train=False is the form for one new snapshot.
+
+        With softmax attention there are no states and resets.  keep uint8 [T, N], as binding.attn_forward has it: snapshots that nobody attends to.  cache
+        [S, N, 2 width], rows at least, of the block's element type, with train=False: X are snapshots at .. at + T - 1; their keys and values are written
+        to those rows, and they attend to all rows up to their own, of which keep [at + T, N] may mask some."""
         self._last = None
+        if self.attention == "softmax":
+            if S0 is not None or SN is not None or reset is not None:
+                raise ValueError("softmax attention has no states and no resets")
+            if cache is not None:
+                if train or lengths is not None:
+                    raise ValueError("a cache goes with train=False and without lengths")
+                if cache.dim() != 3 or cache.shape[1:] != (X.shape[1], 2 * self.width) or cache.dtype != self.dtype or cache.device != self.device:
+                    raise ValueError(f"cache must be [S, {X.shape[1]}, {2 * self.width}] of the block's element type and device")
+                if at < 0 or at + X.shape[0] > cache.shape[0]:
+                    raise ValueError("the snapshots must fit the cache")
+        elif keep is not None or cache is not None:
+            raise ValueError("keep and cache go with softmax attention")
         self._rows(X, "X")
         self._rows(Y, "Y", X)
         if train and self._overlap(X, Y):
             raise ValueError("with train=True Y must lie apart from X, which backward reads")
         T, N = X.shape[:2]
-        b = self._made(T, N, train, stream)
+        b = self._made(T, N, train, stream, cache.shape[0] if cache is not None else 0)
         try:
             if train and self._overlap(S0, SN):
                 S0 = self._kept(b, S0, stream)
-            self._forward(b, X, Y, S0, SN, lengths, reset, stream)
+            self._forward(b, X, Y, S0, SN, lengths, reset if self.attention == "decay" else keep, cache, at, stream)
         finally:
             self._used(b, stream)
-        self._last = (b, X, S0, lengths, reset) if train else None
+        self._last = (b, X, S0, lengths, reset if self.attention == "decay" else keep) if train else None
         return Y
 
-    def _forward(self, b, X, Y, S0, SN, lengths, reset, stream):
+    def _softmax(self):
+        """What every call of the attention has."""
+        return dict(heads=self.heads, scale=(self.width // self.heads) ** -0.5, bias=self._p.get("attn.bias"), bias_map=self._map)
+
+    def _forward(self, b, X, Y, S0, SN, lengths, mask, cache, at, stream):
         p, W = self._p, self.width
         q, k, v = b["qkv"][..., :W], b["qkv"][..., W:2 * W], b["qkv"][..., 2 * W:]
         binding.norm_forward(X, b["n"], gamma=p["norm1.weight"], beta=p["norm1.bias"], mean=b.get("mean1"), rstd=b.get("rstd1"), eps=self.eps,
                              stream=stream)
-        binding.linear_forward(b["n"], p["qkv.weight"], b["qkv"], bias=p["qkv.bias"], stream=stream)
+        if cache is None:
+            binding.linear_forward(b["n"], p["qkv.weight"], b["qkv"], bias=p["qkv.bias"], stream=stream)
+        else:       # keys and values to where they stay
+            end = at + X.shape[0]
+            binding.linear_forward(b["n"], p["qkv.weight"][:W], q, bias=p["qkv.bias"][:W], stream=stream)
+            binding.linear_forward(b["n"], p["qkv.weight"][W:], cache[at:end], bias=p["qkv.bias"][W:], stream=stream)
+            k, v = cache[:end, :, :W], cache[:end, :, W:]
         self._blank(b["o"], lengths, stream)
-        binding.decay_attn_forward(q, k, v, self._decay, b["o"], heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0, sn=SN, lengths=lengths,
-                                   reset=reset, workspace=b["ws"], stream=stream)
+        if self.attention == "softmax":
+            binding.attn_forward(q, k, v, b["o"], lengths=lengths, keep=mask, lse=b.get("lse"), workspace=b["ws"], stream=stream, **self._softmax())
+        else:
+            binding.decay_attn_forward(q, k, v, self._decay, b["o"], heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0, sn=SN, lengths=lengths,
+                                       reset=mask, workspace=b["ws"], stream=stream)
         binding.linear_forward(b["o"], p["out.weight"], b["m"], bias=p["out.bias"], residual=X, stream=stream)
         binding.norm_forward(b["m"], b["n2"], gamma=p["norm2.weight"], beta=p["norm2.bias"], mean=b.get("mean2"), rstd=b.get("rstd2"),
                              eps=self.eps, stream=stream)
@@ -251,19 +315,21 @@ class TimeBlock:
 
     def backward(self, dY, *, dX=None, dSN=None, dS0=None, stream=None):
         """Gradients of the last forward with train=True: of the parameters (get_param("<name>.grad")), of X into dX if given
-        (dX may be dY), and of S0 into dS0.  X, S0, lengths and reset of that forward must be unchanged."""
+        (dX may be dY), and of S0 into dS0.  X, S0, lengths, reset and keep of that forward must be unchanged."""
         if self._last is None:
             raise RuntimeError("backward follows a forward with train=True")
-        b, X, S0, lengths, reset = self._last
+        b, X, S0, lengths, mask = self._last
+        if self.attention == "softmax" and (dSN is not None or dS0 is not None):
+            raise ValueError("softmax attention has no states")
         self._rows(dY, "dY", X)
         if dX is not None:
             self._rows(dX, "dX", X)
         try:
-            self._backward(b, X, S0, lengths, reset, dY, dX, dSN, dS0, stream)
+            self._backward(b, X, S0, lengths, mask, dY, dX, dSN, dS0, stream)
         finally:
             self._used(b, stream)
 
-    def _backward(self, b, X, S0, lengths, reset, dY, dX, dSN, dS0, stream):
+    def _backward(self, b, X, S0, lengths, mask, dY, dX, dSN, dS0, stream):
         p, g, W, ws = self._p, self._g, self.width, b["ws"]
         cut = lambda t: (t[..., :W], t[..., W:2 * W], t[..., 2 * W:])  # noqa: E731
         lin = lambda dy, x, n, dx, **kw: binding.linear_backward(dy, x, p[n + ".weight"], dx=dx, dw=g[n + ".weight"], dbias=g[n + ".bias"],  # noqa: E731
@@ -274,8 +340,12 @@ class TimeBlock:
                               dbeta=g["norm2.bias"], workspace=ws, stream=stream)
         lin(b["dm"], b["o"], "out", b["dw"])
         self._blank(b["dqkv"], lengths, stream)
-        binding.decay_attn_backward(*cut(b["qkv"]), self._decay, b["dw"], *cut(b["dqkv"]), heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0,
-                                    dsn=dSN, ds0=dS0, lengths=lengths, reset=reset, workspace=ws, stream=stream)
+        if self.attention == "softmax":
+            binding.attn_backward(*cut(b["qkv"]), b["o"], b["lse"], b["dw"], *cut(b["dqkv"]), lengths=lengths, keep=mask, dbias=g.get("attn.bias"),
+                                  workspace=ws, stream=stream, **self._softmax())
+        else:
+            binding.decay_attn_backward(*cut(b["qkv"]), self._decay, b["dw"], *cut(b["dqkv"]), heads=self.heads, scale=(W // self.heads) ** -0.5, s0=S0,
+                                        dsn=dSN, ds0=dS0, lengths=lengths, reset=mask, workspace=ws, stream=stream)
         lin(b["dqkv"], b["n"], "qkv", b["dw"])
         binding.norm_backward(b["dw"], X, b["mean1"], b["rstd1"], dX if dX is not None else b["dw"], gamma=p["norm1.weight"], add=b["dm"],
                               dgamma=g["norm1.weight"], dbeta=g["norm1.bias"], workspace=ws, stream=stream)
