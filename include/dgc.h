@@ -533,8 +533,8 @@ dgc_status_t dgc_decay_attn_backward(const void* q, int64_t q_stride_t, int64_t 
  * p = first[n] + i (first NULL: Tk - Tq + i), key j at position j.  For head h, which reads key head h / (heads / kv_heads):
  *   s_j = scale q_i . k_j + bias[h][map[p - j]],   lse_i = log sum e^s_j,   o_i = sum e^(s_j - lse_i) v_j
  * over the keys that it sees: j < lengths[n] (NULL: Tk; clamped to [0, Tk]), keep[j][n] not 0, and with `causal` j <= p.
- *  Queries whose position is not in [0, lengths[n]), and keys from lengths[n] on, belong to no token: their rows, and entries of lse, are neither
- *   read nor written.  A query that sees no key, or only scores of -inf, has o = 0 and lse = -inf, and gives and has no gradient.
+ *  Queries whose position is not in [0, lengths[n]), and keys from lengths[n] on, belong to no token: what their rows hold does not count, and
+ *   their rows and entries of lse are not written.  A query that sees no key, or only scores of -inf, has o = 0 and lse = -inf, and gives and has no gradient.
  *   Keys that keep masks get gradients of 0.  What a masked row holds, infinities and NaN included, reaches nothing.
  *  q, o [heads][d], k, v [kv_heads][d] a row: row (t, n) at base + t * stride_t + n * stride_n elements (both multiples of 16 bytes, bases aligned to
  *   16).  Inputs may repeat rows (a stride of 0); an output's rows lie apart, and outputs lie apart from inputs and each other

@@ -242,6 +242,12 @@ def test_bias_beyond_and_within_reach(T, reach, causal, dtype):
     _both(_case(T, T, 2, 2, 32, dtype, T + reach, causal=causal, buckets=8 if reach > 4 else 4, reach=reach))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_most_shared_memory(d, dtype):
+    _both(_case(200, 200, 2, 2, d, dtype, d, causal=False, buckets=256, reach=1024))
+
+
 def test_any_map_and_numbers_beyond_the_buckets():
     import torch
     for T in (20, 100):
