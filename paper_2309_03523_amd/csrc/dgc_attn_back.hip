@@ -5,7 +5,8 @@
 //
 // Scores are computed again, not kept.  In k_attn_dq queries are columns and keys are summed over, in k_attn_dkv keys are columns and queries are summed over
 // (heads that share a key head one after the other), so no two workgroups add to one number: no atomics on memory, one order of sums, at the price of
-// seven products for five.  k_attn_window_back has a whole window in a wave and needs five.
+// seven products for five.  Windows of up to 32 keys have a whole sequence and head in a wave and need five: k_attn_windows_back where every head has a key head of its
+// own, k_attn_window_back where up to four share one.  The others: k_attn_delta (D), k_attn_dq, k_attn_dkv, k_attn_dkv_join (parts of the queries).
 // Rounding: bf16 tensors enter products as they are, scores, P, dP, D and dS are fp32; P and dS are rounded to bf16 (2^-9 of themselves)
 // for the products of dv, dq and dk, which are summed in fp32; the bias' gradient sums dS as it is, in fp32 and at the end in double.
 //
@@ -25,6 +26,8 @@ namespace {
 __device__ __forceinline__ void add_lds(float* to, float x) { __hip_atomic_fetch_add(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT); }
 
 // ---------------------------------------------------------------------------------------------------- windows
+//
+// A wave takes one sequence and key head after the other; keys, queries and their gradients lie in its part of LDS, so no wave waits for another.
 template <class Tl, int NT, int KS>
 __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
   typedef typename Tl::E E;
@@ -182,7 +185,8 @@ __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
 }
 
 // The same where every head has a key head of its own, and rows go through LDS as they lie (as in the forward pass' k_attn_windows; straight from memory
-// it took 2.6 times as long): all gradients take the place of what they are gradients of, and leave from there.  A wave keeps to one head, or two, so
+// they took 1.2 to 1.6 times as long; 20 000 ragged windows of 32, 4 heads of 32, bf16: 0.42 ms, where 0.14 is what a copy of it all takes; it waits for
+// LDS and its own chain of products at two waves a SIMD, of 256 registers and some spilled): all gradients take the place of what they are gradients of, and leave from there.  A wave keeps to one head, or two, so
 // the bias' gradient is summed in registers, element by element, until the end.
 struct WindowBack {
   Args a;
@@ -490,7 +494,8 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 
 // ---------------------------------------------------------------------------------------------------- dq, and the bias' gradient
 //
-// As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it leaves dP - D.
+// Four sequences of 4096, 8 heads of 64 on 2 key heads, bf16: 0.19 ms, and k_attn_dkv 0.25.  Both are bound by how long a wave's chain LDS, products, powers, products
+// takes with two waves a SIMD.  As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it leaves dP - D.
 // Where a zero gradient would meet a key that is not finite, this kernel leaves dq to the same one with SEEN, which is launched behind it and takes
 // such items alone: with both in one kernel the registers do not do.
 template <class Tl, int KS, bool SEEN>
@@ -605,7 +610,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
       const bool behind = p0 - (j0 + kKeys - 1) >= a.reach, ahead = p1 - j0 <= -a.reach;
       const float one = behind ? bias_behind : bias_ahead;
       const float mult = a.scale * kLog2e, add = (one - lse) * kLog2e;
-#pragma unroll KS >= 4 || SEEN ? 1 : 2
+#pragma unroll KS >= 3 || SEEN ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int first = j0 + t * M;
         if (!PLAIN && (first >= kend || (a.causal && first > p1))) break;
@@ -814,7 +819,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       const int first_p = (int)(q.at + i0);
       const bool behind = first_p - (mine + M - 1) >= a.reach, ahead = first_p + kRows - 1 - mine <= -a.reach;
       const float one = behind ? bias_behind : bias_ahead, mult = a.scale * kLog2e, add = one * kLog2e;
-#pragma unroll KS >= 4 || SEEN ? 1 : 2
+#pragma unroll KS >= 3 || SEEN ? 1 : 2
       for (int t = 0; t < NT; ++t) {
         const int pt = first_p + t * M;
         if (!PLAIN && ((a.causal && pt + M - 1 < mine) || i0 + t * M >= end)) continue;
@@ -947,7 +952,6 @@ __global__ __launch_bounds__(256) void k_attn_dkv_join(Args a) {
   }
 }
 
-
 // ---------------------------------------------------------------------------------------------------- the bias' gradient
 //
 // part[h][slot][x] holds sums of distance from + x: one workgroup a head and bucket sums those of the bucket, in one order, in double: 16 distances at a
@@ -1019,7 +1023,7 @@ void window_back(Args& a, hipStream_t st) {
 template <class Tl, int KS>
 void long_back(Args& a, hipStream_t st) {
   typedef typename Tl::E E;
-  constexpr int M = Tl::M, LPR = KS * 16 / ops::Elem<E>::kPer;
+  constexpr int M = Tl::M, LPR = (KS == 3 ? 4 : KS == 6 ? 8 : KS) * 16 / ops::Elem<E>::kPer;      // a power of two
   const int64_t rows = (int64_t)a.Tq * a.N * a.heads;
   if (rows > 0) hipLaunchKernelGGL((k_attn_delta<E, LPR>), (unsigned)std::min<int64_t>((rows * LPR + 255) / 256, 256 * 32), 256, 0, st, a);
   const unsigned lds = bias_bytes(a);
@@ -1045,6 +1049,8 @@ void long_back(Args& a, hipStream_t st) {
   }
 }
 
+// fp32 heads are padded to 16, 32, 48, 64, 96 or 128 columns (200 x 101 tokens, 4 heads of 40: 168 us with 48 columns, 186 with 64; 40 x 512, 4 of 96: 360 and
+// 440), bf16 ones, whose tiles are 32 wide, to 16, 32, 64 or 128.
 template <class Tl16, class TlLong>
 void backward(Args a, float* dbias, hipStream_t st) {
   int size = table_size(a.reach, a.causal);
@@ -1061,8 +1067,12 @@ void backward(Args a, float* dbias, hipStream_t st) {
     long_back<TlLong, 1>(a, st);
   } else if (a.d <= 32) {
     long_back<TlLong, 2>(a, st);
+  } else if (a.d <= 48 && TlLong::kExact) {
+    long_back<TlLong, TlLong::kExact ? 3 : 4>(a, st);
   } else if (a.d <= 64) {
     long_back<TlLong, 4>(a, st);
+  } else if (a.d <= 96 && TlLong::kExact) {
+    long_back<TlLong, TlLong::kExact ? 6 : 8>(a, st);
   } else {
     long_back<TlLong, 8>(a, st);
   }

@@ -1,4 +1,4 @@
-// Device helpers of the softmax attention kernels: matrix tiles of three kinds, one interface.
+// Device helpers of the softmax attention kernels: matrix tiles of three kinds, one interface; and the host's rules, which kernel and how many parts.
 //
 // A product c += x y on the matrix unit takes x as rows (a lane holds KE consecutive contraction indices of its row) and
 // y as columns, and leaves c with a column a lane and NR rows in its registers.  All kernels here are built on one fact: what a
