@@ -748,19 +748,17 @@ def adamw_create(items, bits: int, dev: int):
     weight_decay.  Returns the handle."""
     lib = _lib if _torch is not None and _lib is not None else _op_init()
     table = (AdamwTensorT * max(1, len(items)))()
+    state = _torch.float32 if bits == 32 else _torch.float8_e4m3fn
     for to, x in zip(table, items):
-        p = x["p"]
-        _, code, _ = _op_first(p, "a parameter")
-        p = p if p.dim() > 1 else p[None]
-        rows = lambda t, name, dtype: _op_rows(t if t is None or t.dim() > 1 else t[None], name, dtype, dev, (_op_count(p), p.shape[-1]))  # noqa: E731
-        R, F = _op_count(p), p.shape[-1]
-        (to.p, to.ldp), (to.g, to.ldg) = rows(p, "a parameter", p.dtype), rows(x["g"], "a gradient", p.dtype)
-        to.master, to.ldmaster = rows(x.get("master"), "a master", _torch.float32)
-        held = R * adamw_pitch(F)
-        state = _torch.float32 if bits == 32 else _torch.float8_e4m3fn
+        p, g, master = (t if t is None or t.dim() > 1 else t[None] for t in (x["p"], x["g"], x.get("master")))
+        code, dt, shape = _op_first(p, "a parameter")[1], p.dtype, (_op_count(p), p.shape[-1])
+        to.p, to.ldp = _op_rows(p, "a parameter", dt, dev, shape)
+        to.g, to.ldg = _op_rows(g, "a gradient", dt, dev, shape)
+        to.master, to.ldmaster = _op_rows(master, "a master", _torch.float32, dev, shape)
+        held = shape[0] * adamw_pitch(shape[1])
         to.m, to.v = _op_flat(x["m"], "m", held, dev, state), _op_flat(x["v"], "v", held, dev, state)
         to.m_scale, to.v_scale = (_op_flat(x.get(n), n, -(-held // 256), dev) for n in ("m_scale", "v_scale"))
-        to.R, to.F, to.dtype, to.weight_decay = R, F, code, x["weight_decay"]
+        (to.R, to.F), to.dtype, to.weight_decay = shape, code, x["weight_decay"]
     out = ct.c_void_p()
     with _torch.cuda.device(dev):
         rc = lib.dgc_adamw_create(table, len(items), int(bits), ct.byref(out))

@@ -13,6 +13,7 @@
 // that can be computed anywhere.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <utility>
 #include <vector>
@@ -328,18 +329,20 @@ dgc_status_t dgc_adamw_create(const dgc_adamw_tensor_t* tensors, int32_t n, int3
         return ops::refuse(DGC_ERR_INVALID_ARG, "adamw: parameters, masters and states lie apart from each other and the gradients");
     }
   }
+  const size_t a = sizeof(Factors) + 4 + all.size() * sizeof(Tensor), bytes = a + chunks.size() * sizeof(Chunk);
+  static_assert(sizeof(Factors) + 4 == 16 && sizeof(Tensor) % 8 == 0, "tensors follow the factors, chunks the tensors");
+  std::vector<char> image(bytes);       // what may throw comes before the handle
   dgc_adamw* h = new (std::nothrow) dgc_adamw;
   if (!h) return ops::refuse(DGC_ERR_OOM, "adamw: out of host memory");
   h->bits = bits;
   h->tensors = (int32_t)all.size();
   h->chunks = (int64_t)chunks.size();
-  const size_t a = sizeof(Factors) + 4 + all.size() * sizeof(Tensor), bytes = a + chunks.size() * sizeof(Chunk);
-  static_assert(sizeof(Factors) + 4 == 16 && sizeof(Tensor) % 8 == 0, "tensors follow the factors, chunks the tensors");
   if (h->chunks > 0) {
+    std::memcpy(image.data() + 16, all.data(), all.size() * sizeof(Tensor));
+    std::memcpy(image.data() + a, chunks.data(), chunks.size() * sizeof(Chunk));
     hipError_t err = hipGetDevice(&h->device);
     if (err == hipSuccess) err = hipMalloc(&h->memory, bytes);
-    if (err == hipSuccess) err = hipMemcpy(static_cast<char*>(h->memory) + 16, all.data(), all.size() * sizeof(Tensor), hipMemcpyHostToDevice);
-    if (err == hipSuccess) err = hipMemcpy(static_cast<char*>(h->memory) + a, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice);
+    if (err == hipSuccess) err = hipMemcpy(h->memory, image.data(), bytes, hipMemcpyHostToDevice);
     if (err != hipSuccess) {
       if (h->memory) (void)hipFree(h->memory);
       delete h;
