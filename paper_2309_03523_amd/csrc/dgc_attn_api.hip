@@ -46,8 +46,8 @@ Room back_room(int64_t Tq, int64_t Tk, int64_t N, int32_t heads, int32_t kv_head
   if (p.heads * p.rows > 1) r.joint = 8 * N * kv_heads * Tk * d * p.heads * p.rows;
   if (buckets) {
     // The larger of both row tiles' numbers of blocks.
-    r.part = 4 * (int64_t)heads * back_slots(false, N, heads, 0, (Tq + 63) / 64) * table_size(reach, causal);
-    if (window) r.part = std::max<int64_t>(r.part, 4 * (int64_t)heads * back_slots(true, N, heads, kv_heads, 0) * 64);
+    r.part = 4 * (int64_t)heads * back_slots(false, N, heads, 0, (Tq + 63) / 64, at_once(dtype == DGC_DTYPE_F32, d)) * table_size(reach, causal);
+    if (window) r.part = std::max<int64_t>(r.part, 4 * (int64_t)heads * back_slots(true, N, heads, kv_heads, 0, 0) * 64);
     if (window) {
       const WindowPlan p = plan_windows(N, heads, d, ops::elem_bytes(dtype));
       r.part = std::max<int64_t>(r.part, 4 * (int64_t)heads * p.slots * p.tables * 64);

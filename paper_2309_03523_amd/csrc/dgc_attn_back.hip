@@ -1013,7 +1013,7 @@ template <class Tl, int NT>
 void window_back(Args& a, hipStream_t st) {
   if (a.group == 1 && windows_back<Tl, NT>(a, st)) return;
   const int kvs = a.heads / a.group;
-  a.slots = back_slots(true, a.N, a.heads, kvs, 0);
+  a.slots = back_slots(true, a.N, a.heads, kvs, 0, 0);
   const unsigned grid = (unsigned)(((int64_t)a.slots * kvs + 3) / 4), lds = a.bias ? 4 * 4 * a.group * 10 * 16 * NT : 0;
   if (a.d <= 16) hipLaunchKernelGGL((k_attn_window_back<Tl, NT, 1>), grid, 256, lds, st, a);
   else if (a.d <= 32) hipLaunchKernelGGL((k_attn_window_back<Tl, NT, 2>), grid, 256, lds, st, a);
@@ -1029,7 +1029,7 @@ void long_back(Args& a, hipStream_t st) {
   const unsigned lds = bias_bytes(a);
   if (rows > 0 && (a.dq.p || a.part)) {
     const int64_t blocks = (a.Tq + 4 * M - 1) / (4 * M);
-    a.slots = a.part ? back_slots(false, a.N, a.heads, 0, blocks) : (int)(a.N * blocks);
+    a.slots = a.part ? back_slots(false, a.N, a.heads, 0, blocks, at_once(Tl::kExact, a.d)) : (int)(a.N * blocks);
     const unsigned more = a.part ? 4 * 4 * (table_size(a.reach, a.causal) + 2 * M * M) : 0;
     hipLaunchKernelGGL((k_attn_dq<Tl, KS, false>), (unsigned)(a.slots * a.heads), 256, lds + more, st, a);
     if (a.causal && a.dq.p) hipLaunchKernelGGL((k_attn_dq<Tl, KS, true>), (unsigned)(a.slots * a.heads), 256, lds, st, a);

@@ -404,9 +404,12 @@ inline bool takes_window_back(int64_t Tk, int32_t d, int32_t group, bool first) 
 constexpr int kTile = 64;
 inline __host__ __device__ int table_from(int32_t reach, int32_t causal) { return causal ? 0 : -(reach + 2 * kTile); }
 inline __host__ __device__ int table_size(int32_t reach, int32_t causal) { return reach + 2 * kTile - table_from(reach, causal); }
+// Workgroups of k_attn_dq that the card holds at a time: two a CU as bf16 tiles and wide heads need registers, three or four in fp32 (1000 x 200 tokens, 4 heads of
+// 32: 802 us with 1024, 863 with 768, 984 with 512, 845 with 4096; 16 x 1001, 8 of 64: 1107 us with 768, 1154 with 1024, 1169 with 512).
+inline int at_once(bool f32, int32_t d) { return !f32 || d > 64 ? 512 : d > 32 ? 768 : 1024; }
 // Workgroups (windows: waves) that share a head's queries where the bias' gradient is wanted: as many as the card holds at a time, each of them leaves a table.
-inline int back_slots(bool window, int64_t N, int64_t heads, int64_t kvs, int64_t blocks) {
-  const int64_t most = window ? (256 * 16 + kvs - 1) / kvs : (512 + heads - 1) / heads, all = window ? N : N * blocks;
+inline int back_slots(bool window, int64_t N, int64_t heads, int64_t kvs, int64_t blocks, int at_once) {
+  const int64_t most = window ? (256 * 16 + kvs - 1) / kvs : (at_once + heads - 1) / heads, all = window ? N : N * blocks;
   return (int)(all < most ? all : most);
 }
 // Where keys have too few workgroups to fill the card, their gradients are summed in parts: of the heads that share them first, then of the queries,
