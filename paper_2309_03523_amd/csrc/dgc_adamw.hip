@@ -3,7 +3,8 @@
 //   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- p - lr (m c1 / (sqrt(v) c2 + eps) + decay p),   c1 = 1 / (1 - b1^t),  c2 = (1 - b2^t)^-1/2
 //
 // What bounds it: memory, 28 bytes a parameter in fp32, 16.06 with bf16 parameters and gradients, fp32 masters and 8-bit states.  A wave
-// takes 256 parameters at a time, four neighbours a lane, and a workgroup 4 such blocks a wave, all loads before the first use.
+// takes 256 parameters at a time, four neighbours a lane, and a workgroup 4 such blocks a wave, all loads before the first use: 53 million
+// parameters in fp32 in 292 us, 5.1 TB/s; 99 million in the other form in 328 to 338 us, 4.8 TB/s; the 12 tensors of a small block in 5 us, a call.
 //
 // States in 8 bits: m, and r = sqrt(v), as e4m3 numbers times a power of two for each 256 of them: the least with which the largest is at most
 // 448, e4m3's largest.  A power of two makes that division exact.  The root and not v is held: it spans half the exponents, and one below the least e4m3
