@@ -484,11 +484,11 @@ __global__ __launch_bounds__(256, NT == 1 && KS < 8 ? 4 : 2) void k_attn_windows
 #pragma unroll
           for (int s = 0; s < KS; ++s) x[t] = Tl::mma(fk[t][s], fq[s], x[t]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[t][r] = fmaf(x[t][r], a.scale, b[r]);
-          if (slow || !all) {
+          for (int r = 0; r < 4; ++r) x[t][r] = b[r] == -__builtin_inff() ? b[r] : fmaf(x[t][r], a.scale, b[r]);      // chosen, not added: a product may be infinite
+          if (!all) {
             const uint32_t bits = keys >> (16 * t + 4 * sub);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[t][r] = (bits >> r & 1) && b[r] != -__builtin_inff() ? x[t][r] : -__builtin_inff();
+            for (int r = 0; r < 4; ++r) x[t][r] = bits >> r & 1 ? x[t][r] : -__builtin_inff();
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) top = fmaxf(top, x[t][r]);

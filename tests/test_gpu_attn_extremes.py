@@ -1,0 +1,36 @@
+"""Softmax attention where tokens hold numbers at the ends of their type's range: what a query does not see, and rows that are no
+tokens, reach nothing, whatever the products with them come to.
+
+Where outputs are compared bit for bit, only what must not count differs between the two calls.  Other tolerances are those of the formulas in test_gpu_attn."""
+import pytest
+
+from test_gpu_attn import _backward, _case, _forward
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", ["one product", "lowest", "highest"])
+@pytest.mark.parametrize("T", [12, 16, 30, 32, 60, 100])
+def test_products_with_later_keys_that_overflow(T, what, dtype):
+    """A finite key whose products with earlier queries are infinite, or infinities of both signs: those queries keep their bits."""
+    import torch
+    J = T - 1 - T // 4
+    c = _case(T, T, 3, 4, 16, dtype, T, kv=2 if T % 3 else 4, buckets=4, reach=8)
+    low = torch.finfo(c["k"].dtype).min
+    q, k = c["q"].clone(), c["k"].clone()
+    if what == "one product":      # of one query and one key, in a column where no other key has anything
+        q[J // 2, 1, 3] = 2.0 ** 70
+        k[..., 3] = 0.0
+    x = dict(c, q=q, k=k)
+    clean = _forward(x)
+    x["k"] = k.clone()
+    if what == "one product":
+        x["k"][J, 1, 3] = 2.0 ** 70
+    else:
+        x["k"][J, 1] = low if what == "lowest" else -low
+    o, lse = _forward(x)
+    assert torch.equal(o[:, 0], clean[0][:, 0]) and torch.equal(o[:, 2], clean[0][:, 2])
+    assert torch.isfinite(clean[0][:J]).all() and torch.equal(o[:J], clean[0][:J]) and torch.equal(lse[..., :J], clean[1][..., :J])
+    want, got = (_backward(dict(y, kw=c["kw"]), *clean) for y in (dict(c, q=q, k=k), x))      # of the same o and lse
+    assert torch.isfinite(want[0][:J]).all() and torch.equal(got[0][:J], want[0][:J])
