@@ -645,6 +645,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
             float s = 0.f;
 #pragma unroll
             for (int r = 0; r < Tl::NR; ++r) s += z[r];
+            if (PLAIN && !live) s = 0.f;       // of a row that only fills the tile up: its zeros times a key that is not finite are NaN
             if (behind) farsum += s;
             else aheadsum += s;
           } else {

@@ -4,7 +4,7 @@ tokens, reach nothing, whatever the products with them come to.
 Where outputs are compared bit for bit, only what must not count differs between the two calls.  Other tolerances are those of the formulas in test_gpu_attn."""
 import pytest
 
-from test_gpu_attn import _backward, _case, _forward
+from test_gpu_attn import _backward, _case, _forward, _join, _near, _reference
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,31 @@ def test_products_with_later_keys_that_overflow(T, what, dtype):
     assert torch.isfinite(clean[0][:J]).all() and torch.equal(o[:J], clean[0][:J]) and torch.equal(lse[..., :J], clean[1][..., :J])
     want, got = (_backward(dict(y, kw=c["kw"]), *clean) for y in (dict(c, q=q, k=k), x))      # of the same o and lse
     assert torch.isfinite(want[0][:J]).all() and torch.equal(got[0][:J], want[0][:J])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [16, 30, 60, 100, 150, 200])
+def test_a_key_of_weight_zero_that_is_not_finite(T, dtype, causal):
+    """Scores of -inf with a key that is -inf where all queries are positive: the queries' gradients and the bias' are those without that key.  Rows
+    that only fill a tile up have no part in it."""
+    import torch
+    J = 5
+    c = _case(T, T, 3, 2, 16, dtype, T, buckets=4, reach=4, causal=causal)
+    c["q"] = c["q"].clone()
+    c["q"][..., 3] = c["q"][..., 3].abs() + 0.125
+    c["q"][..., 16 + 3] = c["q"][..., 16 + 3].abs() + 0.125
+    x = dict(c, k=c["k"].clone())
+    x["k"][J, :, 3] = x["k"][J, :, 16 + 3] = -float("inf")
+    keep = torch.ones(T, 3, dtype=torch.uint8, device="cuda")
+    keep[J] = 0
+    without = dict(c, kw=dict(c["kw"], keep=keep))
+    o, lse = _forward(x)
+    (O, to), (L, tl), _ = _reference(without)
+    _near(o, _join(O), _join(to), "o")
+    _near(lse, L, tl, "lse")
+    dq, _, _, db = _backward(x, o, lse)
+    wants = _reference(without, o, lse)
+    other = [e for e in range(32) if e % 16 != 3]
+    _near(dq[..., other], _join(wants[0][0])[..., other], _join(wants[0][1])[..., other], "dq")      # in column 3 a zero meets the infinity
+    _near(db, *wants[3], "dbias")
