@@ -249,7 +249,8 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
     }
     begun = true;
     if (q.lo >= q.hi) continue;
-    const bool there = lane < q.len && (!a.keep || a.keep[(int64_t)lane * a.N + n]);
+    // A key behind every query counts as masked, whatever it holds.
+    const bool there = lane < q.len && (!a.causal || lane < q.at + q.hi) && (!a.keep || a.keep[(int64_t)lane * a.N + n]);
     const uint64_t keys = __ballot(there);
     Frag fk[NT][KS];
     bool bad = false;

@@ -734,7 +734,8 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     return;
   }
   const int mine = k0 + wave * M, j = mine + col;
-  const bool there = j < q.len && (!a.keep || a.keep[(int64_t)j * a.N + n]);
+  // A key behind every query counts as masked, whatever it holds.
+  const bool there = j < q.len && (!a.causal || j < q.at + q.hi) && (!a.keep || a.keep[(int64_t)j * a.N + n]);
   const BiasTable bt(a);
   const float* const mytable = table - j - bt.from + 4 * sub;      // plus a query's position
   typename Tl::Frag fk[KS], fv[KS];
@@ -749,6 +750,11 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       fv[s] = ok ? *reinterpret_cast<const typename Tl::Frag*>(vrow + c) : Tl::zero();
     }
   }
+  // Rows that are no queries are zeros here, which times a key or value that is not finite are NaN: where a wave has one, such rows are left out one by one.
+  bool odd_keys = false;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) odd_keys = odd_keys || Tl::odd(fk[s]) || Tl::odd(fv[s]);
+  odd_keys = __any(odd_keys);
   typename Tl::Acc dk[DT], dv[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = (typename Tl::Acc)(0.f);
@@ -864,6 +870,14 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
               const float4 u = *reinterpret_cast<const float4*>(stats[buf][0] + t * M + 4 * sub + Tl::row(r));
               x[r] -= u.x; x[r + 1] -= u.y; x[r + 2] -= u.z; x[r + 3] -= u.w;
             }
+            if (odd_keys) {
+#pragma unroll
+              for (int r = 0; r < Tl::NR; ++r) {
+                const bool none = stats[buf][0][t * M + 4 * sub + Tl::row(r)] == __builtin_inff();
+                x[r] = none ? -__builtin_inff() : x[r];
+                z[r] = none ? 0.f : z[r];
+              }
+            }
           }
           const int least = a.causal ? j - pt - 4 * sub : -1;
 #pragma unroll
@@ -903,7 +917,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       if (next) fetch(i0 + kRows);
       if (i0 >= from_i) {
         const float mylse = stats[buf][0][lane % kRows];
-        const bool exact = !started || __any(mylse < __builtin_inff() && far_off(mylse));
+        const bool exact = !started || odd_keys || __any(mylse < __builtin_inff() && far_off(mylse));
         if (!SEEN && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), i0, buf, false, false);
         else tile(std::false_type(), i0, buf, exact, odd);
       }

@@ -62,3 +62,48 @@ def test_a_key_of_weight_zero_that_is_not_finite(T, dtype, causal):
     other = [e for e in range(32) if e % 16 != 3]
     _near(dq[..., other], _join(wants[0][0])[..., other], _join(wants[0][1])[..., other], "dq")      # in column 3 a zero meets the infinity
     _near(db, *wants[3], "dbias")
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [16, 30, 60, 100, 150, 200])
+def test_gradients_of_a_key_of_weight_zero_that_is_not_finite(T, dtype, causal):
+    """The same: its own are zero, the other keys' those without it."""
+    import torch
+    J = 5
+    c = _case(T, T, 3, 2, 16, dtype, T, buckets=4, reach=4, causal=causal)
+    c["q"] = c["q"].clone()
+    c["q"][..., 3] = c["q"][..., 3].abs() + 0.125
+    c["q"][..., 16 + 3] = c["q"][..., 16 + 3].abs() + 0.125
+    x = dict(c, k=c["k"].clone())
+    x["k"][J, :, 3] = x["k"][J, :, 16 + 3] = -float("inf")
+    keep = torch.ones(T, 3, dtype=torch.uint8, device="cuda")
+    keep[J] = 0
+    without = dict(c, kw=dict(c["kw"], keep=keep))
+    o, lse = _forward(x)
+    _, dk, dv, _ = _backward(x, o, lse)
+    wants = _reference(without, o, lse)
+    for got, (want, tol), name in ((dk, wants[1], "dk"), (dv, wants[2], "dv")):
+        _near(got, _join(want), _join(tol), name)
+    assert bool((dk[J] == 0).all()) and bool((dv[J] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("Tq,Tk", [(20, 30), (40, 60), (70, 100), (5, 100), (1, 90), (130, 200), (600, 700)])
+def test_keys_behind_every_query(Tq, Tk, value, dtype):
+    """A cache's rows that are not filled yet, with nothing but positions to mask them: no query sees them, their gradients are zero."""
+    import torch
+    c = _case(Tq, Tk, 2, 4, 16, dtype, Tk, kv=2, buckets=4, reach=8)
+    first = (Tk - Tq) // 2
+    c["kw"]["first"] = torch.tensor([first, 0], dtype=torch.int32, device="cuda")
+    seen = torch.stack([torch.arange(Tk, device="cuda") < f + Tq for f in (first, 0)], 1)[..., None]
+    got = []
+    for fill in (0.0, value):
+        x = dict(c, k=torch.where(seen, c["k"], fill).to(c["k"].dtype), v=torch.where(seen, c["v"], fill).to(c["v"].dtype))
+        o, lse = _forward(x)
+        got.append((o, lse, *_backward(x, o, lse)))
+    for name, a, b in zip(("o", "lse", "dq", "dk", "dv", "dbias"), *got):
+        assert torch.isfinite(a).all() and torch.equal(a, b), name
+    for g in got[1][3:5]:
+        assert bool((torch.where(seen, 0, g) == 0).all())
