@@ -160,7 +160,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
     const float off = top == -__builtin_inff() ? 0.f : top;        // no key seen so far: all terms are zero
     const float f = exp2_((m - off) * kLog2e);
     m = top;
-    if (PLAIN) {
+    if (PLAIN && __any(far_off(off))) {      // so large that the multiply-add below could leave exponents far above 0
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int r = 0; r < Tl::NR; ++r) x[t][r] = exp2_((fmaf(x[t][r], mult, add) - off) * kLog2e);
+      }
+    } else if (PLAIN) {
       mult *= kLog2e;
       add = (add - off) * kLog2e;
 #pragma unroll

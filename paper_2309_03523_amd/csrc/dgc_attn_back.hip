@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
     const float given = row ? a.lse[stat] : -__builtin_inff();
     const bool live = given != -__builtin_inff();
     const float lse = live ? given : __builtin_inff();       // of a query without gradients: all weights are zero
-    const bool clean = !SEEN && !Tl::kExact && !__any(row && !live);
+    const bool clean = !SEEN && !Tl::kExact && !__any(row && (!live || far_off(lse)));
     const bool some = max(mine, q.lo) < min(mine + M, q.hi);
     const int p0 = some ? (int)(q.at + max(mine, q.lo)) : -1, p1 = some ? (int)(q.at + min(mine + M, q.hi) - 1) : -1, p = live ? (int)(q.at + i) : -1;
     const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place

@@ -52,7 +52,8 @@ struct Args {
 };
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, 0 for -inf
-// Biases, and statistics, of the type's lowest value or near it: scores have no bits left beside them, and are to lose them everywhere.
+// Biases and statistics of the type's lowest value or near it: scores have no bits left beside them, and are to lose them everywhere.  The same of large
+// scores: (s - off) log2e by one multiply-add is off by 2^-22 of off, here 0.25, and by more than fp32 has exponents from 10^9 on.
 __device__ __forceinline__ bool far_off(float off) { return fabsf(off) > 1048576.f; }
 // e^(x - off); off is a maximum, -inf if there is nothing.
 __device__ __forceinline__ float weight_of(float x, float off) { return exp2_((x - (off == -__builtin_inff() ? 0.f : off)) * kLog2e); }

@@ -1,10 +1,10 @@
 """Softmax attention where tokens hold numbers at the ends of their type's range: what a query does not see, and rows that are no
-tokens, reach nothing, whatever the products with them come to.
+tokens, reach nothing, whatever the products with them come to; scores of any size that fp32 holds have weights.
 
 Where outputs are compared bit for bit, only what must not count differs between the two calls.  Other tolerances are those of the formulas in test_gpu_attn."""
 import pytest
 
-from test_gpu_attn import _backward, _case, _forward, _join, _near, _reference
+from test_gpu_attn import HALF, _backward, _case, _forward, _join, _near, _reference
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,34 @@ def test_keys_behind_every_query(Tq, Tk, value, dtype):
         assert torch.isfinite(a).all() and torch.equal(a, b), name
     for g in got[1][3:5]:
         assert bool((torch.where(seen, 0, g) == 0).all())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e6, 1e10, 1e17])
+@pytest.mark.parametrize("Tq,Tk", [(16, 16), (30, 30), (60, 60), (1, 300), (8, 300), (150, 150), (300, 300)])
+def test_scores_far_beyond_what_a_weight_can_tell(Tq, Tk, size, dtype, causal):
+    """Scores of up to `size`, whole multiples of a step beside which biases are nothing, no two alike: the largest takes all.  Two columns hold a score's
+    digits, so products and their sums are exact.  o: the weight's rounding and o's own, each half a step of the type, and fp32's.  lse: the
+    largest score rounded once, and the logarithm of its weight, whose exponent is off by three roundings of the score."""
+    import math
+    import torch
+    c = _case(Tq, Tk, 2, 2, 32, dtype, 5, causal=causal, buckets=4, reach=4)
+    c["kw"]["scale"] = 1.0
+    g = torch.Generator(device="cuda").manual_seed(3)
+    step = 2.0 ** round(math.log2(size / Tk))
+    k, q = torch.zeros_like(c["k"]), torch.zeros_like(c["q"])
+    for n in range(2):
+        for h in range(2):
+            rank = torch.randperm(Tk, generator=g, device="cuda")
+            k[:, n, h * 32 + 7], k[:, n, h * 32 + 20] = (rank // 128 * 128 * step).to(k.dtype), (rank % 128 * step).to(k.dtype)
+            sign = torch.where(torch.rand(Tq, generator=g, device="cuda") < 0.5, 1.0, -1.0).to(q.dtype)
+            q[:, n, h * 32 + 7] = q[:, n, h * 32 + 20] = sign
+    c.update(q=q, k=k)
+    o, lse = _forward(c)
+    (O, _), (L, _), _ = _reference(c)
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+    assert float((o.double() - _join(O)).abs().max()) <= (2.02 * HALF[dtype] + 2.0 ** -20) * float(c["v"].double().abs().max())
+    assert bool(((lse.double() - L).abs() <= 2.0 ** -22 * L.abs() + 2.0 ** -20).all())
+    for x in _backward(c, o, lse):
+        assert torch.isfinite(x).all()
