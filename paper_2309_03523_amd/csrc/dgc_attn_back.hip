@@ -718,6 +718,25 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
 }
 
 // ---------------------------------------------------------------------------------------------------- dk, dv
+
+// Whether a lane's part of a key or value is not finite: the largest of the numbers without their signs tells.
+template <class Tl, int KS>
+__device__ __forceinline__ bool odd_rows(const typename Tl::Frag (&a)[KS], const typename Tl::Frag (&b)[KS]) {
+  constexpr bool BF16 = sizeof(typename Tl::E) == 2;
+  uint32_t most = 0;
+  auto add = [&](uint32_t w) __attribute__((always_inline)) {
+    typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+    if (BF16) most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushortx2, most), __builtin_bit_cast(ushortx2, w & 0x7fff7fffu)));
+    else most = max(most, w & 0x7fffffffu);
+  };
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    add(a[s].x), add(a[s].y), add(a[s].z), add(a[s].w);
+    add(b[s].x), add(b[s].y), add(b[s].z), add(b[s].w);
+  }
+  return BF16 ? (most & 0xffffu) >= 0x7f80u || (most >> 16) >= 0x7f80u : most >= 0x7f800000u;
+}
+
 //
 // A workgroup takes 4 M keys of one sequence and key head, a wave M of them in registers, and walks over the queries that see them in tiles of
 // 2 M that lie in LDS, for one head that shares the keys after the other.  The products that form scores and dP start from -lse / scale and -D of
@@ -756,11 +775,6 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       fv[s] = ok ? *reinterpret_cast<const typename Tl::Frag*>(vrow + c) : Tl::zero();
     }
   }
-  // Rows that are no queries are zeros here, which times a key or value that is not finite are NaN: where a wave has one, such rows are left out one by one.
-  bool odd_keys = false;
-#pragma unroll
-  for (int s = 0; s < KS; ++s) odd_keys = odd_keys || Tl::odd(fk[s]) || Tl::odd(fv[s]);
-  odd_keys = __any(odd_keys);
   typename Tl::Acc dk[DT], dv[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = (typename Tl::Acc)(0.f);
@@ -826,7 +840,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
     };
     // One tile.  PLAIN: all its queries see all of the wave's keys, with one bias.
     float bias_behind = 0.f, bias_ahead = 0.f;
-    auto tile = [&](auto plain, int i0, int buf, bool exact, bool odd) __attribute__((always_inline)) {
+    auto tile = [&](auto plain, int i0, int buf, bool exact, bool odd, bool dead) __attribute__((always_inline)) {
       constexpr bool PLAIN = decltype(plain)::value;
       const E *sq = room[buf], *sg = sq + kRows * P;
       const int first_p = (int)(q.at + i0);
@@ -876,7 +890,7 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
               const float4 u = *reinterpret_cast<const float4*>(stats[buf][0] + t * M + 4 * sub + Tl::row(r));
               x[r] -= u.x; x[r + 1] -= u.y; x[r + 2] -= u.z; x[r + 3] -= u.w;
             }
-            if (odd_keys) {
+            if (dead) {
 #pragma unroll
               for (int r = 0; r < Tl::NR; ++r) {
                 const bool none = stats[buf][0][t * M + 4 * sub + Tl::row(r)] == __builtin_inff();
@@ -923,9 +937,11 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       if (next) fetch(i0 + kRows);
       if (i0 >= from_i) {
         const float mylse = stats[buf][0][lane % kRows];
-        const bool exact = !started || odd_keys || __any(mylse < __builtin_inff() && far_off(mylse));
-        if (!SEEN && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), i0, buf, false, false);
-        else tile(std::false_type(), i0, buf, exact, odd);
+        // Rows that are no queries are zeros, which times a key or value that is not finite are NaN: they are left out one by one.
+        const bool dead = __any(mylse == __builtin_inff()) && __any(odd_rows<Tl, KS>(fk, fv));
+        const bool exact = !started || dead || __any(mylse < __builtin_inff() && far_off(mylse));
+        if (!SEEN && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), i0, buf, false, false, false);
+        else tile(std::false_type(), i0, buf, exact, odd, dead);
       }
       if (next) odd = put(i0 + kRows, buf ^ 1), odds |= odd;
     }
