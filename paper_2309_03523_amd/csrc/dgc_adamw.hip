@@ -237,6 +237,7 @@ __global__ __launch_bounds__(256) void k_adamw(StepArgs a) {
 __global__ void k_adamw_count(int64_t* steps, const float* lr_at, float lr, double b1, double b2, Factors* to) {
   const int64_t t = *steps + 1;
   *steps = t;
+  if (!to) return;      // nothing to step: it counts all the same
   to->lr = lr_at ? *lr_at : lr;
   to->c1 = (float)(1. / (1. - pow(b1, (double)t)));
   to->c2 = (float)(1. / sqrt(1. - pow(b2, (double)t)));
@@ -374,7 +375,11 @@ dgc_status_t dgc_adamw_step(dgc_adamw_t* h, double lr, double beta1, double beta
   if (lr_at && !steps) return ops::refuse(DGC_ERR_INVALID_ARG, "adamw: lr on the device goes with steps on the device");
   if (((uintptr_t)steps & 7) || ((uintptr_t)lr_at & 3)) return ops::refuse(DGC_ERR_INVALID_ARG, "adamw: steps needs 8-byte and lr 4-byte alignment");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (h->chunks == 0) return DGC_OK;
+  if (h->chunks == 0) {
+    if (!steps) return DGC_OK;
+    hipLaunchKernelGGL(k_adamw_count, 1, 1, 0, st, steps, lr_at, (float)lr, beta1, beta2, static_cast<Factors*>(nullptr));
+    return ops::launched("adamw");
+  }
   int device = -1;
   if (hipGetDevice(&device) != hipSuccess || device != h->device) return ops::refuse(DGC_ERR_INVALID_ARG, "adamw: another device is current than the handle's");
   char* const mem = static_cast<char*>(h->memory);
