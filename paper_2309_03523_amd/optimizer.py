@@ -27,7 +27,9 @@ class AdamW:
         import torch
         params, grads = list(params), list(grads)
         n = len(params)
-        if n == 0 or len(grads) != n or (isinstance(masters, (list, tuple)) and len(masters) != n) or (states is not None and len(states) != n):
+        if masters is not None and not isinstance(masters, bool):
+            masters = list(masters)
+        if n == 0 or len(grads) != n or (isinstance(masters, list) and len(masters) != n) or (states is not None and len(states) != n):
             raise ValueError("params must not be empty; grads, masters and states go with them, one each")
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
@@ -49,7 +51,7 @@ class AdamW:
         with torch.cuda.device(dev):
             if masters is True:
                 masters = [self._copied(p) if p.dtype == torch.bfloat16 else None for p in params]
-            self.masters = list(masters) if masters is not None else [None] * n
+            self.masters = masters or [None] * n
             self.states = [dict(s) for s in states] if states is not None else [self._state(p) for p in params]
             if on_device:
                 self._at, self._lr_at = torch.full((1,), self._steps, dtype=torch.int64, device=dev), torch.full((1,), self.lr, device=dev)
