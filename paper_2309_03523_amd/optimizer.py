@@ -18,7 +18,7 @@ class AdamW:
     tensor: m, v and, with bits=8, m_scale, v_scale; rows at binding.adamw_pitch(F) places, 8-bit ones as float8_e4m3fn.
 
     on_device=True keeps the number of steps and the learning rate on the device, so that a step that is captured into a graph counts, and takes the rate
-    of set_lr, when it is replayed.  The optimizer keeps its tensors and their addresses: writing new values into them is seen, putting other
+    of set_lr, when it is replayed; without it a step is not captured.  The optimizer keeps its tensors and their addresses: writing new values into them is seen, putting other
     tensors in their place is not.  After parameters that have masters were set from outside, call reload().  It runs one call at a time: a step only enqueues, the
     constructor, release(), reload() and the number of steps on the device wait for the device."""
 
@@ -88,10 +88,20 @@ class AdamW:
         """One step from the gradients as they are when it runs."""
         if self._handle is None:
             raise RuntimeError("the optimizer was released")
+        if self._at is None and self._capturing(stream):
+            raise RuntimeError("a captured step counts on the device: make the optimizer with on_device=True")
         t = self._steps + 1
         binding.adamw_step(self._handle, self.device.index, t, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps, steps=self._at,
                            lr_at=self._lr_at, stream=stream)
         self._steps = t
+
+    def _capturing(self, stream) -> bool:
+        """Whether the call's stream is being captured."""
+        import torch
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):      # None: the device's current one
+            return torch.cuda.is_current_stream_capturing()
 
     def set_lr(self, lr: float, *, stream=None):
         """The learning rate of the steps from here on; with on_device it is enqueued."""

@@ -22,3 +22,26 @@ def test_steps_of_empty_tensors_count(shape, bits):
     for t in (7, 8, 9):
         graph.replay()
         assert there.steps == t
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_a_step_that_the_host_counts_is_not_captured(given):
+    """Its number would be that of the capture in every replay."""
+    import torch
+    from paper_2309_03523_amd.optimizer import AdamW
+    p, g = torch.ones(4, 16, device="cuda"), torch.ones(4, 16, device="cuda")
+    opt = AdamW([p], [g])
+    opt.step()
+    torch.cuda.synchronize()
+    before, graph, s = p.clone(), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=s):
+        p.mul_(2)
+        with pytest.raises(RuntimeError, match="on_device"):
+            opt.step(stream=s if given else None)
+    assert opt.steps == 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(p, 2 * before)
+    opt.step(stream=s if given else None)      # outside the capture it goes on
+    torch.cuda.synchronize()
+    assert opt.steps == 2 and bool((p < 2 * before).all())
