@@ -439,11 +439,13 @@ def chunk_generate(rowptr, colidx, N: int, *, w_s: int, w_t: int, cap: int, max_
 _torch = None
 _raw_stream = None      # device index -> the current stream's handle
 _device = None          # () -> the current device's index
+_capturing = None       # () -> whether the current stream is being captured
 
 
 def _op_init():
-    global _torch, _raw_stream, _device
+    global _torch, _raw_stream, _device, _capturing
     import torch
+    _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
     _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     _torch = torch
@@ -777,5 +779,18 @@ def adamw_destroy(handle):
 
 
 def adamw_step(handle, dev: int, t: int, *, lr: float, beta1: float, beta2: float, eps: float, steps=None, lr_at=None, stream=None):
-    """dgc_adamw_step: step number t, or with `steps` (int64 [1] on the device, raised by one) the next one; lr_at fp32 [1] on the device, read for lr."""
-    _op_call(_lib.dgc_adamw_step, dev, stream, handle, lr, beta1, beta2, eps, t, _op_flat(steps, "steps", 1, dev, _torch.int64), _op_flat(lr_at, "lr", 1, dev))
+    """dgc_adamw_step: step number t, or with `steps` (int64 [1] on the device, raised by one) the next one; lr_at fp32 [1] on the device, read for lr.
+    A step that is captured needs `steps`: every replay of another would have the number t."""
+    if stream is not None and stream.device.index != dev:
+        raise ValueError("stream belongs to another device than the tensors")
+    if stream is not None or _device() != dev:
+        with _torch.cuda.device(dev), _torch.cuda.stream(stream):
+            return adamw_step(handle, dev, t, lr=lr, beta1=beta1, beta2=beta2, eps=eps, steps=steps, lr_at=lr_at)
+    if steps is None:
+        if _capturing():
+            raise RuntimeError("a captured step counts on the device: it needs `steps` (AdamW: on_device=True)")
+        rc = _lib.dgc_adamw_step(handle, lr, beta1, beta2, eps, t, None, None, _raw_stream(dev))
+    else:
+        rc = _lib.dgc_adamw_step(handle, lr, beta1, beta2, eps, t, _op_flat(steps, "steps", 1, dev, _torch.int64), _op_flat(lr_at, "lr", 1, dev), _raw_stream(dev))
+    if rc:
+        raise DgcError(rc, _lib.dgc_last_error(None).decode())

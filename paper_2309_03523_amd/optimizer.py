@@ -88,20 +88,10 @@ class AdamW:
         """One step from the gradients as they are when it runs."""
         if self._handle is None:
             raise RuntimeError("the optimizer was released")
-        if self._at is None and self._capturing(stream):
-            raise RuntimeError("a captured step counts on the device: make the optimizer with on_device=True")
         t = self._steps + 1
         binding.adamw_step(self._handle, self.device.index, t, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps, steps=self._at,
                            lr_at=self._lr_at, stream=stream)
         self._steps = t
-
-    def _capturing(self, stream) -> bool:
-        """Whether the call's stream is being captured."""
-        import torch
-        if stream is None and torch.cuda.current_device() == self.device.index:
-            return torch.cuda.is_current_stream_capturing()
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):      # None: the device's current one
-            return torch.cuda.is_current_stream_capturing()
 
     def set_lr(self, lr: float, *, stream=None):
         """The learning rate of the steps from here on; with on_device it is enqueued."""
