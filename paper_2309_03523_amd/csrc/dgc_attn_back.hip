@@ -495,9 +495,10 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 // ---------------------------------------------------------------------------------------------------- dq, and the bias' gradient
 //
 // Four sequences of 4096, 8 heads of 64 on 2 key heads, bf16: 0.19 ms, and k_attn_dkv 0.25.  Both are bound by how long a wave's chain LDS, products, powers, products
-// takes with two waves a SIMD.  As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  In fp32 the product that forms dP starts from -D, so it
-// leaves dP - D.  In bf16 D is subtracted behind it: that unit cuts sums off, always to one side, which of sums that start from -D the bias' gradient, where
-// millions of them nearly cancel, sums up (4000 x 200 tokens, 4 heads of 32: off by 5.5e-6 of its norm, now 5e-7; times unchanged, 5 % less with heads of 128).
+// takes with two waves a SIMD.  As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it
+// leaves dP - D; in bf16, where the bias' gradient is wanted, D is subtracted behind it: that unit cuts sums off, always to one side, and what it leaves of -D is summed up by the
+// bias' gradient, where millions of dS nearly cancel (4000 x 200 tokens, 4 heads of 32: off by 5.5e-6 of its norm, now 5e-7, at 1 % of the call).  Heads above 64 always do so:
+// one number for a tile of them leaves registers (2 x 4096, 8 heads of 128: 62 spilled and 640 us for all gradients, 41 and 603 us now).
 // Where a zero gradient would meet a key that is not finite, this kernel leaves dq to the same one with SEEN, which is launched behind it and takes
 // such items alone: with both in one kernel the registers do not do.
 template <class Tl, int KS, bool SEEN>
@@ -558,6 +559,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
     const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place
     typename Tl::Frag fq[KS], fg[KS];
     const float minus_D = live ? -a.delta[stat] : 0.f;
+    const bool behind_D = !SEEN && !Tl::kExact && (KS >= 8 || a.part);
     {
       const E* qrow = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
       const E* grow = static_cast<const E*>(a.go.p) + (int64_t)i * a.go.st + n * a.go.sn + h * a.d;
@@ -616,13 +618,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
       for (int t = 0; t < NT; ++t) {
         const int first = j0 + t * M;
         if (!PLAIN && (first >= kend || (a.causal && first > p1))) break;
-        typename Tl::Acc x = (typename Tl::Acc)(0.f), z = (typename Tl::Acc)(Tl::kExact ? minus_D : 0.f);
+        typename Tl::Acc x = (typename Tl::Acc)(0.f), z = (typename Tl::Acc)(behind_D ? 0.f : minus_D);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           x = Tl::mma(Tl::rows(sk + t * M * P, P, s, lane), fq[s], x);
           z = Tl::mma(Tl::rows(sv + t * M * P, P, s, lane), fg[s], z);
         }
-        if constexpr (!Tl::kExact) {
+        if (behind_D) {
 #pragma unroll
           for (int r = 0; r < Tl::NR; ++r) z[r] += minus_D;
         }
@@ -719,22 +721,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
 
 // ---------------------------------------------------------------------------------------------------- dk, dv
 
-// Whether a lane's part of a key or value is not finite: the largest of the numbers without their signs tells.
+// Whether a lane's part of a key or value is not finite: its sum of zero times each number tells.
 template <class Tl, int KS>
 __device__ __forceinline__ bool odd_rows(const typename Tl::Frag (&a)[KS], const typename Tl::Frag (&b)[KS]) {
-  constexpr bool BF16 = sizeof(typename Tl::E) == 2;
-  uint32_t most = 0;
+  float sum = 0.f;
   auto add = [&](uint32_t w) __attribute__((always_inline)) {
-    typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
-    if (BF16) most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushortx2, most), __builtin_bit_cast(ushortx2, w & 0x7fff7fffu)));
-    else most = max(most, w & 0x7fffffffu);
+    if constexpr (sizeof(typename Tl::E) == 2) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{0, 0}, sum, false);
+    else sum = fmaf(__uint_as_float(w), 0.f, sum);
   };
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     add(a[s].x), add(a[s].y), add(a[s].z), add(a[s].w);
     add(b[s].x), add(b[s].y), add(b[s].z), add(b[s].w);
   }
-  return BF16 ? (most & 0xffffu) >= 0x7f80u || (most >> 16) >= 0x7f80u : most >= 0x7f800000u;
+  return sum != sum;
 }
 
 //
@@ -743,7 +743,7 @@ __device__ __forceinline__ bool odd_rows(const typename Tl::Frag (&a)[KS], const
 // their rows, which come from LDS as four numbers at a time: they leave (s - lse) / scale and dP - D.
 // Queries that are not finite: as in k_attn_dq.
 template <class Tl, int KS, bool SEEN>
-__global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args a) {
+__global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : SEEN && Tl::M == 32 && KS <= 2 ? 3 : 2) void k_attn_dkv(Args a) {
   typedef typename Tl::E E;
   constexpr int M = Tl::M, NT = M == 32 && KS >= 4 ? 1 : 2, kRows = NT * M, DT = Geometry<Tl, KS>::DT, P = Geometry<Tl, KS>::P;
   __shared__ __attribute__((aligned(16))) E room[2][2 * kRows * P];
@@ -937,9 +937,12 @@ __global__ __launch_bounds__(256, KS * Tl::M > 128 ? 1 : 2) void k_attn_dkv(Args
       if (next) fetch(i0 + kRows);
       if (i0 >= from_i) {
         const float mylse = stats[buf][0][lane % kRows];
-        // Rows that are no queries are zeros, which times a key or value that is not finite are NaN: they are left out one by one.
-        const bool dead = __any(mylse == __builtin_inff()) && __any(odd_rows<Tl, KS>(fk, fv));
-        const bool exact = !started || dead || __any(mylse < __builtin_inff() && far_off(mylse));
+        bool exact = !started, dead = false;
+        if (__any(far_off(mylse))) {       // a statistic far off, or a row without one
+          // Rows that are no queries are zeros, which times a key or value that is not finite are NaN: they are left out one by one.
+          dead = __any(mylse == __builtin_inff()) && __any(odd_rows<Tl, KS>(fk, fv));
+          exact = exact || dead || __any(mylse < __builtin_inff() && far_off(mylse));
+        }
         if (!SEEN && !exact && (i0 >= plain_from || i0 <= plain_to)) tile(std::true_type(), i0, buf, false, false, false);
         else tile(std::false_type(), i0, buf, exact, odd, dead);
       }
