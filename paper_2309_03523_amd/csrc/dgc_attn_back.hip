@@ -496,9 +496,9 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 //
 // Four sequences of 4096, 8 heads of 64 on 2 key heads, bf16: 0.19 ms, and k_attn_dkv 0.25.  Both are bound by how long a wave's chain LDS, products, powers, products
 // takes with two waves a SIMD.  As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it
-// leaves dP - D; in bf16, where the bias' gradient is wanted, D is subtracted behind it: that unit cuts sums off, always to one side, and what it leaves of -D is summed up by the
-// bias' gradient, where millions of dS nearly cancel (4000 x 200 tokens, 4 heads of 32: off by 5.5e-6 of its norm, now 5e-7, at 1 % of the call).  Heads above 64 always do so:
-// one number for a tile of them leaves registers (2 x 4096, 8 heads of 128: 62 spilled and 640 us for all gradients, 41 and 603 us now).
+// leaves dP - D; in bf16 D is subtracted behind it: that unit cuts sums off, always to one side, and what it leaves of -D is summed up by the bias' gradient, where
+// millions of dS nearly cancel (4000 x 200 tokens, 4 heads of 32: off by 5.5e-6 of its norm, now 5e-7).  It costs 2 to 4 % of this kernel, and leaves registers to heads above
+// 64 (2 x 4096, 8 heads of 128: 62 spilled and 640 us for all gradients, 41 and 603 us now).
 // Where a zero gradient would meet a key that is not finite, this kernel leaves dq to the same one with SEEN, which is launched behind it and takes
 // such items alone: with both in one kernel the registers do not do.
 template <class Tl, int KS, bool SEEN>
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(Args a) {
     const float* const mytable = table + (a.reach + kPast) - (live ? p : p0) + 4 * sub;      // plus a key's place
     typename Tl::Frag fq[KS], fg[KS];
     const float minus_D = live ? -a.delta[stat] : 0.f;
-    const bool behind_D = !SEEN && !Tl::kExact && (KS >= 8 || a.part);
+    constexpr bool behind_D = !SEEN && !Tl::kExact;      // a branch on a.part instead led the compiler to copy dq behind the loop 5 instructions after the product that forms it, of 11 to wait for
     {
       const E* qrow = static_cast<const E*>(a.q.p) + (int64_t)i * a.q.st + n * a.q.sn + h * a.d;
       const E* grow = static_cast<const E*>(a.go.p) + (int64_t)i * a.go.st + n * a.go.sn + h * a.d;
