@@ -535,7 +535,7 @@ dgc_status_t dgc_decay_attn_backward(const void* q, int64_t q_stride_t, int64_t 
  * over the keys that it sees: j < lengths[n] (NULL: Tk; clamped to [0, Tk]), keep[j][n] not 0, and with `causal` j <= p.
  *  Queries whose position is not in [0, lengths[n]), and keys from lengths[n] on, belong to no token: what their rows hold does not count, and
  *   their rows and entries of lse are not written.  A query that sees no key, or only scores of -inf, has o = 0 and lse = -inf, and gives and has no gradient.
- *   Keys that keep masks get gradients of 0.  What a masked row holds, infinities and NaN included, reaches nothing.
+ *   Keys that keep masks, or that lie behind every query with `causal`, get gradients of 0.  What a masked row holds, infinities and NaN included, reaches nothing.
  *  q, o [heads][d], k, v [kv_heads][d] a row: row (t, n) at base + t * stride_t + n * stride_n elements (both multiples of 16 bytes, bases aligned to
  *   16).  Inputs may repeat rows (a stride of 0); an output's rows lie apart, and outputs lie apart from inputs and each other
  *   (side by side in rows of one buffer is apart).
@@ -548,7 +548,7 @@ dgc_status_t dgc_decay_attn_backward(const void* q, int64_t q_stride_t, int64_t 
  *   o and lse as the forward pass left them.
  *  workspace: dgc_attn_workspace_bytes bytes (negative for sizes outside the range; `backward` 0 or 1: which call they are for).
  *  DGC_ERR_UNSUPPORTED for about 2^24 and more sequences x heads x blocks of 64 tokens.
- * Scores, weights, their sums and the gradients of scores are fp32; with bf16, weights and gradients of scores are rounded to bf16 (2^-9 of themselves) for the
+ * Scores, weights, their sums and the gradients of scores are fp32; with bf16, weights and gradients of scores are rounded to bf16 (by up to 2^-8 of themselves) for the
  * products that sum them, o and the gradients are rounded once more, and dbias is summed from what is not rounded.  With fp32 all is as exact as fp32 arithmetic.
  *
  * dgc_attn_buckets (host arithmetic) fills a map of the usual kind: of the buckets (causal), or of half of them a side (then even; keys

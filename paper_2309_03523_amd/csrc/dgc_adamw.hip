@@ -4,11 +4,12 @@
 //
 // What bounds it: memory, 28 bytes a parameter in fp32, 16.06 with bf16 parameters and gradients, fp32 masters and 8-bit states.  A wave
 // takes 256 parameters at a time, four neighbours a lane, and a workgroup 4 such blocks a wave, all loads before the first use: 53 million
-// parameters in fp32 in 292 us, 5.1 TB/s; 99 million in the other form in 328 to 338 us, 4.8 TB/s; the 12 tensors of a small block in 5 us, a call.
+// parameters in fp32 in 292 us, 5.1 TB/s; 99 million in the other form in 328 to 338 us, 4.8 TB/s (a card's first 40 passes take 340 to 440); the 12 tensors of a small block in 5 us, a call.
 //
 // States in 8 bits: m, and r = sqrt(v), as e4m3 numbers times a power of two for each 256 of them: the least with which the largest is at most
 // 448, e4m3's largest.  A power of two makes that division exact.  The root and not v is held: it spans half the exponents, and one below the least e4m3
-// number is raised to it, so no step divides by a root that was lost.  A number is off by at most 2^-4 of itself, or 2^-10 of the scale; that is
+// number is raised to it, so no step divides by a root that was lost.  A number is off by at most 2^-4 of itself, or 2^-10 of the scale, a root that is
+// raised by up to 2^-9 of the scale; that is
 // what 8 bits hold, and the step itself is taken with the states before they are rounded.
 // All arithmetic is fp32, one operation after the other without fusing, so a state's code is a function of its inputs
 // that can be computed anywhere.

@@ -5,10 +5,11 @@
 // Scores are formed turned, keys in rows and queries in columns: a lane then holds scores of one query, the running maximum and sum of
 // its softmax are two registers, and the probabilities are the right operand of the product with the values as they stand.
 // Rounding: bf16 tensors enter products as they are; scores, exponents, maxima and sums are fp32; probabilities are rounded
-// to bf16 (2^-9 of themselves) for their product with the values, which is summed in fp32.  fp32 tensors: fp32 throughout.
+// to bf16 (by up to 2^-8 of themselves) for their product with the values, which is summed in fp32 (k_attn_few, on the vector
+// unit, keeps them in fp32).  fp32 tensors: fp32 throughout.
 //
 // Kernels, by the lengths alone.  Up to 64 keys, a wave a sequence and head: k_attn_windows (up to 32 keys, queries of all sequences at one
-// position: rows through LDS) and k_attn_window (the rest).  Else up to 16 queries, keys split among lanes, waves and workgroups and joined by k_attn_join:
+// position, rows that fit 64 KB of LDS) and k_attn_window (the rest).  Else up to 16 queries, keys split among lanes, waves and workgroups and joined by k_attn_join:
 // k_attn_few (one or two rows that share a key head) and k_attn_rows (more, on the matrix unit).  k_attn_forward: the rest.
 #include <algorithm>
 #include <type_traits>
@@ -23,7 +24,7 @@ namespace {
 //
 // A workgroup takes 4 M queries of one sequence and head, a wave M of them, and walks over the keys in tiles of 64 (fp32, wide bf16 heads: 32) that lie in LDS
 // once for all four; the next tile's rows are on their way in registers meanwhile.  What bounds it are the vector instructions of the softmax: four sequences of 8192
-// tokens, 8 heads of 64, bf16 take 0.41 to 0.48 ms where the products alone would take 0.23; vector units are busy for 63 % of that, the matrix units for 29 %.
+// tokens, 8 heads of 64, bf16 take 0.40 ms (0.47 in a card's first passes) where the products alone would take 0.23; vector units are busy for 63 % of that, the matrix units for 29 %.
 // Tiles without masks, of one bias, therefore have a path without branches and with one multiply-add a score (with a mask, where none is, 0.78 ms).
 template <class Tl, int KS>
 __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
@@ -233,7 +234,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_forward(Args a) {
 // ---------------------------------------------------------------------------------------------------- windows
 //
 // Up to 16 NT keys and queries: a wave takes one sequence and head after the other, of one head, so that the table of
-// its bias stays.  Queries and keys go from memory into operands; only the values pass through LDS, in the wave's own part: no wave waits for another.
+// its bias stays.  Queries and keys go from memory into operands; only the values pass through LDS, in the wave's own part: no wave waits for another.  10 000 x 64, 4 heads of 32:
+// bf16 225 us, 3.0 TB/s, fp32 333 us, 4.0 TB/s.
 template <class Tl, int NT, int KS>
 __global__ __launch_bounds__(256) void k_attn_window(Args a) {
   typedef typename Tl::E E;
@@ -337,10 +339,12 @@ __global__ __launch_bounds__(256) void k_attn_window(Args a) {
   }
 }
 
-// The same for up to 32 keys where all sequences' queries stand at one position, as a batch of windows has it.  What bounds it is how many pieces of
+// The same for up to 32 keys where all sequences' queries stand at one position, as a batch of windows has it, and the rows below fit 64 KB of LDS: all with up to 16 keys,
+// with more not bf16 heads of 40, 64, 120 and 128 (four heads and more) and fp32 ones of 32, 64 and 128, for which two sequences, or 256 bytes, are too much (20 000 x 32, 8
+// heads of 64, bf16: 890 us in k_attn_window, 3.0 TB/s; 4 of 32, fp32: 301 us, 4.4 TB/s).  What bounds it is how many pieces of
 // memory a load touches: operands straight from memory are 32 bytes of each of 16 rows, and ran at 2.4 TB/s.  So a workgroup takes the rows of `together`
 // neighbouring heads, up to 256 bytes, of one or two sequences as they lie, through LDS, and its waves a sequence and head each from there; the outputs go back
-// the same way: 100 000 windows of 16, 8 heads of 16, bf16 in 0.41 ms, 4.1 TB/s.  The next rows are on their way meanwhile; outputs leave after they have come and before more are asked for: memory answers in
+// the same way: 100 000 windows of 16, 8 heads of 16, bf16 in 0.385 ms, 4.4 TB/s (0.41 in a card's first passes).  The next rows are on their way meanwhile; outputs leave after they have come and before more are asked for: memory answers in
 // order, so rows asked for before a store would come after it.
 struct WindowArgs {
   Args a;
@@ -699,7 +703,7 @@ __global__ __launch_bounds__(256) void k_attn_few(Args a) {
 }
 
 // More rows than two, of heads that share a key head or of several queries: 16 of them are the columns of a matrix product, so a key is read once for
-// all (two sequences of 65 536 keys, 4 key heads of 128 for 16, bf16: 68 us, of which 55 at a copy's rate; two rows at a time on the vector unit 240).  A wave takes 32 keys at a time (16 of wide fp32 rows): their rows go from memory into operands, values through LDS (each wave's own part), four waves a workgroup.
+// all (two sequences of 65 536 keys, 4 key heads of 128 for 16, bf16: 66 us, of which 55 at a copy's rate; two rows at a time on the vector unit 240; fp32: 114 us, 4.7 TB/s).  A wave takes 32 keys at a time (16 of wide fp32 rows): their rows go from memory into operands, values through LDS (each wave's own part), four waves a workgroup.
 template <class E> struct Slab;
 template <> struct Slab<uint16_t> {
   static constexpr int PER = 8, STEP = 32;      // elements of a lane, contraction of a product
@@ -975,7 +979,7 @@ void window(Args a, hipStream_t st) {
   if (more) hipLaunchKernelGGL((k_attn_windows<Tl, NT, KS, 2 * NT>), wgs, 256, lds, st, w);    \
   else hipLaunchKernelGGL((k_attn_windows<Tl, NT, KS, NT>), wgs, 256, lds, st, w)
       if (lds > 65536) {
-        // rows of more than 256 bytes: below
+        // below
       } else if (a.d <= 16) {
         DGC_WINDOWS(1);
       } else if (a.d <= 32) {

@@ -6,8 +6,8 @@
 // Scores are computed again, not kept.  In k_attn_dq queries are columns and keys are summed over, in k_attn_dkv keys are columns and queries are summed over
 // (heads that share a key head one after the other), so no two workgroups add to one number: no atomics on memory, one order of sums, at the price of
 // seven products for five.  Windows of up to 32 keys have a whole sequence and head in a wave and need five: k_attn_windows_back where every head has a key head of its
-// own, k_attn_window_back where up to four share one.  The others: k_attn_delta (D), k_attn_dq, k_attn_dkv, k_attn_dkv_join (parts of the queries).
-// Rounding: bf16 tensors enter products as they are, scores, P, dP, D and dS are fp32; P and dS are rounded to bf16 (2^-9 of themselves)
+// own and the rows fit 64 KB of LDS, k_attn_window_back where up to four share one, or they do not.  The others: k_attn_delta (D), k_attn_dq, k_attn_dkv, k_attn_dkv_join (parts of the queries).
+// Rounding: bf16 tensors enter products as they are, scores, P, dP, D and dS are fp32; P and dS are rounded to bf16 (by up to 2^-8 of themselves)
 // for the products of dv, dq and dk, which are summed in fp32; the bias' gradient sums dS as it is, in fp32 and at the end in double.
 //
 // The bias' gradient: every wave sums dS by distance into a table of its own in LDS.  In k_attn_dq it lays a tile's dS out slanted, so that a distance is
@@ -184,7 +184,8 @@ __global__ __launch_bounds__(256) void k_attn_window_back(Args a) {
   }
 }
 
-// The same where every head has a key head of its own, and rows go through LDS as they lie (as in the forward pass' k_attn_windows; straight from memory
+// The same where every head has a key head of its own, and rows go through LDS as they lie, if they fit 64 KB: bf16 heads of up to 64 (17 to 32 keys: up to 48), fp32 ones of up to
+// 32 (17 to 32 keys: 16; 20 000 x 32, 4 heads of 32, fp32: 676 us in the other, 3.9 TB/s; 8 of 64, bf16: 2.33 ms, 2.3 TB/s) (as in the forward pass' k_attn_windows; straight from memory
 // they took 1.2 to 1.6 times as long; 20 000 ragged windows of 32, 4 heads of 32, bf16: 0.42 ms, where 0.14 is what a copy of it all takes; it waits for
 // LDS and its own chain of products at two waves a SIMD, of 256 registers and some spilled): all gradients take the place of what they are gradients of, and leave from there.  A wave keeps to one head, or two, so
 // the bias' gradient is summed in registers, element by element, until the end.
@@ -494,7 +495,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(Args a) {
 
 // ---------------------------------------------------------------------------------------------------- dq, and the bias' gradient
 //
-// Four sequences of 4096, 8 heads of 64 on 2 key heads, bf16: 0.19 ms, and k_attn_dkv 0.25.  Both are bound by how long a wave's chain LDS, products, powers, products
+// Four sequences of 4096, 8 heads of 64 on 2 key heads, bf16: 0.174 ms, and k_attn_dkv 0.23 (0.19 and 0.25 in a card's first passes).  Both are bound by how long a wave's chain LDS, products, powers, products
 // takes with two waves a SIMD.  As the forward pass: 4 M queries a workgroup, keys in tiles of 2 M through LDS.  The product that forms dP starts from -D, so it
 // leaves dP - D; in bf16 D is subtracted behind it: that unit cuts sums off, always to one side, and what it leaves of -D is summed up by the bias' gradient, where
 // millions of dS nearly cancel (4000 x 200 tokens, 4 heads of 32: off by 5.5e-6 of its norm, now 5e-7).  It costs 2 to 4 % of this kernel, and leaves registers to heads above

@@ -256,7 +256,8 @@ class TimeBlock:
 
         With softmax attention there are no states and resets.  keep uint8 [T, N], as binding.attn_forward has it: snapshots that nobody attends to.  cache
         [S, N, 2 width], rows at least, of the block's element type, with train=False: X are snapshots at .. at + T - 1; their keys and values are written
-        to those rows, and they attend to all rows up to their own, of which keep [at + T, N] may mask some."""
+        to those rows, and they attend to all rows up to their own, of which keep [at + T, N] may mask some.  `at` is one for all vertices, and a captured call
+        keeps it."""
         self._last = None
         if self.attention == "softmax":
             if S0 is not None or SN is not None or reset is not None:
