@@ -786,9 +786,9 @@ def adamw_step(handle, dev: int, t: int, *, lr: float, beta1: float, beta2: floa
     if stream is not None or _device() != dev:
         with _torch.cuda.device(dev), _torch.cuda.stream(stream):
             return adamw_step(handle, dev, t, lr=lr, beta1=beta1, beta2=beta2, eps=eps, steps=steps, lr_at=lr_at)
-    if steps is None:
-        if _capturing():
-            raise RuntimeError("a captured step counts on the device: it needs `steps` (AdamW: on_device=True)")
+    if steps is None and _capturing():
+        raise RuntimeError("a captured step counts on the device: it needs `steps` (AdamW: on_device=True)")
+    if steps is None and lr_at is None:
         rc = _lib.dgc_adamw_step(handle, lr, beta1, beta2, eps, t, None, None, _raw_stream(dev))
     else:
         rc = _lib.dgc_adamw_step(handle, lr, beta1, beta2, eps, t, _op_flat(steps, "steps", 1, dev, _torch.int64), _op_flat(lr_at, "lr", 1, dev), _raw_stream(dev))

@@ -45,3 +45,17 @@ def test_a_step_that_the_host_counts_is_not_captured(given):
     opt.step(stream=s if given else None)      # outside the capture it goes on
     torch.cuda.synchronize()
     assert opt.steps == 2 and bool((p < 2 * before).all())
+
+
+def test_a_rate_on_the_device_goes_with_the_number_of_steps_there():
+    import torch
+    from paper_2309_03523_amd import binding
+    from paper_2309_03523_amd.optimizer import AdamW
+    p, g = torch.ones(4, 16, device="cuda"), torch.ones(4, 16, device="cuda")
+    opt = AdamW([p], [g])
+    kw = dict(lr=0.1, beta1=0.9, beta2=0.99, eps=1e-8)
+    with pytest.raises(binding.DgcError, match="lr on the device"):
+        binding.adamw_step(opt._handle, p.device.index, 1, lr_at=torch.ones(1, device="cuda"), **kw)
+    with pytest.raises(ValueError):
+        binding.adamw_step(opt._handle, p.device.index, 1, lr_at=torch.ones(2, device="cuda"), **kw)
+    assert bool((p == 1).all())
